@@ -439,6 +439,127 @@ int dfx_plan_route(int nranks, const dfx_config* cfg, dfx_kind kind, size_t coun
 int dfx_collective_noalloc(int nranks, dfx_kind kind, size_t count, dfx_dtype dtype, dfx_op op, int root,
                            const void* const* sendbufs, void* const* recvbufs, uint32_t* status_dev, void* hip_stream);
 
+/*
+ * ---- The training step around the collectives ----------------------------------------------------------------------
+ * What a data-parallel step does in front of its gradient all-reduce (the loss and its gradient) and behind it (norm of
+ * all gradients, clipping, update).  These calls belong to no context.  Each only enqueues kernels on hip_stream (NULL = the null
+ * stream): none allocates, copies or waits (but dfx_list_create and dfx_list_destroy), so all of them may be captured into a HIP
+ * graph.  Memory that they are given is device memory of the current device, and every tensor starts at a multiple of its
+ * element's size, which is all that is asked of alignment.  Element types are DFX_F32, DFX_BF16 and DFX_F16; sums, norms and
+ * moments are held in 32 bits or more, and a result of 16 bits is rounded once, to nearest even.  Results do not depend on what
+ * else runs: the same call on the same memory gives the same bits.  A NULL stream or a context's daemon that is still resident
+ * may hold back a kernel behind it: see dfx_config.quit_idle_us.
+ */
+
+/* One tensor of a list: count elements from ptr on (ptr is not looked at where count is 0). */
+typedef struct {
+  void* ptr;
+  size_t count;
+  dfx_dtype dtype;
+  uint32_t reserved0; /* must be 0 */
+} dfx_tensor;
+
+/* A list of tensors, such as all gradients of a model: a training program makes one when it has laid its buckets out.  It holds
+   addresses and lengths, never contents; the memory has to stay where it is as long as the list is used. */
+typedef struct dfx_list dfx_list; /* opaque, library-owned */
+typedef enum { DFX_NORM_2 = 0, DFX_NORM_INF = 1 } dfx_norm_kind;
+
+/*
+ * Make a list of n >= 0 tensors (host array, read during the call) on the current device; types may differ from tensor to tensor.
+ * Allocates device memory (16 bytes per 8192 elements, and 16 KiB) and waits for its upload.
+ * Errors: INVALID_ARG (type, NULL or misaligned ptr), TOO_LARGE (above 2^31 chunks of 8192 elements), NO_RESOURCES, HIP.
+ */
+int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n);
+/* Free what the list holds (not the tensors).  No call on it may be running. */
+int dfx_list_destroy(dfx_list* list);
+
+/*
+ * norm_dev (device, 4 bytes) <- the norm of all gradients of the list taken as one vector, times |grad_scale|: the root of the sum
+ * of squares (summed in 64 bits), or the largest magnitude.  NaN where any gradient is NaN; 0 for a list without elements.
+ * grad_scale: what the gradients are still to be multiplied with (1 / ranks behind a sum over ranks, 1 / loss scale).
+ * The list's own scratch memory holds what the workgroups hand each other: calls of dfx_grad_norm or dfx_clip_grad_norm on one
+ * list must not overlap.  Shards on several ranks: the norm of the ranks' norms (gathered, as a list of their own) is the norm of all.
+ * Errors: INVALID_ARG (also: the list is another device's), HIP.
+ */
+int dfx_grad_norm(dfx_list* grads, dfx_norm_kind kind, double grad_scale, float* norm_dev, void* hip_stream);
+
+/*
+ * dst <- src * grad_scale * min(1, max_norm / (*norm_dev + 1e-6)), tensor by tensor: *norm_dev is the norm of the gradients times
+ * grad_scale, as dfx_grad_norm leaves it.  dst: a list of equal counts, whose types may differ (the reduced 16-bit bucket into
+ * 32-bit gradients); NULL or src = in place.  A tensor of dst lies apart from src's, or is the same memory and type.  A norm of
+ * infinity makes finite gradients 0, a norm of NaN makes all of them NaN.
+ * Errors: INVALID_ARG (counts, overlap, max_norm <= 0), HIP.
+ */
+int dfx_grad_clip(dfx_list* src, dfx_list* dst, const float* norm_dev, double max_norm, double grad_scale, void* hip_stream);
+
+/* dfx_grad_norm, then dfx_grad_clip with that norm, which stays in norm_dev. */
+int dfx_clip_grad_norm(dfx_list* src, dfx_list* dst, dfx_norm_kind kind, double max_norm, double grad_scale, float* norm_dev,
+                       void* hip_stream);
+
+/* Of dfx_adamw.  Zero-initialise, call dfx_adamw_default, then override fields. */
+typedef struct {
+  uint32_t struct_bytes;    /* sizeof(dfx_adamw_config) the caller was compiled with */
+  uint32_t step;            /* t: number of this update, from 1 */
+  double lr, beta1, beta2, eps, weight_decay;
+  double grad_scale;        /* as above */
+  double max_norm;          /* > 0; only looked at where there is a norm */
+  const uint32_t* step_dev; /* device, may be NULL: t is read there instead (a captured step counts it up itself) */
+  const float* lr_dev;      /* device, may be NULL: lr is read there instead */
+} dfx_adamw_config;
+int dfx_adamw_default(dfx_adamw_config* cfg);
+
+/*
+ * One AdamW update, the clipping included: with h = gradient * grad_scale * min(1, max_norm / (*norm_dev + 1e-6)),
+ *   m <- beta1 m + (1 - beta1) h;  v <- beta2 v + (1 - beta2) h^2;
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps);  copy <- p rounded
+ * params, exp_avg (m), exp_avg_sq (v): lists of DFX_F32 tensors; grads, copies: any type; all of equal counts, no tensor overlapping
+ * another.  copies may be NULL.  norm_dev: device, or NULL: nothing is clipped.  Where *norm_dev is infinite or NaN the
+ * gradients overflowed: nothing is written.
+ * Errors: INVALID_ARG (counts, types, one list in two places, configuration), HIP.
+ */
+int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* exp_avg_sq, dfx_list* copies,
+              const dfx_adamw_config* cfg, const float* norm_dev, void* hip_stream);
+
+/*
+ * The clipped policy loss with a KL term, and its gradient, for rows of logits z and one target token t each:
+ *   logp = log softmax(z / temperature)[t];  r = exp(logp - old_logp);
+ *   pg = A >= 0 ? -A min(r, 1 + clip_high) : -A max(r, 1 - clip_low);  d = ref_logp - logp;  kl = exp(d) - d - 1
+ *   loss = weight (pg + kl_coef kl);  grad = scale * d loss / d z
+ * A row of weight 0, with a target outside [0, vocab), or with no logit above -infinity has nothing to learn from: its results are 0
+ * (its gradient is written, as 0), it adds nothing to the sums, and its logits are not looked at where weight or target say so.  Logits of
+ * -infinity and of the type's lowest value are ordinary ones: probability 0.  A logit of NaN or +infinity makes its row NaN.
+ * Zero-initialise, set struct_bytes and inv_temperature; pointers are device memory.
+ */
+typedef struct {
+  uint32_t struct_bytes;     /* sizeof(dfx_policy_loss_args) the caller was compiled with */
+  dfx_dtype dtype;           /* of logits and grad */
+  size_t rows, vocab;        /* below 2^31 / below 2^30; either may be 0 */
+  const void* logits;        /* rows of vocab elements, logits_stride elements from one to the next (0 = vocab) */
+  size_t logits_stride;
+  void* grad;                /* may be NULL: forward only.  Apart from logits, or the same memory with the same stride */
+  size_t grad_stride;
+  const int64_t* targets;    /* [rows] */
+  const float* old_logp;     /* [rows], log-probabilities when the tokens were sampled; may be NULL: r = 1 */
+  const float* ref_logp;     /* [rows], of the reference policy; may be NULL with kl_coef = 0: kl = 0 */
+  const float* advantage;    /* [rows], A; may be NULL where neither loss, sums nor grad is asked for */
+  const float* weight;       /* [rows], may be NULL: 1 */
+  const float* scale;        /* one value, may be NULL: 1.  Multiplies the gradient only: 1 / the weights of all ranks' rows */
+  float* logp;               /* [rows], may be NULL */
+  float* loss;               /* [rows], may be NULL */
+  float* sums;               /* 5 values, may be NULL: sums over the rows of weight times loss / weight, pg, kl, [clipped], 1 */
+  void* workspace;           /* dfx_policy_loss_workspace bytes, 8-byte aligned; nothing in it has to outlive the call's work */
+  size_t workspace_bytes;
+  double clip_low, clip_high; /* 0 <= clip_low <= 1, 0 <= clip_high */
+  double kl_coef;            /* needs ref_logp where it is not 0 */
+  double inv_temperature;    /* > 0 */
+} dfx_policy_loss_args;
+
+/* Bytes of workspace for calls of up to so many rows of this length and type (host only, no GPU needed). */
+size_t dfx_policy_loss_workspace(size_t rows, size_t vocab, dfx_dtype dtype);
+
+/* Errors: INVALID_ARG (also: workspace too small), TOO_LARGE, HIP. */
+int dfx_policy_loss(const dfx_policy_loss_args* args, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

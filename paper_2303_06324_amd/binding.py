@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libdfx.so")
 ALLREDUCE, ALLGATHER, REDUCESCATTER, BROADCAST, REDUCE = 0, 1, 2, 3, 4
 F32, BF16, F16, I32 = 0, 1, 2, 3
 SUM, PROD, MAX, MIN = 0, 1, 2, 3
+NORM_2, NORM_INF = 0, 1
 
 OK = 0
 ERR_INVALID_ARG, ERR_NOT_PREPARED, ERR_BUSY, ERR_SQ_FULL = -1, -2, -3, -4
@@ -39,6 +40,31 @@ class Stats(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class Tensor(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("count", C.c_size_t), ("dtype", C.c_int), ("reserved0", C.c_uint32)]
+
+
+class AdamWConfig(C.Structure):
+    """dfx_adamw_config: AdamWConfig(lr=..., step=...) is the library's defaults but for what is named."""
+    _fields_ = [("struct_bytes", C.c_uint32), ("step", C.c_uint32)] + [(n, C.c_double) for n in (
+        "lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale", "max_norm")] + [("step_dev", C.c_void_p), ("lr_dev", C.c_void_p)]
+
+    def __init__(self, **kw):
+        super().__init__()
+        _lib.dfx_adamw_default(C.byref(self))
+        for k, v in kw.items():
+            if not hasattr(self, k):
+                raise KeyError(k)
+            setattr(self, k, v)
+
+
+class PolicyLossArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("rows", C.c_size_t), ("vocab", C.c_size_t),
+                ("logits", C.c_void_p), ("logits_stride", C.c_size_t), ("grad", C.c_void_p), ("grad_stride", C.c_size_t)] + [
+                    (n, C.c_void_p) for n in ("targets", "old_logp", "ref_logp", "advantage", "weight", "scale", "logp", "loss", "sums", "workspace")] + [
+                        ("workspace_bytes", C.c_size_t)] + [(n, C.c_double) for n in ("clip_low", "clip_high", "kl_coef", "inv_temperature")]
 
 
 CALLBACK = C.CFUNCTYPE(None, C.c_void_p, C.c_int, C.c_uint32, C.c_uint32)
@@ -98,6 +124,15 @@ def _load() -> C.CDLL:
         "dfx_copy_calibrate": ([vp, vp, sz, vp, C.POINTER(C.c_float)], i),
         "dfx_check_geometry": ([i, C.POINTER(Config), i, sz, i, i, i, i, C.c_uint32, C.c_char_p, sz], i),
         "dfx_plan_route": ([i, C.POINTER(Config), i, sz, i, i], i),
+        "dfx_list_create": ([C.POINTER(vp), C.POINTER(Tensor), i], i),
+        "dfx_list_destroy": ([vp], i),
+        "dfx_grad_norm": ([vp, i, C.c_double, vp, vp], i),
+        "dfx_grad_clip": ([vp, vp, vp, C.c_double, C.c_double, vp], i),
+        "dfx_clip_grad_norm": ([vp, vp, i, C.c_double, C.c_double, vp, vp], i),
+        "dfx_adamw_default": ([C.POINTER(AdamWConfig)], i),
+        "dfx_adamw": ([vp, vp, vp, vp, vp, C.POINTER(AdamWConfig), vp, vp], i),
+        "dfx_policy_loss_workspace": ([sz, sz, i], sz),
+        "dfx_policy_loss": ([C.POINTER(PolicyLossArgs), vp], i),
         "dfx_collective_noalloc": ([i, i, sz, i, i, i, C.POINTER(vp), C.POINTER(vp), vp, vp], i),
     }
     for name, (args, res) in sig.items():
@@ -301,3 +336,83 @@ def plan_route(nranks: int, kind: int, count: int, dtype: int, root: int = 0, cf
     if rc < 0:
         raise DfxError(rc, "dfx_plan_route")
     return {name for bit, name in enumerate(ROUTES) if rc >> bit & 1}
+
+
+# ---- the training step around the collectives: everything below only enqueues work on `stream` (None or 0: the null stream); pointers are
+# device addresses (0: absent)
+class TensorList:
+    """A list of device tensors (dfx_list), from (address, elements, type) triples; keep the memory alive as long as it is used."""
+
+    def __init__(self, tensors):
+        self._h = C.c_void_p()
+        arr = (Tensor * len(tensors))(*[(p, n, t, 0) for p, n, t in tensors])
+        rc = _lib.dfx_list_create(C.byref(self._h), arr, len(tensors))
+        if rc != OK:
+            self._h = C.c_void_p()
+            raise DfxError(rc, "dfx_list_create")
+
+    def destroy(self) -> int:
+        if not self._h:
+            return OK
+        rc = _lib.dfx_list_destroy(self._h)
+        self._h = C.c_void_p()
+        return rc
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def grad_norm(grads: TensorList, norm: int, kind: int = NORM_2, scale: float = 1.0, stream: Optional[int] = None) -> None:
+    """norm[0] = the norm of all gradients of the list, times |scale|."""
+    rc = _lib.dfx_grad_norm(grads._h, kind, scale, norm, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_grad_norm")
+
+
+def grad_clip(grads: TensorList, norm: int, max_norm: float, out: Optional[TensorList] = None, scale: float = 1.0,
+              stream: Optional[int] = None) -> None:
+    """out (None: in place) = gradients * scale * min(1, max_norm / (norm[0] + 1e-6))."""
+    rc = _lib.dfx_grad_clip(grads._h, out._h if out is not None else None, norm, max_norm, scale, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_grad_clip")
+
+
+def clip_grad_norm(grads: TensorList, norm: int, max_norm: float, out: Optional[TensorList] = None, kind: int = NORM_2,
+                   scale: float = 1.0, stream: Optional[int] = None) -> None:
+    """grad_norm, then grad_clip by that norm."""
+    rc = _lib.dfx_clip_grad_norm(grads._h, out._h if out is not None else None, kind, max_norm, scale, norm, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_clip_grad_norm")
+
+
+def adamw(params: TensorList, grads: TensorList, exp_avg: TensorList, exp_avg_sq: TensorList, config: AdamWConfig,
+          copies: Optional[TensorList] = None, norm: int = 0, stream: Optional[int] = None) -> None:
+    """One AdamW update, clipped by norm[0] on the way; nothing is written where that is infinite or NaN."""
+    rc = _lib.dfx_adamw(params._h, grads._h, exp_avg._h, exp_avg_sq._h, copies._h if copies is not None else None, config, norm, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_adamw")
+
+
+def policy_loss_workspace(rows: int, vocab: int, dtype: int) -> int:
+    """Bytes of workspace that policy_loss needs for up to so many rows (no GPU needed)."""
+    return _lib.dfx_policy_loss_workspace(rows, vocab, dtype)
+
+
+_LOSS_BYTES = C.sizeof(PolicyLossArgs)
+
+
+def policy_loss(rows: int, vocab: int, dtype: int, logits: int, targets: int, *, old_logp: int = 0, ref_logp: int = 0,
+                advantage: int = 0, weight: int = 0, scale: int = 0, logp: int = 0, loss: int = 0, sums: int = 0, grad: int = 0,
+                logits_stride: int = 0, grad_stride: int = 0, clip_low: float = 0.2, clip_high: float = 0.2,
+                kl_coef: float = 0.0, inv_temperature: float = 1.0, workspace: int = 0, workspace_bytes: int = 0,
+                stream: Optional[int] = None) -> None:
+    """The clipped policy loss of rows of logits and, where grad is given, its gradient (dfx_policy_loss)."""
+    a = PolicyLossArgs(_LOSS_BYTES, dtype, rows, vocab, logits, logits_stride, grad, grad_stride, targets, old_logp, ref_logp,
+                       advantage, weight, scale, logp, loss, sums, workspace, workspace_bytes, clip_low, clip_high, kl_coef,
+                       inv_temperature)
+    rc = _lib.dfx_policy_loss(a, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_policy_loss")

@@ -1,0 +1,406 @@
+// Operators over lists of tensors, behind the gradient all-reduce of a step: the norm of all gradients, clipping, AdamW.
+//
+// A list is cut into chunks once, when it is made: a chunk lies in one tensor, has at most kChunk elements and is one entry {address,
+// elements, type} of a table in device memory.  Lists of equal counts have equal tables but for the addresses and types, so a kernel
+// over several lists takes entry c of each.  A call is one kernel (the norm and clipping: two), allocates nothing and copies nothing.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "dfx_step.h"
+
+namespace {
+
+constexpr uint32_t kChunk = 8192;        // elements
+constexpr int kThreads = 256;
+constexpr int kNormGroups = 2048;        // workgroups of a norm, at most: each leaves one partial result
+
+struct ListChunk { uint64_t ptr; uint32_t n; int32_t dtype; };
+static_assert(sizeof(ListChunk) == 16, "a chunk is one 16-byte load");
+
+struct ListScratch {
+  double part[kNormGroups];
+  uint32_t ticket;                       // counts workgroups through; 0 again when the last one is
+};
+
+}  // namespace
+
+struct dfx_list {
+  int device = 0;
+  uint32_t nchunks = 0;
+  std::vector<dfx_tensor> tensors;
+  ListChunk* chunks = nullptr;           // device
+  ListScratch* scratch = nullptr;        // device
+};
+
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// norm: sum of squares (or the largest magnitude) over all elements
+//
+// Squares and their sum are held in 64 bits: no gradient of 32 or 16 bits is too large or too small to be squared there, so no second,
+// scaled pass is needed.
+// ------------------------------------------------------------------------------------------
+template <int DT, bool MAXIMUM>
+__device__ __forceinline__ void norm_chunk(const ListChunk& c, double& sum, uint32_t& top) {
+  constexpr int N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  const void* p = (const void*)c.ptr;
+  const uint32_t nvec = c.n / N;
+  auto take = [&](float x) {
+    if (MAXIMUM) top = max(top, __float_as_uint(x) & 0x7fffffffu);       // as integers: magnitudes in order, NaN above infinity
+    else sum = fma((double)x, (double)x, sum);
+  };
+#pragma unroll 4
+  for (uint32_t v = threadIdx.x; v < nvec; v += kThreads) {
+    const auto r = step_load<DT, N>(p, (size_t)v * N);
+#pragma unroll
+    for (int k = 0; k < N; ++k) take(StepElem<DT>::get(r.x[k]));
+  }
+  const uint32_t i = nvec * N + threadIdx.x;
+  if (i < c.n) take(step_get<DT>(p, i));
+}
+
+template <bool MAXIMUM>
+__global__ void __launch_bounds__(kThreads) dfx_norm_kernel(const ListChunk* __restrict__ chunks, uint32_t nchunks, ListScratch* scratch, double scale, float* norm) {
+  __shared__ double lds[kThreads / kStepWave];
+  __shared__ uint32_t last;
+  double sum = 0.0;
+  uint32_t top = 0;
+  for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
+    const ListChunk e = chunks[c];
+    if (e.dtype == DFX_F32) norm_chunk<DFX_F32, MAXIMUM>(e, sum, top);
+    else if (e.dtype == DFX_BF16) norm_chunk<DFX_BF16, MAXIMUM>(e, sum, top);
+    else norm_chunk<DFX_F16, MAXIMUM>(e, sum, top);
+  }
+  auto joined = [&]() -> double {       // over the workgroup; valid in thread 0
+    const double w = MAXIMUM ? (double)wave_max(top) : wave_sum(sum);
+    if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave] = w;
+    __syncthreads();
+    double r = lds[0];
+    for (int k = 1; k < kThreads / kStepWave; ++k) r = MAXIMUM ? fmax(r, lds[k]) : r + lds[k];
+    return r;
+  };
+  const double mine = joined();
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(&scratch->part[blockIdx.x], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = __hip_atomic_fetch_add(&scratch->ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1u == gridDim.x;
+  }
+  __syncthreads();
+  if (!last) return;
+  // the last workgroup adds up the others' results, in an order that does not depend on who came when
+  sum = 0.0; top = 0;
+  for (uint32_t k = threadIdx.x; k < gridDim.x; k += kThreads) {
+    const double p = __hip_atomic_load(&scratch->part[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (MAXIMUM) top = max(top, (uint32_t)p);
+    else sum += p;
+  }
+  const double all = joined();
+  if (threadIdx.x == 0) {
+    *norm = (float)(fabs(scale) * (MAXIMUM ? (double)__uint_as_float((uint32_t)all) : sqrt(all)));
+    __hip_atomic_store(&scratch->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+// What a gradient is multiplied with: its scale and, where the norm (of the scaled gradients) is above max_norm, the factor that brings
+// it there.  A norm of infinity gives 0 (and NaN from infinite gradients), a norm of NaN gives NaN.
+__device__ __forceinline__ float clip_factor(float norm, float max_norm, float scale) {
+  const float q = max_norm / (norm + 1e-6f);
+  return scale * (q > 1.0f ? 1.0f : q);
+}
+
+template <int SD, int DD>
+__device__ __forceinline__ void clip_chunk(const ListChunk& s, const ListChunk& d, float f) {
+  constexpr int N = 4;
+  const uint32_t nvec = s.n / N;
+#pragma unroll 4
+  for (uint32_t v = threadIdx.x; v < nvec; v += kThreads) {
+    const auto r = step_load<SD, N>((const void*)s.ptr, (size_t)v * N);
+    float x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = StepElem<SD>::get(r.x[k]) * f;
+    step_store<DD, N>((void*)d.ptr, (size_t)v * N, x);
+  }
+  const uint32_t i = nvec * N + threadIdx.x;
+  if (i < s.n) step_put<DD>((void*)d.ptr, i, step_get<SD>((const void*)s.ptr, i) * f);
+}
+
+template <int SD>
+__device__ __forceinline__ void clip_chunk_to(const ListChunk& s, const ListChunk& d, float f) {
+  if (d.dtype == DFX_F32) clip_chunk<SD, DFX_F32>(s, d, f);
+  else if (d.dtype == DFX_BF16) clip_chunk<SD, DFX_BF16>(s, d, f);
+  else clip_chunk<SD, DFX_F16>(s, d, f);
+}
+
+// (src and dst may be the same tensors: no __restrict__ on what the chunks point to)
+__global__ void __launch_bounds__(kThreads) dfx_clip_kernel(const ListChunk* __restrict__ src, const ListChunk* __restrict__ dst, uint32_t nchunks, const float* norm, float max_norm, float scale, bool in_place) {
+  const float f = clip_factor(*norm, max_norm, scale);
+  if (in_place && f == 1.0f) return;      // the gradients are what they are to become
+  for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
+    const ListChunk s = src[c], d = dst[c];
+    if (s.dtype == DFX_F32) clip_chunk_to<DFX_F32>(s, d, f);
+    else if (s.dtype == DFX_BF16) clip_chunk_to<DFX_BF16>(s, d, f);
+    else clip_chunk_to<DFX_F16>(s, d, f);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// AdamW
+// ------------------------------------------------------------------------------------------
+struct AdamArgs {
+  const ListChunk *p, *g, *m, *v, *copy;      // copy: may be null
+  uint32_t nchunks;
+  const float* norm;                          // may be null: nothing is clipped
+  const uint32_t* step_dev;                   // may be null: correct1 / correct2 hold
+  const float* lr_dev;                        // may be null: lr holds
+  double beta1_d, beta2_d;
+  float lr, beta1, beta2, one_beta1, one_beta2, eps, decay, scale, max_norm;
+  float correct1, correct2;                   // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+};
+
+struct AdamRates { float f, keep, beta1, one_beta1, beta2, one_beta2, rate, correct2, eps; };
+
+__device__ __forceinline__ void adam_element(const AdamRates& a, float& p, float g, float& m, float& v) {
+  g *= a.f;
+  m = fmaf(a.beta1, m, a.one_beta1 * g);
+  v = fmaf(a.beta2, v, a.one_beta2 * g * g);
+  p = fmaf(p, a.keep, -(a.rate * m / fmaf(sqrtf(v), a.correct2, a.eps)));
+}
+
+template <int GD, int CD>      // CD < 0: no copy
+__device__ __forceinline__ void adam_chunk(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy) {
+  constexpr int N = 4;
+  constexpr int C = CD < 0 ? DFX_F32 : CD;
+  const uint32_t nvec = p.n / N;
+#pragma unroll 2
+  for (uint32_t k = threadIdx.x; k < nvec; k += kThreads) {
+    const size_t i = (size_t)k * N;
+    const auto rp = step_load<DFX_F32, N>((const void*)p.ptr, i), rm = step_load<DFX_F32, N>((const void*)m.ptr, i), rv = step_load<DFX_F32, N>((const void*)v.ptr, i);
+    const auto rg = step_load<GD, N>((const void*)g.ptr, i);
+    float xp[N], xm[N], xv[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      xp[j] = __uint_as_float(rp.x[j]); xm[j] = __uint_as_float(rm.x[j]); xv[j] = __uint_as_float(rv.x[j]);
+      adam_element(a, xp[j], StepElem<GD>::get(rg.x[j]), xm[j], xv[j]);
+    }
+    step_store<DFX_F32, N>((void*)p.ptr, i, xp);
+    step_store<DFX_F32, N>((void*)m.ptr, i, xm);
+    step_store<DFX_F32, N>((void*)v.ptr, i, xv);
+    if (CD >= 0) step_store<C, N>((void*)copy.ptr, i, xp);
+  }
+  const uint32_t i = nvec * N + threadIdx.x;
+  if (i < p.n) {
+    float xp = step_get<DFX_F32>((const void*)p.ptr, i), xm = step_get<DFX_F32>((const void*)m.ptr, i), xv = step_get<DFX_F32>((const void*)v.ptr, i);
+    adam_element(a, xp, step_get<GD>((const void*)g.ptr, i), xm, xv);
+    step_put<DFX_F32>((void*)p.ptr, i, xp);
+    step_put<DFX_F32>((void*)m.ptr, i, xm);
+    step_put<DFX_F32>((void*)v.ptr, i, xv);
+    if (CD >= 0) step_put<C>((void*)copy.ptr, i, xp);
+  }
+}
+
+template <int GD>
+__device__ __forceinline__ void adam_chunk_copy(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, bool has_copy) {
+  if (!has_copy) adam_chunk<GD, -1>(a, p, g, m, v, copy);
+  else if (copy.dtype == DFX_BF16) adam_chunk<GD, DFX_BF16>(a, p, g, m, v, copy);
+  else if (copy.dtype == DFX_F16) adam_chunk<GD, DFX_F16>(a, p, g, m, v, copy);
+  else adam_chunk<GD, DFX_F32>(a, p, g, m, v, copy);
+}
+
+__global__ void __launch_bounds__(kThreads) dfx_adamw_kernel(AdamArgs a) {
+  float f = a.scale, lr = a.lr, c1 = a.correct1, c2 = a.correct2;
+  if (a.norm) {
+    const float norm = *a.norm;
+    if (!(norm < INFINITY)) return;       // (infinite or NaN: the gradients overflowed, the step is left out)
+    f = clip_factor(norm, a.max_norm, a.scale);
+  }
+  if (a.lr_dev) lr = *a.lr_dev;
+  if (a.step_dev) {
+    const double t = (double)*a.step_dev;
+    c1 = (float)(1.0 / (1.0 - pow(a.beta1_d, t)));
+    c2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2_d, t)));
+  }
+  const AdamRates r = {f, 1.0f - lr * a.decay, a.beta1, a.one_beta1, a.beta2, a.one_beta2, lr * c1, c2, a.eps};
+  for (uint32_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
+    const ListChunk p = a.p[c], g = a.g[c], m = a.m[c], v = a.v[c], copy = a.copy ? a.copy[c] : ListChunk{0, 0, 0};
+    if (g.dtype == DFX_F32) adam_chunk_copy<DFX_F32>(r, p, g, m, v, copy, a.copy != nullptr);
+    else if (g.dtype == DFX_BF16) adam_chunk_copy<DFX_BF16>(r, p, g, m, v, copy, a.copy != nullptr);
+    else adam_chunk_copy<DFX_F16>(r, p, g, m, v, copy, a.copy != nullptr);
+  }
+}
+
+__global__ void dfx_zero_norm_kernel(float* norm) { *norm = 0.0f; }
+
+// ------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------
+bool on_its_device(const dfx_list* l) {
+  int device = -1;
+  return hipGetDevice(&device) == hipSuccess && device == l->device;
+}
+
+bool same_counts(const dfx_list* a, const dfx_list* b) {
+  if (a == b) return true;
+  if (a->device != b->device || a->tensors.size() != b->tensors.size()) return false;
+  for (size_t k = 0; k < a->tensors.size(); ++k)
+    if (a->tensors[k].count != b->tensors[k].count) return false;
+  return true;
+}
+
+bool all_f32(const dfx_list* l) {
+  for (const dfx_tensor& t : l->tensors)
+    if (t.dtype != DFX_F32) return false;
+  return true;
+}
+
+uint32_t stream_groups(uint32_t nchunks) { return std::min<uint32_t>(nchunks, 256u * 8u); }
+
+int launched() { return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP; }
+
+int check_norm(const dfx_list* l, int kind, double scale, const float* norm) {
+  if (!l || !norm || ((uintptr_t)norm & 3u) || (kind != DFX_NORM_2 && kind != DFX_NORM_INF) || !isfinite(scale)) return DFX_ERR_INVALID_ARG;
+  return on_its_device(l) ? DFX_OK : DFX_ERR_INVALID_ARG;
+}
+
+int check_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale) {
+  if (!src || !norm || ((uintptr_t)norm & 3u) || !(max_norm > 0.0) || !isfinite(scale)) return DFX_ERR_INVALID_ARG;
+  if (dst && dst != src) {
+    if (!same_counts(src, dst)) return DFX_ERR_INVALID_ARG;
+    for (size_t k = 0; k < src->tensors.size(); ++k) {       // the same tensor, or apart from it
+      const dfx_tensor &s = src->tensors[k], &d = dst->tensors[k];
+      const uintptr_t a = (uintptr_t)s.ptr, b = (uintptr_t)d.ptr;
+      if (s.count && a < b + d.count * step_elem_bytes(d.dtype) && b < a + s.count * step_elem_bytes(s.dtype) && !(a == b && s.dtype == d.dtype)) return DFX_ERR_INVALID_ARG;
+    }
+  }
+  return on_its_device(src) ? DFX_OK : DFX_ERR_INVALID_ARG;
+}
+
+int launch_norm(const dfx_list* l, int kind, double scale, float* norm, hipStream_t stream) {
+  if (!l->nchunks) {
+    hipLaunchKernelGGL(dfx_zero_norm_kernel, dim3(1), dim3(1), 0, stream, norm);
+    return launched();
+  }
+  const dim3 grid(std::min<uint32_t>(l->nchunks, (uint32_t)kNormGroups));
+  if (kind == DFX_NORM_2) hipLaunchKernelGGL(dfx_norm_kernel<false>, grid, dim3(kThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
+  else hipLaunchKernelGGL(dfx_norm_kernel<true>, grid, dim3(kThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
+  return launched();
+}
+
+int launch_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale, hipStream_t stream) {
+  if (!dst) dst = src;
+  if (!src->nchunks) return DFX_OK;
+  hipLaunchKernelGGL(dfx_clip_kernel, dim3(stream_groups(src->nchunks)), dim3(kThreads), 0, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n) {
+  if (out) *out = nullptr;
+  if (!out || n < 0 || (n && !tensors)) return DFX_ERR_INVALID_ARG;
+  uint64_t nchunks = 0;
+  for (int k = 0; k < n; ++k) {
+    const dfx_tensor& t = tensors[k];
+    if (t.reserved0 || (t.dtype != DFX_F32 && t.dtype != DFX_BF16 && t.dtype != DFX_F16)) return DFX_ERR_INVALID_ARG;
+    if (t.count && (!t.ptr || ((uintptr_t)t.ptr % step_elem_bytes(t.dtype)))) return DFX_ERR_INVALID_ARG;
+    if (t.count > (SIZE_MAX >> 4)) return DFX_ERR_TOO_LARGE;
+    nchunks += (t.count + kChunk - 1) / kChunk;
+    if (nchunks > 0x7fffffffu) return DFX_ERR_TOO_LARGE;
+  }
+  dfx_list* l = nullptr;
+  int rc = DFX_OK;
+  try {
+    l = new dfx_list;
+    l->tensors.assign(tensors, tensors + n);
+    l->nchunks = (uint32_t)nchunks;
+    // scratch in front, zeroed with the table's upload
+    const size_t at = (sizeof(ListScratch) + 255) / 256 * 256, bytes = at + nchunks * sizeof(ListChunk);
+    std::vector<unsigned char> host(bytes, 0);
+    ListChunk* c = (ListChunk*)(host.data() + at);
+    for (const dfx_tensor& t : l->tensors)
+      for (size_t i = 0; i < t.count; i += kChunk) *c++ = {(uint64_t)(uintptr_t)t.ptr + i * step_elem_bytes(t.dtype), (uint32_t)std::min<size_t>(kChunk, t.count - i), (int32_t)t.dtype};
+    unsigned char* dev = nullptr;
+    if (hipGetDevice(&l->device) != hipSuccess || hipMalloc((void**)&dev, bytes) != hipSuccess) rc = DFX_ERR_HIP;
+    else {
+      l->scratch = (ListScratch*)dev;
+      l->chunks = (ListChunk*)(dev + at);
+      if (hipMemcpy(dev, host.data(), bytes, hipMemcpyHostToDevice) != hipSuccess) rc = DFX_ERR_HIP;
+    }
+  } catch (const std::bad_alloc&) {
+    rc = DFX_ERR_NO_RESOURCES;
+  }
+  if (rc != DFX_OK) {
+    if (l && l->scratch) (void)hipFree(l->scratch);
+    delete l;
+    return rc;
+  }
+  *out = l;
+  return DFX_OK;
+}
+
+int dfx_list_destroy(dfx_list* l) {
+  if (!l) return DFX_ERR_INVALID_ARG;
+  const hipError_t e = hipFree(l->scratch);
+  delete l;
+  return e == hipSuccess ? DFX_OK : DFX_ERR_HIP;
+}
+
+int dfx_grad_norm(dfx_list* grads, dfx_norm_kind kind, double grad_scale, float* norm_dev, void* hip_stream) {
+  const int rc = check_norm(grads, kind, grad_scale, norm_dev);
+  return rc != DFX_OK ? rc : launch_norm(grads, kind, grad_scale, norm_dev, (hipStream_t)hip_stream);
+}
+
+int dfx_grad_clip(dfx_list* src, dfx_list* dst, const float* norm_dev, double max_norm, double grad_scale, void* hip_stream) {
+  const int rc = check_clip(src, dst, norm_dev, max_norm, grad_scale);
+  return rc != DFX_OK ? rc : launch_clip(src, dst, norm_dev, max_norm, grad_scale, (hipStream_t)hip_stream);
+}
+
+int dfx_clip_grad_norm(dfx_list* src, dfx_list* dst, dfx_norm_kind kind, double max_norm, double grad_scale, float* norm_dev, void* hip_stream) {
+  int rc = check_norm(src, kind, grad_scale, norm_dev);
+  if (rc == DFX_OK) rc = check_clip(src, dst, norm_dev, max_norm, grad_scale);
+  if (rc == DFX_OK) rc = launch_norm(src, kind, grad_scale, norm_dev, (hipStream_t)hip_stream);
+  return rc != DFX_OK ? rc : launch_clip(src, dst, norm_dev, max_norm, grad_scale, (hipStream_t)hip_stream);
+}
+
+int dfx_adamw_default(dfx_adamw_config* cfg) {
+  if (!cfg) return DFX_ERR_INVALID_ARG;
+  memset(cfg, 0, sizeof(*cfg));
+  cfg->struct_bytes = sizeof(*cfg);
+  cfg->step = 1;
+  cfg->lr = 1e-3; cfg->beta1 = 0.9; cfg->beta2 = 0.999; cfg->eps = 1e-8; cfg->weight_decay = 0.01;
+  cfg->grad_scale = 1.0; cfg->max_norm = 1.0;
+  return DFX_OK;
+}
+
+int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* exp_avg_sq, dfx_list* copies, const dfx_adamw_config* cfg, const float* norm_dev, void* hip_stream) {
+  if (!params || !grads || !exp_avg || !exp_avg_sq || !cfg || cfg->struct_bytes != sizeof(*cfg)) return DFX_ERR_INVALID_ARG;
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps >= 0.0) || !isfinite(cfg->eps) || !isfinite(cfg->lr) ||
+      !isfinite(cfg->weight_decay) || !isfinite(cfg->grad_scale) || (!cfg->step_dev && !cfg->step) || (norm_dev && !(cfg->max_norm > 0.0)))
+    return DFX_ERR_INVALID_ARG;
+  if (((uintptr_t)norm_dev & 3u) || ((uintptr_t)cfg->step_dev & 3u) || ((uintptr_t)cfg->lr_dev & 3u)) return DFX_ERR_INVALID_ARG;
+  if (!same_counts(params, grads) || !same_counts(params, exp_avg) || !same_counts(params, exp_avg_sq) || (copies && !same_counts(params, copies))) return DFX_ERR_INVALID_ARG;
+  if (params == exp_avg || params == exp_avg_sq || exp_avg == exp_avg_sq || params == grads || grads == exp_avg || grads == exp_avg_sq || (copies && (copies == params || copies == grads || copies == exp_avg || copies == exp_avg_sq))) return DFX_ERR_INVALID_ARG;
+  if (!all_f32(params) || !all_f32(exp_avg) || !all_f32(exp_avg_sq) || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
+  if (!params->nchunks) return DFX_OK;
+  AdamArgs a;
+  memset(&a, 0, sizeof(a));
+  a.p = params->chunks; a.g = grads->chunks; a.m = exp_avg->chunks; a.v = exp_avg_sq->chunks; a.copy = copies ? copies->chunks : nullptr;
+  a.nchunks = params->nchunks;
+  a.norm = norm_dev; a.step_dev = cfg->step_dev; a.lr_dev = cfg->lr_dev;
+  a.beta1_d = cfg->beta1; a.beta2_d = cfg->beta2;
+  a.lr = (float)cfg->lr; a.beta1 = (float)cfg->beta1; a.beta2 = (float)cfg->beta2;
+  a.one_beta1 = (float)(1.0 - cfg->beta1); a.one_beta2 = (float)(1.0 - cfg->beta2);
+  a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = (float)cfg->max_norm;
+  a.correct1 = (float)(1.0 / (1.0 - pow(cfg->beta1, (double)cfg->step)));
+  a.correct2 = (float)(1.0 / sqrt(1.0 - pow(cfg->beta2, (double)cfg->step)));
+  hipLaunchKernelGGL(dfx_adamw_kernel, dim3(stream_groups(a.nchunks)), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+  return launched();
+}
+
+}  // extern "C"
