@@ -467,7 +467,7 @@ typedef enum { DFX_NORM_2 = 0, DFX_NORM_INF = 1 } dfx_norm_kind;
 /*
  * Make a list of n >= 0 tensors (host array, read during the call) on the current device; types may differ from tensor to tensor.
  * Allocates device memory (16 bytes per 8192 elements, and 16 KiB) and waits for its upload.
- * Errors: INVALID_ARG (type, NULL or misaligned ptr), TOO_LARGE (above 2^31 chunks of 8192 elements), NO_RESOURCES, HIP.
+ * Errors: INVALID_ARG (type, NULL or misaligned ptr), TOO_LARGE (2^30 chunks of 8192 elements and more), NO_RESOURCES, HIP.
  */
 int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n);
 /* Free what the list holds (not the tensors).  No call on it may be running. */

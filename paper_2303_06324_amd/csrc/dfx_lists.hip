@@ -17,8 +17,13 @@
 namespace {
 
 constexpr uint32_t kChunk = 8192;        // elements
-constexpr int kThreads = 256;
-constexpr int kNormGroups = 2048;        // workgroups of a norm, at most: each leaves one partial result
+constexpr int kNormThreads = 512;
+constexpr int kNormGroups = 512;         // workgroups of a norm, at most: each leaves one partial result
+constexpr int kClipThreads = 1024;
+constexpr int kAdamThreads = 1024;
+constexpr int kAdamParts = 2;            // workgroups that share a chunk
+constexpr uint32_t kAdamStaged = 640;    // chunks from which on a thread's loads wait for one another
+constexpr uint32_t kMaxGroups = 1u << 20;      // (a grid's threads are counted in 32 bits; workgroups of longer lists take several chunks)
 
 struct ListChunk { uint64_t ptr; uint32_t n; int32_t dtype; };
 static_assert(sizeof(ListChunk) == 16, "a chunk is one 16-byte load");
@@ -44,30 +49,44 @@ namespace {
 // norm: sum of squares (or the largest magnitude) over all elements
 //
 // Squares and their sum are held in 64 bits: no gradient of 32 or 16 bits is too large or too small to be squared there, so no second,
-// scaled pass is needed.
+// scaled pass is needed, and the products cost nothing beside the reads (with sums in 32 bits the times are the same).
+//
+// HBM bounds it.  Two workgroups a compute unit, all loads of a chunk under way at once: sixteen 25 MiB bf16 buckets 70.5 us (5.9 TB/s),
+// 1 GiB of fp32 171 us (6.3 TB/s).  Half as many threads 113 and 195 us; 2048 workgroups of 256, all the waves that fit, 85 and 191 us:
+// what is in flight beyond about 16 MiB only gets in its own way.  A short list is its chain of waits (table, data, ticket): 4.0 us.
 // ------------------------------------------------------------------------------------------
 template <int DT, bool MAXIMUM>
 __device__ __forceinline__ void norm_chunk(const ListChunk& c, double& sum, uint32_t& top) {
-  constexpr int N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  constexpr int N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = (int)kChunk / (N * kNormThreads);
   const void* p = (const void*)c.ptr;
-  const uint32_t nvec = c.n / N;
   auto take = [&](float x) {
     if (MAXIMUM) top = max(top, __float_as_uint(x) & 0x7fffffffu);       // as integers: magnitudes in order, NaN above infinity
     else sum = fma((double)x, (double)x, sum);
   };
-#pragma unroll 4
-  for (uint32_t v = threadIdx.x; v < nvec; v += kThreads) {
-    const auto r = step_load<DT, N>(p, (size_t)v * N);
+  if (c.n == kChunk) {                   // every load of the chunk is under way before the first is waited for
+    StepVec<DT, N> r[U];
 #pragma unroll
-    for (int k = 0; k < N; ++k) take(StepElem<DT>::get(r.x[k]));
+    for (int u = 0; u < U; ++u) r[u].load(p, (size_t)(u * kNormThreads + threadIdx.x) * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < N; ++k) take(r[u].get(k));
+    return;
+  }
+  const uint32_t nvec = c.n / N;
+  for (uint32_t v = threadIdx.x; v < nvec; v += kNormThreads) {
+    StepVec<DT, N> r;
+    r.load(p, (size_t)v * N);
+#pragma unroll
+    for (int k = 0; k < N; ++k) take(r.get(k));
   }
   const uint32_t i = nvec * N + threadIdx.x;
   if (i < c.n) take(step_get<DT>(p, i));
 }
 
 template <bool MAXIMUM>
-__global__ void __launch_bounds__(kThreads) dfx_norm_kernel(const ListChunk* __restrict__ chunks, uint32_t nchunks, ListScratch* scratch, double scale, float* norm) {
-  __shared__ double lds[kThreads / kStepWave];
+__global__ void __launch_bounds__(kNormThreads) dfx_norm_kernel(const ListChunk* __restrict__ chunks, uint32_t nchunks, ListScratch* scratch, double scale, float* norm) {
+  __shared__ double lds[kNormThreads / kStepWave];
   __shared__ uint32_t last;
   double sum = 0.0;
   uint32_t top = 0;
@@ -82,30 +101,46 @@ __global__ void __launch_bounds__(kThreads) dfx_norm_kernel(const ListChunk* __r
     if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave] = w;
     __syncthreads();
     double r = lds[0];
-    for (int k = 1; k < kThreads / kStepWave; ++k) r = MAXIMUM ? fmax(r, lds[k]) : r + lds[k];
+    for (int k = 1; k < kNormThreads / kStepWave; ++k) r = MAXIMUM ? fmax(r, lds[k]) : r + lds[k];
     return r;
   };
-  const double mine = joined();
+  auto norm_of = [&](double r) { return (float)(fabs(scale) * (MAXIMUM ? (double)__uint_as_float((uint32_t)r) : sqrt(r))); };
+  double all = joined();
+  if (gridDim.x == 1) {
+    if (threadIdx.x == 0) *norm = norm_of(all);
+    return;
+  }
   if (threadIdx.x == 0) {
-    __hip_atomic_store(&scratch->part[blockIdx.x], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&scratch->ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1u == gridDim.x;
+    __hip_atomic_store(&scratch->part[blockIdx.x], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (the result is stored past the caches of this XCD and has arrived before the ticket is drawn; a ticket that also writes these caches
+    // back costs 50 ns a workgroup, one after the other)
+    __builtin_amdgcn_s_waitcnt(0);
+    last = __hip_atomic_fetch_add(&scratch->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == gridDim.x;
   }
   __syncthreads();
   if (!last) return;
   // the last workgroup adds up the others' results, in an order that does not depend on who came when
   sum = 0.0; top = 0;
-  for (uint32_t k = threadIdx.x; k < gridDim.x; k += kThreads) {
+  for (uint32_t k = threadIdx.x; k < gridDim.x; k += kNormThreads) {
     const double p = __hip_atomic_load(&scratch->part[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (MAXIMUM) top = max(top, (uint32_t)p);
     else sum += p;
   }
-  const double all = joined();
+  all = joined();
   if (threadIdx.x == 0) {
-    *norm = (float)(fabs(scale) * (MAXIMUM ? (double)__uint_as_float((uint32_t)all) : sqrt(all)));
+    *norm = norm_of(all);
     __hip_atomic_store(&scratch->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// clipping
+//
+// A workgroup per chunk, which ends with it; stores go past the caches, which have nothing to keep of them (into fp32, norm and clipping of
+// the sixteen buckets: 253 us, with ordinary stores 289; of the 253, the clipping takes 182, or 6.9 TB/s).  The chunks are taken from the
+// list's end: the norm has just read them in the other order, and the memory-side cache holds the last 256 MiB of that (from the front,
+// with workgroups of 256: 278 instead of 263 us).
+// ------------------------------------------------------------------------------------------
 // What a gradient is multiplied with: its scale and, where the norm (of the scaled gradients) is above max_norm, the factor that brings
 // it there.  A norm of infinity gives 0 (and NaN from infinite gradients), a norm of NaN gives NaN.
 __device__ __forceinline__ float clip_factor(float norm, float max_norm, float scale) {
@@ -113,20 +148,37 @@ __device__ __forceinline__ float clip_factor(float norm, float max_norm, float s
   return scale * (q > 1.0f ? 1.0f : q);
 }
 
+template <int SD, int DD, int N>
+__device__ __forceinline__ StepVec<DD, N> clip_vector(const StepVec<SD, N>& r, float f) {
+  float x[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k] = r.get(k) * f;
+  StepVec<DD, N> o;
+  o.put(x);
+  return o;
+}
+
 template <int SD, int DD>
 __device__ __forceinline__ void clip_chunk(const ListChunk& s, const ListChunk& d, float f) {
-  constexpr int N = 4;
-  const uint32_t nvec = s.n / N;
-#pragma unroll 4
-  for (uint32_t v = threadIdx.x; v < nvec; v += kThreads) {
-    const auto r = step_load<SD, N>((const void*)s.ptr, (size_t)v * N);
-    float x[N];
+  constexpr int N = 4, U = (int)kChunk / (N * kClipThreads);
+  const void* from = (const void*)s.ptr;
+  void* to = (void*)d.ptr;
+  if (s.n == kChunk) {
+    StepVec<SD, N> r[U];
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = StepElem<SD>::get(r.x[k]) * f;
-    step_store<DD, N>((void*)d.ptr, (size_t)v * N, x);
+    for (int u = 0; u < U; ++u) r[u].load(from, (size_t)(u * kClipThreads + threadIdx.x) * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u) clip_vector<SD, DD, N>(r[u], f).template store<true>(to, (size_t)(u * kClipThreads + threadIdx.x) * N);
+    return;
+  }
+  const uint32_t nvec = s.n / N;
+  for (uint32_t v = threadIdx.x; v < nvec; v += kClipThreads) {
+    StepVec<SD, N> r;
+    r.load(from, (size_t)v * N);
+    clip_vector<SD, DD, N>(r, f).template store<true>(to, (size_t)v * N);
   }
   const uint32_t i = nvec * N + threadIdx.x;
-  if (i < s.n) step_put<DD>((void*)d.ptr, i, step_get<SD>((const void*)s.ptr, i) * f);
+  if (i < s.n) step_put<DD>(to, i, step_get<SD>(from, i) * f);
 }
 
 template <int SD>
@@ -137,10 +189,11 @@ __device__ __forceinline__ void clip_chunk_to(const ListChunk& s, const ListChun
 }
 
 // (src and dst may be the same tensors: no __restrict__ on what the chunks point to)
-__global__ void __launch_bounds__(kThreads) dfx_clip_kernel(const ListChunk* __restrict__ src, const ListChunk* __restrict__ dst, uint32_t nchunks, const float* norm, float max_norm, float scale, bool in_place) {
+__global__ void __launch_bounds__(kClipThreads) dfx_clip_kernel(const ListChunk* __restrict__ src, const ListChunk* __restrict__ dst, uint32_t nchunks, const float* norm, float max_norm, float scale, bool in_place) {
   const float f = clip_factor(*norm, max_norm, scale);
   if (in_place && f == 1.0f) return;      // the gradients are what they are to become
-  for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
+  for (uint32_t k = blockIdx.x; k < nchunks; k += gridDim.x) {
+    const uint32_t c = nchunks - 1u - k;
     const ListChunk s = src[c], d = dst[c];
     if (s.dtype == DFX_F32) clip_chunk_to<DFX_F32>(s, d, f);
     else if (s.dtype == DFX_BF16) clip_chunk_to<DFX_BF16>(s, d, f);
@@ -150,6 +203,12 @@ __global__ void __launch_bounds__(kThreads) dfx_clip_kernel(const ListChunk* __r
 
 // ------------------------------------------------------------------------------------------
 // AdamW
+//
+// HBM bounds it: 26 bytes of a parameter with a 16-bit gradient and copy pass through, 372 M of them in 1740 us (6.0 TB/s).  A thread takes one
+// vector of four of every list and its workgroup ends, which leaves the order of requests to the dispatcher.  The lists of a model lie alike in
+// memory, so a thread's loads go to the same channels at the same moment; in a long list the second waits for the first to arrive, and the
+// others for the second: 1740 instead of 2069 us.  Below about 700 chunks the waits cost more than they give (4 M parameters 19.5 and 19.2
+// us, 8 M 43 and 45, 500 k 4.8 and 4.5).  Persistent workgroups (2048 of 256) 2400 us, with ordinary stores 2540.
 // ------------------------------------------------------------------------------------------
 struct AdamArgs {
   const ListChunk *p, *g, *m, *v, *copy;      // copy: may be null
@@ -171,28 +230,53 @@ __device__ __forceinline__ void adam_element(const AdamRates& a, float& p, float
   p = fmaf(p, a.keep, -(a.rate * m / fmaf(sqrtf(v), a.correct2, a.eps)));
 }
 
-template <int GD, int CD>      // CD < 0: no copy
-__device__ __forceinline__ void adam_chunk(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy) {
-  constexpr int N = 4;
-  constexpr int C = CD < 0 ? DFX_F32 : CD;
-  const uint32_t nvec = p.n / N;
-#pragma unroll 2
-  for (uint32_t k = threadIdx.x; k < nvec; k += kThreads) {
-    const size_t i = (size_t)k * N;
-    const auto rp = step_load<DFX_F32, N>((const void*)p.ptr, i), rm = step_load<DFX_F32, N>((const void*)m.ptr, i), rv = step_load<DFX_F32, N>((const void*)v.ptr, i);
-    const auto rg = step_load<GD, N>((const void*)g.ptr, i);
-    float xp[N], xm[N], xv[N];
+// nothing of what follows is begun before every load so far has arrived
+__device__ __forceinline__ void loads_arrived() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0), the other counters at their largest
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int GD, int CD, bool STAGED>      // CD < 0: no copy
+__device__ __forceinline__ void adam_vector(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, size_t i) {
+  constexpr int N = 4, C = CD < 0 ? DFX_F32 : CD;
+  StepVec<DFX_F32, N> rp, rm, rv;
+  StepVec<GD, N> rg;
+  rp.load((const void*)p.ptr, i);
+  if (STAGED) loads_arrived();
+  rm.load((const void*)m.ptr, i);
+  if (STAGED) loads_arrived();
+  rv.load((const void*)v.ptr, i);
+  rg.load((const void*)g.ptr, i);
+  float xp[N], xm[N], xv[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      xp[j] = __uint_as_float(rp.x[j]); xm[j] = __uint_as_float(rm.x[j]); xv[j] = __uint_as_float(rv.x[j]);
-      adam_element(a, xp[j], StepElem<GD>::get(rg.x[j]), xm[j], xv[j]);
-    }
-    step_store<DFX_F32, N>((void*)p.ptr, i, xp);
-    step_store<DFX_F32, N>((void*)m.ptr, i, xm);
-    step_store<DFX_F32, N>((void*)v.ptr, i, xv);
-    if (CD >= 0) step_store<C, N>((void*)copy.ptr, i, xp);
+  for (int j = 0; j < N; ++j) {
+    xp[j] = rp.get(j); xm[j] = rm.get(j); xv[j] = rv.get(j);
+    adam_element(a, xp[j], rg.get(j), xm[j], xv[j]);
   }
-  const uint32_t i = nvec * N + threadIdx.x;
+  rp.put(xp); rm.put(xm); rv.put(xv);
+  rp.template store<true>((void*)p.ptr, i);
+  rm.template store<true>((void*)m.ptr, i);
+  rv.template store<true>((void*)v.ptr, i);
+  if (CD >= 0) {
+    StepVec<C, N> rc;
+    rc.put(xp);
+    rc.template store<true>((void*)copy.ptr, i);
+  }
+}
+
+template <int GD, int CD, bool STAGED>
+__device__ __forceinline__ void adam_chunk(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, uint32_t part) {
+  constexpr int N = 4, C = CD < 0 ? DFX_F32 : CD;
+  constexpr uint32_t stride = kAdamThreads * kAdamParts;
+  const uint32_t nvec = p.n / N, me = part * kAdamThreads + threadIdx.x;
+  static_assert(kChunk == stride * N, "a whole chunk is a vector for each thread of its workgroups");
+  if (p.n == kChunk) {
+    adam_vector<GD, CD, STAGED>(a, p, g, m, v, copy, me * N);
+    return;
+  }
+  if (me < nvec) adam_vector<GD, CD, STAGED>(a, p, g, m, v, copy, me * N);
+  const uint32_t i = nvec * N + me;
   if (i < p.n) {
     float xp = step_get<DFX_F32>((const void*)p.ptr, i), xm = step_get<DFX_F32>((const void*)m.ptr, i), xv = step_get<DFX_F32>((const void*)v.ptr, i);
     adam_element(a, xp, step_get<GD>((const void*)g.ptr, i), xm, xv);
@@ -203,15 +287,16 @@ __device__ __forceinline__ void adam_chunk(const AdamRates& a, const ListChunk& 
   }
 }
 
-template <int GD>
-__device__ __forceinline__ void adam_chunk_copy(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, bool has_copy) {
-  if (!has_copy) adam_chunk<GD, -1>(a, p, g, m, v, copy);
-  else if (copy.dtype == DFX_BF16) adam_chunk<GD, DFX_BF16>(a, p, g, m, v, copy);
-  else if (copy.dtype == DFX_F16) adam_chunk<GD, DFX_F16>(a, p, g, m, v, copy);
-  else adam_chunk<GD, DFX_F32>(a, p, g, m, v, copy);
+template <int GD, bool STAGED>
+__device__ __forceinline__ void adam_chunk_copy(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, uint32_t part, bool has_copy) {
+  if (!has_copy) adam_chunk<GD, -1, STAGED>(a, p, g, m, v, copy, part);
+  else if (copy.dtype == DFX_BF16) adam_chunk<GD, DFX_BF16, STAGED>(a, p, g, m, v, copy, part);
+  else if (copy.dtype == DFX_F16) adam_chunk<GD, DFX_F16, STAGED>(a, p, g, m, v, copy, part);
+  else adam_chunk<GD, DFX_F32, STAGED>(a, p, g, m, v, copy, part);
 }
 
-__global__ void __launch_bounds__(kThreads) dfx_adamw_kernel(AdamArgs a) {
+template <bool STAGED>
+__global__ void __launch_bounds__(kAdamThreads) dfx_adamw_kernel(AdamArgs a) {
   float f = a.scale, lr = a.lr, c1 = a.correct1, c2 = a.correct2;
   if (a.norm) {
     const float norm = *a.norm;
@@ -225,12 +310,11 @@ __global__ void __launch_bounds__(kThreads) dfx_adamw_kernel(AdamArgs a) {
     c2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2_d, t)));
   }
   const AdamRates r = {f, 1.0f - lr * a.decay, a.beta1, a.one_beta1, a.beta2, a.one_beta2, lr * c1, c2, a.eps};
-  for (uint32_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
-    const ListChunk p = a.p[c], g = a.g[c], m = a.m[c], v = a.v[c], copy = a.copy ? a.copy[c] : ListChunk{0, 0, 0};
-    if (g.dtype == DFX_F32) adam_chunk_copy<DFX_F32>(r, p, g, m, v, copy, a.copy != nullptr);
-    else if (g.dtype == DFX_BF16) adam_chunk_copy<DFX_BF16>(r, p, g, m, v, copy, a.copy != nullptr);
-    else adam_chunk_copy<DFX_F16>(r, p, g, m, v, copy, a.copy != nullptr);
-  }
+  const uint32_t c = blockIdx.x / kAdamParts, part = blockIdx.x % kAdamParts;
+  const ListChunk p = a.p[c], g = a.g[c], m = a.m[c], v = a.v[c], copy = a.copy ? a.copy[c] : ListChunk{0, 0, 0};
+  if (g.dtype == DFX_F32) adam_chunk_copy<DFX_F32, STAGED>(r, p, g, m, v, copy, part, a.copy != nullptr);
+  else if (g.dtype == DFX_BF16) adam_chunk_copy<DFX_BF16, STAGED>(r, p, g, m, v, copy, part, a.copy != nullptr);
+  else adam_chunk_copy<DFX_F16, STAGED>(r, p, g, m, v, copy, part, a.copy != nullptr);
 }
 
 __global__ void dfx_zero_norm_kernel(float* norm) { *norm = 0.0f; }
@@ -256,8 +340,6 @@ bool all_f32(const dfx_list* l) {
     if (t.dtype != DFX_F32) return false;
   return true;
 }
-
-uint32_t stream_groups(uint32_t nchunks) { return std::min<uint32_t>(nchunks, 256u * 8u); }
 
 int launched() { return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP; }
 
@@ -285,15 +367,15 @@ int launch_norm(const dfx_list* l, int kind, double scale, float* norm, hipStrea
     return launched();
   }
   const dim3 grid(std::min<uint32_t>(l->nchunks, (uint32_t)kNormGroups));
-  if (kind == DFX_NORM_2) hipLaunchKernelGGL(dfx_norm_kernel<false>, grid, dim3(kThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
-  else hipLaunchKernelGGL(dfx_norm_kernel<true>, grid, dim3(kThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
+  if (kind == DFX_NORM_2) hipLaunchKernelGGL(dfx_norm_kernel<false>, grid, dim3(kNormThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
+  else hipLaunchKernelGGL(dfx_norm_kernel<true>, grid, dim3(kNormThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
   return launched();
 }
 
 int launch_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale, hipStream_t stream) {
   if (!dst) dst = src;
   if (!src->nchunks) return DFX_OK;
-  hipLaunchKernelGGL(dfx_clip_kernel, dim3(stream_groups(src->nchunks)), dim3(kThreads), 0, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
+  hipLaunchKernelGGL(dfx_clip_kernel, dim3(std::min(src->nchunks, kMaxGroups)), dim3(kClipThreads), 0, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
   return launched();
 }
 
@@ -311,7 +393,7 @@ int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n) {
     if (t.count && (!t.ptr || ((uintptr_t)t.ptr % step_elem_bytes(t.dtype)))) return DFX_ERR_INVALID_ARG;
     if (t.count > (SIZE_MAX >> 4)) return DFX_ERR_TOO_LARGE;
     nchunks += (t.count + kChunk - 1) / kChunk;
-    if (nchunks > 0x7fffffffu) return DFX_ERR_TOO_LARGE;
+    if (nchunks > 0x3fffffffu) return DFX_ERR_TOO_LARGE;
   }
   dfx_list* l = nullptr;
   int rc = DFX_OK;
@@ -388,6 +470,7 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   if (params == exp_avg || params == exp_avg_sq || exp_avg == exp_avg_sq || params == grads || grads == exp_avg || grads == exp_avg_sq || (copies && (copies == params || copies == grads || copies == exp_avg || copies == exp_avg_sq))) return DFX_ERR_INVALID_ARG;
   if (!all_f32(params) || !all_f32(exp_avg) || !all_f32(exp_avg_sq) || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
   if (!params->nchunks) return DFX_OK;
+  if (params->nchunks > kMaxGroups) return DFX_ERR_TOO_LARGE;
   AdamArgs a;
   memset(&a, 0, sizeof(a));
   a.p = params->chunks; a.g = grads->chunks; a.m = exp_avg->chunks; a.v = exp_avg_sq->chunks; a.copy = copies ? copies->chunks : nullptr;
@@ -399,7 +482,9 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = (float)cfg->max_norm;
   a.correct1 = (float)(1.0 / (1.0 - pow(cfg->beta1, (double)cfg->step)));
   a.correct2 = (float)(1.0 / sqrt(1.0 - pow(cfg->beta2, (double)cfg->step)));
-  hipLaunchKernelGGL(dfx_adamw_kernel, dim3(stream_groups(a.nchunks)), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+  const dim3 grid(a.nchunks * kAdamParts);
+  if (a.nchunks >= kAdamStaged) hipLaunchKernelGGL(dfx_adamw_kernel<true>, grid, dim3(kAdamThreads), 0, (hipStream_t)hip_stream, a);
+  else hipLaunchKernelGGL(dfx_adamw_kernel<false>, grid, dim3(kAdamThreads), 0, (hipStream_t)hip_stream, a);
   return launched();
 }
 

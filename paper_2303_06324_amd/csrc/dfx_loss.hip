@@ -91,10 +91,11 @@ __global__ void __launch_bounds__(THREADS) dfx_loss_rows_kernel(LossArgs a) {
     float zt = 0.0f;
     if (counts) {
       for (uint32_t v = threadIdx.x; v < nvec; v += THREADS) {
-        const auto r = step_load<DT, N>(z, (size_t)v * N);
+        StepVec<DT, N> r;
+        r.load(z, (size_t)v * N);
         float x[N], m = ms.m;
 #pragma unroll
-        for (int k = 0; k < N; ++k) { x[k] = StepElem<DT>::get(r.x[k]); m = fmaxf(m, x[k]); }
+        for (int k = 0; k < N; ++k) { x[k] = r.get(k); m = fmaxf(m, x[k]); }
         const float base = loss_base(m);
         float s = ms.s * loss_exp(ms.m, base, a.c_log2e);
 #pragma unroll
@@ -134,11 +135,14 @@ __global__ void __launch_bounds__(THREADS) dfx_loss_rows_kernel(LossArgs a) {
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] = 0.0f;
       } else {
-        const auto r = step_load<DT, N>(z, (size_t)v * N);
+        StepVec<DT, N> r;
+        r.load(z, (size_t)v * N);
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = gs * loss_exp(StepElem<DT>::get(r.x[k]), m, a.c_log2e) + (v * N + k == t ? g : 0.0f);
+        for (int k = 0; k < N; ++k) x[k] = gs * loss_exp(r.get(k), m, a.c_log2e) + (v * N + k == t ? g : 0.0f);
       }
-      step_store<DT, N>(out, (size_t)v * N, x);
+      StepVec<DT, N> o;
+      o.put(x);
+      o.store(out, (size_t)v * N);
     }
     if (rest < a.vocab) step_put<DT>(out, rest, nothing ? 0.0f : gs * loss_exp(step_get<DT>(z, rest), m, a.c_log2e) + (rest == t ? g : 0.0f));
   }

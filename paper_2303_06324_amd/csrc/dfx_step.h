@@ -16,9 +16,16 @@ constexpr int kStepWave = 64;
 __host__ __device__ inline uint32_t step_elem_bytes(int dtype) { return dtype == DFX_F32 ? 4u : 2u; }
 
 // A tensor starts at any multiple of its element's size (views into a bucket lie one behind the other), so a vector of elements is read
-// and written wherever it begins: gfx950 takes global accesses of any alignment, and such a type says that they may be.
-template <class T, int N>
-struct __attribute__((packed, aligned(1))) StepVec { T x[N]; };
+// and written wherever it begins: gfx950 takes global accesses of any alignment, and these types say that they may be.
+typedef uint32_t StepWords2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t StepWords4 __attribute__((ext_vector_type(4), aligned(2)));
+template <int WORDS> struct StepWordsOf;
+template <> struct StepWordsOf<2> { typedef StepWords2 type; };
+template <> struct StepWordsOf<4> { typedef StepWords4 type; };
+
+// Addresses come out of tables and argument blocks: said to be global ones, accesses take global instructions, which are waited for on one
+// counter, where a generic pointer would take flat ones.
+#define STEP_GLOBAL __attribute__((address_space(1)))
 
 template <int DT> struct StepElem;
 template <> struct StepElem<DFX_F32> {
@@ -34,26 +41,54 @@ template <> struct StepElem<DFX_BF16> {
 template <> struct StepElem<DFX_F16> {
   typedef uint16_t raw;
   static __device__ __forceinline__ float get(raw v) { return (float)__builtin_bit_cast(_Float16, v); }
-  static __device__ __forceinline__ raw put(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+  // (of the 32-bit value: left to itself the compiler takes an operation and this conversion as one, whose result differs where the
+  // 32-bit one is stored as well)
+  static __device__ __forceinline__ raw put(float v) {
+    asm("" : "+v"(v));
+    return __builtin_bit_cast(uint16_t, (_Float16)v);
+  }
 };
 
 template <int DT>
-__device__ __forceinline__ float step_get(const void* p, size_t i) { return StepElem<DT>::get(((const StepVec<typename StepElem<DT>::raw, 1>*)p)[i].x[0]); }
+__device__ __forceinline__ float step_get(const void* p, size_t i) {
+  typedef typename StepElem<DT>::raw raw;
+  return StepElem<DT>::get(*((const STEP_GLOBAL raw*)p + i));
+}
 template <int DT>
-__device__ __forceinline__ void step_put(void* p, size_t i, float v) { ((StepVec<typename StepElem<DT>::raw, 1>*)p)[i].x[0] = StepElem<DT>::put(v); }
+__device__ __forceinline__ void step_put(void* p, size_t i, float v) {
+  typedef typename StepElem<DT>::raw raw;
+  *((STEP_GLOBAL raw*)p + i) = StepElem<DT>::put(v);
+}
 
-// N elements at element i
+// N elements from element i on, as words; what is read or written once and is larger than the caches goes past them (STREAM)
 template <int DT, int N>
-__device__ __forceinline__ StepVec<typename StepElem<DT>::raw, N> step_load(const void* p, size_t i) {
-  return *(const StepVec<typename StepElem<DT>::raw, N>*)((const typename StepElem<DT>::raw*)p + i);
-}
-template <int DT, int N>
-__device__ __forceinline__ void step_store(void* p, size_t i, const float* v) {
-  StepVec<typename StepElem<DT>::raw, N> r;
+struct StepVec {
+  typedef typename StepElem<DT>::raw raw;
+  typedef typename StepWordsOf<N * (int)sizeof(raw) / 4>::type words;
+  words w;
+
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const void* p, size_t i) {
+    const STEP_GLOBAL words* q = (const STEP_GLOBAL words*)((const STEP_GLOBAL raw*)p + i);
+    w = STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  template <bool STREAM = false>
+  __device__ __forceinline__ void store(void* p, size_t i) const {
+    STEP_GLOBAL words* q = (STEP_GLOBAL words*)((STEP_GLOBAL raw*)p + i);
+    if (STREAM) __builtin_nontemporal_store(w, q);
+    else *q = w;
+  }
+  __device__ __forceinline__ float get(int k) const {
+    if (DT == DFX_F32) return StepElem<DT>::get((raw)w[k]);
+    if (DT == DFX_BF16) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+    return StepElem<DT>::get((raw)(k & 1 ? w[k / 2] >> 16 : w[k / 2]));
+  }
+  __device__ __forceinline__ void put(const float* v) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) r.x[k] = StepElem<DT>::put(v[k]);
-  *(StepVec<typename StepElem<DT>::raw, N>*)((typename StepElem<DT>::raw*)p + i) = r;
-}
+    for (int k = 0; k < N * (int)sizeof(raw) / 4; ++k)
+      w[k] = DT == DFX_F32 ? (uint32_t)StepElem<DT>::put(v[k]) : (uint32_t)StepElem<DT>::put(v[2 * k]) | ((uint32_t)StepElem<DT>::put(v[2 * k + 1]) << 16);
+  }
+};
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
