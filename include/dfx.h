@@ -547,11 +547,12 @@ typedef struct {
   float* logp;               /* [rows], may be NULL */
   float* loss;               /* [rows], may be NULL */
   float* sums;               /* 5 values, may be NULL: sums over the rows of weight times loss / weight, pg, kl, [clipped], 1 */
-  void* workspace;           /* dfx_policy_loss_workspace bytes, 8-byte aligned; nothing in it has to outlive the call's work */
+  void* workspace;           /* dfx_policy_loss_workspace bytes, 8-byte aligned; nothing in it has to outlive the call's work.  May be
+                                NULL without sums, which makes a few rows of a long vocabulary slower */
   size_t workspace_bytes;
   double clip_low, clip_high; /* 0 <= clip_low <= 1, 0 <= clip_high */
   double kl_coef;            /* needs ref_logp where it is not 0 */
-  double inv_temperature;    /* > 0 */
+  double inv_temperature;    /* > 0, and 1.45 times it a normal number in 32 bits */
 } dfx_policy_loss_args;
 
 /* Bytes of workspace for calls of up to so many rows of this length and type (host only, no GPU needed). */

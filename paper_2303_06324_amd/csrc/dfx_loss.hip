@@ -2,6 +2,7 @@
 //
 // A row's softmax is taken around its largest logit m: S = sum exp(c (z - m)), logp = c (z_t - m) - log S, and the gradient of z_j is
 // g ([j = t] - exp(c (z_j - m)) / S) with one number g for the row.  So a row is read, reduced to (m, S), and written once g is known.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -13,9 +14,17 @@
 
 namespace {
 
-constexpr uint32_t kGroups = 2048;       // workgroups of a call, at most: each leaves its share of the sums
 constexpr int kSums = 5;
-constexpr int kSumThreads = 256;
+constexpr uint32_t kGroups = 4096;       // workgroups of a call, at most: each leaves its share of the sums
+constexpr int kSumWaves = 3;             // waves that share a sum
+constexpr int kSumThreads = kSums * kSumWaves * kStepWave;
+// Few rows of a long vocabulary are split over workgroups.
+constexpr int kSplitThreads = 256;
+constexpr uint32_t kSplitGroups = 512;   // workgroups, at most
+constexpr uint32_t kSplitRows = 64;      // rows, at most
+constexpr uint32_t kSplitGrad = 40000, kSplitForward = 65536;      // elements of a row, at least
+
+struct LossPart { float m, s, zt, none; };      // of a segment of a row; zt: the target's logit, where the segment has it
 
 struct LossArgs {
   const void* logits;
@@ -24,49 +33,104 @@ struct LossArgs {
   const int64_t* targets;
   const float *old_logp, *ref_logp, *advantage, *weight, *scale;
   float *logp, *loss, *sums;
-  double* part;                          // [workgroups][kSums]
+  double* part;                          // [kSums][workgroups]
+  LossPart* parts;                       // [rows][segments], where rows are split
   uint32_t rows, vocab;
-  double clip_low, clip_high, kl_coef, c;
-  float c_log2e;                         // c / log 2: exponents are taken to base 2
+  double c;                              // 1 / temperature
+  float least, most, kl_coef;            // 1 - clip_low, 1 + clip_high
+  float k;                               // c / log 2: exponents are taken to base 2
 };
 
-// exp(c (z - m)): the difference first, which is exact where it matters and cannot overflow for logits of the type's lowest value
-__device__ __forceinline__ float loss_exp(float z, float m, float c_log2e) { return __builtin_amdgcn_exp2f((z - m) * c_log2e); }
+// exp(c (z - m)) = 2^(k (z - m)), k = c / log 2.  The difference first: it is 0 for the largest logit, exact where it matters, and cannot
+// overflow for logits of the type's lowest or largest value.
+struct MaxSum { float m, s; };           // s = sum 2^(k (z - m)); nothing seen yet: m = -infinity, s = 0
 
-struct MaxSum { float m, s; };           // s = sum exp(c (z - m)); nothing seen yet: m = -infinity, s = 0
-
-// m to take differences from: of a row that has only seen -infinity, any finite one (exp(-infinity - 0) = 0, and NaN stays NaN)
+// m to take differences from: where only -infinity was seen, any finite one (2^(-infinity - 0) = 0, and NaN stays NaN)
 __device__ __forceinline__ float loss_base(float m) { return m == -INFINITY ? 0.0f : m; }
+__device__ __forceinline__ float loss_exp(float z, float base, float k) { return __builtin_amdgcn_exp2f((z - base) * k); }
 
-__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c_log2e) {
-  const float m = fmaxf(a.m, b.m), base = loss_base(m);
-  return {m, a.s * loss_exp(a.m, base, c_log2e) + b.s * loss_exp(b.m, base, c_log2e)};
+// over the first N of each 64 lanes' entries, for all of them
+template <int N>
+__device__ __forceinline__ MaxSum join_lanes(MaxSum ms, float k) {
+  float top = ms.m;
+#pragma unroll
+  for (int d = N / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  ms.s *= loss_exp(ms.m, loss_base(top), k);
+#pragma unroll
+  for (int d = N / 2; d; d >>= 1) ms.s += __shfl_xor(ms.s, d);
+  return {top, ms.s};
 }
 
-// What a row comes to, by one thread.  In 64 bits: a logp of -10 holds no more than 5e-7 in 32, which would be the ratio's error.
-struct RowEnd { double logp, loss, pg, kl, clipped, w; float g; };
+// over a workgroup of T threads, for all of them; one barrier.  lds: T / 64 entries that nobody reads any more
+template <int T>
+__device__ __forceinline__ MaxSum join_all(MaxSum ms, float k, MaxSum* lds) {
+  ms = join_lanes<kStepWave>(ms, k);
+  if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave] = ms;
+  __syncthreads();
+  return join_lanes<T / kStepWave>(lds[threadIdx.x % (T / kStepWave)], k);      // every wave joins them once more, an entry a lane
+}
 
-__device__ __forceinline__ RowEnd row_end(const LossArgs& a, uint32_t row, MaxSum ms, float zt) {
-  RowEnd e = {0, 0, 0, 0, 0, 0, 0};
-  if (ms.s == 0.0f) return e;            // no logit above -infinity
-  e.logp = a.c * ((double)zt - (double)loss_base(ms.m)) - log((double)ms.s);
+constexpr double kLog2 = 0.69314718055994530942, kLog2e = 1.44269504088896340736;
+
+__device__ __forceinline__ float loss_exp_of(double x) { return __builtin_amdgcn_exp2f((float)(x * kLog2e)); }
+
+// exp(d) - 1 - d: where that cancels by its series, whose next term is d^10 / 10! (d = 1/2: 3e-10 of 0.15)
+__device__ __forceinline__ float loss_penalty(double d) {
+  const float x = (float)d;
+  if (fabsf(x) > 0.5f) return (float)((double)loss_exp_of(d) - 1.0 - d);
+  float r = 1.0f / 362880.0f;
+  r = fmaf(r, x, 1.0f / 40320.0f);
+  r = fmaf(r, x, 1.0f / 5040.0f);
+  r = fmaf(r, x, 1.0f / 720.0f);
+  r = fmaf(r, x, 1.0f / 120.0f);
+  r = fmaf(r, x, 1.0f / 24.0f);
+  r = fmaf(r, x, 1.0f / 6.0f);
+  r = fmaf(r, x, 0.5f);
+  return r * x * x;
+}
+
+// What a row comes to.  far: z_t - m in 64 bits; s: the sum around that m.  log2 s = e + log2 f, f in [1/2, 1): what 32 bits lose there is
+// 6e-8 of a logarithm, the sum's own error is more.  Differences of log-probabilities are taken in 64 bits (a logp of -10 holds 5e-7 in
+// 32, which would be the ratio's error), what is made of them in 32.
+struct RowValue { float logp, loss, pg, kl, clipped, w, g; };      // pg, kl, clipped times the weight w; nothing: all 0
+
+__device__ __forceinline__ RowValue row_value(const LossArgs& a, uint32_t row, double far, float s) {
+  RowValue e = {0, 0, 0, 0, 0, 0, 0};
+  if (s == 0.0f) return e;               // no logit above -infinity
+  int two;
+  const float f = frexpf(s, &two);
+  const double logp = a.c * far - ((double)two + (double)__builtin_amdgcn_logf(f)) * kLog2;
+  e.logp = (float)logp;
   if (!a.advantage) return e;
-  e.w = a.weight ? (double)a.weight[row] : 1.0;
-  const double A = (double)a.advantage[row];
-  const double r = a.old_logp ? exp(e.logp - (double)a.old_logp[row]) : 1.0;
-  const bool clipped = A >= 0.0 ? r > 1.0 + a.clip_high : r < 1.0 - a.clip_low;
-  const double used = clipped ? (A >= 0.0 ? 1.0 + a.clip_high : 1.0 - a.clip_low) : r;
-  e.pg = e.w * (-A * used);
-  double slope = clipped ? 0.0 : -A * r;
+  e.w = a.weight ? a.weight[row] : 1.0f;
+  const float A = a.advantage[row], r = a.old_logp ? loss_exp_of(logp - (double)a.old_logp[row]) : 1.0f;
+  const bool up = A >= 0.0f, clipped = up ? r > a.most : r < a.least;
+  const float pg = -A * (clipped ? up ? a.most : a.least : r);
+  float slope = clipped ? 0.0f : -A * r, kl = 0.0f;
   if (a.ref_logp) {
-    const double d = (double)a.ref_logp[row] - e.logp, x = expm1(d);
-    e.kl = e.w * (x - d);
-    slope -= a.kl_coef * x;
+    const double d = (double)a.ref_logp[row] - logp;
+    kl = loss_penalty(d);
+    slope -= a.kl_coef * (float)(d + (double)kl);
   }
-  e.clipped = clipped ? e.w : 0.0;
-  e.loss = e.pg + a.kl_coef * e.kl;
-  e.g = (float)(a.c * e.w * slope * (a.scale ? (double)*a.scale : 1.0));
+  e.pg = e.w * pg; e.kl = e.w * kl; e.clipped = clipped ? e.w : 0.0f;
+  e.loss = e.w * fmaf(a.kl_coef, kl, pg);
+  e.g = (float)a.c * e.w * slope * (a.scale ? *a.scale : 1.0f);
   return e;
+}
+
+__device__ __forceinline__ void add_sums(double* sums, const RowValue& e) {
+  sums[0] += (double)e.loss; sums[1] += (double)e.pg; sums[2] += (double)e.kl; sums[3] += (double)e.clipped; sums[4] += (double)e.w;
+}
+
+// ... by every thread alike; one of them writes it down.  Returns g
+__device__ __forceinline__ float row_end(const LossArgs& a, uint32_t row, double far, float s, bool writes, double* sums) {
+  const RowValue e = row_value(a, row, far, s);
+  if (writes) {
+    if (a.logp) a.logp[row] = e.logp;
+    if (a.loss) a.loss[row] = e.loss;
+    if (sums) add_sums(sums, e);
+  }
+  return e.g;
 }
 
 // whether a row has anything to learn from, by what is known before its logits
@@ -75,105 +139,289 @@ __device__ __forceinline__ bool row_counts(const LossArgs& a, uint32_t row) {
   return t >= 0 && t < (int64_t)a.vocab && (!a.weight || a.weight[row] != 0.0f);
 }
 
-template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS) dfx_loss_rows_kernel(LossArgs a) {
-  typedef typename StepElem<DT>::raw raw;
-  constexpr int N = 16 / (int)sizeof(raw), WAVES = THREADS / kStepWave;
-  __shared__ MaxSum lds[WAVES];
-  __shared__ float row_g, row_m, row_s;
-  const uint32_t nvec = a.vocab / N, rest = nvec * N + threadIdx.x;
-  double sums[kSums] = {0, 0, 0, 0, 0};
-  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
-    raw* out = a.grad ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
-    const bool counts = row_counts(a, row);
-    MaxSum ms = {-INFINITY, 0.0f};
-    float zt = 0.0f;
-    if (counts) {
-      for (uint32_t v = threadIdx.x; v < nvec; v += THREADS) {
-        StepVec<DT, N> r;
-        r.load(z, (size_t)v * N);
-        float x[N], m = ms.m;
+// what of a row is in vectors, joined into ms
+template <int DT, int N, int U>
+__device__ __forceinline__ void take_vectors(StepVec<DT, N>* r, float k, MaxSum& ms) {
+  float z = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < N; ++k) { x[k] = r.get(k); m = fmaxf(m, x[k]); }
-        const float base = loss_base(m);
-        float s = ms.s * loss_exp(ms.m, base, a.c_log2e);
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int k = 0; k < N; ++k) s += loss_exp(x[k], base, a.c_log2e);
-        ms = {m, s};
-      }
-      if (rest < a.vocab) {
-        const float x = step_get<DT>(z, rest);
-        ms = join(ms, {x, x == -INFINITY ? 0.0f : 1.0f}, a.c_log2e);
-      }
-      if (threadIdx.x == 0) zt = step_get<DT>(z, (size_t)a.targets[row]);
+    for (int j = 0; j < N; ++j) z = fmaxf(z, r[u].get(j));
+  const float m = fmaxf(ms.m, z), base = loss_base(m);
+  float s = ms.s * loss_exp(ms.m, base, k);
 #pragma unroll
-      for (int d = kStepWave / 2; d; d >>= 1) ms = join(ms, {__shfl_xor(ms.m, d), __shfl_xor(ms.s, d)}, a.c_log2e);
-      if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave] = ms;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      RowEnd e = {0, 0, 0, 0, 0, 0, 0};
-      if (counts) {
-        ms = lds[0];
-        for (int k = 1; k < WAVES; ++k) ms = join(ms, lds[k], a.c_log2e);
-        e = row_end(a, row, ms, zt);
-      }
-      row_g = e.g; row_m = loss_base(ms.m); row_s = ms.s == 0.0f ? 0.0f : 1.0f / ms.s;
-      if (a.logp) a.logp[row] = (float)e.logp;
-      if (a.loss) a.loss[row] = (float)e.loss;
-      sums[0] += e.loss; sums[1] += e.pg; sums[2] += e.kl; sums[3] += e.clipped; sums[4] += e.w;
-    }
-    __syncthreads();
-    if (!out) continue;
-    const float g = row_g, m = row_m, gs = -row_g * row_s;
-    const uint32_t t = counts ? (uint32_t)a.targets[row] : 0xffffffffu;
-    const bool nothing = !counts || row_s == 0.0f;
-    for (uint32_t v = threadIdx.x; v < nvec; v += THREADS) {
-      float x[N];
-      if (nothing) {
+  for (int u = 0; u < U; ++u) {
+    r[u].again();
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = 0.0f;
-      } else {
-        StepVec<DT, N> r;
-        r.load(z, (size_t)v * N);
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = gs * loss_exp(r.get(k), m, a.c_log2e) + (v * N + k == t ? g : 0.0f);
-      }
-      StepVec<DT, N> o;
-      o.put(x);
-      o.store(out, (size_t)v * N);
-    }
-    if (rest < a.vocab) step_put<DT>(out, rest, nothing ? 0.0f : gs * loss_exp(step_get<DT>(z, rest), m, a.c_log2e) + (rest == t ? g : 0.0f));
+    for (int j = 0; j < N; ++j) s += loss_exp(r[u].get(j), base, k);
   }
-  if (a.sums && threadIdx.x == 0)
-    for (int k = 0; k < kSums; ++k) a.part[(size_t)blockIdx.x * kSums + k] = sums[k];
+  ms = {m, s};
 }
 
-// the workgroups' shares, in an order that is always the same
-__global__ void __launch_bounds__(kSumThreads) dfx_loss_sums_kernel(const double* part, uint32_t n, float* out) {
-  __shared__ double lds[kSumThreads / kStepWave][kSums];
-  double s[kSums] = {0, 0, 0, 0, 0};
-  for (uint32_t i = threadIdx.x; i < n; i += kSumThreads)
-    for (int k = 0; k < kSums; ++k) s[k] += part[(size_t)i * kSums + k];
-  for (int k = 0; k < kSums; ++k) {
-    s[k] = wave_sum(s[k]);
-    if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave][k] = s[k];
+template <int DT, int N>
+__device__ __forceinline__ void grad_vector(const StepVec<DT, N>& r, float k, float base, float gs, void* out, uint32_t bytes) {
+  float x[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = gs * loss_exp(r.get(j), base, k);
+  StepVec<DT, N> o;
+  o.put(x);
+  o.stream_at(out, bytes);
+}
+
+// what every lane holds alike, in a scalar register
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+
+// this thread's number; what is made of it is made where it is used, not kept from row to row
+__device__ __forceinline__ uint32_t thread_here() {
+  uint32_t me = threadIdx.x;
+  asm("" : "+v"(me));
+  return me;
+}
+
+template <int DT, int T>
+__device__ __forceinline__ void zero_row(void* out, uint32_t vocab) {
+  constexpr int N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  const uint32_t nvec = vocab / N, me = thread_here();
+  StepVec<DT, N> zero;
+  zero.w = 0;
+  for (uint32_t v = me; v < nvec; v += T) zero.stream_at(out, v * 16u);
+  if (nvec * N + me < vocab) step_put<DT>(out, nvec * N + me, 0.0f);
+}
+
+// A workgroup of T threads per row.  A thread keeps the row's vectors v = thread + u T, u < U, in registers from the reduction to the
+// gradient; what a longer row has beyond them is read again, from its end, and comes from the memory-side cache.
+//
+// HBM bounds it, the exponentials are the next (two an element with gradient: half of the time of 16-bit rows).  So that one row's reads pass
+// while another's exponentials do, a kernel has at most 64 registers and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every
+// sixth row masked, 394 us (5.0 TB/s of what has to move); with one workgroup of up to 128 registers 417 to 435, with workgroups of 512 that
+// read more of the row again 450.  1024 x 50257 fp32 82.5 us (4.7 TB/s); loads of what stays in registers go past the caches, which keep the
+// rest of the row instead (without: 92 us).  Forward 2048 x 32000 bf16 22.6 us (5.0 TB/s), with workgroups of 1024 29, of 256 42.
+template <int DT, int T, int U, bool GRAD>
+__global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
+  typedef typename StepElem<DT>::raw raw;
+  constexpr int N = 16 / (int)sizeof(raw);
+  __shared__ MaxSum lds[2][T / kStepWave];
+  const uint32_t nvec = a.vocab / N;
+  const float k = a.k;
+  __shared__ double sums[kSums];         // (thread 0's)
+  if (threadIdx.x == 0)
+    for (int i = 0; i < kSums; ++i) sums[i] = 0.0;
+  uint32_t turn = 0;
+  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
+    raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
+    if (!row_counts(a, row)) {           // (the whole workgroup)
+      if (threadIdx.x == 0) {
+        if (a.logp) a.logp[row] = 0.0f;
+        if (a.loss) a.loss[row] = 0.0f;
+      }
+      if (GRAD) zero_row<DT, T>(out, a.vocab);
+      continue;
+    }
+    const uint32_t t = (uint32_t)a.targets[row];
+    uint32_t me = thread_here();
+    const uint32_t rest = nvec * N + me;
+    StepVec<DT, N> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t v = u * T + me;
+      if (v < nvec) r[u].template load_at<true>(z, v * 16u);
+      else r[u].fill_lowest();
+    }
+    const float zt = step_get<DT>(z, t);
+    MaxSum ms = {-INFINITY, 0.0f};
+    float last = -INFINITY;
+    if (rest < a.vocab) {
+      last = step_get<DT>(z, rest);
+      ms = {last, loss_exp(last, loss_base(last), k)};
+    }
+    take_vectors<DT, N, U>(r, k, ms);
+    for (uint32_t v = U * T + me; v < nvec; v += T) {
+      StepVec<DT, N> more;
+      more.load_at(z, v * 16u);
+      take_vectors<DT, N, 1>(&more, k, ms);
+    }
+    ms = join_all<T>(ms, k, lds[turn]);
+    turn ^= 1u;                          // (of the rows that come here: whoever writes a half again is behind the other one's barrier)
+    ms = {uniform(loss_base(ms.m)), uniform(ms.s)};
+    const float g = uniform(row_end(a, row, (double)zt - (double)ms.m, ms.s, threadIdx.x == 0, sums));
+    if (!GRAD) continue;
+    if (ms.s == 0.0f) {                  // no logit above -infinity
+      zero_row<DT, T>(out, a.vocab);
+      continue;
+    }
+    const float base = ms.m, gs = -g / ms.s;
+    asm("" : "+v"(me));
+    if (U * T + me < nvec)
+      for (uint32_t n = (nvec - 1u - U * T - me) / T + 1u; n-- != 0;) {
+        const uint32_t at = (U * T + me + n * T) * 16u;
+        StepVec<DT, N> more;
+        more.load_at(z, at);
+        grad_vector<DT, N>(more, k, base, gs, out, at);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t v = u * T + me;
+      r[u].again();
+      if (v < nvec) grad_vector<DT, N>(r[u], k, base, gs, out, v * 16u);
+    }
+    if (rest < a.vocab) step_put<DT>(out, rest, gs * loss_exp(last, base, k));
+    // the target's element once more, by the thread that has just written it
+    if (t < nvec * N ? t / N % T == threadIdx.x : t == rest) step_put<DT>(out, t, gs * loss_exp(zt, base, k) + g);
   }
+  if (a.sums && threadIdx.x == 0)
+    for (int i = 0; i < kSums; ++i) a.part[(size_t)i * gridDim.x + blockIdx.x] = sums[i];
+}
+
+// ------------------------------------------------------------------------------------------
+// few rows: each split over workgroups, in two kernels: the segments' parts, then all of them joined by everyone who needs them.  No row's
+// logits are read behind a write of another workgroup, so the gradient may take their place.
+// ------------------------------------------------------------------------------------------
+struct Split { uint32_t segments, vectors; };   // of a row; vectors of a segment (a multiple of kSplitThreads)
+
+template <int DT>
+__device__ __forceinline__ uint32_t segment_of(const Split& sp, uint32_t vocab, uint32_t t) {
+  constexpr uint32_t N = 16 / sizeof(typename StepElem<DT>::raw);
+  return min(t / N / sp.vectors, sp.segments - 1u);      // (what is behind the last whole vector goes with the last segment)
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kSplitThreads) dfx_loss_parts_kernel(LossArgs a, Split sp) {
+  constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
+  __shared__ MaxSum lds[T / kStepWave];
+  const uint32_t row = blockIdx.x / sp.segments, seg = blockIdx.x % sp.segments, nvec = a.vocab / N;
+  if (!row_counts(a, row)) return;
+  const void* z = (const typename StepElem<DT>::raw*)a.logits + (size_t)row * a.logits_stride;
+  const uint32_t end = min(nvec, (seg + 1u) * sp.vectors), t = (uint32_t)a.targets[row];
+  const float k = a.k;
+  MaxSum ms = {-INFINITY, 0.0f};
+  for (uint32_t v = seg * sp.vectors + threadIdx.x; v < end; v += U * T) {
+    StepVec<DT, N> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (v + u * T < end) r[u].load_at(z, (v + u * T) * 16u);
+      else r[u].fill_lowest();
+    }
+    take_vectors<DT, N, U>(r, k, ms);
+  }
+  if (seg + 1u == sp.segments && nvec * N + threadIdx.x < a.vocab) {
+    const float x = step_get<DT>(z, nvec * N + threadIdx.x), m = fmaxf(ms.m, x), base = loss_base(m);
+    ms = {m, ms.s * loss_exp(ms.m, base, k) + loss_exp(x, base, k)};
+  }
+  ms = join_all<T>(ms, k, lds);
+  if (threadIdx.x == 0) {
+    a.parts[(size_t)row * sp.segments + seg] = {ms.m, ms.s, segment_of<DT>(sp, a.vocab, t) == seg ? step_get<DT>(z, t) : 0.0f, 0.0f};
+  }
+}
+
+// Every workgroup joins its row's parts again.
+template <int DT, bool GRAD>
+__global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs a, Split sp, uint32_t groups_per_row) {
+  constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
+  const float k = a.k;
+  const uint32_t row = blockIdx.x / groups_per_row, seg = blockIdx.x % groups_per_row, lane = threadIdx.x % kStepWave;
+  typedef typename StepElem<DT>::raw raw;
+  const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
+  raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
+  const uint32_t nvec = a.vocab / N, first = seg * sp.vectors + threadIdx.x, end = min(nvec, (seg + 1u) * sp.vectors);
+  const uint32_t rest = seg + 1u == sp.segments ? nvec * N + threadIdx.x : a.vocab;
+  const bool writes = seg == 0 && threadIdx.x == 0, counts = row_counts(a, row);
+  float s = 0.0f, g = 0.0f, base = 0.0f, zt = 0.0f;
+  double sums[kSums] = {0, 0, 0, 0, 0};
+  StepVec<DT, N> r[U];
+  if (GRAD && counts)                    // (under way while the parts are joined)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (first + u * T < end) r[u].load_at(z, (first + u * T) * 16u);
+  const uint32_t t = counts ? (uint32_t)a.targets[row] : 0u;
+  if (counts) {
+    const LossPart* p = a.parts + (size_t)row * sp.segments;
+    MaxSum ms = {-INFINITY, 0.0f};
+    if (lane < sp.segments) ms = {p[lane].m, p[lane].s};
+    zt = p[segment_of<DT>(sp, a.vocab, t)].zt;
+    ms = join_lanes<kStepWave>(ms, k);
+    base = loss_base(ms.m); s = ms.s;
+    g = row_end(a, row, (double)zt - (double)base, s, writes, sums);
+  } else if (writes) {
+    if (a.logp) a.logp[row] = 0.0f;
+    if (a.loss) a.loss[row] = 0.0f;
+  }
+  if (a.sums && writes)
+    for (int i = 0; i < kSums; ++i) a.part[(size_t)i * a.rows + row] = sums[i];
+  if (!GRAD) return;
+  const float gs = s == 0.0f ? 0.0f : -g / s;
+  if (s == 0.0f) {                       // nothing to learn from (the whole workgroup)
+    StepVec<DT, N> zero;
+    zero.w = 0;
+    for (uint32_t v = first; v < end; v += T) zero.stream_at(out, v * 16u);
+    if (rest < a.vocab) step_put<DT>(out, rest, 0.0f);
+    return;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (first + u * T < end) grad_vector<DT, N>(r[u], k, base, gs, out, (first + u * T) * 16u);
+  for (uint32_t v = first + U * T; v < end; v += T) {
+    r[0].load_at(z, v * 16u);
+    grad_vector<DT, N>(r[0], k, base, gs, out, v * 16u);
+  }
+  if (rest < a.vocab) step_put<DT>(out, rest, gs * loss_exp(step_get<DT>(z, rest), base, k));
+  if (t < nvec * N ? t / N >= seg * sp.vectors && t / N < end && t / N % T == threadIdx.x : t == rest) step_put<DT>(out, t, gs * loss_exp(zt, base, k) + g);
+}
+
+// the workgroups' shares, in an order that is always the same: a wave to a sum, three waves to each
+__global__ void __launch_bounds__(kSumThreads) dfx_loss_sums_kernel(const double* part, uint32_t n, float* out) {
+  __shared__ double lds[kSumThreads / kStepWave];
+  const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave;
+  const double* mine = part + (size_t)(wave % kSums) * n;
+  double s = 0.0;
+#pragma unroll 4
+  for (uint32_t i = wave / kSums * kStepWave + lane; i < n; i += kSumWaves * kStepWave) s += mine[i];
+  s = wave_sum(s);
+  if (lane == 0) lds[wave] = s;
   __syncthreads();
   if (threadIdx.x < kSums) {
-    double t = 0;
-    for (int w = 0; w < kSumThreads / kStepWave; ++w) t += lds[w][threadIdx.x];
+    double t = lds[threadIdx.x];
+    for (int w = 1; w < kSumWaves; ++w) t += lds[threadIdx.x + w * kSums];
     out[threadIdx.x] = (float)t;
   }
 }
 
 uint32_t loss_groups(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows, kGroups); }
+uint32_t loss_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows * kStepWave, kSplitGroups); }      // at most
+
+// How a call is split, or segments = 0.  A row alone on its workgroup takes as long as that needs for its elements, whatever their type: with
+// gradient 9.7 us of 32000 elements, 10.5 of 50257, 20.5 of 131072, forward 4.5, 5.5 and 10.5; split 8.1 us and 5.2 at every length, so from
+// the lengths below on it is worth the launch more.  Above 64 rows the two ways meet (128 rows of 131072 bf16: 24.8 and 24.4 us; 256: 31.7 and
+// 40.7), since a split row is read twice.
+Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
+  Split sp = {0, 0};
+  if (a.rows == 0 || a.rows > kSplitRows || a.vocab < (a.grad ? kSplitGrad : kSplitForward)) return sp;
+  const uint32_t nvec = a.vocab / (16u / elem_bytes), want = std::min<uint32_t>(kStepWave, kSplitGroups / a.rows);
+  sp.vectors = ((nvec + want - 1) / want + kSplitThreads - 1) / kSplitThreads * kSplitThreads;
+  sp.segments = (nvec + sp.vectors - 1) / sp.vectors;
+  return sp;
+}
+
+template <int DT>
+void launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
+  hipLaunchKernelGGL((dfx_loss_parts_kernel<DT>), dim3(a.rows * sp.segments), dim3(kSplitThreads), 0, s, a, sp);
+  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(a.rows * sp.segments), dim3(kSplitThreads), 0, s, a, sp, sp.segments);
+  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(a.rows), dim3(kSplitThreads), 0, s, a, sp, 1u);
+}
 
 template <int DT>
 void launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
-  if (a.vocab <= 4096) hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, 256>), dim3(groups), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, 1024>), dim3(groups), dim3(1024), 0, s, a);
+  const uint32_t nvec = a.vocab / (16 / step_elem_bytes(DT));
+#define ROWS(T, U) \
+  if (a.grad) hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, T, U, true>), dim3(groups), dim3(T), 0, s, a); \
+  else hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, T, U, false>), dim3(groups), dim3(T), 0, s, a)
+  if (nvec <= 256) { ROWS(256, 1); }
+  else if (nvec <= 512) { ROWS(256, 2); }
+  else if (nvec <= 1024) { ROWS(256, 4); }
+  else if (nvec <= 2048) { ROWS(512, 4); }
+  else if (nvec <= 4096) { ROWS(512, 8); }
+  else { ROWS(1024, 6); }
+#undef ROWS
 }
 
 // rows of n elements, stride elements apart, from p on: [first, second) in bytes
@@ -188,17 +436,18 @@ extern "C" {
 
 size_t dfx_policy_loss_workspace(size_t rows, size_t vocab, dfx_dtype dtype) {
   (void)vocab; (void)dtype;
-  return std::max<size_t>(1, loss_groups(rows)) * kSums * sizeof(double);
+  return loss_parts(rows) * sizeof(LossPart) + std::max(1u, loss_groups(rows)) * kSums * sizeof(double);
 }
 
 int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   if (!u || u->struct_bytes != sizeof(*u)) return DFX_ERR_INVALID_ARG;
   if (u->dtype != DFX_F32 && u->dtype != DFX_BF16 && u->dtype != DFX_F16) return DFX_ERR_INVALID_ARG;
   if (u->rows > 0x7fffffffull || u->vocab > (1ull << 30)) return DFX_ERR_TOO_LARGE;
+  if (!(u->inv_temperature * kLog2e >= (double)FLT_MIN && u->inv_temperature * kLog2e <= (double)FLT_MAX)) return DFX_ERR_INVALID_ARG;
   const size_t eb = step_elem_bytes(u->dtype), ls = u->logits_stride ? u->logits_stride : u->vocab, gs = u->grad_stride ? u->grad_stride : u->vocab;
   if (ls < u->vocab || (u->grad && gs < u->vocab)) return DFX_ERR_INVALID_ARG;
   if (u->rows && ((ls > SIZE_MAX / 8 / u->rows) || (u->grad && gs > SIZE_MAX / 8 / u->rows))) return DFX_ERR_TOO_LARGE;
-  if (!isfinite(u->clip_low) || u->clip_low < 0.0 || u->clip_low > 1.0 || !isfinite(u->clip_high) || u->clip_high < 0.0 || !isfinite(u->kl_coef) || !isfinite(u->inv_temperature) || !(u->inv_temperature > 0.0)) return DFX_ERR_INVALID_ARG;
+  if (!isfinite(u->clip_low) || u->clip_low < 0.0 || u->clip_low > 1.0 || !isfinite(u->clip_high) || u->clip_high < 0.0 || !isfinite(u->kl_coef)) return DFX_ERR_INVALID_ARG;
   if (u->kl_coef != 0.0 && !u->ref_logp) return DFX_ERR_INVALID_ARG;
   if (!u->advantage && (u->loss || u->sums || u->grad)) return DFX_ERR_INVALID_ARG;
   if (u->rows && (!u->targets || (u->vocab && !u->logits))) return DFX_ERR_INVALID_ARG;
@@ -214,13 +463,19 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   memset(&a, 0, sizeof(a));
   a.logits = u->logits; a.grad = u->grad; a.logits_stride = ls; a.grad_stride = gs;
   a.targets = u->targets; a.old_logp = u->old_logp; a.ref_logp = u->ref_logp; a.advantage = u->advantage; a.weight = u->weight; a.scale = u->scale;
-  a.logp = u->logp; a.loss = u->loss; a.sums = u->sums; a.part = (double*)u->workspace;
+  a.logp = u->logp; a.loss = u->loss; a.sums = u->sums; a.parts = (LossPart*)u->workspace; a.part = (double*)(a.parts + loss_parts(u->rows));
   a.rows = (uint32_t)u->rows; a.vocab = (uint32_t)u->vocab;
-  a.clip_low = u->clip_low; a.clip_high = u->clip_high; a.kl_coef = u->kl_coef; a.c = u->inv_temperature;
-  a.c_log2e = (float)(u->inv_temperature * 1.4426950408889634);
+  a.least = (float)(1.0 - u->clip_low); a.most = (float)(1.0 + u->clip_high); a.kl_coef = (float)u->kl_coef; a.c = u->inv_temperature;
+  a.k = (float)(u->inv_temperature * kLog2e);
   hipStream_t s = (hipStream_t)hip_stream;
   const uint32_t groups = loss_groups(u->rows);
-  if (groups) {
+  const Split sp = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype) ? loss_split(a, (uint32_t)eb) : Split{0, 0};
+  if (sp.segments) {
+    if (u->dtype == DFX_F32) launch_split<DFX_F32>(a, sp, s);
+    else if (u->dtype == DFX_BF16) launch_split<DFX_BF16>(a, sp, s);
+    else launch_split<DFX_F16>(a, sp, s);
+    if (hipGetLastError() != hipSuccess) return DFX_ERR_HIP;
+  } else if (groups) {
     if (u->dtype == DFX_F32) launch_rows<DFX_F32>(a, groups, s);
     else if (u->dtype == DFX_BF16) launch_rows<DFX_BF16>(a, groups, s);
     else launch_rows<DFX_F16>(a, groups, s);

@@ -72,12 +72,22 @@ struct StepVec {
     const STEP_GLOBAL words* q = (const STEP_GLOBAL words*)((const STEP_GLOBAL raw*)p + i);
     w = STREAM ? __builtin_nontemporal_load(q) : *q;
   }
+  // at a 32-bit offset in bytes from an address that all lanes share: one register where an address of their own takes two
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load_at(const void* p, uint32_t bytes) {
+    const STEP_GLOBAL words* q = (const STEP_GLOBAL words*)((const STEP_GLOBAL unsigned char*)p + bytes);
+    w = STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  __device__ __forceinline__ void stream_at(void* p, uint32_t bytes) const { __builtin_nontemporal_store(w, (STEP_GLOBAL words*)((STEP_GLOBAL unsigned char*)p + bytes)); }
   template <bool STREAM = false>
   __device__ __forceinline__ void store(void* p, size_t i) const {
     STEP_GLOBAL words* q = (STEP_GLOBAL words*)((STEP_GLOBAL raw*)p + i);
     if (STREAM) __builtin_nontemporal_store(w, q);
     else *q = w;
   }
+  __device__ __forceinline__ void fill_lowest() { w = DT == DFX_F32 ? 0xff800000u : DT == DFX_BF16 ? 0xff80ff80u : 0xfc00fc00u; }      // -infinity
+  // what was made of the elements so far is made anew behind this, not kept: a vector of 16-bit elements takes half the registers of its values
+  __device__ __forceinline__ void again() { asm("" : "+v"(w)); }
   __device__ __forceinline__ float get(int k) const {
     if (DT == DFX_F32) return StepElem<DT>::get((raw)w[k]);
     if (DT == DFX_BF16) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
