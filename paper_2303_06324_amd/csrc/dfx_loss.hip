@@ -18,6 +18,10 @@ constexpr int kSums = 5;
 constexpr uint32_t kGroups = 4096;       // workgroups of a call, at most: each leaves its share of the sums
 constexpr int kSumWaves = 3;             // waves that share a sum
 constexpr int kSumThreads = kSums * kSumWaves * kStepWave;
+// Logits of more bytes than this are read past the caches where they stay in registers, and the caches keep what is read again.  Below it, what
+// produced them has left them in the memory-side cache (256 MiB), where such loads find less.  Behind a matrix product, bf16 with gradient:
+// 1024 x 50257 (98 MiB) 36 us, past the caches 47; 1536 (147 MiB) 53 and 67; 1792 (172 MiB) 94 and 81; 2048 (196 MiB) 120 and 87.
+constexpr size_t kStreamBytes = 160u << 20;
 // Few rows of a long vocabulary are split over workgroups.
 constexpr int kSplitThreads = 256;
 constexpr uint32_t kSplitGroups = 512;   // workgroups, at most
@@ -193,10 +197,10 @@ __device__ __forceinline__ void zero_row(void* out, uint32_t vocab) {
 //
 // HBM bounds it, the exponentials are the next (two an element with gradient: half of the time of 16-bit rows).  So that one row's reads pass
 // while another's exponentials do, a kernel has at most 64 registers and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every
-// sixth row masked, 394 us (5.0 TB/s of what has to move); with one workgroup of up to 128 registers 417 to 435, with workgroups of 512 that
-// read more of the row again 450.  1024 x 50257 fp32 82.5 us (4.7 TB/s); loads of what stays in registers go past the caches, which keep the
-// rest of the row instead (without: 92 us).  Forward 2048 x 32000 bf16 22.6 us (5.0 TB/s), with workgroups of 1024 29, of 256 42.
-template <int DT, int T, int U, bool GRAD>
+// sixth row masked, 390 us (5.0 TB/s of what has to move); with one workgroup of up to 128 registers 417 to 435, with workgroups of 512 that
+// read more of the row again 450.  1024 x 50257 fp32 82 us (4.7 TB/s); loads of what stays in registers go past the caches, which keep the
+// rest of the row instead (without: 92 us).  Forward 2048 x 32000 bf16 24.5 us (4.6 TB/s), with workgroups of 1024 29, of 256 42.
+template <int DT, int T, int U, bool GRAD, bool STREAM>
 __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
   typedef typename StepElem<DT>::raw raw;
   constexpr int N = 16 / (int)sizeof(raw);
@@ -225,7 +229,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t v = u * T + me;
-      if (v < nvec) r[u].template load_at<true>(z, v * 16u);
+      if (v < nvec) r[u].template load_at<STREAM>(z, v * 16u);
       else r[u].fill_lowest();
     }
     const float zt = step_get<DT>(z, t);
@@ -373,9 +377,15 @@ __global__ void __launch_bounds__(kSumThreads) dfx_loss_sums_kernel(const double
   __shared__ double lds[kSumThreads / kStepWave];
   const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave;
   const double* mine = part + (size_t)(wave % kSums) * n;
+  constexpr uint32_t U = 8, stride = kSumWaves * kStepWave;
   double s = 0.0;
-#pragma unroll 4
-  for (uint32_t i = wave / kSums * kStepWave + lane; i < n; i += kSumWaves * kStepWave) s += mine[i];
+  for (uint32_t i = wave / kSums * kStepWave + lane; i < n; i += U * stride) {      // (eight loads under way at once)
+    double x[U];
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) x[u] = i + u * stride < n ? mine[i + u * stride] : 0.0;
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) s += x[u];
+  }
   s = wave_sum(s);
   if (lane == 0) lds[wave] = s;
   __syncthreads();
@@ -409,18 +419,20 @@ void launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
   else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(a.rows), dim3(kSplitThreads), 0, s, a, sp, 1u);
 }
 
+void launch_row_kernel(void (*kernel)(LossArgs), int threads, uint32_t groups, const LossArgs& a, hipStream_t s) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, s, a); }
+
 template <int DT>
 void launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t nvec = a.vocab / (16 / step_elem_bytes(DT));
-#define ROWS(T, U) \
-  if (a.grad) hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, T, U, true>), dim3(groups), dim3(T), 0, s, a); \
-  else hipLaunchKernelGGL((dfx_loss_rows_kernel<DT, T, U, false>), dim3(groups), dim3(T), 0, s, a)
-  if (nvec <= 256) { ROWS(256, 1); }
-  else if (nvec <= 512) { ROWS(256, 2); }
-  else if (nvec <= 1024) { ROWS(256, 4); }
-  else if (nvec <= 2048) { ROWS(512, 4); }
-  else if (nvec <= 4096) { ROWS(512, 8); }
-  else { ROWS(1024, 6); }
+  const bool stream = (size_t)a.rows * a.vocab * step_elem_bytes(DT) > kStreamBytes;
+#define ROWS(T, U) launch_row_kernel(a.grad ? stream ? dfx_loss_rows_kernel<DT, T, U, true, true> : dfx_loss_rows_kernel<DT, T, U, true, false> \
+                                            : stream ? dfx_loss_rows_kernel<DT, T, U, false, true> : dfx_loss_rows_kernel<DT, T, U, false, false>, T, groups, a, s)
+  if (nvec <= 256) ROWS(128, 2);
+  else if (nvec <= 512) ROWS(128, 4);
+  else if (nvec <= 1024) ROWS(256, 4);
+  else if (nvec <= 2048) ROWS(512, 4);
+  else if (nvec <= 4096) ROWS(512, 8);
+  else ROWS(1024, 6);
 #undef ROWS
 }
 
