@@ -447,8 +447,8 @@ int dfx_collective_noalloc(int nranks, dfx_kind kind, size_t count, dfx_dtype dt
  * graph.  Memory that they are given is device memory of the current device, and every tensor starts at a multiple of its
  * element's size, which is all that is asked of alignment.  Element types are DFX_F32, DFX_BF16 and DFX_F16; sums, norms and
  * moments are held in 32 bits or more, and a result of 16 bits is rounded once, to nearest even.  Results do not depend on what
- * else runs: the same call on the same memory gives the same bits.  A NULL stream or a context's daemon that is still resident
- * may hold back a kernel behind it: see dfx_config.quit_idle_us.
+ * else runs: the same call on the same memory gives the same bits.  A context's
+ * daemon that is still resident may hold back a kernel behind it (dfx_config.quit_idle_us).
  */
 
 /* One tensor of a list: count elements from ptr on (ptr is not looked at where count is 0). */
@@ -544,7 +544,7 @@ typedef struct {
   const float* advantage;    /* [rows], A; may be NULL where neither loss, sums nor grad is asked for */
   const float* weight;       /* [rows], may be NULL: 1 */
   const float* scale;        /* one value, may be NULL: 1.  Multiplies the gradient only: 1 / the weights of all ranks' rows */
-  float* logp;               /* [rows], may be NULL */
+  float* logp;               /* [rows], may be NULL; like loss, apart from all that is read */
   float* loss;               /* [rows], may be NULL */
   float* sums;               /* 5 values, may be NULL: sums over the rows of weight times loss / weight, pg, kl, [clipped], 1 */
   void* workspace;           /* dfx_policy_loss_workspace bytes, 8-byte aligned; nothing in it has to outlive the call's work.  May be

@@ -471,6 +471,11 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
     const Extent a = extent(u->logits, u->rows, u->vocab, ls, eb), b = extent(u->grad, u->rows, u->vocab, gs, eb);
     if (a.lo < b.hi && b.lo < a.hi) return DFX_ERR_INVALID_ARG;
   }
+  for (const void* o : {(const void*)u->logp, (const void*)u->loss})      // what is written for a row lies apart from what is read for it
+    for (const void* i : {(const void*)u->targets, (const void*)u->old_logp, (const void*)u->ref_logp, (const void*)u->advantage, (const void*)u->weight, (const void*)u->scale, o == u->logp ? (const void*)u->loss : nullptr}) {
+      const size_t held = i == u->targets ? 8 * u->rows : i == u->scale ? 4 : 4 * u->rows;
+      if (o && i && u->rows && (uintptr_t)o < (uintptr_t)i + held && (uintptr_t)i < (uintptr_t)o + 4 * u->rows) return DFX_ERR_INVALID_ARG;
+    }
   LossArgs a;
   memset(&a, 0, sizeof(a));
   a.logits = u->logits; a.grad = u->grad; a.logits_stride = ls; a.grad_stride = gs;

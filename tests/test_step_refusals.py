@@ -74,3 +74,11 @@ def test_defaults():
     assert c.struct_bytes == ctypes.sizeof(c) and c.lr == 0.5 and c.beta1 == 0.9 and c.grad_scale == 1.0 and not c.step_dev
     with pytest.raises(KeyError):
         dfx.AdamWConfig(momentum=0.9)
+
+
+@pytest.mark.parametrize("kw", [dict(logp=0x30000), dict(loss=0x30000), dict(logp=0x3000c, loss=0x90000), dict(logp=0x90000, loss=0x90008), dict(logp=0x20010),
+                                dict(loss=0x20000 - 12), dict(old_logp=0x90000, logp=0x90000), dict(ref_logp=0x90000, loss=0x90004), dict(weight=0x90000, logp=0x8fff4), dict(scale=0x90000, loss=0x8fff4)])
+def test_loss_refuses_results_that_lie_on_what_is_read(kw):
+    import paper_2303_06324_amd as dfx
+    from paper_2303_06324_amd import binding
+    assert binding._lib.dfx_policy_loss(_args(dfx, **kw), None) == dfx.ERR_INVALID_ARG
