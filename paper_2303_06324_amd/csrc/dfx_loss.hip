@@ -35,7 +35,7 @@ struct LossArgs {
   void* grad;
   size_t logits_stride, grad_stride;
   const int64_t* targets;
-  const float *old_logp, *ref_logp, *advantage, *weight, *scale;
+  const float *old_logp, *ref_logp, *advantage, *weight, *scale;      // absent: the targets' address, so that all are read alike (has_...)
   float *logp, *loss, *sums;
   double* part;                          // [kSums][workgroups]
   LossPart* parts;                       // [rows][segments], where rows are split
@@ -43,6 +43,7 @@ struct LossArgs {
   double c;                              // 1 / temperature
   float least, most, kl_coef;            // 1 - clip_low, 1 + clip_high
   float k;                               // c / log 2: exponents are taken to base 2
+  bool has_old, has_ref, has_advantage, has_weight, has_scale;
 };
 
 // exp(c (z - m)) = 2^(k (z - m)), k = c / log 2.  The difference first: it is 0 for the largest logit, exact where it matters, and cannot
@@ -93,32 +94,46 @@ __device__ __forceinline__ float loss_penalty(double d) {
   return r * x * x;
 }
 
+// What is known of a row before its logits.  Read at once when the row is begun, through the scalar cache (nobody writes it while the kernel
+// runs), so that no wait for it comes behind the reduction.
+struct RowIn { int64_t t; float w, A, old, ref, scale; };
+
+#define LOSS_CONST __attribute__((address_space(4)))
+__device__ __forceinline__ RowIn row_in(const LossArgs& a, uint32_t row) {
+  const LOSS_CONST float *w = (const LOSS_CONST float*)a.weight, *A = (const LOSS_CONST float*)a.advantage, *old = (const LOSS_CONST float*)a.old_logp, *ref = (const LOSS_CONST float*)a.ref_logp, *scale = (const LOSS_CONST float*)a.scale;
+  const RowIn in = {((const LOSS_CONST int64_t*)a.targets)[row], w[row], A[row], old[row], ref[row], scale[0]};
+  return {in.t, a.has_weight ? in.w : 1.0f, in.A, in.old, in.ref, a.has_scale ? in.scale : 1.0f};
+}
+
+// whether it has anything to learn from, as far as that says
+__device__ __forceinline__ bool row_counts(const LossArgs& a, const RowIn& in) { return in.t >= 0 && in.t < (int64_t)a.vocab && in.w != 0.0f; }
+
 // What a row comes to.  far: z_t - m in 64 bits; s: the sum around that m.  log2 s = e + log2 f, f in [1/2, 1): what 32 bits lose there is
 // 6e-8 of a logarithm, the sum's own error is more.  Differences of log-probabilities are taken in 64 bits (a logp of -10 holds 5e-7 in
 // 32, which would be the ratio's error), what is made of them in 32.
 struct RowValue { float logp, loss, pg, kl, clipped, w, g; };      // pg, kl, clipped times the weight w; nothing: all 0
 
-__device__ __forceinline__ RowValue row_value(const LossArgs& a, uint32_t row, double far, float s) {
+__device__ __forceinline__ RowValue row_value(const LossArgs& a, const RowIn& in, double far, float s) {
   RowValue e = {0, 0, 0, 0, 0, 0, 0};
   if (s == 0.0f) return e;               // no logit above -infinity
   int two;
   const float f = frexpf(s, &two);
   const double logp = a.c * far - ((double)two + (double)__builtin_amdgcn_logf(f)) * kLog2;
   e.logp = (float)logp;
-  if (!a.advantage) return e;
-  e.w = a.weight ? a.weight[row] : 1.0f;
-  const float A = a.advantage[row], r = a.old_logp ? loss_exp_of(logp - (double)a.old_logp[row]) : 1.0f;
+  if (!a.has_advantage) return e;
+  e.w = in.w;
+  const float A = in.A, r = a.has_old ? loss_exp_of(logp - (double)in.old) : 1.0f;
   const bool up = A >= 0.0f, clipped = up ? r > a.most : r < a.least;
   const float pg = -A * (clipped ? up ? a.most : a.least : r);
   float slope = clipped ? 0.0f : -A * r, kl = 0.0f;
-  if (a.ref_logp) {
-    const double d = (double)a.ref_logp[row] - logp;
+  if (a.has_ref) {
+    const double d = (double)in.ref - logp;
     kl = loss_penalty(d);
     slope -= a.kl_coef * (float)(d + (double)kl);
   }
   e.pg = e.w * pg; e.kl = e.w * kl; e.clipped = clipped ? e.w : 0.0f;
   e.loss = e.w * fmaf(a.kl_coef, kl, pg);
-  e.g = (float)a.c * e.w * slope * (a.scale ? *a.scale : 1.0f);
+  e.g = (float)a.c * e.w * slope * in.scale;
   return e;
 }
 
@@ -127,20 +142,14 @@ __device__ __forceinline__ void add_sums(double* sums, const RowValue& e) {
 }
 
 // ... by every thread alike; one of them writes it down.  Returns g
-__device__ __forceinline__ float row_end(const LossArgs& a, uint32_t row, double far, float s, bool writes, double* sums) {
-  const RowValue e = row_value(a, row, far, s);
+__device__ __forceinline__ float row_end(const LossArgs& a, uint32_t row, const RowIn& in, double far, float s, bool writes, double* sums) {
+  const RowValue e = row_value(a, in, far, s);
   if (writes) {
     if (a.logp) a.logp[row] = e.logp;
     if (a.loss) a.loss[row] = e.loss;
     if (sums) add_sums(sums, e);
   }
   return e.g;
-}
-
-// whether a row has anything to learn from, by what is known before its logits
-__device__ __forceinline__ bool row_counts(const LossArgs& a, uint32_t row) {
-  const int64_t t = a.targets[row];
-  return t >= 0 && t < (int64_t)a.vocab && (!a.weight || a.weight[row] != 0.0f);
 }
 
 // what of a row is in vectors, joined into ms
@@ -214,7 +223,8 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
   for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
     raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
-    if (!row_counts(a, row)) {           // (the whole workgroup)
+    const RowIn in = row_in(a, row);
+    if (!row_counts(a, in)) {            // (the whole workgroup)
       if (threadIdx.x == 0) {
         if (a.logp) a.logp[row] = 0.0f;
         if (a.loss) a.loss[row] = 0.0f;
@@ -222,7 +232,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
       if (GRAD) zero_row<DT, T>(out, a.vocab);
       continue;
     }
-    const uint32_t t = (uint32_t)a.targets[row];
+    const uint32_t t = (uint32_t)in.t;
     uint32_t me = thread_here();
     const uint32_t rest = nvec * N + me;
     StepVec<DT, N> r[U];
@@ -248,7 +258,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
     ms = join_all<T>(ms, k, lds[turn]);
     turn ^= 1u;                          // (of the rows that come here: whoever writes a half again is behind the other one's barrier)
     ms = {uniform(loss_base(ms.m)), uniform(ms.s)};
-    const float g = uniform(row_end(a, row, (double)zt - (double)ms.m, ms.s, threadIdx.x == 0, sums));
+    const float g = uniform(row_end(a, row, in, (double)zt - (double)ms.m, ms.s, threadIdx.x == 0, sums));
     if (!GRAD) continue;
     if (ms.s == 0.0f) {                  // no logit above -infinity
       zero_row<DT, T>(out, a.vocab);
@@ -294,9 +304,10 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_parts_kernel(LossArgs 
   constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
   __shared__ MaxSum lds[T / kStepWave];
   const uint32_t row = blockIdx.x / sp.segments, seg = blockIdx.x % sp.segments, nvec = a.vocab / N;
-  if (!row_counts(a, row)) return;
+  const RowIn in = row_in(a, row);
+  if (!row_counts(a, in)) return;
   const void* z = (const typename StepElem<DT>::raw*)a.logits + (size_t)row * a.logits_stride;
-  const uint32_t end = min(nvec, (seg + 1u) * sp.vectors), t = (uint32_t)a.targets[row];
+  const uint32_t end = min(nvec, (seg + 1u) * sp.vectors), t = (uint32_t)in.t;
   const float k = a.k;
   MaxSum ms = {-INFINITY, 0.0f};
   for (uint32_t v = seg * sp.vectors + threadIdx.x; v < end; v += U * T) {
@@ -329,7 +340,8 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
   raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
   const uint32_t nvec = a.vocab / N, first = seg * sp.vectors + threadIdx.x, end = min(nvec, (seg + 1u) * sp.vectors);
   const uint32_t rest = seg + 1u == sp.segments ? nvec * N + threadIdx.x : a.vocab;
-  const bool writes = seg == 0 && threadIdx.x == 0, counts = row_counts(a, row);
+  const RowIn in = row_in(a, row);
+  const bool writes = seg == 0 && threadIdx.x == 0, counts = row_counts(a, in);
   float s = 0.0f, g = 0.0f, base = 0.0f, zt = 0.0f;
   double sums[kSums] = {0, 0, 0, 0, 0};
   StepVec<DT, N> r[U];
@@ -337,7 +349,7 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (first + u * T < end) r[u].load_at(z, (first + u * T) * 16u);
-  const uint32_t t = counts ? (uint32_t)a.targets[row] : 0u;
+  const uint32_t t = (uint32_t)in.t;
   if (counts) {
     const LossPart* p = a.parts + (size_t)row * sp.segments;
     MaxSum ms = {-INFINITY, 0.0f};
@@ -345,7 +357,7 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
     zt = p[segment_of<DT>(sp, a.vocab, t)].zt;
     ms = join_lanes<kStepWave>(ms, k);
     base = loss_base(ms.m); s = ms.s;
-    g = row_end(a, row, (double)zt - (double)base, s, writes, sums);
+    g = row_end(a, row, in, (double)zt - (double)base, s, writes, sums);
   } else if (writes) {
     if (a.logp) a.logp[row] = 0.0f;
     if (a.loss) a.loss[row] = 0.0f;
@@ -479,7 +491,11 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   LossArgs a;
   memset(&a, 0, sizeof(a));
   a.logits = u->logits; a.grad = u->grad; a.logits_stride = ls; a.grad_stride = gs;
-  a.targets = u->targets; a.old_logp = u->old_logp; a.ref_logp = u->ref_logp; a.advantage = u->advantage; a.weight = u->weight; a.scale = u->scale;
+  a.targets = u->targets;
+  const float* any = (const float*)u->targets;       // (8 bytes a row)
+  a.old_logp = u->old_logp ? u->old_logp : any; a.ref_logp = u->ref_logp ? u->ref_logp : any; a.advantage = u->advantage ? u->advantage : any;
+  a.weight = u->weight ? u->weight : any; a.scale = u->scale ? u->scale : any;
+  a.has_old = u->old_logp; a.has_ref = u->ref_logp; a.has_advantage = u->advantage; a.has_weight = u->weight; a.has_scale = u->scale;
   a.logp = u->logp; a.loss = u->loss; a.sums = u->sums; a.parts = (LossPart*)u->workspace; a.part = (double*)(a.parts + loss_parts(u->rows));
   a.rows = (uint32_t)u->rows; a.vocab = (uint32_t)u->vocab;
   a.least = (float)(1.0 - u->clip_low); a.most = (float)(1.0 + u->clip_high); a.kl_coef = (float)u->kl_coef; a.c = u->inv_temperature;
