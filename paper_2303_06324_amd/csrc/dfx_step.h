@@ -60,6 +60,9 @@ __device__ __forceinline__ void step_put(void* p, size_t i, float v) {
   *((STEP_GLOBAL raw*)p + i) = StepElem<DT>::put(v);
 }
 
+typedef float StepPair __attribute__((ext_vector_type(2)));
+typedef __bf16 StepBf16Pair __attribute__((ext_vector_type(2)));
+
 // N elements from element i on, as words; what is read or written once and is larger than the caches goes past them (STREAM)
 template <int DT, int N>
 struct StepVec {
@@ -95,8 +98,13 @@ struct StepVec {
   }
   __device__ __forceinline__ void put(const float* v) {
 #pragma unroll
-    for (int k = 0; k < N * (int)sizeof(raw) / 4; ++k)
-      w[k] = DT == DFX_F32 ? (uint32_t)StepElem<DT>::put(v[k]) : (uint32_t)StepElem<DT>::put(v[2 * k]) | ((uint32_t)StepElem<DT>::put(v[2 * k + 1]) << 16);
+    for (int k = 0; k < N * (int)sizeof(raw) / 4; ++k) {
+      if (DT == DFX_F32) w[k] = (uint32_t)StepElem<DT>::put(v[k]);
+      else if (DT == DFX_BF16) {           // (both halves in one instruction)
+        const StepPair two = {v[2 * k], v[2 * k + 1]};
+        w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, StepBf16Pair));
+      } else w[k] = (uint32_t)StepElem<DT>::put(v[2 * k]) | ((uint32_t)StepElem<DT>::put(v[2 * k + 1]) << 16);
+    }
   }
 };
 
