@@ -28,7 +28,7 @@ constexpr uint32_t kSplitGroups = 512;   // workgroups, at most
 constexpr uint32_t kSplitRows = 64;      // rows, at most
 constexpr uint32_t kSplitGrad = 40000, kSplitForward = 65536;      // elements of a row, at least
 
-struct LossPart { float m, s, zt, none; };      // of a segment of a row; zt: the target's logit, where the segment has it
+struct LossPart { float m, s, zt, has; };       // of a segment of a row; zt: the target's logit, where the segment has it (has = 1, else both 0)
 
 struct LossArgs {
   const void* logits;
@@ -311,19 +311,18 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
 // few rows: each split over workgroups, in two kernels: the segments' parts, then all of them joined by everyone who needs them.  No row's
 // logits are read behind a write of another workgroup, so the gradient may take their place.
 // ------------------------------------------------------------------------------------------
-struct Split { uint32_t segments, vectors; };   // of a row; vectors of a segment (a multiple of kSplitThreads)
+struct Split { uint32_t segments, vectors; };   // of a row; vectors of a segment (a multiple of kSplitThreads).  What lies outside a row's vectors goes with the last
 
-// (the elements outside a row's vectors go with the last segment)
 template <int DT>
-__device__ __forceinline__ uint32_t segment_of(const Split& sp, const RowPlace<DT, true>& at, uint32_t t) {
-  return at.in_vectors(t) ? at.vector_of(t) / sp.vectors : sp.segments - 1u;
+__device__ __forceinline__ bool segment_has(const Split& sp, const RowPlace<DT, true>& at, uint32_t seg, uint32_t t) {
+  return at.in_vectors(t) ? at.vector_of(t) - seg * sp.vectors < sp.vectors : seg + 1u == sp.segments;
 }
 
 template <int DT>
 __global__ void __launch_bounds__(kSplitThreads) dfx_loss_parts_kernel(LossArgs a, Split sp) {
   constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
   __shared__ MaxSum lds[T / kStepWave];
-  const uint32_t row = blockIdx.x / sp.segments, seg = blockIdx.x % sp.segments;
+  const uint32_t row = blockIdx.y, seg = blockIdx.x;
   const RowIn in = row_in(a, row);
   if (!row_counts(a, in)) return;
   const auto* z = (const typename StepElem<DT>::raw*)a.logits + (size_t)row * a.logits_stride;
@@ -347,16 +346,17 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_parts_kernel(LossArgs 
   }
   ms = join_all<T>(ms, k, lds);
   if (threadIdx.x == 0) {
-    a.parts[(size_t)row * sp.segments + seg] = {ms.m, ms.s, segment_of(sp, at, t) == seg ? step_get<DT>(z, t) : 0.0f, 0.0f};
+    const bool has = segment_has(sp, at, seg, t);
+    a.parts[row * sp.segments + seg] = {ms.m, ms.s, has ? step_get<DT>(z, t) : 0.0f, has ? 1.0f : 0.0f};
   }
 }
 
 // Every workgroup joins its row's parts again.
 template <int DT, bool GRAD>
-__global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs a, Split sp, uint32_t groups_per_row) {
+__global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs a, Split sp) {
   constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
   const float k = a.k;
-  const uint32_t row = blockIdx.x / groups_per_row, seg = blockIdx.x % groups_per_row, lane = threadIdx.x % kStepWave;
+  const uint32_t row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x % kStepWave;      // (without gradient there is one of a row)
   typedef typename StepElem<DT>::raw raw;
   const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
   raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
@@ -376,10 +376,10 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
       if (first + u * T < end) r[u].load_at(zv, (first + u * T) * 16u);
   const uint32_t t = (uint32_t)in.t;
   if (counts) {
-    const LossPart* p = a.parts + (size_t)row * sp.segments;
-    MaxSum ms = {-INFINITY, 0.0f};
-    if (lane < sp.segments) ms = {p[lane].m, p[lane].s};
-    zt = p[segment_of(sp, at, t)].zt;
+    LossPart part = {-INFINITY, 0.0f, 0.0f, 0.0f};
+    if (lane < sp.segments) part = a.parts[row * sp.segments + lane];
+    zt = __shfl(part.zt, __ffsll(__ballot(part.has != 0.0f)) - 1);      // (a target that counts lies in one of them)
+    MaxSum ms = {part.m, part.s};
     ms = join_lanes<kStepWave>(ms, k);
     base = loss_base(ms.m); s = ms.s;
     g = row_end(a, row, in, (double)zt - (double)base, s, writes, sums);
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
     grad_vector<DT, N>(r[0], k, base, gs, ov, v * 16u);
   }
   if (lone < a.vocab) step_put<DT>(out, lone, gs * loss_exp(step_get<DT>(z, lone), base, k));
-  if (at.in_vectors(t) ? at.vector_of(t) / sp.vectors == seg && at.vector_of(t) % T == threadIdx.x : t == lone) step_put<DT>(out, t, gs * loss_exp(zt, base, k) + g);
+  if (at.in_vectors(t) ? segment_has(sp, at, seg, t) && at.vector_of(t) % T == threadIdx.x : t == lone) step_put<DT>(out, t, gs * loss_exp(zt, base, k) + g);
 }
 
 // the workgroups' shares, in an order that is always the same: a wave to a sum, three waves to each
@@ -451,9 +451,9 @@ Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
 
 template <int DT>
 void launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
-  hipLaunchKernelGGL((dfx_loss_parts_kernel<DT>), dim3(a.rows * sp.segments), dim3(kSplitThreads), 0, s, a, sp);
-  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(a.rows * sp.segments), dim3(kSplitThreads), 0, s, a, sp, sp.segments);
-  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(a.rows), dim3(kSplitThreads), 0, s, a, sp, 1u);
+  hipLaunchKernelGGL((dfx_loss_parts_kernel<DT>), dim3(sp.segments, a.rows), dim3(kSplitThreads), 0, s, a, sp);
+  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(sp.segments, a.rows), dim3(kSplitThreads), 0, s, a, sp);
+  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(1, a.rows), dim3(kSplitThreads), 0, s, a, sp);
 }
 
 void launch_row_kernel(void (*kernel)(LossArgs), int threads, uint32_t groups, const LossArgs& a, hipStream_t s) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, s, a); }
