@@ -237,13 +237,6 @@ __device__ __forceinline__ void adam_element(const AdamRates& a, float& p, float
   p = fmaf(p, a.keep, -(a.rate * m / fmaf(sqrtf(v), a.correct2, a.eps)));
 }
 
-// nothing of what follows is begun before every load so far has arrived
-__device__ __forceinline__ void loads_arrived() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0), the other counters at their largest
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 template <int GD, int CD, bool STAGED>      // CD < 0: no copy
 __device__ __forceinline__ void adam_vector(const AdamRates& a, const ListChunk& p, const ListChunk& g, const ListChunk& m, const ListChunk& v, const ListChunk& copy, size_t i) {
   constexpr int N = 4, C = CD < 0 ? DFX_F32 : CD;

@@ -152,15 +152,16 @@ __device__ __forceinline__ float row_end(const LossArgs& a, uint32_t row, const 
   return e.g;
 }
 
-// How a row of logits lies in memory: head elements up to a multiple of 16 bytes (PEEL), nvec vectors of N, and at most N - 1 elements behind
-// them.  Vectors off that multiple cost rows of an odd length 15 to 20 % (with gradient, 4096 x 50257 bf16 182 and 156 us, x 32001 130 and 111);
-// short rows, of workgroups below 512, are quicker without the head (x 8001 27.5 and 30.9).
+// How a row of logits lies in memory: head elements up to a multiple of 128 bytes (PEEL), nvec vectors of N, and at most N - 1 elements behind
+// them.  A wave's vectors then fill whole lines, of the gradient too, whose rows begin where the logits' do.  Rows of an odd length, with gradient:
+// 4096 x 50257 bf16 182 us, from a multiple of 16 bytes on 155, of 128 148; fp32 338 and 310; x 32001 bf16 130 and 111.  Short rows, of workgroups
+// below 512, are quicker without a head (x 8001 27.5 and 30.9).
 template <int DT, bool PEEL>
 struct RowPlace {
   static constexpr uint32_t N = 16 / sizeof(typename StepElem<DT>::raw);
   uint32_t head, nvec, vocab;
   __device__ __forceinline__ RowPlace(const void* row, uint32_t vocab_) : vocab(vocab_) {
-    head = !PEEL ? 0u : min((uint32_t)(-(uintptr_t)row & 15u) / (uint32_t)sizeof(typename StepElem<DT>::raw), vocab);
+    head = !PEEL ? 0u : min((uint32_t)(-(uintptr_t)row & 127u) / (uint32_t)sizeof(typename StepElem<DT>::raw), vocab);
     nvec = (vocab - head) / N;
   }
   // the i-th of the elements outside the vectors; from vocab on: there is none
@@ -208,6 +209,11 @@ __device__ __forceinline__ uint32_t thread_here() {
   return me;
 }
 
+// 16 bytes a lane from an address that is a multiple of 16, straight to LDS: lane i's to the i-th place behind `to`, which all lanes share
+__device__ __forceinline__ void load_to_lds(const void* p, uint32_t bytes, uint4* to) {
+  __builtin_amdgcn_global_load_lds((const STEP_GLOBAL uint32_t*)((const STEP_GLOBAL unsigned char*)p + bytes), (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+
 template <int DT, int T>
 __device__ __forceinline__ void zero_row(typename StepElem<DT>::raw* out, uint32_t vocab) {
   const RowPlace<DT, false> at(out, vocab);
@@ -218,23 +224,28 @@ __device__ __forceinline__ void zero_row(typename StepElem<DT>::raw* out, uint32
   if (end < vocab) step_put<DT>(out, end, 0.0f);
 }
 
-// A workgroup of T threads per row.  A thread keeps the row's vectors v = thread + u T, u < U, in registers from the reduction to the
-// gradient; what a longer row has beyond them is read again, from its end, and comes from the memory-side cache.
+// A workgroup of T threads per row.  From the reduction to the gradient a thread keeps the row's vectors v = thread + u T, u < U, in registers
+// and the next L of them in LDS, where loads put them without a register in between; what a longer row has beyond these is read again, from
+// its end, and comes from the memory-side cache.
 //
-// HBM bounds it, the exponentials are the next (two an element with gradient: half of the time of 16-bit rows).  So that one row's reads pass
-// while another's exponentials do, a kernel has at most 64 registers and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every
-// sixth row masked, 390 us (5.0 TB/s of what has to move); with one workgroup of up to 128 registers 417 to 435, with workgroups of 512 that
-// read more of the row again 450.  1024 x 50257 fp32 82 us (4.7 TB/s); loads of what stays in registers go past the caches, which keep the
-// rest of the row instead (without: 92 us).  Forward 2048 x 32000 bf16 24.5 us (4.6 TB/s), with workgroups of 1024 29, of 256 42.
-template <int DT, int T, int U, bool GRAD, bool STREAM>
+// HBM bounds it, with reads and writes of 512 rows at once (5.2 TB/s; the exponentials keep the vector units busy for 60 % of 16-bit rows' time, and
+// fewer instructions do not make it shorter).  So that one row's reads pass while another's exponentials do, a kernel has at most 64 registers and
+// half of the LDS, and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every sixth row masked, 375 us; with one workgroup of up
+// to 128 registers 417 to 435, with workgroups of 512 that read more of the row again 450, without LDS 384.  1024 x 50257 fp32 76 us (5.1 TB/s);
+// loads of what stays in registers go past the caches, which keep the rest of the row instead (without: 10 us more).  Forward 2048 x 32000
+// bf16 24.5 us (4.6 TB/s), with workgroups of 1024 29, of 256 42.
+template <int DT, int T, int U, int L, bool GRAD, bool STREAM>
 __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
   typedef typename StepElem<DT>::raw raw;
   constexpr int N = 16 / (int)sizeof(raw);
-  __shared__ MaxSum lds[2][T / kStepWave];
+  __shared__ struct {
+    uint4 kept[L * T + 1];               // (at 0, as where loads straight to LDS go is said in 16 bits)
+    MaxSum lds[2][T / kStepWave];
+    double sums[kSums];                  // (thread 0's)
+  } sh;
   const float k = a.k;
-  __shared__ double sums[kSums];         // (thread 0's)
   if (threadIdx.x == 0)
-    for (int i = 0; i < kSums; ++i) sums[i] = 0.0;
+    for (int i = 0; i < kSums; ++i) sh.sums[i] = 0.0;
   uint32_t turn = 0;
   for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
@@ -261,6 +272,9 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
       if (v < nvec) r[u].template load_at<STREAM>(zv, v * 16u);
       else r[u].fill_lowest();
     }
+#pragma unroll
+    for (int l = 0; l < L; ++l)
+      if ((U + l) * T + me < nvec) load_to_lds(zv, ((U + l) * T + me) * 16u, &sh.kept[l * T + (threadIdx.x & ~(kStepWave - 1u))]);
     const float zt = step_get<DT>(z, t);
     MaxSum ms = {-INFINITY, 0.0f};
     float last = -INFINITY;
@@ -269,15 +283,23 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
       ms = {last, loss_exp(last, loss_base(last), k)};
     }
     take_vectors<DT, N, U>(r, k, ms);
-    for (uint32_t v = U * T + me; v < nvec; v += T) {
+    if (L) loads_arrived();
+#pragma unroll 1
+    for (int l = 0; l < L; ++l)
+      if ((U + l) * T + me < nvec) {
+        StepVec<DT, N> more;
+        more.from(sh.kept[l * T + me]);
+        take_vectors<DT, N, 1>(&more, k, ms);
+      }
+    for (uint32_t v = (U + L) * T + me; v < nvec; v += T) {
       StepVec<DT, N> more;
       more.load_at(zv, v * 16u);
       take_vectors<DT, N, 1>(&more, k, ms);
     }
-    ms = join_all<T>(ms, k, lds[turn]);
+    ms = join_all<T>(ms, k, sh.lds[turn]);
     turn ^= 1u;                          // (of the rows that come here: whoever writes a half again is behind the other one's barrier)
     ms = {uniform(loss_base(ms.m)), uniform(ms.s)};
-    const float g = uniform(row_end(a, row, in, (double)zt - (double)ms.m, ms.s, threadIdx.x == 0, sums));
+    const float g = uniform(row_end(a, row, in, (double)zt - (double)ms.m, ms.s, threadIdx.x == 0, sh.sums));
     if (!GRAD) continue;
     if (ms.s == 0.0f) {                  // no logit above -infinity
       zero_row<DT, T>(out, a.vocab);
@@ -286,12 +308,19 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
     const float base = ms.m, gs = -g / ms.s;
     asm("" : "+v"(me));
     raw* ov = out + at.head;
-    if (U * T + me < nvec)
-      for (uint32_t n = (nvec - 1u - U * T - me) / T + 1u; n-- != 0;) {
-        const uint32_t bytes = (U * T + me + n * T) * 16u;
+    if ((U + L) * T + me < nvec)
+      for (uint32_t n = (nvec - 1u - (U + L) * T - me) / T + 1u; n-- != 0;) {
+        const uint32_t bytes = ((U + L) * T + me + n * T) * 16u;
         StepVec<DT, N> more;
         more.load_at(zv, bytes);
         grad_vector<DT, N>(more, k, base, gs, ov, bytes);
+      }
+#pragma unroll 1
+    for (int l = 0; l < L; ++l)
+      if ((U + l) * T + me < nvec) {
+        StepVec<DT, N> more;
+        more.from(sh.kept[l * T + me]);
+        grad_vector<DT, N>(more, k, base, gs, ov, ((U + l) * T + me) * 16u);
       }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -304,7 +333,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
     if (at.in_vectors(t) ? at.vector_of(t) % T == threadIdx.x : t == end) step_put<DT>(out, t, gs * loss_exp(zt, base, k) + g);
   }
   if (a.sums && threadIdx.x == 0)
-    for (int i = 0; i < kSums; ++i) a.part[(size_t)i * gridDim.x + blockIdx.x] = sums[i];
+    for (int i = 0; i < kSums; ++i) a.part[(size_t)i * gridDim.x + blockIdx.x] = sh.sums[i];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -462,14 +491,15 @@ template <int DT>
 void launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t nvec = a.vocab / (16 / step_elem_bytes(DT));
   const bool stream = (size_t)a.rows * a.vocab * step_elem_bytes(DT) > kStreamBytes;
-#define ROWS(T, U) launch_row_kernel(a.grad ? stream ? dfx_loss_rows_kernel<DT, T, U, true, true> : dfx_loss_rows_kernel<DT, T, U, true, false> \
-                                            : stream ? dfx_loss_rows_kernel<DT, T, U, false, true> : dfx_loss_rows_kernel<DT, T, U, false, false>, T, groups, a, s)
-  if (nvec <= 256) ROWS(128, 2);
-  else if (nvec <= 512) ROWS(128, 4);
-  else if (nvec <= 1024) ROWS(256, 4);
-  else if (nvec <= 2048) ROWS(512, 4);
-  else if (nvec <= 4096) ROWS(512, 8);
-  else ROWS(1024, 6);
+#define ROWS(T, U, L, F) launch_row_kernel(a.grad ? stream ? dfx_loss_rows_kernel<DT, T, U, L, true, true> : dfx_loss_rows_kernel<DT, T, U, L, true, false> \
+                                                  : stream ? dfx_loss_rows_kernel<DT, T, F, 0, false, true> : dfx_loss_rows_kernel<DT, T, F, 0, false, false>, T, groups, a, s)
+  if (nvec <= 256) ROWS(128, 2, 0, 2);
+  else if (nvec <= 512) ROWS(128, 4, 0, 4);
+  else if (nvec <= 1024) ROWS(256, 4, 0, 4);
+  else if (nvec <= 2048) ROWS(512, 4, 0, 4);
+  else if (nvec <= 4096) ROWS(512, 8, 0, 8);
+  else if (nvec <= 10240) ROWS(1024, 6, 4, 6);
+  else ROWS(1024, 8, 4, 6);              // (where more is read again, a few spilled registers are the lesser evil: 4096 x 131072 bf16 380 and 375 us; x 65536 195 and 199)
 #undef ROWS
 }
 

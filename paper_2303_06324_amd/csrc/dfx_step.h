@@ -89,6 +89,7 @@ struct StepVec {
     else *q = w;
   }
   __device__ __forceinline__ void fill_lowest() { w = DT == DFX_F32 ? 0xff800000u : DT == DFX_BF16 ? 0xff80ff80u : 0xfc00fc00u; }      // -infinity
+  __device__ __forceinline__ void from(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }      // (16 bytes of them)
   // what was made of the elements so far is made anew behind this, not kept: a vector of 16-bit elements takes half the registers of its values
   __device__ __forceinline__ void again() { asm("" : "+v"(w)); }
   __device__ __forceinline__ float get(int k) const {
@@ -107,6 +108,13 @@ struct StepVec {
     }
   }
 };
+
+// nothing of what follows is begun before every load so far has arrived
+__device__ __forceinline__ void loads_arrived() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0), the other counters at their largest
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
