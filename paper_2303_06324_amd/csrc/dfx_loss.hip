@@ -18,10 +18,6 @@ constexpr int kSums = 5;
 constexpr uint32_t kGroups = 4096;       // workgroups of a call, at most: each leaves its share of the sums
 constexpr int kSumWaves = 3;             // waves that share a sum
 constexpr int kSumThreads = kSums * kSumWaves * kStepWave;
-// Logits of more bytes than this are read past the caches where they stay in registers, and the caches keep what is read again.  Below it, what
-// produced them has left them in the memory-side cache (256 MiB), where such loads find less.  Behind a matrix product, bf16 with gradient:
-// 1024 x 50257 (98 MiB) 36 us, past the caches 47; 1536 (147 MiB) 53 and 67; 1792 (172 MiB) 94 and 81; 2048 (196 MiB) 120 and 87.
-constexpr size_t kStreamBytes = 160u << 20;
 // Few rows of a long vocabulary are split over workgroups.
 constexpr int kSplitThreads = 256;
 constexpr uint32_t kSplitGroups = 512;   // workgroups, at most
@@ -232,12 +228,14 @@ __device__ __forceinline__ void zero_row(typename StepElem<DT>::raw* out, uint32
 // fewer instructions do not make it shorter).  So that one row's reads pass while another's exponentials do, a kernel has at most 64 registers and
 // half of the LDS, and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every sixth row masked, 375 us; with one workgroup of up
 // to 128 registers 417 to 435, with workgroups of 512 that read more of the row again 450, without LDS 384.  1024 x 50257 fp32 76 us (5.1 TB/s);
-// loads of what stays in registers go past the caches, which keep the rest of the row instead (without: 10 us more).  Forward 2048 x 32000
-// bf16 24.5 us (4.6 TB/s), with workgroups of 1024 29, of 256 42.
-template <int DT, int T, int U, int L, bool GRAD, bool STREAM>
+// loads of what stays in registers go past the caches, which keep the rest of the row instead (without: 84).  Behind the matrix product that leaves
+// its logits in the memory-side cache that costs nothing (1024 x 50257 bf16 29 and 28 us, forward 16 and 14; 2048 x 50257 65 and 98, 30 and 63).
+// Forward 2048 x 32000 bf16 22.6 us (5.0 TB/s), with workgroups of 1024 29, of 256 42.
+template <int DT, int T, int U, int L, bool GRAD>
 __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
   typedef typename StepElem<DT>::raw raw;
   constexpr int N = 16 / (int)sizeof(raw);
+  constexpr bool LINES = T >= 512;       // vectors fill whole lines, and what stays in registers is read past the caches
   __shared__ struct {
     uint4 kept[L * T + 1];               // (at 0, as where loads straight to LDS go is said in 16 bits)
     MaxSum lds[2][T / kStepWave];
@@ -260,7 +258,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
       continue;
     }
     const uint32_t t = (uint32_t)in.t;
-    const RowPlace<DT, (T >= 512)> at(z, a.vocab);
+    const RowPlace<DT, LINES> at(z, a.vocab);
     const uint32_t nvec = at.nvec;
     const raw* zv = z + at.head;
     uint32_t me = thread_here();
@@ -269,7 +267,7 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t v = u * T + me;
-      if (v < nvec) r[u].template load_at<STREAM>(zv, v * 16u);
+      if (v < nvec) r[u].template load_at<LINES>(zv, v * 16u);
       else r[u].fill_lowest();
     }
 #pragma unroll
@@ -490,9 +488,7 @@ void launch_row_kernel(void (*kernel)(LossArgs), int threads, uint32_t groups, c
 template <int DT>
 void launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t nvec = a.vocab / (16 / step_elem_bytes(DT));
-  const bool stream = (size_t)a.rows * a.vocab * step_elem_bytes(DT) > kStreamBytes;
-#define ROWS(T, U, L, F) launch_row_kernel(a.grad ? stream ? dfx_loss_rows_kernel<DT, T, U, L, true, true> : dfx_loss_rows_kernel<DT, T, U, L, true, false> \
-                                                  : stream ? dfx_loss_rows_kernel<DT, T, F, 0, false, true> : dfx_loss_rows_kernel<DT, T, F, 0, false, false>, T, groups, a, s)
+#define ROWS(T, U, L, F) launch_row_kernel(a.grad ? dfx_loss_rows_kernel<DT, T, U, L, true> : dfx_loss_rows_kernel<DT, T, F, 0, false>, T, groups, a, s)
   if (nvec <= 256) ROWS(128, 2, 0, 2);
   else if (nvec <= 512) ROWS(128, 4, 0, 4);
   else if (nvec <= 1024) ROWS(256, 4, 0, 4);
