@@ -5,7 +5,9 @@ fallback: importing this module without the built library raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import itertools
 import os
 from typing import List, Optional, Tuple
 
@@ -345,8 +347,12 @@ class TensorList:
 
     def __init__(self, tensors):
         self._h = C.c_void_p()
-        arr = (Tensor * len(tensors))(*[(p, n, t, 0) for p, n, t in tensors])
-        rc = _lib.dfx_list_create(C.byref(self._h), arr, len(tensors))
+        # three 64-bit words are a dfx_tensor (type and reserved word share the last)
+        words = array.array("Q", itertools.chain.from_iterable(tensors))
+        n = len(words) // 3
+        if len(words) % 3 or n != len(tensors):
+            raise ValueError("a tensor is (address, elements, type)")
+        rc = _lib.dfx_list_create(C.byref(self._h), C.cast(words.buffer_info()[0], C.POINTER(Tensor)) if n else None, n)
         if rc != OK:
             self._h = C.c_void_p()
             raise DfxError(rc, "dfx_list_create")

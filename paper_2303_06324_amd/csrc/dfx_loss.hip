@@ -50,25 +50,22 @@ struct MaxSum { float m, s; };           // s = sum 2^(k (z - m)); nothing seen 
 __device__ __forceinline__ float loss_base(float m) { return m == -INFINITY ? 0.0f : m; }
 __device__ __forceinline__ float loss_exp(float z, float base, float k) { return __builtin_amdgcn_exp2f((z - base) * k); }
 
-// over the first N of each 64 lanes' entries, for all of them
-template <int N>
-__device__ __forceinline__ MaxSum join_lanes(MaxSum ms, float k) {
+// over each n (a power of two) lanes' entries, for all of them
+__device__ __forceinline__ MaxSum join_lanes(MaxSum ms, float k, uint32_t n) {
   float top = ms.m;
-#pragma unroll
-  for (int d = N / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  for (uint32_t d = n / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, (int)d));
   ms.s *= loss_exp(ms.m, loss_base(top), k);
-#pragma unroll
-  for (int d = N / 2; d; d >>= 1) ms.s += __shfl_xor(ms.s, d);
+  for (uint32_t d = n / 2; d; d >>= 1) ms.s += __shfl_xor(ms.s, (int)d);
   return {top, ms.s};
 }
 
 // over a workgroup of T threads, for all of them; one barrier.  lds: T / 64 entries that nobody reads any more
 template <int T>
 __device__ __forceinline__ MaxSum join_all(MaxSum ms, float k, MaxSum* lds) {
-  ms = join_lanes<kStepWave>(ms, k);
+  ms = join_lanes(ms, k, kStepWave);
   if ((threadIdx.x & (kStepWave - 1)) == 0) lds[threadIdx.x / kStepWave] = ms;
   __syncthreads();
-  return join_lanes<T / kStepWave>(lds[threadIdx.x % (T / kStepWave)], k);      // every wave joins them once more, an entry a lane
+  return join_lanes(lds[threadIdx.x % (T / kStepWave)], k, T / kStepWave);      // every wave joins them once more, an entry a lane
 }
 
 constexpr double kLog2 = 0.69314718055994530942, kLog2e = 1.44269504088896340736;
@@ -338,7 +335,9 @@ __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
 // few rows: each split over workgroups, in two kernels: the segments' parts, then all of them joined by everyone who needs them.  No row's
 // logits are read behind a write of another workgroup, so the gradient may take their place.
 // ------------------------------------------------------------------------------------------
-struct Split { uint32_t segments, vectors; };   // of a row; vectors of a segment (a multiple of kSplitThreads).  What lies outside a row's vectors goes with the last
+// Segments of a row (at most 64), vectors of a segment (a multiple of kSplitThreads), and the power of two that holds the segments.  What lies outside
+// a row's vectors goes with the last segment.
+struct Split { uint32_t segments, vectors, lanes, lanes_log2; };
 
 template <int DT>
 __device__ __forceinline__ bool segment_has(const Split& sp, const RowPlace<DT, true>& at, uint32_t seg, uint32_t t) {
@@ -378,12 +377,48 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_parts_kernel(LossArgs 
   }
 }
 
+// The sums over split rows, by one workgroup beside the rows' own: as many lanes to a row as it has segments, so that a few steps do for any
+// number of rows (their product is bounded).
+template <int DT>
+__device__ __forceinline__ void split_sums(const LossArgs& a, const Split& sp) {
+  constexpr int T = kSplitThreads;
+  __shared__ double lds[T / kStepWave][kSums];
+  const uint32_t me = threadIdx.x, i = me & (sp.lanes - 1u), step = T >> sp.lanes_log2;
+  double s[kSums] = {0, 0, 0, 0, 0};
+  for (uint32_t first = 0; first < a.rows; first += step) {
+    const uint32_t row = first + (me >> sp.lanes_log2);
+    LossPart part = {-INFINITY, 0.0f, 0.0f, 0.0f};
+    RowIn in = {-1, 0, 0, 0, 0, 0};
+    if (row < a.rows) in = row_in(a, row);
+    const bool counts = row_counts(a, in);
+    if (counts && i < sp.segments) part = a.parts[row * sp.segments + i];
+    const MaxSum ms = join_lanes({part.m, part.s}, a.k, sp.lanes);
+    float zt = part.zt;                  // (0 but where the target is)
+    for (uint32_t d = sp.lanes / 2u; d; d >>= 1) zt += __shfl_xor(zt, (int)d);
+    if (counts && i == 0) add_sums(s, row_value(a, in, (double)zt - (double)loss_base(ms.m), ms.s));
+  }
+  for (int q = 0; q < kSums; ++q) {
+    s[q] = wave_sum(s[q]);
+    if ((me & (kStepWave - 1)) == 0) lds[me / kStepWave][q] = s[q];
+  }
+  __syncthreads();
+  if (me < kSums) {
+    double all = lds[0][me];
+    for (int w = 1; w < T / kStepWave; ++w) all += lds[w][me];
+    a.sums[me] = (float)all;
+  }
+}
+
 // Every workgroup joins its row's parts again.
 template <int DT, bool GRAD>
 __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs a, Split sp) {
   constexpr int T = kSplitThreads, N = 16 / (int)sizeof(typename StepElem<DT>::raw), U = 2;
   const float k = a.k;
   const uint32_t row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x % kStepWave;      // (without gradient there is one of a row)
+  if (row == a.rows) {
+    if (seg == 0) split_sums<DT>(a, sp);
+    return;
+  }
   typedef typename StepElem<DT>::raw raw;
   const raw* z = (const raw*)a.logits + (size_t)row * a.logits_stride;
   raw* out = GRAD ? (raw*)a.grad + (size_t)row * a.grad_stride : nullptr;
@@ -395,7 +430,6 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
   const RowIn in = row_in(a, row);
   const bool writes = seg == 0 && threadIdx.x == 0, counts = row_counts(a, in);
   float s = 0.0f, g = 0.0f, base = 0.0f, zt = 0.0f;
-  double sums[kSums] = {0, 0, 0, 0, 0};
   StepVec<DT, N> r[U];
   if (GRAD && counts)                    // (under way while the parts are joined)
 #pragma unroll
@@ -407,15 +441,13 @@ __global__ void __launch_bounds__(kSplitThreads) dfx_loss_split_kernel(LossArgs 
     if (lane < sp.segments) part = a.parts[row * sp.segments + lane];
     zt = __shfl(part.zt, __ffsll(__ballot(part.has != 0.0f)) - 1);      // (a target that counts lies in one of them)
     MaxSum ms = {part.m, part.s};
-    ms = join_lanes<kStepWave>(ms, k);
+    ms = join_lanes(ms, k, kStepWave);
     base = loss_base(ms.m); s = ms.s;
-    g = row_end(a, row, in, (double)zt - (double)base, s, writes, sums);
+    g = row_end(a, row, in, (double)zt - (double)base, s, writes, nullptr);
   } else if (writes) {
     if (a.logp) a.logp[row] = 0.0f;
     if (a.loss) a.loss[row] = 0.0f;
   }
-  if (a.sums && writes)
-    for (int i = 0; i < kSums; ++i) a.part[(size_t)i * a.rows + row] = sums[i];
   if (!GRAD) return;
   const float gs = s == 0.0f ? 0.0f : -g / s;
   if (s == 0.0f) {                       // nothing to learn from (the whole workgroup)
@@ -468,19 +500,21 @@ uint32_t loss_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows * 
 // the lengths below on it is worth the launch more.  Above 64 rows the two ways meet (128 rows of 131072 bf16: 24.8 and 24.4 us; 256: 31.7 and
 // 40.7), since a split row is read twice.
 Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
-  Split sp = {0, 0};
+  Split sp = {0, 0, 1, 0};
   if (a.rows == 0 || a.rows > kSplitRows || a.vocab < (a.grad ? kSplitGrad : kSplitForward)) return sp;
   const uint32_t nvec = a.vocab / (16u / elem_bytes), want = std::min<uint32_t>(kStepWave, kSplitGroups / a.rows);
   sp.vectors = ((nvec + want - 1) / want + kSplitThreads - 1) / kSplitThreads * kSplitThreads;
   sp.segments = (nvec + sp.vectors - 1) / sp.vectors;
+  for (; sp.lanes < sp.segments; sp.lanes *= 2) ++sp.lanes_log2;
   return sp;
 }
 
 template <int DT>
 void launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
   hipLaunchKernelGGL((dfx_loss_parts_kernel<DT>), dim3(sp.segments, a.rows), dim3(kSplitThreads), 0, s, a, sp);
-  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(sp.segments, a.rows), dim3(kSplitThreads), 0, s, a, sp);
-  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(1, a.rows), dim3(kSplitThreads), 0, s, a, sp);
+  const uint32_t more = a.sums ? 1u : 0u;
+  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(sp.segments, a.rows + more), dim3(kSplitThreads), 0, s, a, sp);
+  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(1, a.rows + more), dim3(kSplitThreads), 0, s, a, sp);
 }
 
 void launch_row_kernel(void (*kernel)(LossArgs), int threads, uint32_t groups, const LossArgs& a, hipStream_t s) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, s, a); }
@@ -553,13 +587,14 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   a.k = (float)(u->inv_temperature * kLog2e);
   hipStream_t s = (hipStream_t)hip_stream;
   const uint32_t groups = loss_groups(u->rows);
-  const Split sp = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype) ? loss_split(a, (uint32_t)eb) : Split{0, 0};
+  const Split sp = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype) ? loss_split(a, (uint32_t)eb) : Split{0, 0, 1, 0};
   if (sp.segments) {
     if (u->dtype == DFX_F32) launch_split<DFX_F32>(a, sp, s);
     else if (u->dtype == DFX_BF16) launch_split<DFX_BF16>(a, sp, s);
     else launch_split<DFX_F16>(a, sp, s);
-    if (hipGetLastError() != hipSuccess) return DFX_ERR_HIP;
-  } else if (groups) {
+    return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP;
+  }
+  if (groups) {
     if (u->dtype == DFX_F32) launch_rows<DFX_F32>(a, groups, s);
     else if (u->dtype == DFX_BF16) launch_rows<DFX_BF16>(a, groups, s);
     else launch_rows<DFX_F16>(a, groups, s);

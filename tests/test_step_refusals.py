@@ -82,3 +82,15 @@ def test_loss_refuses_results_that_lie_on_what_is_read(kw):
     import paper_2303_06324_amd as dfx
     from paper_2303_06324_amd import binding
     assert binding._lib.dfx_policy_loss(_args(dfx, **kw), None) == dfx.ERR_INVALID_ARG
+
+
+def test_lists_of_what_is_no_tensor():
+    import paper_2303_06324_amd as dfx
+    for bad in ([(0x1000, 4)], [(0x1000, 4, dfx.F32), (0x1000, 4)], [(0x1000, 4, dfx.F32, 0)]):
+        with pytest.raises(ValueError):
+            dfx.TensorList(bad)
+    with pytest.raises(OverflowError):
+        dfx.TensorList([(0x1000, -1, dfx.F32)])
+    for bad in ([(0x1000, 4, 1 << 32)], [(0x1000, 4, 3)], [(0x1001, 4, dfx.F32)]):
+        with pytest.raises(dfx.DfxError):
+            dfx.TensorList(bad)
