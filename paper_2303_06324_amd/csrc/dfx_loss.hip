@@ -22,7 +22,7 @@ constexpr int kSumThreads = kSums * kSumWaves * kStepWave;
 constexpr int kSplitThreads = 256;
 constexpr uint32_t kSplitGroups = 512;   // workgroups, at most
 constexpr uint32_t kSplitRows = 64;      // rows, at most
-constexpr uint32_t kSplitGrad = 40000, kSplitForward = 65536;      // elements of a row, at least
+constexpr uint32_t kSplitGrad = 20000, kSplitForward = 65536;      // elements of a row, at least
 
 struct LossPart { float m, s, zt, has; };       // of a segment of a row; zt: the target's logit, where the segment has it (has = 1, else both 0)
 
@@ -495,10 +495,10 @@ __global__ void __launch_bounds__(kSumThreads) dfx_loss_sums_kernel(const double
 uint32_t loss_groups(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows, kGroups); }
 uint32_t loss_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows * kStepWave, kSplitGroups); }      // at most
 
-// How a call is split, or segments = 0.  A row alone on its workgroup takes as long as that needs for its elements, whatever their type: with
-// gradient 9.7 us of 32000 elements, 10.5 of 50257, 20.5 of 131072, forward 4.5, 5.5 and 10.5; split 8.1 us and 5.2 at every length, so from
-// the lengths below on it is worth the launch more.  Above 64 rows the two ways meet (128 rows of 131072 bf16: 24.8 and 24.4 us; 256: 31.7 and
-// 40.7), since a split row is read twice.
+// How a call is split, or segments = 0.  A row alone on its workgroup takes as long as that needs for its elements.  One row of bf16, us, alone and
+// split: with gradient and sums (two kernels either way) 20000 elements 7.8 and 6.7, 50257 10.3 and 7.2, 131072 19.2 and 7.2; forward (a launch
+// more, which costs the host 3) 32000 4.4 and 4.9, 70000 6.7 and 4.9, 131072 10.5 and 5.1.  64 rows with gradient 9.1 and 8.7, 12.1 and 9.7, 21.8 and
+// 12.5.  At 128 the two ways meet (9.6 and 9.7, 12.6 and 11.9, 23.4 and 20.7), since a split row is read twice; 200 rows of 131072 27.5 and 33.6.
 Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
   Split sp = {0, 0, 1, 0};
   if (a.rows == 0 || a.rows > kSplitRows || a.vocab < (a.grad ? kSplitGrad : kSplitForward)) return sp;
