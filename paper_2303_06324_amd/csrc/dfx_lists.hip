@@ -40,7 +40,9 @@ struct ListScratch {
 struct dfx_list {
   int device = 0;
   uint32_t nchunks = 0;
+  bool all_f32 = true;
   std::vector<dfx_tensor> tensors;
+  std::vector<size_t> counts;            // the tensors', for comparisons between lists
   ListChunk* chunks = nullptr;           // device
   ListScratch* scratch = nullptr;        // device
 };
@@ -328,20 +330,8 @@ bool on_its_device(const dfx_list* l) {
 }
 
 bool same_counts(const dfx_list* a, const dfx_list* b) {
-  if (a == b) return true;
-  if (a->device != b->device || a->tensors.size() != b->tensors.size()) return false;
-  for (size_t k = 0; k < a->tensors.size(); ++k)
-    if (a->tensors[k].count != b->tensors[k].count) return false;
-  return true;
+  return a == b || (a->device == b->device && a->counts.size() == b->counts.size() && (a->counts.empty() || !memcmp(a->counts.data(), b->counts.data(), a->counts.size() * sizeof(size_t))));
 }
-
-bool all_f32(const dfx_list* l) {
-  for (const dfx_tensor& t : l->tensors)
-    if (t.dtype != DFX_F32) return false;
-  return true;
-}
-
-int launched() { return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP; }
 
 int check_norm(const dfx_list* l, int kind, double scale, const float* norm) {
   if (!l || !norm || ((uintptr_t)norm & 3u) || (kind != DFX_NORM_2 && kind != DFX_NORM_INF) || !isfinite(scale)) return DFX_ERR_INVALID_ARG;
@@ -363,20 +353,16 @@ int check_clip(const dfx_list* src, const dfx_list* dst, const float* norm, doub
 
 int launch_norm(const dfx_list* l, int kind, double scale, float* norm, hipStream_t stream) {
   if (!l->nchunks) {
-    hipLaunchKernelGGL(dfx_zero_norm_kernel, dim3(1), dim3(1), 0, stream, norm);
-    return launched();
+    return step_launch(dfx_zero_norm_kernel, dim3(1), 1, stream, norm);
   }
   const dim3 grid(std::min<uint32_t>(l->nchunks, (uint32_t)kNormGroups));
-  if (kind == DFX_NORM_2) hipLaunchKernelGGL(dfx_norm_kernel<false>, grid, dim3(kNormThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
-  else hipLaunchKernelGGL(dfx_norm_kernel<true>, grid, dim3(kNormThreads), 0, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
-  return launched();
+  return step_launch(kind == DFX_NORM_2 ? dfx_norm_kernel<false> : dfx_norm_kernel<true>, grid, kNormThreads, stream, l->chunks, l->nchunks, l->scratch, scale, norm);
 }
 
 int launch_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale, hipStream_t stream) {
   if (!dst) dst = src;
   if (!src->nchunks) return DFX_OK;
-  hipLaunchKernelGGL(dfx_clip_kernel, dim3(std::min(src->nchunks, kMaxGroups)), dim3(kClipThreads), 0, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
-  return launched();
+  return step_launch(dfx_clip_kernel, dim3(std::min(src->nchunks, kMaxGroups)), kClipThreads, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
 }
 
 }  // namespace
@@ -400,6 +386,10 @@ int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n) {
   try {
     l = new dfx_list;
     l->tensors.assign(tensors, tensors + n);
+    for (const dfx_tensor& t : l->tensors) {
+      l->counts.push_back(t.count);
+      l->all_f32 = l->all_f32 && t.dtype == DFX_F32;
+    }
     l->nchunks = (uint32_t)nchunks;
     // scratch in front, zeroed with the table's upload
     const size_t at = (sizeof(ListScratch) + 255) / 256 * 256, bytes = at + nchunks * sizeof(ListChunk);
@@ -414,7 +404,7 @@ int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n) {
       l->chunks = (ListChunk*)(dev + at);
       if (hipMemcpy(dev, host.data(), bytes, hipMemcpyHostToDevice) != hipSuccess) rc = DFX_ERR_HIP;
     }
-  } catch (const std::bad_alloc&) {
+  } catch (...) {                          // (host memory)
     rc = DFX_ERR_NO_RESOURCES;
   }
   if (rc != DFX_OK) {
@@ -468,7 +458,7 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   if (((uintptr_t)norm_dev & 3u) || ((uintptr_t)cfg->step_dev & 3u) || ((uintptr_t)cfg->lr_dev & 3u)) return DFX_ERR_INVALID_ARG;
   if (!same_counts(params, grads) || !same_counts(params, exp_avg) || !same_counts(params, exp_avg_sq) || (copies && !same_counts(params, copies))) return DFX_ERR_INVALID_ARG;
   if (params == exp_avg || params == exp_avg_sq || exp_avg == exp_avg_sq || params == grads || grads == exp_avg || grads == exp_avg_sq || (copies && (copies == params || copies == grads || copies == exp_avg || copies == exp_avg_sq))) return DFX_ERR_INVALID_ARG;
-  if (!all_f32(params) || !all_f32(exp_avg) || !all_f32(exp_avg_sq) || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
+  if (!params->all_f32 || !exp_avg->all_f32 || !exp_avg_sq->all_f32 || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
   if (!params->nchunks) return DFX_OK;
   if (params->nchunks > kMaxGroups) return DFX_ERR_TOO_LARGE;
   AdamArgs a;
@@ -482,10 +472,7 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = (float)cfg->max_norm;
   a.correct1 = (float)(1.0 / (1.0 - pow(cfg->beta1, (double)cfg->step)));
   a.correct2 = (float)(1.0 / sqrt(1.0 - pow(cfg->beta2, (double)cfg->step)));
-  const dim3 grid(a.nchunks * kAdamParts);
-  if (a.nchunks >= kAdamStaged) hipLaunchKernelGGL(dfx_adamw_kernel<true>, grid, dim3(kAdamThreads), 0, (hipStream_t)hip_stream, a);
-  else hipLaunchKernelGGL(dfx_adamw_kernel<false>, grid, dim3(kAdamThreads), 0, (hipStream_t)hip_stream, a);
-  return launched();
+  return step_launch(a.nchunks >= kAdamStaged ? dfx_adamw_kernel<true> : dfx_adamw_kernel<false>, dim3(a.nchunks * kAdamParts), kAdamThreads, (hipStream_t)hip_stream, a);
 }
 
 }  // extern "C"

@@ -510,26 +510,25 @@ Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
 }
 
 template <int DT>
-void launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
-  hipLaunchKernelGGL((dfx_loss_parts_kernel<DT>), dim3(sp.segments, a.rows), dim3(kSplitThreads), 0, s, a, sp);
+int launch_split(const LossArgs& a, const Split& sp, hipStream_t s) {
   const uint32_t more = a.sums ? 1u : 0u;
-  if (a.grad) hipLaunchKernelGGL((dfx_loss_split_kernel<DT, true>), dim3(sp.segments, a.rows + more), dim3(kSplitThreads), 0, s, a, sp);
-  else hipLaunchKernelGGL((dfx_loss_split_kernel<DT, false>), dim3(1, a.rows + more), dim3(kSplitThreads), 0, s, a, sp);
+  const int rc = step_launch(dfx_loss_parts_kernel<DT>, dim3(sp.segments, a.rows), kSplitThreads, s, a, sp);
+  if (rc != DFX_OK) return rc;
+  if (a.grad) return step_launch(dfx_loss_split_kernel<DT, true>, dim3(sp.segments, a.rows + more), kSplitThreads, s, a, sp);
+  return step_launch(dfx_loss_split_kernel<DT, false>, dim3(1, a.rows + more), kSplitThreads, s, a, sp);
 }
 
-void launch_row_kernel(void (*kernel)(LossArgs), int threads, uint32_t groups, const LossArgs& a, hipStream_t s) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, s, a); }
-
 template <int DT>
-void launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
+int launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t nvec = a.vocab / (16 / step_elem_bytes(DT));
-#define ROWS(T, U, L, F) launch_row_kernel(a.grad ? dfx_loss_rows_kernel<DT, T, U, L, true> : dfx_loss_rows_kernel<DT, T, F, 0, false>, T, groups, a, s)
+#define ROWS(T, U, L, F) return step_launch(a.grad ? dfx_loss_rows_kernel<DT, T, U, L, true> : dfx_loss_rows_kernel<DT, T, F, 0, false>, dim3(groups), T, s, a)
   if (nvec <= 256) ROWS(128, 2, 0, 2);
-  else if (nvec <= 512) ROWS(128, 4, 0, 4);
-  else if (nvec <= 1024) ROWS(256, 4, 0, 4);
-  else if (nvec <= 2048) ROWS(512, 4, 0, 4);
-  else if (nvec <= 4096) ROWS(512, 8, 0, 8);
-  else if (nvec <= 10240) ROWS(1024, 6, 4, 6);
-  else ROWS(1024, 8, 4, 6);              // (where more is read again, a few spilled registers are the lesser evil: 4096 x 131072 bf16 380 and 375 us; x 65536 195 and 199)
+  if (nvec <= 512) ROWS(128, 4, 0, 4);
+  if (nvec <= 1024) ROWS(256, 4, 0, 4);
+  if (nvec <= 2048) ROWS(512, 4, 0, 4);
+  if (nvec <= 4096) ROWS(512, 8, 0, 8);
+  if (nvec <= 10240) ROWS(1024, 6, 4, 6);
+  ROWS(1024, 8, 4, 6);                   // (where more is read again, a few spilled registers are the lesser evil: 4096 x 131072 bf16 380 and 375 us; x 65536 195 and 199)
 #undef ROWS
 }
 
@@ -588,20 +587,13 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   hipStream_t s = (hipStream_t)hip_stream;
   const uint32_t groups = loss_groups(u->rows);
   const Split sp = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype) ? loss_split(a, (uint32_t)eb) : Split{0, 0, 1, 0};
-  if (sp.segments) {
-    if (u->dtype == DFX_F32) launch_split<DFX_F32>(a, sp, s);
-    else if (u->dtype == DFX_BF16) launch_split<DFX_BF16>(a, sp, s);
-    else launch_split<DFX_F16>(a, sp, s);
-    return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP;
-  }
+  const bool f32 = u->dtype == DFX_F32, bf16 = u->dtype == DFX_BF16;
+  if (sp.segments) return f32 ? launch_split<DFX_F32>(a, sp, s) : bf16 ? launch_split<DFX_BF16>(a, sp, s) : launch_split<DFX_F16>(a, sp, s);
   if (groups) {
-    if (u->dtype == DFX_F32) launch_rows<DFX_F32>(a, groups, s);
-    else if (u->dtype == DFX_BF16) launch_rows<DFX_BF16>(a, groups, s);
-    else launch_rows<DFX_F16>(a, groups, s);
-    if (hipGetLastError() != hipSuccess) return DFX_ERR_HIP;
+    const int rc = f32 ? launch_rows<DFX_F32>(a, groups, s) : bf16 ? launch_rows<DFX_BF16>(a, groups, s) : launch_rows<DFX_F16>(a, groups, s);
+    if (rc != DFX_OK) return rc;
   }
-  if (u->sums) hipLaunchKernelGGL(dfx_loss_sums_kernel, dim3(1), dim3(kSumThreads), 0, s, a.part, groups, u->sums);
-  return hipGetLastError() == hipSuccess ? DFX_OK : DFX_ERR_HIP;
+  return u->sums ? step_launch(dfx_loss_sums_kernel, dim3(1), kSumThreads, s, (const double*)a.part, groups, u->sums) : DFX_OK;
 }
 
 }  // extern "C"

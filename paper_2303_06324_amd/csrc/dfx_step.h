@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <tuple>
+
 #include "../../include/dfx.h"
 
 namespace {
@@ -108,6 +110,18 @@ struct StepVec {
     }
   }
 };
+
+// One kernel on a stream; the launch's own outcome, whatever error an earlier call of the caller's has left behind.
+template <class... P, class... A>
+int step_launch(void (*kernel)(P...), dim3 grid, int threads, hipStream_t stream, A... args) {
+  std::tuple<P...> held(static_cast<P>(args)...);
+  void* at[sizeof...(P)];
+  std::apply([&](auto&... x) {
+    size_t k = 0;
+    ((at[k++] = (void*)&x), ...);
+  }, held);
+  return hipLaunchKernel((const void*)kernel, grid, dim3(threads), at, 0, stream) == hipSuccess ? DFX_OK : DFX_ERR_HIP;
+}
 
 // nothing of what follows is begun before every load so far has arrived
 __device__ __forceinline__ void loads_arrived() {

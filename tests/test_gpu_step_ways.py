@@ -186,3 +186,31 @@ def test_loss_of_rows_that_begin_anywhere(vocab, dt):
         out = ts._run_loss(z, t, cols, 2, vocab, dt, stride=vocab + 1, goff=(off * 3 + 1) % n, **KW)
         ts._check_loss(out, zh, t, cols, 2, vocab, dt, **KW)
         z.check()
+
+
+def test_an_error_that_another_call_left_behind_is_not_this_ones():
+    """A call of the program's own that failed (a device that there is not) leaves its error with the runtime; the calls here report their own."""
+    import ctypes
+    import glob
+    import os
+    import torch
+    dfx, _ = ts._dfx()
+    libs = glob.glob(os.path.join(torch.__path__[0], "lib", "libamdhip64.so*"))
+    if not libs:
+        pytest.skip("the runtime's library is not beside torch")
+    hip = ctypes.CDLL(libs[0])
+    lists, bufs = ts._adam_state([(300, "f32")], 1, "bf16", "bf16")
+    n = ts._scalar()
+    z, zh, t, cols = ts._loss_case(4, 30000, "bf16", 3)
+    lp, tt = ts.Guarded(4, "f32"), t.cuda()
+    torch.cuda.synchronize()
+    assert hip.hipSetDevice(999) != 0
+    try:
+        dfx.grad_norm(lists[1], n.ptr())
+        dfx.clip_grad_norm(lists[1], n.ptr(), 1.0)
+        dfx.adamw(*lists[:4], dfx.AdamWConfig(), copies=lists[4], norm=n.ptr())
+        dfx.policy_loss(4, 30000, dfx.BF16, z.ptr(), tt.data_ptr(), logp=lp.ptr())
+    finally:
+        hip.hipGetLastError()
+    torch.cuda.synchronize()
+    assert float(n.t) > 0 and bool((lp.t < 0).all())
