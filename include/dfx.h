@@ -52,7 +52,7 @@ typedef enum {
   DFX_ERR_HIP = -6,       /* a HIP runtime call failed; see dfx_last_hip_error */
   DFX_ERR_NO_RESOURCES = -7, /* grid does not fit the GPU / connector pool exhausted */
   DFX_ERR_ABORTED = -8,   /* the daemon was aborted; context must be finalized */
-  DFX_ERR_TOO_LARGE = -9  /* dfx_collective_noalloc: beyond the sizes its static scratch memory is laid out for */
+  DFX_ERR_TOO_LARGE = -9  /* beyond the sizes the call is laid out for (dfx_collective_noalloc: its static scratch memory) */
 } dfx_status;
 
 /* One completion.  In the paper the CQE carries only the collective's ID (Sec. 5); the invocation

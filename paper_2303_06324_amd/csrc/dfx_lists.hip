@@ -9,7 +9,6 @@
 #include <string.h>
 
 #include <algorithm>
-#include <new>
 #include <vector>
 
 #include "dfx_step.h"
@@ -24,7 +23,7 @@ constexpr int kClipThreads = 1024;
 constexpr int kAdamThreads = 1024;
 constexpr int kAdamParts = 2;            // workgroups that share a chunk
 constexpr uint32_t kAdamStaged = 640;    // chunks from which on a thread's loads wait for one another
-constexpr uint32_t kMaxGroups = 1u << 20;      // (a grid's threads are counted in 32 bits; workgroups of longer lists take several chunks)
+constexpr uint32_t kMaxGroups = 1u << 20;      // (a grid's threads are counted in 32 bits) of a launch over a list
 
 struct ListChunk { uint64_t ptr; uint32_t n; int32_t dtype; };
 static_assert(sizeof(ListChunk) == 16, "a chunk is one 16-byte load");
@@ -55,8 +54,8 @@ namespace {
 // Squares and their sum are held in 64 bits: no gradient of 32 or 16 bits is too large or too small to be squared there, so no second,
 // scaled pass is needed, and the products cost nothing beside the reads (with sums in 32 bits the times are the same).
 //
-// HBM bounds it.  Two workgroups a compute unit, all loads of a chunk under way at once: sixteen 25 MiB bf16 buckets 70.5 us (5.9 TB/s),
-// 1 GiB of fp32 171 us (6.3 TB/s).  Half as many threads 113 and 195 us; 2048 workgroups of 256, all the waves that fit, 85 and 191 us:
+// HBM bounds it.  Two workgroups a compute unit, all loads of a chunk under way at once: sixteen 25 MiB bf16 buckets 69 us (6.1 TB/s),
+// 1 GiB of fp32 170 us (6.3 TB/s).  Half as many threads 113 and 195 us; 2048 workgroups of 256, all the waves that fit, 85 and 191 us:
 // what is in flight beyond about 16 MiB only gets in its own way.  A short list is its chain of waits (table, data, ticket): 4.0 us.
 // ------------------------------------------------------------------------------------------
 template <int DT, bool MAXIMUM>
@@ -146,7 +145,7 @@ __global__ void __launch_bounds__(kNormThreads) dfx_norm_kernel(const ListChunk*
 // clipping
 //
 // A workgroup per chunk, which ends with it; stores go past the caches, which have nothing to keep of them (into fp32, norm and clipping of
-// the sixteen buckets: 253 us, with ordinary stores 289; of the 253, the clipping takes 182, or 6.9 TB/s).  The chunks are taken from the
+// the sixteen buckets: 250 us, with ordinary stores 289; of the 250, the clipping takes 182, or 6.9 TB/s).  The chunks are taken from the
 // list's end: the norm has just read them in the other order, and the memory-side cache holds the last 256 MiB of that (from the front,
 // with workgroups of 256: 278 instead of 263 us).
 // ------------------------------------------------------------------------------------------
@@ -177,14 +176,14 @@ __device__ __forceinline__ void clip_chunk(const ListChunk& s, const ListChunk& 
 #pragma unroll
     for (int u = 0; u < U; ++u) r[u].load(from, (size_t)(u * kClipThreads + threadIdx.x) * N);
 #pragma unroll
-    for (int u = 0; u < U; ++u) clip_vector<SD, DD, N>(r[u], f).template store<true>(to, (size_t)(u * kClipThreads + threadIdx.x) * N);
+    for (int u = 0; u < U; ++u) clip_vector<SD, DD, N>(r[u], f).stream(to, (size_t)(u * kClipThreads + threadIdx.x) * N);
     return;
   }
   const uint32_t nvec = s.n / N;
   for (uint32_t v = threadIdx.x; v < nvec; v += kClipThreads) {
     StepVec<SD, N> r;
     r.load(from, (size_t)v * N);
-    clip_vector<SD, DD, N>(r, f).template store<true>(to, (size_t)v * N);
+    clip_vector<SD, DD, N>(r, f).stream(to, (size_t)v * N);
   }
   const uint32_t i = nvec * N + threadIdx.x;
   if (i < s.n) step_put<DD>(to, i, step_get<SD>(from, i) * f);
@@ -221,7 +220,6 @@ __global__ void __launch_bounds__(kClipThreads) dfx_clip_kernel(const ListChunk*
 // ------------------------------------------------------------------------------------------
 struct AdamArgs {
   const ListChunk *p, *g, *m, *v, *copy;      // copy: may be null
-  uint32_t nchunks;
   const float* norm;                          // may be null: nothing is clipped
   const uint32_t* step_dev;                   // may be null: correct1 / correct2 hold
   const float* lr_dev;                        // may be null: lr holds
@@ -257,13 +255,13 @@ __device__ __forceinline__ void adam_vector(const AdamRates& a, const ListChunk&
     adam_element(a, xp[j], rg.get(j), xm[j], xv[j]);
   }
   rp.put(xp); rm.put(xm); rv.put(xv);
-  rp.template store<true>((void*)p.ptr, i);
-  rm.template store<true>((void*)m.ptr, i);
-  rv.template store<true>((void*)v.ptr, i);
+  rp.stream((void*)p.ptr, i);
+  rm.stream((void*)m.ptr, i);
+  rv.stream((void*)v.ptr, i);
   if (CD >= 0) {
     StepVec<C, N> rc;
     rc.put(xp);
-    rc.template store<true>((void*)copy.ptr, i);
+    rc.stream((void*)copy.ptr, i);
   }
 }
 
@@ -460,11 +458,9 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   if (params == exp_avg || params == exp_avg_sq || exp_avg == exp_avg_sq || params == grads || grads == exp_avg || grads == exp_avg_sq || (copies && (copies == params || copies == grads || copies == exp_avg || copies == exp_avg_sq))) return DFX_ERR_INVALID_ARG;
   if (!params->all_f32 || !exp_avg->all_f32 || !exp_avg_sq->all_f32 || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
   if (!params->nchunks) return DFX_OK;
-  if (params->nchunks > kMaxGroups) return DFX_ERR_TOO_LARGE;
   AdamArgs a;
   memset(&a, 0, sizeof(a));
   a.p = params->chunks; a.g = grads->chunks; a.m = exp_avg->chunks; a.v = exp_avg_sq->chunks; a.copy = copies ? copies->chunks : nullptr;
-  a.nchunks = params->nchunks;
   a.norm = norm_dev; a.step_dev = cfg->step_dev; a.lr_dev = cfg->lr_dev;
   a.beta1_d = cfg->beta1; a.beta2_d = cfg->beta2;
   a.lr = (float)cfg->lr; a.beta1 = (float)cfg->beta1; a.beta2 = (float)cfg->beta2;
@@ -472,7 +468,14 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = (float)cfg->max_norm;
   a.correct1 = (float)(1.0 / (1.0 - pow(cfg->beta1, (double)cfg->step)));
   a.correct2 = (float)(1.0 / sqrt(1.0 - pow(cfg->beta2, (double)cfg->step)));
-  return step_launch(a.nchunks >= kAdamStaged ? dfx_adamw_kernel<true> : dfx_adamw_kernel<false>, dim3(a.nchunks * kAdamParts), kAdamThreads, (hipStream_t)hip_stream, a);
+  for (uint32_t done = 0; done < params->nchunks; done += kMaxGroups) {      // (more than one launch beyond 2^20 chunks)
+    const uint32_t n = std::min(params->nchunks - done, kMaxGroups);
+    const int rc = step_launch(params->nchunks >= kAdamStaged ? dfx_adamw_kernel<true> : dfx_adamw_kernel<false>, dim3(n * kAdamParts), kAdamThreads, (hipStream_t)hip_stream, a);
+    if (rc != DFX_OK) return rc;
+    a.p += n; a.g += n; a.m += n; a.v += n;
+    if (a.copy) a.copy += n;
+  }
+  return DFX_OK;
 }
 
 }  // extern "C"

@@ -221,13 +221,13 @@ __device__ __forceinline__ void zero_row(typename StepElem<DT>::raw* out, uint32
 // and the next L of them in LDS, where loads put them without a register in between; what a longer row has beyond these is read again, from
 // its end, and comes from the memory-side cache.
 //
-// HBM bounds it, with reads and writes of 512 rows at once (5.2 TB/s; the exponentials keep the vector units busy for 60 % of 16-bit rows' time, and
+// HBM bounds it, with reads and writes of 512 rows at once (5.2 TB/s; the exponentials keep the vector units busy for 57 % of 16-bit rows' time, and
 // fewer instructions do not make it shorter).  So that one row's reads pass while another's exponentials do, a kernel has at most 64 registers and
-// half of the LDS, and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every sixth row masked, 375 us; with one workgroup of up
-// to 128 registers 417 to 435, with workgroups of 512 that read more of the row again 450, without LDS 384.  1024 x 50257 fp32 76 us (5.1 TB/s);
+// half of the LDS, and two workgroups of 1024 fit a compute unit: 4096 x 131072 bf16, every sixth row masked, 370 us; with one workgroup of up
+// to 128 registers 417 to 435, with workgroups of 512 that read more of the row again 450, without LDS 384.  1024 x 50257 fp32 74.5 us (5.2 TB/s);
 // loads of what stays in registers go past the caches, which keep the rest of the row instead (without: 84).  Behind the matrix product that leaves
 // its logits in the memory-side cache that costs nothing (1024 x 50257 bf16 29 and 28 us, forward 16 and 14; 2048 x 50257 65 and 98, 30 and 63).
-// Forward 2048 x 32000 bf16 22.6 us (5.0 TB/s), with workgroups of 1024 29, of 256 42.
+// Forward 2048 x 32000 bf16 21.2 us (5.3 TB/s), with workgroups of 1024 29, of 256 42.
 template <int DT, int T, int U, int L, bool GRAD>
 __global__ void __launch_bounds__(T, 8) dfx_loss_rows_kernel(LossArgs a) {
   typedef typename StepElem<DT>::raw raw;
@@ -550,7 +550,7 @@ size_t dfx_policy_loss_workspace(size_t rows, size_t vocab, dfx_dtype dtype) {
 int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   if (!u || u->struct_bytes != sizeof(*u)) return DFX_ERR_INVALID_ARG;
   if (u->dtype != DFX_F32 && u->dtype != DFX_BF16 && u->dtype != DFX_F16) return DFX_ERR_INVALID_ARG;
-  if (u->rows > 0x7fffffffull || u->vocab > (1ull << 30)) return DFX_ERR_TOO_LARGE;
+  if (u->rows > 0x7fffffffull || u->vocab >= (1ull << 30)) return DFX_ERR_TOO_LARGE;
   if (!(u->inv_temperature * kLog2e >= (double)FLT_MIN && u->inv_temperature * kLog2e <= (double)FLT_MAX)) return DFX_ERR_INVALID_ARG;
   const size_t eb = step_elem_bytes(u->dtype), ls = u->logits_stride ? u->logits_stride : u->vocab, gs = u->grad_stride ? u->grad_stride : u->vocab;
   if (ls < u->vocab || (u->grad && gs < u->vocab)) return DFX_ERR_INVALID_ARG;

@@ -65,18 +65,14 @@ __device__ __forceinline__ void step_put(void* p, size_t i, float v) {
 typedef float StepPair __attribute__((ext_vector_type(2)));
 typedef __bf16 StepBf16Pair __attribute__((ext_vector_type(2)));
 
-// N elements from element i on, as words; what is read or written once and is larger than the caches goes past them (STREAM)
+// N elements from element i on, as words; what is read or written once and is larger than the caches goes past them (STREAM, stream)
 template <int DT, int N>
 struct StepVec {
   typedef typename StepElem<DT>::raw raw;
   typedef typename StepWordsOf<N * (int)sizeof(raw) / 4>::type words;
   words w;
 
-  template <bool STREAM = false>
-  __device__ __forceinline__ void load(const void* p, size_t i) {
-    const STEP_GLOBAL words* q = (const STEP_GLOBAL words*)((const STEP_GLOBAL raw*)p + i);
-    w = STREAM ? __builtin_nontemporal_load(q) : *q;
-  }
+  __device__ __forceinline__ void load(const void* p, size_t i) { w = *(const STEP_GLOBAL words*)((const STEP_GLOBAL raw*)p + i); }
   // at a 32-bit offset in bytes from an address that all lanes share: one register where an address of their own takes two
   template <bool STREAM = false>
   __device__ __forceinline__ void load_at(const void* p, uint32_t bytes) {
@@ -84,12 +80,7 @@ struct StepVec {
     w = STREAM ? __builtin_nontemporal_load(q) : *q;
   }
   __device__ __forceinline__ void stream_at(void* p, uint32_t bytes) const { __builtin_nontemporal_store(w, (STEP_GLOBAL words*)((STEP_GLOBAL unsigned char*)p + bytes)); }
-  template <bool STREAM = false>
-  __device__ __forceinline__ void store(void* p, size_t i) const {
-    STEP_GLOBAL words* q = (STEP_GLOBAL words*)((STEP_GLOBAL raw*)p + i);
-    if (STREAM) __builtin_nontemporal_store(w, q);
-    else *q = w;
-  }
+  __device__ __forceinline__ void stream(void* p, size_t i) const { __builtin_nontemporal_store(w, (STEP_GLOBAL words*)((STEP_GLOBAL raw*)p + i)); }
   __device__ __forceinline__ void fill_lowest() { w = DT == DFX_F32 ? 0xff800000u : DT == DFX_BF16 ? 0xff80ff80u : 0xfc00fc00u; }      // -infinity
   __device__ __forceinline__ void from(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }      // (16 bytes of them)
   // what was made of the elements so far is made anew behind this, not kept: a vector of 16-bit elements takes half the registers of its values
@@ -133,11 +124,6 @@ __device__ __forceinline__ void loads_arrived() {
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int d = kStepWave / 2; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = kStepWave / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {

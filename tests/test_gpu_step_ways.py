@@ -214,3 +214,26 @@ def test_an_error_that_another_call_left_behind_is_not_this_ones():
         hip.hipGetLastError()
     torch.cuda.synchronize()
     assert float(n.t) > 0 and bool((lp.t < 0).all())
+
+
+def test_lists_of_more_chunks_than_a_launch_has_workgroups():
+    """2^20 + 3 tensors of one or two elements, so that a list begins a second launch: norm, clipping in place, AdamW with a copy."""
+    dfx, _ = ts._dfx()
+    n = (1 << 20) + 3
+    _, bufs = ts._adam_state([(n + 1, "f32")], 41, "bf16", "f16")
+    lists = []
+    for bb in bufs:
+        at, eb, dt = bb[0].ptr(), bb[0].t.element_size(), {"torch.float32": dfx.F32, "torch.bfloat16": dfx.BF16, "torch.float16": dfx.F16}[str(bb[0].t.dtype)]
+        lists.append(dfx.TensorList([(at + k * eb, 1 if k < n - 1 else 2, dt) for k in range(n)]))
+    norm = ts._scalar()
+    g = bufs[1][0].host()
+    dfx.grad_norm(lists[1], norm.ptr())
+    want = math.sqrt(float((g * g).sum()))
+    assert abs(float(norm.t) - want) <= 2 * ts.U * want
+    f = st.clip_factor(float(norm.t), want / 4)
+    dfx.grad_clip(lists[1], norm.ptr(), want / 4)
+    ts._near(bufs[1][0].host(), g * f, np.abs(g * f) * (2.0 ** -9 + 8 * ts.U) + ts.TINY["bf16"], "clipped")
+    before = [[b.host() for b in bb] for bb in bufs[:4]]
+    dfx.adamw(*lists[:4], dfx.AdamWConfig(lr=0.01, step=3, weight_decay=0.1), copies=lists[4])
+    ts._check_adam(before, bufs, "f16", 3, 0.01, 0.9, 0.999, 1e-8, 0.1, 1.0)
+    norm.check()

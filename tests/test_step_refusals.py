@@ -94,3 +94,9 @@ def test_lists_of_what_is_no_tensor():
     for bad in ([(0x1000, 4, 1 << 32)], [(0x1000, 4, 3)], [(0x1001, 4, dfx.F32)]):
         with pytest.raises(dfx.DfxError):
             dfx.TensorList(bad)
+
+
+def test_the_longest_vocabulary_is_below_its_bound():
+    import paper_2303_06324_amd as dfx
+    from paper_2303_06324_amd import binding
+    assert binding._lib.dfx_policy_loss(_args(dfx, vocab=1 << 30), None) == dfx.ERR_TOO_LARGE
