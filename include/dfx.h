@@ -528,6 +528,9 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
  * A row of weight 0, with a target outside [0, vocab), or with no logit above -infinity has nothing to learn from: its results are 0
  * (its gradient is written, as 0), it adds nothing to the sums, and its logits are not looked at where weight or target say so.  Logits of
  * -infinity and of the type's lowest value are ordinary ones: probability 0.  A logit of NaN or +infinity makes its row NaN.
+ * A token that the policy or the reference bans (log-probability -infinity) has an infinite kl.  With kl_coef = 0 that shows in the kl's sum and nowhere
+ * else; otherwise the row's loss is infinite, and its gradient is finite where the reference bans the token (exp(d) - 1 is -1) and not where
+ * the policy does.  Where both do, d and what is made of it is NaN.
  * Zero-initialise, set struct_bytes and inv_temperature; pointers are device memory.
  */
 typedef struct {

@@ -33,12 +33,14 @@ def policy_loss(z, targets, old=None, ref=None, adv=None, weight=None, scale=1.0
                 used, clipped = max(r, 1.0 - clip_low), r < 1.0 - clip_low
             used = r if np.isnan(r) else used
             pg, slope = -a * used, 0.0 if clipped else -a * r
-            kl = 0.0
+            kl, value = 0.0, pg
             if ref is not None:
                 d = float(ref[i]) - logp[i]
-                kl = np.expm1(d) - d
-                slope -= kl_coef * np.expm1(d)
-            loss[i] = w[i] * (pg + kl_coef * kl)
+                kl = np.inf if d == np.inf else np.expm1(d) - d
+                if kl_coef != 0:            # (an infinite penalty that is only watched is not part of the loss)
+                    slope -= kl_coef * np.expm1(d)
+                    value = pg + kl_coef * kl
+            loss[i] = w[i] * value
             sums += np.array([loss[i], w[i] * pg, w[i] * kl, w[i] * clipped, w[i]])
             onehot = np.zeros(vocab)
             onehot[t] = 1.0

@@ -72,10 +72,16 @@ constexpr double kLog2 = 0.69314718055994530942, kLog2e = 1.44269504088896340736
 
 __device__ __forceinline__ float loss_exp_of(double x) { return __builtin_amdgcn_exp2f((float)(x * kLog2e)); }
 
-// exp(d) - 1 - d: where that cancels by its series, whose next term is d^10 / 10! (d = 1/2: 3e-10 of 0.15)
-__device__ __forceinline__ float loss_penalty(double d) {
+// exp(d) - 1, which the gradient takes, and the penalty exp(d) - 1 - d, each rounded once.  Near 0, where they cancel, by the penalty's series, whose
+// next term is d^10 / 10! (d = 1/2: 3e-10 of 0.15); elsewhere by the exponential, so that neither carries the other's rounding (exp(d) - 1 as d + penalty
+// would be off by |d| units).  d = -infinity, a token that the reference bans: -1 and infinity; d = +infinity: infinity twice.
+struct LossPenalty { float grows, kl; };
+__device__ __forceinline__ LossPenalty loss_penalty(double d) {
   const float x = (float)d;
-  if (fabsf(x) > 0.5f) return (float)((double)loss_exp_of(d) - 1.0 - d);
+  if (fabsf(x) > 0.5f) {
+    const double e = (double)loss_exp_of(d);
+    return {(float)(e - 1.0), e == INFINITY ? INFINITY : (float)(e - 1.0 - d)};
+  }
   float r = 1.0f / 362880.0f;
   r = fmaf(r, x, 1.0f / 40320.0f);
   r = fmaf(r, x, 1.0f / 5040.0f);
@@ -84,7 +90,8 @@ __device__ __forceinline__ float loss_penalty(double d) {
   r = fmaf(r, x, 1.0f / 24.0f);
   r = fmaf(r, x, 1.0f / 6.0f);
   r = fmaf(r, x, 0.5f);
-  return r * x * x;
+  r = r * x * x;
+  return {(float)(d + (double)r), r};
 }
 
 // What is known of a row before its logits.  Read at once when the row is begun, through the scalar cache (nobody writes it while the kernel
@@ -118,14 +125,17 @@ __device__ __forceinline__ RowValue row_value(const LossArgs& a, const RowIn& in
   const float A = in.A, r = a.has_old ? loss_exp_of(logp - (double)in.old) : 1.0f;
   const bool up = A >= 0.0f, clipped = up ? r > a.most : r < a.least;
   const float pg = -A * (clipped ? up ? a.most : a.least : r);
-  float slope = clipped ? 0.0f : -A * r, kl = 0.0f;
+  float slope = clipped ? 0.0f : -A * r, value = pg;
   if (a.has_ref) {
-    const double d = (double)in.ref - logp;
-    kl = loss_penalty(d);
-    slope -= a.kl_coef * (float)(d + (double)kl);
+    const LossPenalty x = loss_penalty((double)in.ref - logp);
+    e.kl = e.w * x.kl;
+    if (a.kl_coef != 0.0f) {             // (0 times an infinite penalty is not a number)
+      slope -= a.kl_coef * x.grows;
+      value = fmaf(a.kl_coef, x.kl, pg);
+    }
   }
-  e.pg = e.w * pg; e.kl = e.w * kl; e.clipped = clipped ? e.w : 0.0f;
-  e.loss = e.w * fmaf(a.kl_coef, kl, pg);
+  e.pg = e.w * pg; e.clipped = clipped ? e.w : 0.0f;
+  e.loss = e.w * value;
   e.g = (float)a.c * e.w * slope * in.scale;
   return e;
 }

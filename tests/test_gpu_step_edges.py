@@ -1,0 +1,107 @@
+"""Values and layouts at the edge of what the training step's operators are asked for: log-probabilities of -infinity, penalties far from 0.
+Helpers and tolerances are those of test_gpu_step.py, whose docstring derives them."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import step as st
+from tests import test_gpu_step as ts
+
+pytestmark = pytest.mark.gpu
+
+U = ts.U
+
+
+def _banned(rows, vocab, dt, big):
+    """Rows whose penalty is beyond 32 bits: the policy bans the token, the reference does, d is 1000, the token's logit is the type's lowest, that and the
+    reference bans it too, d is `big`; the others are ordinary."""
+    import torch
+    z, _, t, cols = ts._loss_case(rows, vocab, dt, 17)
+    x = z.t.view(rows, vocab)
+    lowest = float(torch.finfo(x.dtype).min)
+    x[0, int(t[0])] = -math.inf
+    x[3, int(t[3])] = lowest
+    x[4, int(t[4])] = lowest
+    zh = z.host().reshape(rows, vocab)
+    lp = st.policy_loss(zh, t.numpy())["logp"]
+    old, ref = lp - 0.1, lp + 0.1
+    for k in (0, 3, 4):
+        old[k] = ref[k] = -3.0
+    ref[1] = ref[4] = -math.inf
+    ref[2], ref[5] = lp[2] + 1000.0, lp[5] + big
+    cols.update(old=old.astype(np.float32), ref=ref.astype(np.float32), weight=np.ones(rows, np.float32))
+    return z, zh, t, cols
+
+
+WAYS = [(12, 100), (12, 30011), (70, 30011)]        # a row to a workgroup; split; too many rows to split
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab", WAYS)
+def test_a_penalty_that_is_only_watched(rows, vocab, dt):
+    """kl_coef = 0 with reference log-probabilities: whatever the penalty comes to, loss and gradient are those without a reference."""
+    z, zh, t, cols = _banned(rows, vocab, dt, 90.0)
+    out = ts._run_loss(z, t, cols, rows, vocab, dt, kl_coef=0.0)
+    assert float(out["sums"].t[2]) == math.inf
+    out["sums"].t[2] = 0.0
+    del cols["ref"]
+    want = ts._check_loss(out, zh, t, cols, rows, vocab, dt, kl_coef=0.0)
+    assert np.isfinite(want["loss"]).all() and np.isfinite(want["grad"]).all() and want["logp"][0] == -math.inf
+    fwd = ts._run_loss(z, t, dict(cols, ref=np.full(rows, -np.inf, np.float32)), rows, vocab, dt, grad=False, kl_coef=0.0)
+    fwd["sums"].t[2] = 0.0
+    ts._check_loss(fwd, zh, t, cols, rows, vocab, dt, grad=False, kl_coef=0.0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab", WAYS)
+def test_a_penalty_that_is_infinite(rows, vocab, dt):
+    """The loss is infinite; the gradient of a row whose token the reference bans is finite, exp(d) - 1 being -1 there, and no other row is touched."""
+    kl = 0.1
+    z, zh, t, cols = _banned(rows, vocab, dt, 0.1)
+    out = ts._run_loss(z, t, cols, rows, vocab, dt, kl_coef=kl)
+    want = st.policy_loss(zh, t.numpy(), cols["old"], cols["ref"], cols["adv"], cols["weight"], float(np.float32(0.37)), kl_coef=kl)
+    loss = out["loss"].host()
+    assert np.all(loss[:5] == math.inf) and float(out["sums"].t[0]) == math.inf and float(out["sums"].t[2]) == math.inf
+    assert float(out["logp"].t[0]) == -math.inf
+    got, logv = out["grad"].host().reshape(rows, vocab), math.log(vocab)
+    e_s = (vocab / 256 + 68 + 3 * logv) * U
+    dl = e_s + 4 * U
+    for k in [1, 4] + list(range(5, rows)):
+        lp = want["logp"][k]
+        per = abs(float(cols["adv"][k])) * math.exp(lp - float(cols["old"][k])) + kl * math.exp(float(cols["ref"][k]) - lp)
+        if k >= 5:
+            ts._near(loss[k], want["loss"][k], 2 * (per + kl) * dl + 4 * U * abs(want["loss"][k]), "loss")
+        far = zh[k].max() - zh[k]
+        p = np.exp(-far)
+        p /= p.sum()
+        coef, g = 0.37 * (per + kl), want["grad"][k]
+        assert np.isfinite(g).all()
+        tol = coef * p * (3 * U * far + 8 * U + 2 * e_s + dl) + np.abs(g) * (2 * dl + 4 * U + ts.HALF[dt]) + ts.TINY[dt]
+        tol[int(t[k])] += 3 * coef * dl
+        ts._near(got[k], g, tol, "grad of row %d" % k)
+
+
+@pytest.mark.parametrize("vocab", [64, 32768])
+def test_the_penalty_and_its_slope_far_from_zero(vocab):
+    """Rows of equal logits (probability, sum and log-probability are exact), an advantage of 0: loss and gradient are the penalty and its slope times
+    powers of two.  exp(d) is off by the rounding of d / log 2, |d| u, and its own 2 u; the slope exp(d) - 1 is rounded once, the penalty twice (and
+    its series' 4 u below 1/2), the gradient of an element beside the target once more."""
+    d = np.array([-80.2, -33.3, -16.7, -8.1, -4.3, -1.7, -0.6, -0.4, -0.01, 0.01, 0.3, 0.7, 1.9, 5.2, 21.7, 60.3])
+    rows = len(d)
+    z = ts.Guarded(rows * vocab, "f32")
+    z.t.fill_(1.5)
+    lp = -math.log(vocab)
+    ref = (lp + d).astype(np.float32)
+    d = ref.astype(np.float64) - lp
+    import torch
+    t = torch.arange(rows) % vocab
+    cols = {"ref": ref, "adv": np.zeros(rows, np.float32), "weight": np.full(rows, 0.5, np.float32)}
+    out = ts._run_loss(z, t, cols, rows, vocab, "f32", kl_coef=0.25)
+    e, kl, grows = np.exp(d), np.expm1(d) - d, np.expm1(d)
+    ts._near(out["loss"].host(), 0.125 * kl, 0.125 * (e * (np.abs(d) + 3) * (np.abs(d) > 0.4) + 8 * kl) * U, "loss")
+    scale = float(np.float32(0.37))
+    got = out["grad"].host().reshape(rows, vocab)[np.arange(rows), (np.arange(rows) + 1) % vocab]
+    # -g p, g = -0.125 scale grows
+    want = 0.125 * scale * grows / vocab
+    ts._near(got, want, np.abs(want) * 3 * U + 0.125 * scale / vocab * e * (np.abs(d) + 3) * U * (np.abs(d) > 0.4) + ts.TINY["f32"], "grad")
