@@ -228,13 +228,14 @@ struct AdamArgs {
   float correct1, correct2;                   // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
 };
 
-struct AdamRates { float f, keep, beta1, one_beta1, beta2, one_beta2, rate, correct2, eps; };
+struct AdamRates { float f, decay, beta1, one_beta1, beta2, one_beta2, rate, correct2, eps; };
 
 __device__ __forceinline__ void adam_element(const AdamRates& a, float& p, float g, float& m, float& v) {
   g *= a.f;
   m = fmaf(a.beta1, m, a.one_beta1 * g);
   v = fmaf(a.beta2, v, a.one_beta2 * g * g);
-  p = fmaf(p, a.keep, -(a.rate * m / fmaf(sqrtf(v), a.correct2, a.eps)));
+  // (what p loses is made up apart from p: 1 - lr decay holds 32-bit numbers below 1 to 6e-8 only, which is all of a decay of lr 1e-6 and 0.01)
+  p -= fmaf(a.decay, p, a.rate * m / fmaf(sqrtf(v), a.correct2, a.eps));
 }
 
 template <int GD, int CD, bool STAGED>      // CD < 0: no copy
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(kAdamThreads) dfx_adamw_kernel(AdamArgs a) {
     c1 = (float)(1.0 / (1.0 - pow(a.beta1_d, t)));
     c2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2_d, t)));
   }
-  const AdamRates r = {f, 1.0f - lr * a.decay, a.beta1, a.one_beta1, a.beta2, a.one_beta2, lr * c1, c2, a.eps};
+  const AdamRates r = {f, lr * a.decay, a.beta1, a.one_beta1, a.beta2, a.one_beta2, lr * c1, c2, a.eps};
   const uint32_t c = blockIdx.x / kAdamParts, part = blockIdx.x % kAdamParts;
   const ListChunk p = a.p[c], g = a.g[c], m = a.m[c], v = a.v[c], copy = a.copy ? a.copy[c] : ListChunk{0, 0, 0};
   if (g.dtype == DFX_F32) adam_chunk_copy<DFX_F32, STAGED>(r, p, g, m, v, copy, part, a.copy != nullptr);

@@ -105,3 +105,28 @@ def test_the_penalty_and_its_slope_far_from_zero(vocab):
     # -g p, g = -0.125 scale grows
     want = 0.125 * scale * grows / vocab
     ts._near(got, want, np.abs(want) * 3 * U + 0.125 * scale / vocab * e * (np.abs(d) + 3) * U * (np.abs(d) > 0.4) + ts.TINY["f32"], "grad")
+
+
+@pytest.mark.parametrize("on_device", [False, True])
+@pytest.mark.parametrize("lr,decay", [(1e-6, 0.01), (1e-6, 0.1), (1e-5, 0.01)])
+def test_adamw_decays_at_small_rates(lr, decay, on_device):
+    """1000 steps of noise at rates of fine-tuning.  A parameter's rounding is 2^-25 a step at most, as likely up as down: the mean over 16384 parameters is off by
+    2^-25 sqrt(1000 / 16384) < 1e-8, where the decay moves it by 7.5e-6 at least.  2 % of that are allowed."""
+    import torch
+    dfx, _ = ts._dfx()
+    n, steps = 16384, 1000
+    gen = torch.Generator("cuda").manual_seed(7)
+    p = ts.Guarded(n, "f32")
+    p.t.uniform_(0.5, 1.0, generator=gen)
+    g, m, v = (ts.Guarded(n, "f32", fill=np.zeros(n)) for _ in range(3))
+    lists = [dfx.TensorList([(b.ptr(), n, dfx.F32)]) for b in (p, g, m, v)]
+    rate = torch.full((), lr, device="cuda")
+    want = [p.host(), m.host(), v.host()]
+    for step in range(1, steps + 1):
+        g.t.normal_(generator=gen)
+        cfg = dfx.AdamWConfig(lr=7.0, step=step, weight_decay=decay, lr_dev=rate.data_ptr()) if on_device else dfx.AdamWConfig(lr=lr, step=step, weight_decay=decay)
+        dfx.adamw(*lists, cfg, stream=torch.cuda.current_stream().cuda_stream)
+        want = st.adamw(want[0], g.host(), want[1], want[2], step, lr, 0.9, 0.999, 1e-8, decay)
+    asked = lr * decay * steps * 0.75
+    assert asked > 7e-6
+    assert abs(float((p.host() - want[0]).mean())) < 0.02 * asked
