@@ -514,7 +514,7 @@ int dfx_adamw_default(dfx_adamw_config* cfg);
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps);  copy <- p rounded
  * params, exp_avg (m), exp_avg_sq (v): lists of DFX_F32 tensors; grads, copies: any type; all of equal counts, no tensor overlapping
  * another.  copies may be NULL.  norm_dev: device, or NULL: nothing is clipped.  Where *norm_dev is infinite or NaN the
- * gradients overflowed: nothing is written.
+ * gradients overflowed: nothing is written.  Nor is anything where t is read on the device and is 0.
  * Errors: INVALID_ARG (counts, types, one list in two places, configuration), HIP.
  */
 int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* exp_avg_sq, dfx_list* copies,

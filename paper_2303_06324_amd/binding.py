@@ -396,7 +396,7 @@ def clip_grad_norm(grads: TensorList, norm: int, max_norm: float, out: Optional[
 
 def adamw(params: TensorList, grads: TensorList, exp_avg: TensorList, exp_avg_sq: TensorList, config: AdamWConfig,
           copies: Optional[TensorList] = None, norm: int = 0, stream: Optional[int] = None) -> None:
-    """One AdamW update, clipped by norm[0] on the way; nothing is written where that is infinite or NaN."""
+    """One AdamW update, clipped by norm[0] on the way; nothing is written where that is infinite or NaN, or a step on the device is 0."""
     rc = _lib.dfx_adamw(params._h, grads._h, exp_avg._h, exp_avg_sq._h, copies._h if copies is not None else None, config, norm, stream)
     if rc != OK:
         raise DfxError(rc, "dfx_adamw")

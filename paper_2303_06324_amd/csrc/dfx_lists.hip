@@ -307,6 +307,7 @@ __global__ void __launch_bounds__(kAdamThreads) dfx_adamw_kernel(AdamArgs a) {
   if (a.lr_dev) lr = *a.lr_dev;
   if (a.step_dev) {
     const double t = (double)*a.step_dev;
+    if (t == 0.0) return;                 // (no update has this number: the corrections would be infinite and every parameter NaN)
     c1 = (float)(1.0 / (1.0 - pow(a.beta1_d, t)));
     c2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2_d, t)));
   }

@@ -130,3 +130,19 @@ def test_adamw_decays_at_small_rates(lr, decay, on_device):
     asked = lr * decay * steps * 0.75
     assert asked > 7e-6
     assert abs(float((p.host() - want[0]).mean())) < 0.02 * asked
+
+
+def test_adamw_of_no_step_on_the_device():
+    """A counter that has not been counted up yet: there is no update 0, and nothing is written."""
+    import torch
+    dfx, _ = ts._dfx()
+    lists, bufs = ts._adam_state(ts.LISTS["odd"], 51, "bf16", "bf16")
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    before = [b.raw.clone() for bb in bufs for b in bb]
+    cfg = dfx.AdamWConfig(step_dev=step.data_ptr())
+    dfx.adamw(*lists[:4], cfg, copies=lists[4])
+    assert all(bool((a == b.raw).all()) for a, b in zip(before, [b for bb in bufs for b in bb]))
+    step.add_(1)
+    host = [[b.host() for b in bb] for bb in bufs[:4]]
+    dfx.adamw(*lists[:4], cfg, copies=lists[4])
+    ts._check_adam(host, bufs, "bf16", 1, 1e-3, 0.9, 0.999, 1e-8, 0.01, 1.0)
