@@ -531,7 +531,8 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
  * A token that the policy or the reference bans (log-probability -infinity) has an infinite kl.  With kl_coef = 0 that shows in the kl's sum and nowhere
  * else; otherwise the row's loss is infinite, and its gradient is finite where the reference bans the token (exp(d) - 1 is -1) and not where
  * the policy does.  Where both do, d and what is made of it is NaN.
- * Zero-initialise, set struct_bytes and inv_temperature; pointers are device memory.
+ * Zero-initialise, set struct_bytes and inv_temperature; pointers are device memory.  What is written (logp, loss, sums, grad, workspace) lies apart from
+ * what is read and from each other, but for grad in the logits' place; the space from the first to the last row of grad lies apart from that of logits.
  */
 typedef struct {
   uint32_t struct_bytes;     /* sizeof(dfx_policy_loss_args) the caller was compiled with */
@@ -547,7 +548,7 @@ typedef struct {
   const float* advantage;    /* [rows], A; may be NULL where neither loss, sums nor grad is asked for */
   const float* weight;       /* [rows], may be NULL: 1 */
   const float* scale;        /* one value, may be NULL: 1.  Multiplies the gradient only: 1 / the weights of all ranks' rows */
-  float* logp;               /* [rows], may be NULL; like loss, apart from all that is read */
+  float* logp;               /* [rows], may be NULL */
   float* loss;               /* [rows], may be NULL */
   float* sums;               /* 5 values, may be NULL: sums over the rows of weight times loss / weight, pg, kl, [clipped], 1 */
   void* workspace;           /* dfx_policy_loss_workspace bytes, 8-byte aligned; nothing in it has to outlive the call's work.  May be
@@ -561,7 +562,7 @@ typedef struct {
 /* Bytes of workspace for calls of up to so many rows of this length and type (host only, no GPU needed). */
 size_t dfx_policy_loss_workspace(size_t rows, size_t vocab, dfx_dtype dtype);
 
-/* Errors: INVALID_ARG (also: workspace too small), TOO_LARGE, HIP. */
+/* Errors: INVALID_ARG (also: workspace too small, something written lies on something else), TOO_LARGE, HIP. */
 int dfx_policy_loss(const dfx_policy_loss_args* args, void* hip_stream);
 
 #ifdef __cplusplus

@@ -548,6 +548,19 @@ Extent extent(const void* p, size_t rows, size_t vocab, size_t stride, size_t eb
   return {(uintptr_t)p, (uintptr_t)p + ((rows - 1) * stride + vocab) * eb};
 }
 
+// n pieces of so many bytes, step bytes from one to the next; nothing: n = 0
+struct Span { uintptr_t at; size_t n, bytes, step; };
+Span flat(const void* p, size_t bytes) { return {(uintptr_t)p, p && bytes ? (size_t)1 : 0, bytes, bytes}; }
+
+// whether a span of one piece shares a byte with another: with the last piece that begins at or before it, or the one behind that
+bool meet(const Span& one, const Span& s) {
+  if (!one.n || !s.n) return false;
+  const uintptr_t lo = one.at, hi = lo + one.bytes;
+  const size_t k = lo <= s.at ? 0 : std::min<size_t>((lo - s.at) / s.step, s.n - 1);
+  const uintptr_t p = s.at + k * s.step;
+  return (lo < p + s.bytes && p < hi) || (k + 1 < s.n && p + s.step < hi);
+}
+
 }  // namespace
 
 extern "C" {
@@ -577,11 +590,22 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
     const Extent a = extent(u->logits, u->rows, u->vocab, ls, eb), b = extent(u->grad, u->rows, u->vocab, gs, eb);
     if (a.lo < b.hi && b.lo < a.hi) return DFX_ERR_INVALID_ARG;
   }
-  for (const void* o : {(const void*)u->logp, (const void*)u->loss})      // what is written for a row lies apart from what is read for it
-    for (const void* i : {(const void*)u->targets, (const void*)u->old_logp, (const void*)u->ref_logp, (const void*)u->advantage, (const void*)u->weight, (const void*)u->scale, o == u->logp ? (const void*)u->loss : nullptr}) {
-      const size_t held = i == u->targets ? 8 * u->rows : i == u->scale ? 4 : 4 * u->rows;
-      if (o && i && u->rows && (uintptr_t)o < (uintptr_t)i + held && (uintptr_t)i < (uintptr_t)o + 4 * u->rows) return DFX_ERR_INVALID_ARG;
-    }
+  // What is written lies apart from what is read (but for the gradient in the logits' place) and from what else is written: rows are read by some
+  // workgroups while others write theirs, and the sums of split rows while the rows are written.
+  const size_t rows = u->rows, work = dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype);
+  const bool has_work = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= work;
+  const Span z = {(uintptr_t)u->logits, u->vocab ? rows : 0, u->vocab * eb, ls * eb}, g = {(uintptr_t)u->grad, u->grad && u->vocab ? rows : 0, u->vocab * eb, gs * eb};
+  const Span reads[] = {flat(u->targets, 8 * rows), flat(u->old_logp, 4 * rows), flat(u->ref_logp, 4 * rows), flat(u->advantage, 4 * rows), flat(u->weight, 4 * rows), flat(u->scale, rows ? 4 : 0)};
+  const Span writes[] = {flat(u->logp, 4 * rows), flat(u->loss, 4 * rows), flat(u->sums, 4 * kSums), flat(u->workspace, has_work ? work : 0)};
+  for (size_t k = 0; k < sizeof(writes) / sizeof(writes[0]); ++k) {
+    if (meet(writes[k], z) || meet(writes[k], g)) return DFX_ERR_INVALID_ARG;
+    for (const Span& r : reads)
+      if (meet(writes[k], r)) return DFX_ERR_INVALID_ARG;
+    for (size_t j = 0; j < k; ++j)
+      if (meet(writes[k], writes[j])) return DFX_ERR_INVALID_ARG;
+  }
+  for (const Span& r : reads)
+    if (meet(r, g)) return DFX_ERR_INVALID_ARG;
   LossArgs a;
   memset(&a, 0, sizeof(a));
   a.logits = u->logits; a.grad = u->grad; a.logits_stride = ls; a.grad_stride = gs;
@@ -596,7 +620,7 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   a.k = (float)(u->inv_temperature * kLog2e);
   hipStream_t s = (hipStream_t)hip_stream;
   const uint32_t groups = loss_groups(u->rows);
-  const Split sp = u->workspace && !((uintptr_t)u->workspace & 7u) && u->workspace_bytes >= dfx_policy_loss_workspace(u->rows, u->vocab, u->dtype) ? loss_split(a, (uint32_t)eb) : Split{0, 0, 1, 0};
+  const Split sp = has_work ? loss_split(a, (uint32_t)eb) : Split{0, 0, 1, 0};
   const bool f32 = u->dtype == DFX_F32, bf16 = u->dtype == DFX_BF16;
   if (sp.segments) return f32 ? launch_split<DFX_F32>(a, sp, s) : bf16 ? launch_split<DFX_BF16>(a, sp, s) : launch_split<DFX_F16>(a, sp, s);
   if (groups) {

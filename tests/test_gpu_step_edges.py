@@ -146,3 +146,29 @@ def test_adamw_of_no_step_on_the_device():
     host = [[b.host() for b in bb] for bb in bufs[:4]]
     dfx.adamw(*lists[:4], cfg, copies=lists[4])
     ts._check_adam(host, bufs, "bf16", 1, 1e-3, 0.9, 0.999, 1e-8, 0.01, 1.0)
+
+
+def test_results_in_the_space_between_rows():
+    """What is written may lie between rows of logits, where nothing is read."""
+    import torch
+    dfx, _ = ts._dfx()
+    rows, vocab, stride = 5, 100, 120
+    z, zh, t, cols = ts._loss_case(rows, vocab, "f32", 9, stride=stride)
+    want = st.policy_loss(zh, t.numpy(), cols["old"], None, cols["adv"], cols["weight"])
+    dev = {k: torch.from_numpy(v).cuda() for k, v in cols.items()}
+    tt, ws = t.cuda(), torch.empty(dfx.policy_loss_workspace(rows, vocab, dfx.F32), dtype=torch.uint8, device="cuda")
+    x = z.t.view(rows, stride)
+    x[:, vocab:] = 7.0
+    at = [x[k, vocab:].data_ptr() for k in range(rows)]
+    dfx.policy_loss(rows, vocab, dfx.F32, z.ptr(), tt.data_ptr(), old_logp=dev["old"].data_ptr(), advantage=dev["adv"].data_ptr(), weight=dev["weight"].data_ptr(), logp=at[0],
+                    loss=at[0] + 4 * rows, sums=at[3], logits_stride=stride, workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+    e = (vocab / 256 + 68 + 3 * math.log(vocab)) * U + 4 * U
+    size = 4 * np.abs(cols["adv"])
+    ts._near(x[0, vocab:vocab + rows].double().cpu().numpy(), want["logp"], e + 4 * U * np.abs(want["logp"]))
+    ts._near(x[0, vocab + rows:vocab + 2 * rows].double().cpu().numpy(), want["loss"], size * e + 4 * U * np.abs(want["loss"]))
+    ts._near(x[3, vocab:vocab + 5].double().cpu().numpy(), want["sums"], size.sum() * e + 2 * U * np.abs(want["sums"]))
+    assert bool((x[1, vocab:] == 7.0).all()) and bool((x[3, vocab + 5:] == 7.0).all()) and bool((x[0, vocab + 2 * rows:] == 7.0).all())
+    for k in (x[0, vocab - 1:].data_ptr(), x[1].data_ptr() - 4 * rows + 4):
+        with pytest.raises(dfx.DfxError):
+            dfx.policy_loss(rows, vocab, dfx.F32, z.ptr(), tt.data_ptr(), logp=k, logits_stride=stride)
+    z.check()
