@@ -487,8 +487,9 @@ int dfx_grad_norm(dfx_list* grads, dfx_norm_kind kind, double grad_scale, float*
  * dst <- src * grad_scale * min(1, max_norm / (*norm_dev + 1e-6)), tensor by tensor: *norm_dev is the norm of the gradients times
  * grad_scale, as dfx_grad_norm leaves it.  dst: a list of equal counts, whose types may differ (the reduced 16-bit bucket into
  * 32-bit gradients); NULL or src = in place.  A tensor of dst lies apart from src's, or is the same memory and type.  A norm of
- * infinity makes finite gradients 0, a norm of NaN makes all of them NaN.
- * Errors: INVALID_ARG (counts, overlap, max_norm <= 0), HIP.
+ * infinity makes finite gradients 0, a norm of NaN makes all of them NaN.  grad_scale: 0 or a normal number in 32 bits; a max_norm above the largest
+ * of these counts as that.
+ * Errors: INVALID_ARG (counts, overlap, max_norm <= 0, grad_scale), HIP.
  */
 int dfx_grad_clip(dfx_list* src, dfx_list* dst, const float* norm_dev, double max_norm, double grad_scale, void* hip_stream);
 
@@ -500,9 +501,9 @@ int dfx_clip_grad_norm(dfx_list* src, dfx_list* dst, dfx_norm_kind kind, double 
 typedef struct {
   uint32_t struct_bytes;    /* sizeof(dfx_adamw_config) the caller was compiled with */
   uint32_t step;            /* t: number of this update, from 1 */
-  double lr, beta1, beta2, eps, weight_decay;
-  double grad_scale;        /* as above */
-  double max_norm;          /* > 0; only looked at where there is a norm */
+  double lr, beta1, beta2, eps, weight_decay; /* lr, weight_decay: finite in 32 bits; eps >= 0: 0 or a normal number there */
+  double grad_scale;        /* as of dfx_grad_clip */
+  double max_norm;          /* the same; > 0; only looked at where there is a norm */
   const uint32_t* step_dev; /* device, may be NULL: t is read there instead (a captured step counts it up itself) */
   const float* lr_dev;      /* device, may be NULL: lr is read there instead */
 } dfx_adamw_config;
@@ -555,7 +556,7 @@ typedef struct {
                                 NULL without sums, which makes a few rows of a long vocabulary slower */
   size_t workspace_bytes;
   double clip_low, clip_high; /* 0 <= clip_low <= 1, 0 <= clip_high */
-  double kl_coef;            /* needs ref_logp where it is not 0 */
+  double kl_coef;            /* finite in 32 bits; needs ref_logp where it is not 0 */
   double inv_temperature;    /* > 0, and 1.45 times it a normal number in 32 bits */
 } dfx_policy_loss_args;
 

@@ -339,7 +339,7 @@ int check_norm(const dfx_list* l, int kind, double scale, const float* norm) {
 }
 
 int check_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale) {
-  if (!src || !norm || ((uintptr_t)norm & 3u) || !(max_norm > 0.0) || !isfinite(scale)) return DFX_ERR_INVALID_ARG;
+  if (!src || !norm || ((uintptr_t)norm & 3u) || !(max_norm > 0.0) || !step_normal(scale)) return DFX_ERR_INVALID_ARG;
   if (dst && dst != src) {
     if (!same_counts(src, dst)) return DFX_ERR_INVALID_ARG;
     for (size_t k = 0; k < src->tensors.size(); ++k) {       // the same tensor, or apart from it
@@ -350,6 +350,9 @@ int check_clip(const dfx_list* src, const dfx_list* dst, const float* norm, doub
   }
   return on_its_device(src) ? DFX_OK : DFX_ERR_INVALID_ARG;
 }
+
+// in 32 bits: none is above the largest, so that a norm of infinity is above each
+float max_norm_of(double max_norm) { return (float)std::min(max_norm, (double)FLT_MAX); }
 
 int launch_norm(const dfx_list* l, int kind, double scale, float* norm, hipStream_t stream) {
   if (!l->nchunks) {
@@ -362,7 +365,7 @@ int launch_norm(const dfx_list* l, int kind, double scale, float* norm, hipStrea
 int launch_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale, hipStream_t stream) {
   if (!dst) dst = src;
   if (!src->nchunks) return DFX_OK;
-  return step_launch(dfx_clip_kernel, dim3(std::min(src->nchunks, kMaxGroups)), kClipThreads, stream, src->chunks, dst->chunks, src->nchunks, norm, (float)max_norm, (float)scale, dst == src);
+  return step_launch(dfx_clip_kernel, dim3(std::min(src->nchunks, kMaxGroups)), kClipThreads, stream, src->chunks, dst->chunks, src->nchunks, norm, max_norm_of(max_norm), (float)scale, dst == src);
 }
 
 }  // namespace
@@ -452,8 +455,8 @@ int dfx_adamw_default(dfx_adamw_config* cfg) {
 
 int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* exp_avg_sq, dfx_list* copies, const dfx_adamw_config* cfg, const float* norm_dev, void* hip_stream) {
   if (!params || !grads || !exp_avg || !exp_avg_sq || !cfg || cfg->struct_bytes != sizeof(*cfg)) return DFX_ERR_INVALID_ARG;
-  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps >= 0.0) || !isfinite(cfg->eps) || !isfinite(cfg->lr) ||
-      !isfinite(cfg->weight_decay) || !isfinite(cfg->grad_scale) || (!cfg->step_dev && !cfg->step) || (norm_dev && !(cfg->max_norm > 0.0)))
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps >= 0.0) || !step_normal(cfg->eps) || !step_fits(cfg->lr) ||
+      !step_fits(cfg->weight_decay) || !step_normal(cfg->grad_scale) || (!cfg->step_dev && !cfg->step) || (norm_dev && !(cfg->max_norm > 0.0)))
     return DFX_ERR_INVALID_ARG;
   if (((uintptr_t)norm_dev & 3u) || ((uintptr_t)cfg->step_dev & 3u) || ((uintptr_t)cfg->lr_dev & 3u)) return DFX_ERR_INVALID_ARG;
   if (!same_counts(params, grads) || !same_counts(params, exp_avg) || !same_counts(params, exp_avg_sq) || (copies && !same_counts(params, copies))) return DFX_ERR_INVALID_ARG;
@@ -467,7 +470,7 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   a.beta1_d = cfg->beta1; a.beta2_d = cfg->beta2;
   a.lr = (float)cfg->lr; a.beta1 = (float)cfg->beta1; a.beta2 = (float)cfg->beta2;
   a.one_beta1 = (float)(1.0 - cfg->beta1); a.one_beta2 = (float)(1.0 - cfg->beta2);
-  a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = (float)cfg->max_norm;
+  a.eps = (float)cfg->eps; a.decay = (float)cfg->weight_decay; a.scale = (float)cfg->grad_scale; a.max_norm = max_norm_of(cfg->max_norm);
   a.correct1 = (float)(1.0 / (1.0 - pow(cfg->beta1, (double)cfg->step)));
   a.correct2 = (float)(1.0 / sqrt(1.0 - pow(cfg->beta2, (double)cfg->step)));
   for (uint32_t done = 0; done < params->nchunks; done += kMaxGroups) {      // (more than one launch beyond 2^20 chunks)

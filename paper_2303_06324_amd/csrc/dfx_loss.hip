@@ -578,7 +578,7 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   const size_t eb = step_elem_bytes(u->dtype), ls = u->logits_stride ? u->logits_stride : u->vocab, gs = u->grad_stride ? u->grad_stride : u->vocab;
   if (ls < u->vocab || (u->grad && gs < u->vocab)) return DFX_ERR_INVALID_ARG;
   if (u->rows && ((ls > SIZE_MAX / 8 / u->rows) || (u->grad && gs > SIZE_MAX / 8 / u->rows))) return DFX_ERR_TOO_LARGE;
-  if (!isfinite(u->clip_low) || u->clip_low < 0.0 || u->clip_low > 1.0 || !isfinite(u->clip_high) || u->clip_high < 0.0 || !isfinite(u->kl_coef)) return DFX_ERR_INVALID_ARG;
+  if (!isfinite(u->clip_low) || u->clip_low < 0.0 || u->clip_low > 1.0 || !isfinite(u->clip_high) || u->clip_high < 0.0 || !step_fits(u->kl_coef)) return DFX_ERR_INVALID_ARG;
   if (u->kl_coef != 0.0 && !u->ref_logp) return DFX_ERR_INVALID_ARG;
   if (!u->advantage && (u->loss || u->sums || u->grad)) return DFX_ERR_INVALID_ARG;
   if (u->rows && (!u->targets || (u->vocab && !u->logits))) return DFX_ERR_INVALID_ARG;
@@ -616,7 +616,7 @@ int dfx_policy_loss(const dfx_policy_loss_args* u, void* hip_stream) {
   a.has_old = u->old_logp; a.has_ref = u->ref_logp; a.has_advantage = u->advantage; a.has_weight = u->weight; a.has_scale = u->scale;
   a.logp = u->logp; a.loss = u->loss; a.sums = u->sums; a.parts = (LossPart*)u->workspace; a.part = (double*)(a.parts + loss_parts(u->rows));
   a.rows = (uint32_t)u->rows; a.vocab = (uint32_t)u->vocab;
-  a.least = (float)(1.0 - u->clip_low); a.most = (float)(1.0 + u->clip_high); a.kl_coef = (float)u->kl_coef; a.c = u->inv_temperature;
+  a.least = (float)(1.0 - u->clip_low); a.most = (float)std::min(1.0 + u->clip_high, (double)FLT_MAX); a.kl_coef = (float)u->kl_coef; a.c = u->inv_temperature;
   a.k = (float)(u->inv_temperature * kLog2e);
   hipStream_t s = (hipStream_t)hip_stream;
   const uint32_t groups = loss_groups(u->rows);

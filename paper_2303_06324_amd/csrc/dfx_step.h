@@ -3,7 +3,9 @@
 #ifndef DFX_STEP_H
 #define DFX_STEP_H
 
+#include <float.h>
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -61,6 +63,11 @@ __device__ __forceinline__ void step_put(void* p, size_t i, float v) {
   typedef typename StepElem<DT>::raw raw;
   *((STEP_GLOBAL raw*)p + i) = StepElem<DT>::put(v);
 }
+
+// The caller's numbers are of 64 bits, the kernels take most of them in 32: whether one is finite there, and whether it keeps its digits there
+// as well (is 0 or no smaller than the smallest normal number).
+inline bool step_fits(double v) { return fabs(v) <= (double)FLT_MAX; }
+inline bool step_normal(double v) { return v == 0.0 || (step_fits(v) && fabs(v) >= (double)FLT_MIN); }
 
 typedef float StepPair __attribute__((ext_vector_type(2)));
 typedef __bf16 StepBf16Pair __attribute__((ext_vector_type(2)));

@@ -172,3 +172,45 @@ def test_results_in_the_space_between_rows():
         with pytest.raises(dfx.DfxError):
             dfx.policy_loss(rows, vocab, dfx.F32, z.ptr(), tt.data_ptr(), logp=k, logits_stride=stride)
     z.check()
+
+
+@pytest.mark.parametrize("max_norm", [1e300, math.inf])
+def test_a_bound_beyond_32_bits(max_norm):
+    """The largest norm that there may be is one: finite norms are below it, and a norm of infinity still makes finite gradients 0."""
+    dfx, _ = ts._dfx()
+    lst, bufs = ts._list(ts.LISTS["odd"], 5)
+    src = [b.host() for b in bufs]
+    norm = ts._scalar(3e38)
+    dfx.grad_clip(lst, norm.ptr(), max_norm, scale=0.5)
+    assert all(np.array_equal(b.host(), b.t.new_tensor(0.5 * x).double().cpu().numpy()) for x, b in zip(src, bufs))
+    norm.t.fill_(math.inf)
+    dfx.grad_clip(lst, norm.ptr(), max_norm)
+    assert not any(b.host().any() for b in bufs)
+
+
+def test_a_clip_beyond_32_bits():
+    """A ratio that overflows is clipped by any bound, so that an advantage of 0 gives 0 there too."""
+    rows, vocab = 4, 50
+    z, zh, t, cols = ts._loss_case(rows, vocab, "f32", 3)
+    cols.update(old=np.full(rows, -800.0, np.float32), adv=np.zeros(rows, np.float32), weight=np.ones(rows, np.float32))
+    out = ts._run_loss(z, t, cols, rows, vocab, "f32", clip_high=1e300)
+    assert out["loss"].t.tolist() == [0.0] * rows and not bool(out["grad"].t.any()) and float(out["sums"].t[3]) == rows
+
+
+def test_numbers_that_32_bits_do_not_hold_are_refused():
+    dfx, _ = ts._dfx()
+    a, b, c, d = (ts._list([(5, "f32"), (6, "f32")], k)[0] for k in range(4))
+    n = ts._scalar(2.0)
+    for scale in (1e39, -1e300, 1e-39, 1e-60, math.nan):
+        for call in (dfx.grad_clip, dfx.clip_grad_norm):
+            with pytest.raises(dfx.DfxError) as e:
+                call(a, n.ptr(), 1.0, scale=scale)
+            assert e.value.status == dfx.ERR_INVALID_ARG
+    for kw in (dict(grad_scale=1e39), dict(grad_scale=1e-40), dict(lr=1e39), dict(lr=-1e200), dict(weight_decay=1e39), dict(eps=1e39), dict(eps=1e-40)):
+        with pytest.raises(dfx.DfxError) as e:
+            dfx.adamw(a, b, c, d, dfx.AdamWConfig(**kw))
+        assert e.value.status == dfx.ERR_INVALID_ARG
+    dfx.grad_norm(a, n.ptr(), scale=1e-60)              # (a norm's scale is taken in 64 bits)
+    assert float(n.t) == 0.0
+    dfx.grad_clip(a, n.ptr(), 1.0, scale=0.0)
+    dfx.adamw(a, b, c, d, dfx.AdamWConfig(lr=1e-60, eps=1e-37))
