@@ -486,9 +486,9 @@ int dfx_grad_norm(dfx_list* grads, dfx_norm_kind kind, double grad_scale, float*
 /*
  * dst <- src * grad_scale * min(1, max_norm / (*norm_dev + 1e-6)), tensor by tensor: *norm_dev is the norm of the gradients times
  * grad_scale, as dfx_grad_norm leaves it.  dst: a list of equal counts, whose types may differ (the reduced 16-bit bucket into
- * 32-bit gradients); NULL or src = in place.  A tensor of dst lies apart from src's, or is the same memory and type.  A norm of
- * infinity makes finite gradients 0, a norm of NaN makes all of them NaN.  grad_scale: 0 or a normal number in 32 bits; a max_norm above the largest
- * of these counts as that.
+ * 32-bit gradients); NULL or src = in place.  The tensors that are written lie apart from one another, and each from all of src, but that it may be the
+ * tensor of src at its own place (same memory and type).  A norm of infinity makes finite gradients 0, a norm of NaN makes all of them
+ * NaN.  grad_scale: 0 or a normal number in 32 bits; a max_norm above the largest of these counts as that.
  * Errors: INVALID_ARG (counts, overlap, max_norm <= 0, grad_scale), HIP.
  */
 int dfx_grad_clip(dfx_list* src, dfx_list* dst, const float* norm_dev, double max_norm, double grad_scale, void* hip_stream);
@@ -516,7 +516,7 @@ int dfx_adamw_default(dfx_adamw_config* cfg);
  * params, exp_avg (m), exp_avg_sq (v): lists of DFX_F32 tensors; grads, copies: any type; all of equal counts, no tensor overlapping
  * another.  copies may be NULL.  norm_dev: device, or NULL: nothing is clipped.  Where *norm_dev is infinite or NaN the
  * gradients overflowed: nothing is written.  Nor is anything where t is read on the device and is 0.
- * Errors: INVALID_ARG (counts, types, one list in two places, configuration), HIP.
+ * Errors: INVALID_ARG (counts, types, one list in two places, a written list whose own tensors overlap, configuration), HIP.
  */
 int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* exp_avg_sq, dfx_list* copies,
               const dfx_adamw_config* cfg, const float* norm_dev, void* hip_stream);

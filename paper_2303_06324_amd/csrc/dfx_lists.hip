@@ -28,6 +28,8 @@ constexpr uint32_t kMaxGroups = 1u << 20;      // (a grid's threads are counted 
 struct ListChunk { uint64_t ptr; uint32_t n; int32_t dtype; };
 static_assert(sizeof(ListChunk) == 16, "a chunk is one 16-byte load");
 
+struct ListSpan { uintptr_t lo, hi; size_t k; };      // a tensor's memory, and its place in the list
+
 struct ListScratch {
   double part[kNormGroups];
   // count workgroups through, 0 again when the last one is: a counter (128 bytes apart) for every kNormTurn of them, and one for these
@@ -42,6 +44,8 @@ struct dfx_list {
   bool all_f32 = true;
   std::vector<dfx_tensor> tensors;
   std::vector<size_t> counts;            // the tensors', for comparisons between lists
+  std::vector<ListSpan> spans;           // of the tensors that have elements, in the order of their addresses
+  bool apart = true;                     // none of them shares memory with another
   ListChunk* chunks = nullptr;           // device
   ListScratch* scratch = nullptr;        // device
 };
@@ -333,6 +337,21 @@ bool same_counts(const dfx_list* a, const dfx_list* b) {
   return a == b || (a->device == b->device && a->counts.size() == b->counts.size() && (a->counts.empty() || !memcmp(a->counts.data(), b->counts.data(), a->counts.size() * sizeof(size_t))));
 }
 
+// Whether no tensor of dst, whose own lie apart, shares memory with one of src, but for the same tensor at the same place.  Both go by addresses, so one
+// walk does; lists in buckets of their own do not meet at all.
+bool written_apart(const dfx_list* src, const dfx_list* dst) {
+  const std::vector<ListSpan>&s = src->spans, &d = dst->spans;
+  if (s.empty() || d.empty() || d.back().hi <= s.front().lo || (src->apart && s.back().hi <= d.front().lo)) return true;
+  size_t j = 0;
+  for (const ListSpan& x : s) {
+    while (j < d.size() && d[j].hi <= x.lo) ++j;
+    for (size_t i = j; i < d.size() && d[i].lo < x.hi; ++i)
+      if (d[i].k != x.k || d[i].lo != x.lo || src->tensors[x.k].dtype != dst->tensors[x.k].dtype) return false;
+    if (j == d.size()) break;
+  }
+  return true;
+}
+
 int check_norm(const dfx_list* l, int kind, double scale, const float* norm) {
   if (!l || !norm || ((uintptr_t)norm & 3u) || (kind != DFX_NORM_2 && kind != DFX_NORM_INF) || !isfinite(scale)) return DFX_ERR_INVALID_ARG;
   return on_its_device(l) ? DFX_OK : DFX_ERR_INVALID_ARG;
@@ -340,14 +359,7 @@ int check_norm(const dfx_list* l, int kind, double scale, const float* norm) {
 
 int check_clip(const dfx_list* src, const dfx_list* dst, const float* norm, double max_norm, double scale) {
   if (!src || !norm || ((uintptr_t)norm & 3u) || !(max_norm > 0.0) || !step_normal(scale)) return DFX_ERR_INVALID_ARG;
-  if (dst && dst != src) {
-    if (!same_counts(src, dst)) return DFX_ERR_INVALID_ARG;
-    for (size_t k = 0; k < src->tensors.size(); ++k) {       // the same tensor, or apart from it
-      const dfx_tensor &s = src->tensors[k], &d = dst->tensors[k];
-      const uintptr_t a = (uintptr_t)s.ptr, b = (uintptr_t)d.ptr;
-      if (s.count && a < b + d.count * step_elem_bytes(d.dtype) && b < a + s.count * step_elem_bytes(s.dtype) && !(a == b && s.dtype == d.dtype)) return DFX_ERR_INVALID_ARG;
-    }
-  }
+  if (!(dst ? dst : src)->apart || (dst && dst != src && (!same_counts(src, dst) || !written_apart(src, dst)))) return DFX_ERR_INVALID_ARG;
   return on_its_device(src) ? DFX_OK : DFX_ERR_INVALID_ARG;
 }
 
@@ -392,7 +404,11 @@ int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n) {
     for (const dfx_tensor& t : l->tensors) {
       l->counts.push_back(t.count);
       l->all_f32 = l->all_f32 && t.dtype == DFX_F32;
+      if (t.count) l->spans.push_back({(uintptr_t)t.ptr, (uintptr_t)t.ptr + t.count * step_elem_bytes(t.dtype), l->counts.size() - 1});
     }
+    const auto before = [](const ListSpan& a, const ListSpan& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(l->spans.begin(), l->spans.end(), before)) std::sort(l->spans.begin(), l->spans.end(), before);
+    for (size_t k = 1; k < l->spans.size(); ++k) l->apart = l->apart && l->spans[k - 1].hi <= l->spans[k].lo;
     l->nchunks = (uint32_t)nchunks;
     // scratch in front, zeroed with the table's upload
     const size_t at = (sizeof(ListScratch) + 255) / 256 * 256, bytes = at + nchunks * sizeof(ListChunk);
@@ -461,6 +477,7 @@ int dfx_adamw(dfx_list* params, dfx_list* grads, dfx_list* exp_avg, dfx_list* ex
   if (((uintptr_t)norm_dev & 3u) || ((uintptr_t)cfg->step_dev & 3u) || ((uintptr_t)cfg->lr_dev & 3u)) return DFX_ERR_INVALID_ARG;
   if (!same_counts(params, grads) || !same_counts(params, exp_avg) || !same_counts(params, exp_avg_sq) || (copies && !same_counts(params, copies))) return DFX_ERR_INVALID_ARG;
   if (params == exp_avg || params == exp_avg_sq || exp_avg == exp_avg_sq || params == grads || grads == exp_avg || grads == exp_avg_sq || (copies && (copies == params || copies == grads || copies == exp_avg || copies == exp_avg_sq))) return DFX_ERR_INVALID_ARG;
+  if (!params->apart || !exp_avg->apart || !exp_avg_sq->apart || (copies && !copies->apart)) return DFX_ERR_INVALID_ARG;
   if (!params->all_f32 || !exp_avg->all_f32 || !exp_avg_sq->all_f32 || !on_its_device(params)) return DFX_ERR_INVALID_ARG;
   if (!params->nchunks) return DFX_OK;
   AdamArgs a;

@@ -214,3 +214,52 @@ def test_numbers_that_32_bits_do_not_hold_are_refused():
     assert float(n.t) == 0.0
     dfx.grad_clip(a, n.ptr(), 1.0, scale=0.0)
     dfx.adamw(a, b, c, d, dfx.AdamWConfig(lr=1e-60, eps=1e-37))
+
+
+def test_lists_that_would_be_written_over_are_refused():
+    """A tensor that is written lies on no other tensor of its list and on none of the source but itself; what is only read may lie anywhere."""
+    import torch
+    dfx, _ = ts._dfx()
+    x, y, m, v = (ts.Guarded(40, "f32") for _ in range(4))
+    for k, b in enumerate((x, y, m, v)):
+        b.t.copy_(torch.arange(40) + k)
+    n = ts._scalar(2.0)
+
+    def lst(*at, kind=dfx.F32, of=x, eb=4):
+        return dfx.TensorList([(of.ptr() + eb * a, c, kind) for a, c in at])
+
+    def refused(f, *args, **kw):
+        with pytest.raises(dfx.DfxError) as e:
+            f(*args, **kw)
+        assert e.value.status == dfx.ERR_INVALID_ARG
+
+    src = lst((0, 8), (8, 8), (20, 8))
+    bad = [lst((28, 8), (0, 8), (8, 8)), lst((8, 8), (0, 8), (20, 8)), lst((0, 8), (8, 8), (13, 8)), lst((0, 8), (27, 8), (28, 8)), lst((0, 8), (1, 8), (20, 8)),
+           lst((28, 8), (28, 8), (20, 8)), lst((30, 8), (16, 8), (12, 8))]
+    # widened in the bucket itself: the second result lies on the third source
+    half = dfx.TensorList([(x.ptr() + 2 * a, 8, dfx.BF16) for a in (0, 8, 40)])
+    wide = dfx.TensorList([(y.ptr(), 8, dfx.F32), (x.ptr() + 68, 8, dfx.F32), (y.ptr() + 40, 8, dfx.F32)])
+    twice = lst((0, 8), (30, 8), (0, 8))
+    for call in (dfx.grad_clip, dfx.clip_grad_norm):
+        for out in bad:
+            refused(call, src, n.ptr(), 1.0, out=out)
+        refused(call, half, n.ptr(), 1.0, out=wide)
+        refused(call, twice, n.ptr(), 1.0)
+    one, g = lst((0, 8), (8, 8), (16, 8), of=y), lst((0, 8), (8, 8), (16, 8))
+    good = [lst((0, 8), (8, 8), (16, 8), of=b) for b in (y, m, v)]
+    over = lst((0, 8), (7, 8), (16, 8), of=y)
+    refused(dfx.adamw, over, g, good[1], good[2], dfx.AdamWConfig())
+    refused(dfx.adamw, good[0], g, lst((0, 8), (0, 8), (16, 8), of=m), good[2], dfx.AdamWConfig())
+    refused(dfx.adamw, good[0], g, good[1], lst((0, 8), (9, 8), (16, 8), of=v), dfx.AdamWConfig())
+    refused(dfx.adamw, good[0], g, good[1], good[2], dfx.AdamWConfig(), copies=lst((20, 8), (28, 8), (35, 8)))
+    assert all(bool((b.t == torch.arange(40, device="cuda") + k).all()) for k, b in enumerate((x, y, m, v)))
+    # taken: read twice, written once; the same tensors under another list, in part and between the others; with an empty tensor on them
+    want = x.t.clone()
+    dfx.grad_clip(twice, n.ptr(), 1.0, out=lst((0, 8), (8, 8), (16, 8), of=y), scale=2.0)
+    for a, b in ((0, 0), (30, 8), (0, 16)):
+        assert torch.allclose(y.t[b:b + 8], want[a:a + 8], rtol=1e-6)
+    dfx.grad_clip(lst((0, 8), (8, 0), (20, 8)), n.ptr(), 1.0, out=lst((0, 8), (4, 0), (30, 8)), scale=0.5)
+    assert torch.allclose(x.t[:8], 0.25 * want[:8], rtol=1e-6) and torch.allclose(x.t[30:38], 0.25 * want[20:28], rtol=1e-6)
+    assert bool((x.t[8:30] == want[8:30]).all()) and bool((x.t[38:] == want[38:]).all())
+    for b in (x, y, m, v):
+        b.check()
