@@ -478,7 +478,7 @@ int dfx_list_destroy(dfx_list* list);
  * of squares (summed in 64 bits), or the largest magnitude.  NaN where any gradient is NaN; 0 for a list without elements.
  * grad_scale: what the gradients are still to be multiplied with (1 / ranks behind a sum over ranks, 1 / loss scale).
  * The list's own scratch memory holds what the workgroups hand each other: calls of dfx_grad_norm or dfx_clip_grad_norm on one
- * list must not overlap.  Shards on several ranks: the norm of the ranks' norms (gathered, as a list of their own) is the norm of all.
+ * list must not overlap (the norms of those that do are wrong; later ones are not).  Shards on several ranks: the norm of the ranks' norms (gathered, as a list of their own) is the norm of all.
  * Errors: INVALID_ARG (also: the list is another device's), HIP.
  */
 int dfx_grad_norm(dfx_list* grads, dfx_norm_kind kind, double grad_scale, float* norm_dev, void* hip_stream);

@@ -91,12 +91,9 @@ __device__ __forceinline__ void norm_chunk(const ListChunk& c, double& sum, uint
   if (i < c.n) take(step_get<DT>(p, i));
 }
 
-// whether this is the last of n tickets, behind which the counter starts over
-__device__ __forceinline__ bool draw(uint32_t* counter, uint32_t n) {
-  if (__hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u != n) return false;
-  __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return true;
-}
+// Whether this is the last of n tickets.  The counter starts over behind it, in the same atomic: a multiple of n draws leaves 0, also where two calls on one
+// list overlapped after all and drew from it together (with a reset of its own a draw in between was lost, and every later norm of the list wrong).
+__device__ __forceinline__ bool draw(uint32_t* counter, uint32_t n) { return atomicInc(counter, n - 1u) == n - 1u; }
 
 template <bool MAXIMUM>
 __global__ void __launch_bounds__(kNormThreads) dfx_norm_kernel(const ListChunk* __restrict__ chunks, uint32_t nchunks, ListScratch* scratch, double scale, float* norm) {

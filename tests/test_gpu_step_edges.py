@@ -263,3 +263,30 @@ def test_lists_that_would_be_written_over_are_refused():
     assert bool((x.t[8:30] == want[8:30]).all()) and bool((x.t[38:] == want[38:]).all())
     for b in (x, y, m, v):
         b.check()
+
+
+@pytest.mark.parametrize("chunks", [2, 31, 33, 100, 544])
+def test_norms_behind_calls_that_overlapped(chunks):
+    """Calls on one list from two streams at once leave norms that mean nothing, and the list as good as new."""
+    import torch
+    dfx, _ = ts._dfx()
+    n = chunks * 8192 - 3
+    g = ts.Guarded(n, "f32")
+    g.t.fill_(0.25)
+    lst = dfx.TensorList([(g.ptr(), n, dfx.F32)])
+    outs = [ts._scalar() for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    want = 0.25 * math.sqrt(n)
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for _ in range(50):
+            for s, o in zip(streams, outs):
+                dfx.grad_norm(lst, o.ptr(), stream=s.cuda_stream)
+        torch.cuda.synchronize()
+        for _ in range(2):
+            outs[0].t.fill_(-1.0)
+            dfx.grad_norm(lst, outs[0].ptr())
+            torch.cuda.synchronize()
+            assert abs(float(outs[0].t) - want) <= 2 * U * want
+    for o in outs:
+        o.check()
