@@ -347,11 +347,11 @@ class TensorList:
 
     def __init__(self, tensors):
         self._h = C.c_void_p()
+        n = len(tensors)
+        if not all(map((3).__eq__, map(len, tensors))):
+            raise ValueError("a tensor is (address, elements, type)")
         # three 64-bit words are a dfx_tensor (type and reserved word share the last)
         words = array.array("Q", itertools.chain.from_iterable(tensors))
-        n = len(words) // 3
-        if len(words) % 3 or n != len(tensors):
-            raise ValueError("a tensor is (address, elements, type)")
         rc = _lib.dfx_list_create(C.byref(self._h), C.cast(words.buffer_info()[0], C.POINTER(Tensor)) if n else None, n)
         if rc != OK:
             self._h = C.c_void_p()
