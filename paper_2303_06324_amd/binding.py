@@ -371,6 +371,15 @@ class TensorList:
             pass
 
 
+def _if_any(lst: Optional[TensorList], what: str):
+    """The handle of a list that may be absent (None); a destroyed one is not absent."""
+    if lst is None:
+        return None
+    if not lst._h:
+        raise DfxError(ERR_INVALID_ARG, what)
+    return lst._h
+
+
 def grad_norm(grads: TensorList, norm: int, kind: int = NORM_2, scale: float = 1.0, stream: Optional[int] = None) -> None:
     """norm[0] = the norm of all gradients of the list, times |scale|."""
     rc = _lib.dfx_grad_norm(grads._h, kind, scale, norm, stream)
@@ -381,7 +390,7 @@ def grad_norm(grads: TensorList, norm: int, kind: int = NORM_2, scale: float = 1
 def grad_clip(grads: TensorList, norm: int, max_norm: float, out: Optional[TensorList] = None, scale: float = 1.0,
               stream: Optional[int] = None) -> None:
     """out (None: in place) = gradients * scale * min(1, max_norm / (norm[0] + 1e-6))."""
-    rc = _lib.dfx_grad_clip(grads._h, out._h if out is not None else None, norm, max_norm, scale, stream)
+    rc = _lib.dfx_grad_clip(grads._h, _if_any(out, "dfx_grad_clip"), norm, max_norm, scale, stream)
     if rc != OK:
         raise DfxError(rc, "dfx_grad_clip")
 
@@ -389,7 +398,7 @@ def grad_clip(grads: TensorList, norm: int, max_norm: float, out: Optional[Tenso
 def clip_grad_norm(grads: TensorList, norm: int, max_norm: float, out: Optional[TensorList] = None, kind: int = NORM_2,
                    scale: float = 1.0, stream: Optional[int] = None) -> None:
     """grad_norm, then grad_clip by that norm."""
-    rc = _lib.dfx_clip_grad_norm(grads._h, out._h if out is not None else None, kind, max_norm, scale, norm, stream)
+    rc = _lib.dfx_clip_grad_norm(grads._h, _if_any(out, "dfx_clip_grad_norm"), kind, max_norm, scale, norm, stream)
     if rc != OK:
         raise DfxError(rc, "dfx_clip_grad_norm")
 
@@ -397,7 +406,7 @@ def clip_grad_norm(grads: TensorList, norm: int, max_norm: float, out: Optional[
 def adamw(params: TensorList, grads: TensorList, exp_avg: TensorList, exp_avg_sq: TensorList, config: AdamWConfig,
           copies: Optional[TensorList] = None, norm: int = 0, stream: Optional[int] = None) -> None:
     """One AdamW update, clipped by norm[0] on the way; nothing is written where that is infinite or NaN, or a step on the device is 0."""
-    rc = _lib.dfx_adamw(params._h, grads._h, exp_avg._h, exp_avg_sq._h, copies._h if copies is not None else None, config, norm, stream)
+    rc = _lib.dfx_adamw(params._h, grads._h, exp_avg._h, exp_avg_sq._h, _if_any(copies, "dfx_adamw"), config, norm, stream)
     if rc != OK:
         raise DfxError(rc, "dfx_adamw")
 
