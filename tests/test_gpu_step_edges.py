@@ -290,3 +290,89 @@ def test_norms_behind_calls_that_overlapped(chunks):
             assert abs(float(outs[0].t) - want) <= 2 * U * want
     for o in outs:
         o.check()
+
+
+KW = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 64, 65])
+@pytest.mark.parametrize("vocab", [19999, 20000])
+def test_loss_where_rows_with_gradient_begin_to_be_split(rows, vocab, dt):
+    z, zh, t, cols = ts._loss_case(rows, vocab, dt, vocab + rows)
+    cols["old"][0] = st.policy_loss(zh[:1], t[:1].numpy())["logp"][0] + 0.05
+    out = ts._run_loss(z, t, cols, rows, vocab, dt, goff=1, **KW)
+    ts._check_loss(out, zh, t, cols, rows, vocab, dt, **KW)
+    out = ts._run_loss(z, t, cols, rows, vocab, dt, in_place=True, **KW)
+    ts._check_loss(out, zh, t, cols, rows, vocab, dt, **KW)
+
+
+@pytest.mark.parametrize("dt,vocab", [("f32", 60001), ("bf16", 131071), ("f16", 106500)])
+def test_gradient_in_the_place_of_logits_that_are_read_again(dt, vocab):
+    """Rows that neither are split nor fit registers and LDS: what is left of a row is read a second time, with gradients already written around it."""
+    rows, stride = 66, vocab + 3
+    z, zh, t, cols = ts._loss_case(rows, vocab, dt, 23, stride=stride, off=1)
+    z.t.view(rows, stride)[:, vocab:] = 7.0
+    out = ts._run_loss(z, t, cols, rows, vocab, dt, in_place=True, stride=stride, gstride=stride, **KW)
+    ts._check_loss(out, zh, t, cols, rows, vocab, dt, gstride=stride, **KW)
+    assert bool((z.t.view(rows, stride)[:, vocab:] == 7.0).all())
+
+
+def test_the_update_behind_a_contexts_all_reduce():
+    """Three buckets all-reduced over eight virtual ranks by a context, then norm and update on what they have become, with the daemon still there; three
+    steps, the next gradients written behind it each time."""
+    import torch
+    import paper_2303_06324_amd as dfx
+    from paper_2303_06324_amd import harness as gh
+    R, sizes, lr = 8, (70001, 8, 300000), 0.01
+    gen = torch.Generator("cuda").manual_seed(5)
+    send = [[torch.empty(n, dtype=torch.bfloat16, device="cuda") for n in sizes] for _ in range(R)]
+    recv = [[torch.empty(n, dtype=torch.bfloat16, device="cuda") for n in sizes] for _ in range(R)]
+    state = [[torch.zeros(n, device="cuda") for n in sizes] for _ in range(3)]
+    for p in state[0]:
+        p.normal_(generator=gen)
+    copy = [torch.empty(n, dtype=torch.bfloat16, device="cuda") for n in sizes]
+    kind = {torch.float32: dfx.F32, torch.bfloat16: dfx.BF16}
+    p, m, v, c = (dfx.TensorList([(t.data_ptr(), t.numel(), kind[t.dtype]) for t in tt]) for tt in (*state, copy))
+    grads = [dfx.TensorList([(t.data_ptr(), t.numel(), dfx.BF16) for t in recv[r]]) for r in range(R)]
+    norms = torch.zeros(R, device="cuda")
+    want = [[t.double().cpu().numpy() for t in tt] for tt in state]
+    torch.cuda.synchronize()
+    ctx = dfx.Context(R, gh.make_config())
+    try:
+        for k, n in enumerate(sizes):
+            ctx.prepare(k, dfx.ALLREDUCE, n, dfx.BF16)
+        for step in range(1, 4):
+            for r in range(R):
+                for t in send[r]:
+                    t.normal_(generator=gen)
+            ready = torch.cuda.Event()
+            ready.record()
+            ready.synchronize()
+            for r in range(R):
+                for k in np.random.default_rng(r + step).permutation(len(sizes)):       # any order
+                    assert ctx.submit(r, int(k), send[r][k].data_ptr(), recv[r][k].data_ptr()) == dfx.OK
+            assert ctx.wait_all(20.0) == dfx.OK
+            stream = torch.cuda.current_stream().cuda_stream
+            for r in range(R):
+                dfx.grad_norm(grads[r], norms[r].data_ptr(), scale=1.0 / R, stream=stream)
+            dfx.adamw(p, grads[3], m, v, dfx.AdamWConfig(lr=lr, step=step, grad_scale=1.0 / R, max_norm=1.0), copies=c, norm=norms[3].data_ptr(), stream=stream)
+            torch.cuda.synchronize()
+            g = [t.double().cpu().numpy() for t in recv[0]]
+            assert all(torch.equal(recv[r][k], recv[0][k]) for r in range(R) for k in range(len(sizes)))
+            total = sum(send[r][0].double() for r in range(R)).cpu().numpy()
+            assert np.abs(g[0] - total).max() <= R * 2.0 ** -8 * 16         # (a sum of eight normal numbers, rounded at each)
+            n = st.grad_norm(g, "2", 1.0 / R)
+            ts._near(norms.double().cpu().numpy(), np.full(R, n), 2 * U * n)
+            f = st.clip_factor(n, 1.0, 1.0 / R)
+            for k in range(len(sizes)):
+                wp, wm, wv = st.adamw(want[0][k], g[k], want[1][k], want[2][k], step, lr, 0.9, 0.999, 1e-8, 0.01, f)
+                got = state[0][k].double().cpu().numpy()
+                dm = 8 * U * (0.9 * np.abs(want[1][k]) + 0.1 * np.abs(g[k] * f))
+                move = lr / (1 - 0.9 ** step) * (np.abs(wm) * 24 * U + dm) / (np.sqrt(wv / (1 - 0.999 ** step)) + 1e-8)
+                ts._near(got, wp, move + 3 * U * (np.abs(want[0][k]) + np.abs(wp)), "p")
+                assert torch.equal(copy[k], state[0][k].to(torch.bfloat16))
+                for q in range(3):
+                    want[q][k] = state[q][k].double().cpu().numpy()
+    finally:
+        assert ctx.finalize() == dfx.OK
