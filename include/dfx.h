@@ -447,8 +447,8 @@ int dfx_collective_noalloc(int nranks, dfx_kind kind, size_t count, dfx_dtype dt
  * graph.  Memory that they are given is device memory of the current device, and every tensor starts at a multiple of its
  * element's size, which is all that is asked of alignment.  Element types are DFX_F32, DFX_BF16 and DFX_F16; sums, norms and
  * moments are held in 32 bits or more, and a result of 16 bits is rounded once, to nearest even.  Results do not depend on what
- * else runs: the same call on the same memory gives the same bits.  A context's
- * daemon that is still resident may hold back a kernel behind it (dfx_config.quit_idle_us).
+ * else runs: the same call on the same memory gives the same bits.  A context's daemon that is still resident holds back what is launched behind it
+ * until it leaves (dfx_config.quit_idle_us; dfx_stop).
  */
 
 /* One tensor of a list: count elements from ptr on (ptr is not looked at where count is 0). */
@@ -466,7 +466,7 @@ typedef enum { DFX_NORM_2 = 0, DFX_NORM_INF = 1 } dfx_norm_kind;
 
 /*
  * Make a list of n >= 0 tensors (host array, read during the call) on the current device; types may differ from tensor to tensor.
- * Allocates device memory (16 bytes per 8192 elements, and 16 KiB) and waits for its upload.
+ * Allocates device memory (16 bytes for every 8192 elements that a tensor begins, and 6400) and waits for its upload.
  * Errors: INVALID_ARG (type, NULL or misaligned ptr), TOO_LARGE (2^30 chunks of 8192 elements and more), NO_RESOURCES, HIP.
  */
 int dfx_list_create(dfx_list** out, const dfx_tensor* tensors, int n);

@@ -58,7 +58,7 @@ namespace {
 // Squares and their sum are held in 64 bits: no gradient of 32 or 16 bits is too large or too small to be squared there, so no second,
 // scaled pass is needed, and the products cost nothing beside the reads (with sums in 32 bits the times are the same).
 //
-// HBM bounds it.  Two workgroups a compute unit, all loads of a chunk under way at once: sixteen 25 MiB bf16 buckets 69 us (6.1 TB/s),
+// HBM bounds it.  Two workgroups a compute unit, all loads of a chunk under way at once (8 MiB of 16 bits, 16 of 32): sixteen 25 MiB bf16 buckets 69 us (6.1 TB/s),
 // 1 GiB of fp32 170 us (6.3 TB/s).  Half as many threads 113 and 195 us; 2048 workgroups of 256, all the waves that fit, 85 and 191 us:
 // what is in flight beyond about 16 MiB only gets in its own way.  A short list is its chain of waits (table, data, ticket): 4.0 us.
 // ------------------------------------------------------------------------------------------
@@ -213,11 +213,12 @@ __global__ void __launch_bounds__(kClipThreads) dfx_clip_kernel(const ListChunk*
 // ------------------------------------------------------------------------------------------
 // AdamW
 //
-// HBM bounds it: 26 bytes of a parameter with a 16-bit gradient and copy pass through, 372 M of them in 1740 us (6.0 TB/s).  A thread takes one
+// HBM bounds it: 28 bytes of a parameter with a 16-bit gradient and copy pass through, 372 M of them in 1740 us (6.0 TB/s).  A thread takes one
 // vector of four of every list and its workgroup ends, which leaves the order of requests to the dispatcher.  The lists of a model lie alike in
 // memory, so a thread's loads go to the same channels at the same moment; in a long list the second waits for the first to arrive, and the
 // others for the second: 1740 instead of 2069 us.  Below about 700 chunks the waits cost more than they give (4 M parameters 19.5 and 19.2
-// us, 8 M 43 and 45, 500 k 4.8 and 4.5).  Persistent workgroups (2048 of 256) 2400 us, with ordinary stores 2540.
+// us, 8 M 43 and 45, 500 k 4.8 and 4.5).  Persistent workgroups (2048 of 256) 2400 us, with ordinary stores 2540.  A step number that is read on
+// the device costs every thread two powers in 64 bits ahead of its loads: the 372 M then take 2100 us, 500 k 7.0 a call instead of 6.4.
 // ------------------------------------------------------------------------------------------
 struct AdamArgs {
   const ListChunk *p, *g, *m, *v, *copy;      // copy: may be null

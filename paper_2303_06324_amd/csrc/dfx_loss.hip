@@ -44,6 +44,8 @@ struct LossArgs {
 
 // exp(c (z - m)) = 2^(k (z - m)), k = c / log 2.  The difference first: it is 0 for the largest logit, exact where it matters, and cannot
 // overflow for logits of the type's lowest or largest value.
+// The product is rounded to 32 bits, k as well: an exponential is off by 4e-7 of its size at a distance of 10, 9e-7 at 20, and weighs as little in
+// the sum.  It shows in single elements of 32-bit gradients that far from the largest.
 struct MaxSum { float m, s; };           // s = sum 2^(k (z - m)); nothing seen yet: m = -infinity, s = 0
 
 // m to take differences from: where only -infinity was seen, any finite one (2^(-infinity - 0) = 0, and NaN stays NaN)
@@ -508,7 +510,8 @@ uint32_t loss_parts(uint64_t rows) { return (uint32_t)std::min<uint64_t>(rows * 
 // How a call is split, or segments = 0.  A row alone on its workgroup takes as long as that needs for its elements.  One row of bf16, us, alone and
 // split: with gradient and sums (two kernels either way) 20000 elements 7.8 and 6.7, 50257 10.3 and 7.2, 131072 19.2 and 7.2; forward (a launch
 // more, which costs the host 3) 32000 4.4 and 4.9, 70000 6.7 and 4.9, 131072 10.5 and 5.1.  64 rows with gradient 9.1 and 8.7, 12.1 and 9.7, 21.8 and
-// 12.5.  At 128 the two ways meet (9.6 and 9.7, 12.6 and 11.9, 23.4 and 20.7), since a split row is read twice; 200 rows of 131072 27.5 and 33.6.
+// 12.5.  A split row is read twice, so that it gains less the more rows there are: 128 rows 9.6 and 9.7, 12.6 and 11.9, 23.4 and 20.7, 200 of 131072 27.5 and
+// 33.6.  Between 64, where every length gains, and 200 the place where the ways meet depends on the length and was not looked for.
 Split loss_split(const LossArgs& a, uint32_t elem_bytes) {
   Split sp = {0, 0, 1, 0};
   if (a.rows == 0 || a.rows > kSplitRows || a.vocab < (a.grad ? kSplitGrad : kSplitForward)) return sp;
@@ -536,7 +539,7 @@ int launch_rows(const LossArgs& a, uint32_t groups, hipStream_t s) {
   if (nvec <= 512) ROWS(128, 4, 0, 4);
   if (nvec <= 1024) ROWS(256, 4, 0, 4);
   if (nvec <= 2048) ROWS(512, 4, 0, 4);
-  if (nvec <= 4096) ROWS(512, 8, 0, 8);
+  if (nvec <= 4096) ROWS(512, 8, 0, 8);  // (with gradient 32 to 40 bytes a thread are spilled; 4096 x 32000 bf16 103 us)
   if (nvec <= 10240) ROWS(1024, 6, 4, 6);
   ROWS(1024, 8, 4, 6);                   // (where more is read again, a few spilled registers are the lesser evil: 4096 x 131072 bf16 380 and 375 us; x 65536 195 and 199)
 #undef ROWS
