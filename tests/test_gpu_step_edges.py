@@ -1,4 +1,5 @@
-"""Values and layouts at the edge of what the training step's operators are asked for: log-probabilities of -infinity, penalties far from 0.
+"""Values and layouts at the edge of what the training step's operators are asked for: log-probabilities of -infinity, penalties far from 0,
+small rates, numbers beyond 32 bits, memory that is named twice, calls that overlap, rows where they begin to be split, a context in front.
 Helpers and tolerances are those of test_gpu_step.py, whose docstring derives them."""
 import math
 
