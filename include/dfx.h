@@ -566,6 +566,147 @@ size_t dfx_policy_loss_workspace(size_t rows, size_t vocab, dfx_dtype dtype);
 /* Errors: INVALID_ARG (also: workspace too small, something written lies on something else), TOO_LARGE, HIP. */
 int dfx_policy_loss(const dfx_policy_loss_args* args, void* hip_stream);
 
+/*
+ * ---- The two ends of a language model in that step -------------------------------------------------------------------
+ * From tokens into rows of a table, and from the last layer norm through the product with the vocabulary into the loss; on the way back the
+ * gradients of both ends, which are the largest tensors of the buckets.  What is said of the calls above holds for these: no context, nothing
+ * is allocated or waited for, captured or not, any alignment to the element's size, sums in 32 bits or more, one rounding of each result, the same bits
+ * from the same memory.  A 16-bit input may have its parameters' gradients in 32 bits, which a later call adds to (accumulate: what the gradient holds and
+ * the new sum are added in 32 bits, and rounded once).  Strides are elements from one row to the next, 0 = the row's length; rows may not
+ * overlap.  Workspaces hold nothing between calls, and calls that may overlap (two graphs that are replayed at once among them) need one each.
+ * Zero-initialise the arguments and set struct_bytes.  What is written lies apart from what is read and from each other, unless it says otherwise; all space
+ * from a matrix's first to its last row counts as that matrix's.
+ * Tokens and targets outside [0, vocab) stand for none: padding, a prompt.
+ * Errors of all: INVALID_ARG (NULL or misaligned memory, types, strides, overlap, workspace too small, numbers that are not finite in 32 bits), TOO_LARGE
+ * (rows or vocab of 2^31 - 2^10 and more, dim or a stride of 2^20 and more, memory beyond 2^62 bytes), HIP.
+ */
+
+/* out[i] = scale * table[tokens[i]]; zeros where there is no token. */
+typedef struct {
+  uint32_t struct_bytes;
+  dfx_dtype dtype;           /* of table and out */
+  size_t rows, dim, vocab;   /* tokens, elements of a row of the table, its rows; any may be 0 */
+  const int64_t* tokens;     /* [rows] */
+  const void* table;
+  size_t table_stride;
+  void* out;
+  size_t out_stride;
+  double scale;
+} dfx_embed_args;
+int dfx_embed(const dfx_embed_args* args, void* hip_stream);
+
+/*
+ * The gradient of dfx_embed's table: table_grad[v] = scale * sum of grad[i] over the i with tokens[i] = v.  accumulate: that is added to what
+ * table_grad holds, and rows that no token names are neither read nor written; otherwise all of it is written.  The rows of a token are
+ * added up in 32 bits, in their order.
+ */
+typedef struct {
+  uint32_t struct_bytes;
+  dfx_dtype dtype;           /* of grad */
+  dfx_dtype out_dtype;       /* of table_grad: the same, or DFX_F32 */
+  uint32_t accumulate;
+  size_t rows, dim, vocab;
+  const int64_t* tokens;
+  const void* grad;
+  size_t grad_stride;
+  void* table_grad;
+  size_t table_grad_stride;
+  double scale;
+  void* workspace;           /* dfx_embed_grad_workspace bytes, 16-byte aligned */
+  size_t workspace_bytes;
+} dfx_embed_grad_args;
+size_t dfx_embed_grad_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype);
+int dfx_embed_grad(const dfx_embed_grad_args* args, void* hip_stream);
+
+/*
+ * Layer norm of rows: h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps);  y = h weight + bias.  y may take x's place (same memory and stride).
+ * A row with an infinity or NaN is NaN.
+ */
+typedef struct {
+  uint32_t struct_bytes;
+  dfx_dtype dtype;           /* of x and y */
+  dfx_dtype param_dtype;     /* of weight and bias: the same, or DFX_F32 */
+  uint32_t reserved0;        /* must be 0 */
+  size_t rows, dim;          /* rows may be 0 */
+  const void* x;
+  size_t x_stride;
+  const void* weight;        /* [dim], may be NULL: 1 */
+  const void* bias;          /* [dim], may be NULL: 0 */
+  void* y;
+  size_t y_stride;
+  double eps;                /* >= 0: 0 or a normal number in 32 bits */
+} dfx_layer_norm_args;
+int dfx_layer_norm(const dfx_layer_norm_args* args, void* hip_stream);
+
+/*
+ * Its gradients, by the gradient dy of y; mean and deviation of a row are made again from x, so that the forward call leaves nothing to keep:
+ *   g = dy weight;  dx = (g - mean g - h mean(g h)) / sqrt(...);  grad_weight = sum over rows of dy h;  grad_bias = sum over rows of dy
+ * Any of dx, grad_weight and grad_bias may be NULL.  dx may take dy's place, or x's.  Without rows the sums are 0.
+ */
+typedef struct {
+  uint32_t struct_bytes;
+  dfx_dtype dtype;           /* of x, dy and dx */
+  dfx_dtype param_dtype;     /* of weight: the same, or DFX_F32 */
+  dfx_dtype grad_dtype;      /* of grad_weight and grad_bias: dtype or DFX_F32 */
+  uint32_t accumulate;       /* add to what grad_weight and grad_bias hold */
+  uint32_t reserved0;        /* must be 0 */
+  size_t rows, dim;
+  const void* x;
+  size_t x_stride;
+  const void* dy;
+  size_t dy_stride;
+  const void* weight;        /* may be NULL: 1 */
+  void* dx;
+  size_t dx_stride;
+  void* grad_weight;
+  void* grad_bias;
+  double eps;
+  void* workspace;           /* dfx_layer_norm_grad_workspace bytes, 16-byte aligned; may be NULL without grad_weight and grad_bias */
+  size_t workspace_bytes;
+} dfx_layer_norm_grad_args;
+size_t dfx_layer_norm_grad_workspace(size_t rows, size_t dim, dfx_dtype dtype);
+int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* args, void* hip_stream);
+
+/*
+ * Softmax cross entropy of a vocabulary's logits that are never kept, and its gradients: with z = inv_temperature * hidden weight^T
+ *   logp = log softmax(z)[target];  loss = -row_weight logp;  dz = scale inv_temperature row_weight (softmax(z) - [j = target])
+ *   grad_hidden = dz weight;  grad_weight = dz^T hidden
+ * The products are made on the matrix cores in pieces of the vocabulary, and their sums in 32 bits; 32-bit inputs are taken as three terms of 8 bits of
+ * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time, piece by piece, and dz is rounded
+ * to the type of the inputs on its way into the products (32-bit inputs: to three such terms).
+ * A row of weight 0 or without a target has nothing to learn from: it takes no part in the products, its hidden state is not looked at, its
+ * logp, loss and grad_hidden are 0.  So has a row with no logit above -infinity.  A logit of NaN or +infinity makes its row NaN, and with it
+ * grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of rows are finite.
+ */
+typedef struct {
+  uint32_t struct_bytes;
+  dfx_dtype dtype;           /* of hidden, weight and grad_hidden */
+  dfx_dtype grad_dtype;      /* of grad_weight: the same, or DFX_F32 */
+  uint32_t accumulate;       /* add to what grad_weight holds */
+  size_t rows, dim, vocab;   /* rows and vocab may be 0 */
+  const void* hidden;        /* [rows][dim] */
+  size_t hidden_stride;
+  const void* weight;        /* [vocab][dim] */
+  size_t weight_stride;
+  const int64_t* targets;    /* [rows] */
+  const float* row_weight;   /* [rows], may be NULL: 1 */
+  const float* scale;        /* one value, may be NULL: 1.  Multiplies the gradients only: 1 / the weights of all ranks' rows */
+  float* logp;               /* [rows], may be NULL */
+  float* loss;               /* [rows], may be NULL */
+  float* sums;               /* 2 values, may be NULL: sum of loss, and of the weights of the rows that count */
+  void* grad_hidden;         /* may be NULL */
+  size_t grad_hidden_stride;
+  void* grad_weight;         /* may be NULL */
+  size_t grad_weight_stride;
+  double inv_temperature;    /* > 0, and 1.45 times it a normal number in 32 bits */
+  size_t piece;              /* rows of weight whose dz is held at a time, a multiple of 256; 0 = the library's choice */
+  void* workspace;           /* dfx_vocab_loss_workspace bytes, 256-byte aligned */
+  size_t workspace_bytes;
+} dfx_vocab_loss_args;
+/* grad: whether a gradient is asked for.  A call of fewer rows has room in it as well. */
+size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece);
+int dfx_vocab_loss(const dfx_vocab_loss_args* args, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

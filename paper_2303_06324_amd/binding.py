@@ -69,6 +69,42 @@ class PolicyLossArgs(C.Structure):
                         ("workspace_bytes", C.c_size_t)] + [(n, C.c_double) for n in ("clip_low", "clip_high", "kl_coef", "inv_temperature")]
 
 
+class EmbedArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("rows", C.c_size_t), ("dim", C.c_size_t), ("vocab", C.c_size_t),
+                ("tokens", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_size_t), ("out", C.c_void_p), ("out_stride", C.c_size_t),
+                ("scale", C.c_double)]
+
+
+class EmbedGradArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("out_dtype", C.c_int), ("accumulate", C.c_uint32), ("rows", C.c_size_t),
+                ("dim", C.c_size_t), ("vocab", C.c_size_t), ("tokens", C.c_void_p), ("grad", C.c_void_p), ("grad_stride", C.c_size_t),
+                ("table_grad", C.c_void_p), ("table_grad_stride", C.c_size_t), ("scale", C.c_double), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class LayerNormArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("param_dtype", C.c_int), ("reserved0", C.c_uint32), ("rows", C.c_size_t),
+                ("dim", C.c_size_t), ("x", C.c_void_p), ("x_stride", C.c_size_t), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("y", C.c_void_p), ("y_stride", C.c_size_t), ("eps", C.c_double)]
+
+
+class LayerNormGradArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("param_dtype", C.c_int), ("grad_dtype", C.c_int),
+                ("accumulate", C.c_uint32), ("reserved0", C.c_uint32), ("rows", C.c_size_t), ("dim", C.c_size_t), ("x", C.c_void_p),
+                ("x_stride", C.c_size_t), ("dy", C.c_void_p), ("dy_stride", C.c_size_t), ("weight", C.c_void_p), ("dx", C.c_void_p),
+                ("dx_stride", C.c_size_t), ("grad_weight", C.c_void_p), ("grad_bias", C.c_void_p), ("eps", C.c_double),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class VocabLossArgs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_uint32), ("dtype", C.c_int), ("grad_dtype", C.c_int), ("accumulate", C.c_uint32), ("rows", C.c_size_t),
+                ("dim", C.c_size_t), ("vocab", C.c_size_t), ("hidden", C.c_void_p), ("hidden_stride", C.c_size_t), ("weight", C.c_void_p),
+                ("weight_stride", C.c_size_t)] + [(n, C.c_void_p) for n in ("targets", "row_weight", "scale", "logp", "loss", "sums")] + [
+                    ("grad_hidden", C.c_void_p), ("grad_hidden_stride", C.c_size_t), ("grad_weight", C.c_void_p),
+                    ("grad_weight_stride", C.c_size_t), ("inv_temperature", C.c_double), ("piece", C.c_size_t), ("workspace", C.c_void_p),
+                    ("workspace_bytes", C.c_size_t)]
+
+
 CALLBACK = C.CFUNCTYPE(None, C.c_void_p, C.c_int, C.c_uint32, C.c_uint32)
 
 
@@ -135,6 +171,14 @@ def _load() -> C.CDLL:
         "dfx_adamw": ([vp, vp, vp, vp, vp, C.POINTER(AdamWConfig), vp, vp], i),
         "dfx_policy_loss_workspace": ([sz, sz, i], sz),
         "dfx_policy_loss": ([C.POINTER(PolicyLossArgs), vp], i),
+        "dfx_embed": ([C.POINTER(EmbedArgs), vp], i),
+        "dfx_embed_grad_workspace": ([sz, sz, sz, i], sz),
+        "dfx_embed_grad": ([C.POINTER(EmbedGradArgs), vp], i),
+        "dfx_layer_norm": ([C.POINTER(LayerNormArgs), vp], i),
+        "dfx_layer_norm_grad_workspace": ([sz, sz, i], sz),
+        "dfx_layer_norm_grad": ([C.POINTER(LayerNormGradArgs), vp], i),
+        "dfx_vocab_loss_workspace": ([sz, sz, sz, i, i, sz], sz),
+        "dfx_vocab_loss": ([C.POINTER(VocabLossArgs), vp], i),
         "dfx_collective_noalloc": ([i, i, sz, i, i, i, C.POINTER(vp), C.POINTER(vp), vp, vp], i),
     }
     for name, (args, res) in sig.items():
@@ -431,3 +475,78 @@ def policy_loss(rows: int, vocab: int, dtype: int, logits: int, targets: int, *,
     rc = _lib.dfx_policy_loss(a, stream)
     if rc != OK:
         raise DfxError(rc, "dfx_policy_loss")
+
+
+# ---- the two ends of a language model in that step, under the same conventions; strides of 0: rows lie one behind the other
+_EMBED_BYTES, _EMBED_GRAD_BYTES = C.sizeof(EmbedArgs), C.sizeof(EmbedGradArgs)
+_NORM_BYTES, _NORM_GRAD_BYTES, _VOCAB_BYTES = C.sizeof(LayerNormArgs), C.sizeof(LayerNormGradArgs), C.sizeof(VocabLossArgs)
+
+
+def embed(rows: int, dim: int, vocab: int, dtype: int, tokens: int, table: int, out: int, *, table_stride: int = 0, out_stride: int = 0,
+          scale: float = 1.0, stream: Optional[int] = None) -> None:
+    """out[i] = scale * table[tokens[i]]; zeros for a token outside [0, vocab) (dfx_embed)."""
+    rc = _lib.dfx_embed(EmbedArgs(_EMBED_BYTES, dtype, rows, dim, vocab, tokens, table, table_stride, out, out_stride, scale), stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_embed")
+
+
+def embed_grad_workspace(rows: int, dim: int, vocab: int, dtype: int) -> int:
+    """Bytes of workspace that embed_grad needs for up to so many rows (no GPU needed)."""
+    return _lib.dfx_embed_grad_workspace(rows, dim, vocab, dtype)
+
+
+def embed_grad(rows: int, dim: int, vocab: int, dtype: int, tokens: int, grad: int, table_grad: int, *, out_dtype: Optional[int] = None,
+               grad_stride: int = 0, table_grad_stride: int = 0, scale: float = 1.0, accumulate: bool = False, workspace: int = 0,
+               workspace_bytes: int = 0, stream: Optional[int] = None) -> None:
+    """table_grad[v] = scale * the sum of grad[i] over the tokens that are v, or that added to it (dfx_embed_grad)."""
+    a = EmbedGradArgs(_EMBED_GRAD_BYTES, dtype, dtype if out_dtype is None else out_dtype, accumulate, rows, dim, vocab, tokens, grad,
+                      grad_stride, table_grad, table_grad_stride, scale, workspace, workspace_bytes)
+    rc = _lib.dfx_embed_grad(a, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_embed_grad")
+
+
+def layer_norm(rows: int, dim: int, dtype: int, x: int, y: int, *, weight: int = 0, bias: int = 0, param_dtype: Optional[int] = None,
+               x_stride: int = 0, y_stride: int = 0, eps: float = 1e-5, stream: Optional[int] = None) -> None:
+    """y = (x - mean) / sqrt(variance + eps) * weight + bias, row by row (dfx_layer_norm)."""
+    a = LayerNormArgs(_NORM_BYTES, dtype, dtype if param_dtype is None else param_dtype, 0, rows, dim, x, x_stride, weight, bias, y, y_stride, eps)
+    rc = _lib.dfx_layer_norm(a, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_layer_norm")
+
+
+def layer_norm_grad_workspace(rows: int, dim: int, dtype: int) -> int:
+    """Bytes of workspace that layer_norm_grad needs for up to so many rows (no GPU needed)."""
+    return _lib.dfx_layer_norm_grad_workspace(rows, dim, dtype)
+
+
+def layer_norm_grad(rows: int, dim: int, dtype: int, x: int, dy: int, dx: int = 0, *, weight: int = 0, grad_weight: int = 0, grad_bias: int = 0,
+                    param_dtype: Optional[int] = None, grad_dtype: Optional[int] = None, x_stride: int = 0, dy_stride: int = 0,
+                    dx_stride: int = 0, eps: float = 1e-5, accumulate: bool = False, workspace: int = 0, workspace_bytes: int = 0,
+                    stream: Optional[int] = None) -> None:
+    """The gradients of layer_norm's input, weight and bias by that of y; grad_dtype: the parameters' type unless given (dfx_layer_norm_grad)."""
+    params = dtype if param_dtype is None else param_dtype
+    a = LayerNormGradArgs(_NORM_GRAD_BYTES, dtype, params, params if grad_dtype is None else grad_dtype, accumulate, 0, rows, dim, x, x_stride,
+                          dy, dy_stride, weight, dx, dx_stride, grad_weight, grad_bias, eps, workspace, workspace_bytes)
+    rc = _lib.dfx_layer_norm_grad(a, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_layer_norm_grad")
+
+
+def vocab_loss_workspace(rows: int, dim: int, vocab: int, dtype: int, grad: bool = False, piece: int = 0) -> int:
+    """Bytes of workspace that vocab_loss needs for up to so many rows, with a gradient or without (no GPU needed)."""
+    return _lib.dfx_vocab_loss_workspace(rows, dim, vocab, dtype, grad, piece)
+
+
+def vocab_loss(rows: int, dim: int, vocab: int, dtype: int, hidden: int, weight: int, targets: int, *, row_weight: int = 0, scale: int = 0,
+               logp: int = 0, loss: int = 0, sums: int = 0, grad_hidden: int = 0, grad_weight: int = 0, grad_dtype: Optional[int] = None,
+               accumulate: bool = False, hidden_stride: int = 0, weight_stride: int = 0, grad_hidden_stride: int = 0,
+               grad_weight_stride: int = 0, inv_temperature: float = 1.0, piece: int = 0, workspace: int = 0, workspace_bytes: int = 0,
+               stream: Optional[int] = None) -> None:
+    """Cross entropy under softmax(hidden weight^T), whose logits are never kept, and where asked for its gradients (dfx_vocab_loss)."""
+    a = VocabLossArgs(_VOCAB_BYTES, dtype, dtype if grad_dtype is None else grad_dtype, accumulate, rows, dim, vocab, hidden, hidden_stride,
+                      weight, weight_stride, targets, row_weight, scale, logp, loss, sums, grad_hidden, grad_hidden_stride, grad_weight,
+                      grad_weight_stride, inv_temperature, piece, workspace, workspace_bytes)
+    rc = _lib.dfx_vocab_loss(a, stream)
+    if rc != OK:
+        raise DfxError(rc, "dfx_vocab_loss")

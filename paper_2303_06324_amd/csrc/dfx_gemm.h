@@ -1,0 +1,193 @@
+// Products of matrices for the loss over a vocabulary (dfx_vocab.hip): C[n][m] = sum over k of A[m][k] B[n][k] by workgroups that each hold a tile of C in
+// registers, and hand it to an epilogue there.  An operand lies in memory with k along its rows, or across them ("turned": [k][m]).
+//
+// 16-bit elements on the matrix cores, sums in 32 bits.  A 32-bit matrix comes as three planes of bf16, its mantissa's 24 bits cut into three parts of 8,
+// which hold it exactly: a = a0 + a1 + a2, |a1| <= 2^-8 |a|, |a2| <= 2^-16 |a|, and a b = a0 b0 + (a0 b1 + a1 b0) + (a1 b1 + a0 b2 + a2 b0) but for
+// a1 b2 + a2 b1 + a2 b2, which are below 2^-23 + 2^-32 of it.  These six products follow one another along k, the small ones first, and cost six of a peak that is
+// sixteen times that of 32-bit products.
+#ifndef DFX_GEMM_H
+#define DFX_GEMM_H
+
+#include "dfx_step.h"
+
+namespace {
+
+typedef __bf16 GemmBf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 GemmF16x8 __attribute__((ext_vector_type(8)));
+typedef short GemmShort4 __attribute__((ext_vector_type(4)));
+typedef short GemmShort8 __attribute__((ext_vector_type(8)));
+typedef float GemmAcc __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char GemmLds;
+
+constexpr int kGemmK = 64;               // elements of k in a step: 128 bytes of a row
+
+__host__ __device__ constexpr int gemm_planes(int dt) { return dt == DFX_F32 ? 3 : 1; }
+__host__ __device__ constexpr int gemm_pairs(int dt) { return dt == DFX_F32 ? 6 : 1; }
+__device__ __forceinline__ int gemm_plane_a(int pair) { return (0x201100 >> (4 * (5 - pair))) & 0xf; }      // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+__device__ __forceinline__ int gemm_plane_b(int pair) { return (0x021010 >> (4 * (5 - pair))) & 0xf; }
+
+// rows: of a matrix with k along them, how many there are; of a turned one, how many k's.  cols: of a turned one, elements of a row that may be read
+// (a multiple of 8).  Tiles that go beyond read the last row or the last 8 elements again; what is made of those is not used.  Every row begins at a
+// multiple of 16 bytes, and rows with k along them hold whole steps.
+struct GemmOperand {
+  const uint16_t* p;
+  size_t plane;                          // elements from one plane to the next
+  uint32_t stride, rows, cols;
+};
+
+struct GemmShape {
+  uint32_t mtiles, ntiles, splits;       // workgroups; splits along k
+  uint32_t ksteps;                       // (or of what count says)
+  const uint32_t* count;                 // device, may be null: what it holds bounds n (n_counted), or k
+  bool k_counted;
+};
+
+// Workgroups go round the 8 XCDs; each XCD gets tiles that lie together, so that what it reads is in its own L2: kGroup tiles of n, then the next of m.
+struct GemmPlace { uint32_t m, n, split; bool any; };
+__device__ __forceinline__ GemmPlace gemm_place(const GemmShape& s) {
+  constexpr uint32_t kGroup = 8;
+  const uint32_t tiles = s.mtiles * s.ntiles, total = tiles * s.splits, each = (total + 7u) / 8u;
+  const uint32_t j = (blockIdx.x & 7u) * each + (blockIdx.x >> 3);
+  if (j >= total || (blockIdx.x >> 3) >= each) return {0, 0, 0, false};
+  const uint32_t split = j / tiles, t = j % tiles, group = t / (kGroup * s.mtiles), in = t % (kGroup * s.mtiles);
+  const uint32_t width = min(kGroup, s.ntiles - group * kGroup);
+  return {in / width, group * kGroup + in % width, split, true};
+}
+inline uint32_t gemm_groups(const GemmShape& s) { return (uint32_t)(((uint64_t)s.mtiles * s.ntiles * s.splits + 7) / 8 * 8); }
+
+// Tiles in LDS.  k along the rows: a row's 128 bytes, whose 16-byte parts are exchanged by the row's number, so that 16 rows' parts of one k lie in
+// different banks.  Turned: a k's 2 COLS bytes, whose 32-byte parts (16 elements, a tile of the matrix instruction) are exchanged by k.
+__device__ __forceinline__ uint32_t gemm_turned_swap(uint32_t k) { return (k & 3u) | ((k >> 1) & 4u); }
+
+template <int COLS, int THREADS, bool TURNED>
+__device__ __forceinline__ void gemm_fetch(const GemmOperand& o, int plane, uint32_t first, uint32_t k0, unsigned char* lds) {
+  constexpr int LOADS = COLS * 8 / THREADS;
+  const uint32_t t = threadIdx.x, wave = t / kStepWave;
+  if (!TURNED) {
+    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)first * o.stride + k0;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, -1, 0x00020000);
+    const uint32_t last = o.rows - 1u - first;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const uint32_t row = j * (THREADS / 8) + t / 8, part = (t & 7u) ^ ((row >> 1) & 7u);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)(min(row, last) * o.stride * 2u + part * 16u), 0, 0, 0);
+    }
+  } else {
+    constexpr int PARTS = COLS / 8;      // of 16 bytes in a k's row
+    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)k0 * o.stride;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, -1, 0x00020000);
+    const uint32_t last = o.rows - 1u - k0;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const uint32_t k = j * (THREADS / PARTS) + t / PARTS, slot = t % PARTS;
+      const uint32_t part = (((slot >> 1) ^ gemm_turned_swap(k)) << 1) | (slot & 1u);
+      const uint32_t col = min(first + part * 8u, o.cols - 8u);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)((min(k, last) * o.stride + col) * 2u), 0, 0, 0);
+    }
+  }
+}
+
+// what a lane holds of 16 rows and 32 k's: row lane % 16, k's 8 (lane / 16) on
+template <int COLS, bool TURNED>
+__device__ __forceinline__ GemmShort8 gemm_read(const unsigned char* lds, uint32_t first, int kk) {
+  const uint32_t lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u;
+  if (!TURNED) {
+    const uint32_t row = first + l;
+    return *(const __attribute__((address_space(3))) GemmShort8*)((GemmLds*)lds + row * 128u + (((uint32_t)kk * 4u + g) ^ ((l >> 1) & 7u)) * 16u);
+  }
+  const uint32_t k = kk * 32u + 8u * g + l / 4u;
+  GemmLds* at = (GemmLds*)lds + k * (COLS * 2u) + (((first / 16u) ^ gemm_turned_swap(k)) * 32u) + (l & 3u) * 8u;
+  const GemmShort4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)at);
+  const GemmShort4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)(at + 4u * COLS * 2u));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <int DT>
+__device__ __forceinline__ GemmAcc gemm_mac(GemmShort8 a, GemmShort8 b, GemmAcc c) {
+  if (DT == DFX_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(GemmF16x8, a), __builtin_bit_cast(GemmF16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(GemmBf16x8, a), __builtin_bit_cast(GemmBf16x8, b), c, 0, 0, 0);
+}
+
+// A tile of 256 m and WN NT 16 n by WM WN waves; a lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
+template <int WM_, int WN_, int MT_, int NT_>
+struct GemmTile {
+  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, M = WM * MT * 16, N = WN * NT * 16, THREADS = WM * WN * kStepWave;
+  static constexpr int STAGE = (M + N) * kGemmK * 2, LDS = 2 * STAGE;
+  uint32_t m0, n0;                       // of the workgroup's tile
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave / WN * (MT * 16); }
+  __device__ __forceinline__ uint32_t wave_n() const { return threadIdx.x / kStepWave % WN * (NT * 16); }
+  __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16 + threadIdx.x % kStepWave / 16 * 4; }
+  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + wave_n() + nt * 16 + threadIdx.x % 16; }
+};
+
+typedef GemmTile<2, 4, 8, 4> GemmWide;   // 256 m by 256 n, 512 threads
+typedef GemmTile<4, 1, 4, 4> GemmFlat;   // 256 m by 64 n, 256 threads: few rows
+
+template <int DT, class TILE, bool TA, bool TB, class EPI>
+__global__ void __launch_bounds__(TILE::THREADS) dfx_gemm_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  __shared__ __align__(1024) unsigned char gemm_lds[TILE::LDS];
+  const GemmPlace at = gemm_place(s);
+  if (!at.any) return;
+  TILE tile;
+  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
+  uint32_t steps = s.ksteps;
+  if (s.count) {
+    const uint32_t count = *s.count;
+    if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
+    else if (tile.n0 >= count) return;
+  }
+  const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
+  GemmAcc acc[TILE::MT][TILE::NT];
+#pragma unroll
+  for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  const uint32_t span = end - begin, total = span * gemm_pairs(DT);
+  const uint32_t wm = tile.wave_m(), wn = tile.wave_n();
+  uint32_t k = begin;
+  int pair = 0;
+  auto fetch = [&](uint32_t stage) {
+    const int pa = gemm_planes(DT) == 1 ? 0 : gemm_plane_a(pair), pb = gemm_planes(DT) == 1 ? 0 : gemm_plane_b(pair);
+    unsigned char* lds = gemm_lds + stage * TILE::STAGE;
+    gemm_fetch<TILE::M, TILE::THREADS, TA>(a, pa, tile.m0, k * kGemmK, lds);
+    gemm_fetch<TILE::N, TILE::THREADS, TB>(b, pb, tile.n0, k * kGemmK, lds + TILE::M * kGemmK * 2);
+    if (++k == end) { k = begin; ++pair; }
+  };
+  if (total) fetch(0);
+  for (uint32_t q = 0; q < total; ++q) {
+    __syncthreads();                     // this step's tiles have arrived, and nobody reads the other stage any more
+    if (q + 1 < total) fetch((q + 1) & 1u);
+    const unsigned char* la = gemm_lds + (q & 1u) * TILE::STAGE;
+    const unsigned char* lb = la + TILE::M * kGemmK * 2;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      GemmShort8 fa[TILE::MT], fb[TILE::NT];
+#pragma unroll
+      for (int j = 0; j < TILE::NT; ++j) fb[j] = gemm_read<TILE::N, TB>(lb, wn + j * 16, kk);
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i) fa[i] = gemm_read<TILE::M, TA>(la, wm + i * 16, kk);
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < TILE::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i], fb[j], acc[i][j]);
+    }
+  }
+  epi(tile, at, acc, gemm_lds);
+}
+
+// The three planes of a 32-bit value, each the nearest bf16 to what is left of it (the largest values' first: towards zero, since the nearest is
+// infinite).  Of an infinity or NaN the first is one, the others 0.
+__device__ __forceinline__ void gemm_cut(float v, uint16_t* part) {
+  const uint32_t b = __float_as_uint(v);
+  part[0] = StepElem<DFX_BF16>::put(v);
+  part[1] = part[2] = 0;
+  if ((b & 0x7f800000u) == 0x7f800000u) return;
+  if ((part[0] & 0x7f80u) == 0x7f80u) part[0] = (uint16_t)(b >> 16);
+  const float rest = v - StepElem<DFX_BF16>::get(part[0]);
+  part[1] = StepElem<DFX_BF16>::put(rest);
+  part[2] = StepElem<DFX_BF16>::put(rest - StepElem<DFX_BF16>::get(part[1]));
+}
+
+}  // namespace
+
+#endif

@@ -551,19 +551,6 @@ Extent extent(const void* p, size_t rows, size_t vocab, size_t stride, size_t eb
   return {(uintptr_t)p, (uintptr_t)p + ((rows - 1) * stride + vocab) * eb};
 }
 
-// n pieces of so many bytes, step bytes from one to the next; nothing: n = 0
-struct Span { uintptr_t at; size_t n, bytes, step; };
-Span flat(const void* p, size_t bytes) { return {(uintptr_t)p, p && bytes ? (size_t)1 : 0, bytes, bytes}; }
-
-// whether a span of one piece shares a byte with another: with the last piece that begins at or before it, or the one behind that
-bool meet(const Span& one, const Span& s) {
-  if (!one.n || !s.n) return false;
-  const uintptr_t lo = one.at, hi = lo + one.bytes;
-  const size_t k = lo <= s.at ? 0 : std::min<size_t>((lo - s.at) / s.step, s.n - 1);
-  const uintptr_t p = s.at + k * s.step;
-  return (lo < p + s.bytes && p < hi) || (k + 1 < s.n && p + s.step < hi);
-}
-
 }  // namespace
 
 extern "C" {

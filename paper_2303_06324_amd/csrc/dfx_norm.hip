@@ -1,0 +1,374 @@
+// Layer norm over rows, forward and backward.
+//
+// h = (x - mean) r, r = 1 / sqrt(var + eps), y = h w + b;  with g = dy w:  dx = r (g - mean g - h mean(g h)), dw = sum dy h, db = sum dy.
+// A row stays in registers from its mean to its results: mean and variance are taken one behind the other, so that a large mean costs no digits.
+// The backward pass makes both again rather than read what the forward pass would have to keep.
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "dfx_step.h"
+
+namespace {
+
+constexpr uint32_t kNormDim = 32768;     // elements of a row, at most: what a workgroup of 1024 keeps in registers
+constexpr uint32_t kNormGroups = 512;    // workgroups of the backward pass, at most: each leaves its share of the sums over rows
+
+struct NormArgs {
+  const void *x, *dy, *weight, *bias;
+  void *y, *dx;
+  size_t x_stride, dy_stride, y_stride, dx_stride;
+  float* part;                           // [workgroups][2][dim]: a workgroup's share of grad_weight and grad_bias; may be null
+  uint32_t rows, dim;
+  float eps;
+  bool param_f32;
+};
+
+// N elements from element e of a row; behind its end: `beyond`
+template <int DT, int N>
+__device__ __forceinline__ void row_take(const void* row, uint32_t e, uint32_t dim, float* v, float beyond) {
+  if (e + N <= dim) {
+    if constexpr (N * (DT == DFX_F32 ? 4 : 2) == 32) {
+      StepVec<DT, N / 2> a, b;
+      a.load(row, e); b.load(row, e + N / 2);
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k) { v[k] = a.get(k); v[k + N / 2] = b.get(k); }
+    } else {
+      StepVec<DT, N> a;
+      a.load(row, e);
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = a.get(k);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = e + k < dim ? step_get<DT>(row, e + k) : beyond;
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void row_put(void* row, uint32_t e, uint32_t dim, const float* v) {
+  if (e + N <= dim) {
+    StepVec<DT, N> a;
+    a.put(v);
+    *(STEP_GLOBAL typename StepVec<DT, N>::words*)((STEP_GLOBAL typename StepElem<DT>::raw*)row + e) = a.w;
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (e + k < dim) step_put<DT>(row, e + k, v[k]);
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void param_take(const void* p, bool f32, uint32_t e, uint32_t dim, float* v, float absent) {
+  if (!p) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = absent;
+  } else if (f32) row_take<DFX_F32, N>(p, e, dim, v, 0.0f);
+  else row_take<DT, N>(p, e, dim, v, 0.0f);
+}
+
+template <int DT>
+__device__ __forceinline__ const void* row_of(const void* p, size_t stride, uint32_t row) { return (const typename StepElem<DT>::raw*)p + (size_t)row * stride; }
+template <int DT>
+__device__ __forceinline__ void* row_of(void* p, size_t stride, uint32_t row) { return (typename StepElem<DT>::raw*)p + (size_t)row * stride; }
+
+// Sums over the T threads of a row, for all of them.  T > 64: through lds, two of whose halves are used in turn, one barrier each.
+template <int T, int THREADS, int NUM>
+__device__ __forceinline__ void row_sum(float (&s)[NUM], float (*lds)[2][THREADS / kStepWave], uint32_t& turn) {
+#pragma unroll
+  for (int d = kStepWave / 2; d; d >>= 1)
+#pragma unroll
+    for (int q = 0; q < NUM; ++q) s[q] += __shfl_xor(s[q], d);
+  if constexpr (T > kStepWave) {
+    constexpr int W = T / kStepWave;
+    const uint32_t wave = threadIdx.x / kStepWave;
+    if (threadIdx.x % kStepWave == 0)
+#pragma unroll
+      for (int q = 0; q < NUM; ++q) lds[turn][q][wave] = s[q];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NUM; ++q) {
+      s[q] = lds[turn][q][wave / W * W];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s[q] += lds[turn][q][wave / W * W + w];
+    }
+    turn ^= 1u;
+  }
+}
+
+// T threads to a row, U vectors a thread, THREADS / T rows of a workgroup at once.
+template <int DT, int T, int U>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_kernel(NormArgs a) {
+  constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  __shared__ float lds[2][2][THREADS / kStepWave];
+  const uint32_t me = threadIdx.x % T, row = blockIdx.x * ROWS + threadIdx.x / T;
+  uint32_t turn = 0;
+  if (ROWS > 1 && row >= a.rows) return;  // (T is a wave or more of one: nobody waits for it)
+  const void* x = row_of<DT>(a.x, a.x_stride, row);
+  float v[U][N], s[1] = {0.0f};
+#pragma unroll
+  for (int u = 0; u < U; ++u) row_take<DT, N>(x, (u * T + me) * N, a.dim, v[u], 0.0f);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[0] += v[u][k];
+  row_sum<T, THREADS, 1>(s, lds, turn);
+  const float mean = s[0] / (float)a.dim;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[u][k] = (u * T + me) * N + k < a.dim ? v[u][k] - mean : 0.0f;
+      s[0] = fmaf(v[u][k], v[u][k], s[0]);
+    }
+  row_sum<T, THREADS, 1>(s, lds, turn);
+  const float r = 1.0f / sqrtf(s[0] / (float)a.dim + a.eps);
+  void* y = row_of<DT>(a.y, a.y_stride, row);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t e = (u * T + me) * N;
+    if (e >= a.dim) break;
+    float w[N], b[N];
+    param_take<DT, N>(a.weight, a.param_f32, e, a.dim, w, 1.0f);
+    param_take<DT, N>(a.bias, a.param_f32, e, a.dim, b, 0.0f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[u][k] = fmaf(v[u][k] * r, w[k], b[k]);
+    row_put<DT, N>(y, e, a.dim, v[u]);
+  }
+}
+
+// The same for the gradients.  A thread's columns are the same in every row, so that the sums over rows stay in its registers.
+template <int DT, int T, int U>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_grad_kernel(NormArgs a) {
+  constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  __shared__ float lds[2][2][THREADS / kStepWave];
+  const uint32_t me = threadIdx.x % T, sub = threadIdx.x / T;
+  uint32_t turn = 0;
+  float dw[U][N], db[U][N];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < N; ++k) dw[u][k] = db[u][k] = 0.0f;
+  for (uint32_t row0 = blockIdx.x * ROWS; row0 < a.rows; row0 += gridDim.x * ROWS) {
+    const uint32_t row = row0 + sub;
+    if (ROWS > 1 && row >= a.rows) break;  // (a wave or more of one)
+    const void *x = row_of<DT>(a.x, a.x_stride, row), *dy = row_of<DT>(a.dy, a.dy_stride, row);
+    float v[U][N], g[U][N], s[1] = {0.0f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) row_take<DT, N>(x, (u * T + me) * N, a.dim, v[u], 0.0f);
+#pragma unroll
+    for (int u = 0; u < U; ++u) row_take<DT, N>(dy, (u * T + me) * N, a.dim, g[u], 0.0f);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < N; ++k) s[0] += v[u][k];
+    row_sum<T, THREADS, 1>(s, lds, turn);
+    const float mean = s[0] / (float)a.dim;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        v[u][k] = (u * T + me) * N + k < a.dim ? v[u][k] - mean : 0.0f;
+        s[0] = fmaf(v[u][k], v[u][k], s[0]);
+      }
+    row_sum<T, THREADS, 1>(s, lds, turn);
+    const float r = 1.0f / sqrtf(s[0] / (float)a.dim + a.eps);
+    float c[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t e = (u * T + me) * N;
+      float w[N];
+      if (e < a.dim) param_take<DT, N>(a.weight, a.param_f32, e, a.dim, w, 1.0f);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        v[u][k] *= r;
+        dw[u][k] = fmaf(g[u][k], v[u][k], dw[u][k]);
+        db[u][k] += g[u][k];
+        if (e < a.dim) g[u][k] *= w[k];
+        c[0] += g[u][k];
+        c[1] = fmaf(g[u][k], v[u][k], c[1]);
+      }
+    }
+    if (!a.dx) continue;                 // (all alike)
+    row_sum<T, THREADS, 2>(c, lds, turn);
+    c[0] /= (float)a.dim; c[1] /= (float)a.dim;
+    void* dx = row_of<DT>(a.dx, a.dx_stride, row);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t e = (u * T + me) * N;
+      if (e >= a.dim) break;
+#pragma unroll
+      for (int k = 0; k < N; ++k) g[u][k] = r * (g[u][k] - c[0] - v[u][k] * c[1]);
+      row_put<DT, N>(dx, e, a.dim, g[u]);
+    }
+  }
+  if (!a.part) return;
+  // the rows of a workgroup at once: one behind the other through LDS
+  float* part = a.part + (size_t)blockIdx.x * 2u * a.dim;
+  if constexpr (ROWS > 1) {
+    __shared__ float sums[2][T * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      for (uint32_t q = 1; q < ROWS; ++q) {
+        __syncthreads();
+        if (sub == q)
+#pragma unroll
+          for (int k = 0; k < N; ++k) { sums[0][k * T + me] = dw[u][k]; sums[1][k * T + me] = db[u][k]; }
+        __syncthreads();
+        if (sub == 0)
+#pragma unroll
+          for (int k = 0; k < N; ++k) { dw[u][k] += sums[0][k * T + me]; db[u][k] += sums[1][k * T + me]; }
+      }
+    }
+    if (sub) return;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t e = (u * T + me) * N;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (e + k < a.dim) { part[e + k] = dw[u][k]; part[a.dim + e + k] = db[u][k]; }
+  }
+}
+
+// The workgroups' shares of a column, in their order: 32 columns of a workgroup, 8 threads to each.
+template <int OUT>
+__global__ void __launch_bounds__(256) dfx_norm_sums_kernel(const float* part, uint32_t groups, uint32_t dim, void* grad_weight, void* grad_bias, bool accumulate) {
+  __shared__ float lds[8][32];
+  const uint32_t i = threadIdx.x % 32u, slice = threadIdx.x / 32u, col = blockIdx.x * 32u + i;
+  const bool bias = blockIdx.y != 0;
+  void* to = bias ? grad_bias : grad_weight;
+  if (!to) return;
+  float s = 0.0f;
+  if (col < dim) {
+    const float* p = part + (bias ? dim : 0u) + col;
+    const uint32_t each = (groups + 7u) / 8u, end = min((slice + 1u) * each, groups);
+#pragma unroll 8
+    for (uint32_t g = slice * each; g < end; ++g) s += p[(size_t)g * 2u * dim];
+  }
+  lds[slice][i] = s;
+  __syncthreads();
+  if (slice || col >= dim) return;
+  for (int k = 1; k < 8; ++k) s += lds[k][i];
+  if (accumulate) s += step_get<OUT>(to, col);
+  step_put<OUT>(to, col, s);
+}
+
+uint32_t norm_groups(size_t rows) { return (uint32_t)std::min<size_t>(rows, kNormGroups); }
+
+template <int DT>
+int norm_launch(const NormArgs& a, hipStream_t s) {
+  constexpr uint32_t N = 16 / (DT == DFX_F32 ? 4 : 2);
+  const uint32_t nvec = (a.dim + N - 1) / N;
+#define NORM(T, U) return step_launch(dfx_norm_kernel<DT, T, U>, dim3((a.rows + (T < 256 ? 256 / T : 1) - 1) / (T < 256 ? 256 / T : 1)), T < 256 ? 256 : T, s, a)
+  if (nvec <= 64) NORM(64, 1);
+  if (nvec <= 128) NORM(64, 2);
+  if (nvec <= 256) NORM(256, 1);
+  if (nvec <= 512) NORM(256, 2);
+  if (nvec <= 1024) NORM(256, 4);
+  if (nvec <= 2048) NORM(1024, 2);
+  if constexpr (DT == DFX_F32)
+    if (nvec > 4096) NORM(1024, 8);
+  NORM(1024, 4);
+#undef NORM
+}
+
+template <int DT>
+int norm_grad_launch(const NormArgs& a, uint32_t groups, hipStream_t s) {
+  constexpr uint32_t N = 16 / (DT == DFX_F32 ? 4 : 2);
+  const uint32_t nvec = (a.dim + N - 1) / N;
+#define NORM(T, U) return step_launch(dfx_norm_grad_kernel<DT, T, U>, dim3(groups), T < 256 ? 256 : T, s, a)
+  if (nvec <= 64) NORM(64, 1);
+  if (nvec <= 128) NORM(64, 2);
+  if (nvec <= 256) NORM(256, 1);
+  if (nvec <= 512) NORM(256, 2);
+  if (nvec <= 1024) NORM(256, 4);
+  if (nvec <= 2048) NORM(1024, 2);
+  if constexpr (DT == DFX_F32)
+    if (nvec > 4096) NORM(1024, 8);
+  NORM(1024, 4);
+#undef NORM
+}
+
+constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
+
+bool norm_types(int dtype, int other) { return (dtype == DFX_F32 || dtype == DFX_BF16 || dtype == DFX_F16) && (other == dtype || other == DFX_F32); }
+
+// two matrices of rows: apart, or the same memory with the same stride
+bool rows_lie_well(const void* a, size_t as, const void* b, size_t bs, size_t rows, size_t dim, size_t eb, bool in_place) {
+  if (!rows || !a || !b || (in_place && a == b && as == bs)) return true;
+  return !meet(flat(a, ((rows - 1) * as + dim) * eb), flat(b, ((rows - 1) * bs + dim) * eb));
+}
+
+}  // namespace
+
+extern "C" {
+
+int dfx_layer_norm(const dfx_layer_norm_args* u, void* hip_stream) {
+  if (!u || u->struct_bytes != sizeof(*u) || u->reserved0 || !norm_types(u->dtype, u->param_dtype)) return DFX_ERR_INVALID_ARG;
+  if (u->rows >= kMostRows || u->dim > kNormDim || u->x_stride >= kMostStride || u->y_stride >= kMostStride) return DFX_ERR_TOO_LARGE;
+  const size_t eb = step_elem_bytes(u->dtype), pb = step_elem_bytes(u->param_dtype), xs = u->x_stride ? u->x_stride : u->dim, ys = u->y_stride ? u->y_stride : u->dim;
+  if (!u->dim || xs < u->dim || ys < u->dim || !(u->eps >= 0.0) || !step_normal(u->eps)) return DFX_ERR_INVALID_ARG;
+  if ((u->rows && (!u->x || !u->y)) || (uintptr_t)u->x % eb || (uintptr_t)u->y % eb || (uintptr_t)u->weight % pb || (uintptr_t)u->bias % pb) return DFX_ERR_INVALID_ARG;
+  if (!u->rows) return DFX_OK;
+  if (!rows_lie_well(u->x, xs, u->y, ys, u->rows, u->dim, eb, true)) return DFX_ERR_INVALID_ARG;
+  const Span y = {(uintptr_t)u->y, u->rows, u->dim * eb, ys * eb};
+  if (meet(flat(u->weight, u->dim * pb), y) || meet(flat(u->bias, u->dim * pb), y)) return DFX_ERR_INVALID_ARG;
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = u->x; a.weight = u->weight; a.bias = u->bias; a.y = u->y; a.x_stride = xs; a.y_stride = ys;
+  a.rows = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.eps = (float)u->eps; a.param_f32 = u->param_dtype == DFX_F32;
+  hipStream_t s = (hipStream_t)hip_stream;
+  return u->dtype == DFX_F32 ? norm_launch<DFX_F32>(a, s) : u->dtype == DFX_BF16 ? norm_launch<DFX_BF16>(a, s) : norm_launch<DFX_F16>(a, s);
+}
+
+size_t dfx_layer_norm_grad_workspace(size_t rows, size_t dim, dfx_dtype dtype) {
+  (void)dtype;
+  if (rows >= kMostRows || dim > kNormDim) return 0;
+  return std::max<size_t>(16, (size_t)norm_groups(rows) * 2 * dim * sizeof(float));
+}
+
+int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* u, void* hip_stream) {
+  if (!u || u->struct_bytes != sizeof(*u) || u->reserved0 || !norm_types(u->dtype, u->param_dtype) || !norm_types(u->dtype, u->grad_dtype)) return DFX_ERR_INVALID_ARG;
+  if (u->rows >= kMostRows || u->dim > kNormDim || u->x_stride >= kMostStride || u->dy_stride >= kMostStride || u->dx_stride >= kMostStride) return DFX_ERR_TOO_LARGE;
+  const size_t eb = step_elem_bytes(u->dtype), pb = step_elem_bytes(u->param_dtype), gb = step_elem_bytes(u->grad_dtype);
+  const size_t xs = u->x_stride ? u->x_stride : u->dim, dys = u->dy_stride ? u->dy_stride : u->dim, dxs = u->dx_stride ? u->dx_stride : u->dim;
+  if (!u->dim || xs < u->dim || dys < u->dim || dxs < u->dim || !(u->eps >= 0.0) || !step_normal(u->eps)) return DFX_ERR_INVALID_ARG;
+  if ((u->rows && (!u->x || !u->dy)) || (uintptr_t)u->x % eb || (uintptr_t)u->dy % eb || (uintptr_t)u->dx % eb || (uintptr_t)u->weight % pb ||
+      (uintptr_t)u->grad_weight % gb || (uintptr_t)u->grad_bias % gb)
+    return DFX_ERR_INVALID_ARG;
+  const bool sums = u->grad_weight || u->grad_bias;
+  const size_t need = dfx_layer_norm_grad_workspace(u->rows, u->dim, u->dtype);
+  if (sums && (!u->workspace || (uintptr_t)u->workspace % 16 || u->workspace_bytes < need)) return DFX_ERR_INVALID_ARG;
+  if (!rows_lie_well(u->x, xs, u->dx, dxs, u->rows, u->dim, eb, true) || !rows_lie_well(u->dy, dys, u->dx, dxs, u->rows, u->dim, eb, true)) return DFX_ERR_INVALID_ARG;
+  const size_t rows = u->rows;
+  const Span x = {(uintptr_t)u->x, rows, u->dim * eb, xs * eb}, dy = {(uintptr_t)u->dy, rows, u->dim * eb, dys * eb}, dx = {(uintptr_t)u->dx, u->dx ? rows : 0, u->dim * eb, dxs * eb};
+  const Span w = flat(u->weight, u->dim * pb), writes[] = {flat(u->grad_weight, u->dim * gb), flat(u->grad_bias, u->dim * gb), flat(sums ? u->workspace : nullptr, need)};
+  if (meet(w, dx)) return DFX_ERR_INVALID_ARG;
+  for (int k = 0; k < 3; ++k) {
+    if (meet(writes[k], x) || meet(writes[k], dy) || meet(writes[k], dx) || meet(writes[k], w)) return DFX_ERR_INVALID_ARG;
+    for (int j = 0; j < k; ++j)
+      if (meet(writes[k], writes[j])) return DFX_ERR_INVALID_ARG;
+  }
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = u->x; a.dy = u->dy; a.weight = u->weight; a.dx = u->dx; a.x_stride = xs; a.dy_stride = dys; a.dx_stride = dxs;
+  a.part = sums ? (float*)u->workspace : nullptr;
+  a.rows = (uint32_t)rows; a.dim = (uint32_t)u->dim; a.eps = (float)u->eps; a.param_f32 = u->param_dtype == DFX_F32;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const uint32_t groups = norm_groups(rows);
+  if (groups && (sums || u->dx)) {
+    const int rc = u->dtype == DFX_F32 ? norm_grad_launch<DFX_F32>(a, groups, s) : u->dtype == DFX_BF16 ? norm_grad_launch<DFX_BF16>(a, groups, s) : norm_grad_launch<DFX_F16>(a, groups, s);
+    if (rc != DFX_OK) return rc;
+  }
+  if (!sums) return DFX_OK;
+  const dim3 grid((a.dim + 31u) / 32u, 2);
+  auto k = u->grad_dtype == DFX_F32 ? dfx_norm_sums_kernel<DFX_F32> : u->grad_dtype == DFX_BF16 ? dfx_norm_sums_kernel<DFX_BF16> : dfx_norm_sums_kernel<DFX_F16>;
+  return step_launch(k, grid, 256, s, (const float*)a.part, groups, a.dim, u->grad_weight, u->grad_bias, u->accumulate != 0);
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-// What the operators of the training step around the collectives share (dfx_lists.hip, dfx_loss.hip): 16-bit and 32-bit elements read
+// What the operators of the training step around the collectives share (dfx_lists.hip, dfx_loss.hip, dfx_embed.hip, dfx_norm.hip, dfx_vocab.hip): 16-bit and 32-bit elements read
 // into 32 bits and rounded back once, sums over a workgroup.
 #ifndef DFX_STEP_H
 #define DFX_STEP_H
@@ -9,6 +9,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <tuple>
 
 #include "../../include/dfx.h"
@@ -108,6 +109,19 @@ struct StepVec {
     }
   }
 };
+
+// n pieces of so many bytes, step bytes from one to the next; nothing: n = 0
+struct Span { uintptr_t at; size_t n, bytes, step; };
+inline Span flat(const void* p, size_t bytes) { return {(uintptr_t)p, p && bytes ? (size_t)1 : 0, bytes, bytes}; }
+
+// whether a span of one piece shares a byte with another: with the last piece that begins at or before it, or the one behind that
+inline bool meet(const Span& one, const Span& s) {
+  if (!one.n || !s.n) return false;
+  const uintptr_t lo = one.at, hi = lo + one.bytes;
+  const size_t k = lo <= s.at ? 0 : std::min<size_t>((lo - s.at) / s.step, s.n - 1);
+  const uintptr_t p = s.at + k * s.step;
+  return (lo < p + s.bytes && p < hi) || (k + 1 < s.n && p + s.step < hi);
+}
 
 // One kernel on a stream; the launch's own outcome, whatever error an earlier call of the caller's has left behind.
 template <class... P, class... A>

@@ -1,0 +1,570 @@
+// Softmax cross entropy over a vocabulary whose logits are never kept, and its gradients: the head of a language model and the loss in one.
+//
+// With z = hidden weight^T and, for a row, m its largest logit and S = sum exp(c (z - m)):  logp = c (z_t - m) - log S.  Tiles of z are made on the matrix
+// cores and reduced to (m, S) of each row where they lie; a second kernel joins the tiles' parts.  For the gradients a piece of the vocabulary at
+// a time is made again, turned into dz = softmax - [target], and goes as the operand into dX += dz W and dW = dz^T X.
+//
+// Rows that have nothing to learn from are left out first: the others' hidden states are laid one behind the other (and padded to whole steps of
+// the products), so that masked rows cost nothing.
+//
+// dz is held relative to the largest weight of a row and times 2^15, which is at most 2^15 in size: in f16 a probability keeps its digits down to 2e-9
+// instead of 6e-5.  What is left out comes back as one factor in 32 bits behind the products.
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "dfx_gemm.h"
+
+namespace {
+
+constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.44269504088896340736;
+constexpr float kDzScale = 32768.0f;
+constexpr uint32_t kRowsThreads = 1024;
+constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
+constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles
+constexpr size_t kPieceElems = 64ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
+
+// what is known of a call on the device; first in the workspace
+struct VocabState { uint32_t count; float g; };       // rows that count; scale * largest weight * c / 2^15
+
+struct VocabRow { float m, f, w; int32_t t; };        // largest logit, w / S, weight (relative, times 2^15), target
+
+struct VocabArgs {
+  const int64_t* targets;
+  const float *row_weight, *scale;
+  float *logp, *loss, *sums;
+  VocabState* state;
+  int32_t *idx, *target, *map;           // [Rp] rows that count, their targets (-1 behind them); [rows] where a row went, or -1
+  float *weight, *zt, *row_loss, *row_w; // [Rp]
+  float* top_weight;                     // largest |weight|
+  VocabRow* row;                         // [Rp]
+  float2* parts;                         // [tiles of the vocabulary][Rp]: (m, S) of a tile's part of a row
+  uint32_t rows, rp, vocab, tiles;
+  double c;
+  float k;                               // c / log 2
+};
+
+__device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
+__device__ __forceinline__ float vocab_exp(float z, float base, float k) { return __builtin_amdgcn_exp2f((z - base) * k); }
+
+// The rows that count, in their order, by one workgroup; logp and loss of the others.
+__global__ void __launch_bounds__(kRowsThreads) dfx_vocab_rows_kernel(VocabArgs a) {
+  constexpr uint32_t W = kRowsThreads / kStepWave;
+  __shared__ uint32_t counts[2][W];
+  __shared__ float tops[W];
+  const uint32_t me = threadIdx.x, wave = me / kStepWave, lane = me % kStepWave;
+  uint32_t done = 0, turn = 0;
+  float top = 0.0f;
+  for (uint32_t first = 0; first < a.rows; first += kRowsThreads, turn ^= 1u) {
+    const uint32_t i = first + me;
+    const int64_t t = i < a.rows ? a.targets[i] : -1;
+    const float w = i < a.rows && a.row_weight ? a.row_weight[i] : 1.0f;
+    const bool counts_here = t >= 0 && t < (int64_t)a.vocab && w != 0.0f;
+    const uint64_t mask = __ballot(counts_here);
+    if (lane == 0) counts[turn][wave] = (uint32_t)__popcll(mask);
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (uint32_t k = 0; k < W; ++k) {
+      before += k < wave ? counts[turn][k] : 0u;
+      all += counts[turn][k];
+    }
+    const uint32_t place = done + before + (uint32_t)__popcll(mask & ((1ull << lane) - 1ull));
+    if (i < a.rows) {
+      a.map[i] = counts_here ? (int32_t)place : -1;
+      if (counts_here) {
+        a.idx[place] = (int32_t)i; a.target[place] = (int32_t)t; a.weight[place] = w;
+        top = fmaxf(top, fabsf(w));
+      } else {
+        if (a.logp) a.logp[i] = 0.0f;
+        if (a.loss) a.loss[i] = 0.0f;
+      }
+    }
+    done += all;
+  }
+  for (uint32_t i = done + me; i < a.rp; i += kRowsThreads) {
+    a.idx[i] = -1; a.target[i] = -1; a.weight[i] = 0.0f;
+  }
+  top = __uint_as_float(wave_max(__float_as_uint(top)));      // (none is negative)
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  if (me == 0) {
+    for (uint32_t k = 1; k < W; ++k) top = fmaxf(top, tops[k]);
+    top = fmaxf(top, tops[0]);
+    a.state->count = done;
+    a.state->g = done ? (float)((a.scale ? (double)a.scale[0] : 1.0) * (double)top * a.c / (double)kDzScale) : 0.0f;
+    *a.top_weight = top;
+  }
+}
+
+// Rows of a matrix for the products: padded with zeros to whole steps, 32 bits cut into planes; idx: which rows (-1: zeros), or null: row for row.
+template <int DT>
+__global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, size_t stride, const int32_t* idx, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
+  const uint32_t r = blockIdx.x;
+  const int64_t from = idx ? (int64_t)idx[r] : (int64_t)r;
+  const unsigned char* row = (const unsigned char*)src + (from < 0 ? 0 : (size_t)from) * stride * step_elem_bytes(DT);
+  uint16_t* to = dst + (size_t)r * padded;
+  for (uint32_t e = threadIdx.x * 8u; e < padded; e += 256u * 8u) {
+    if constexpr (DT == DFX_F32) {
+      uint16_t part[3][8];
+      for (int j = 0; j < 8; ++j) {
+        uint16_t p[3] = {0, 0, 0};
+        if (from >= 0 && e + j < dim) gemm_cut(step_get<DT>(row, e + j), p);
+        for (int q = 0; q < 3; ++q) part[q][j] = p[q];
+      }
+      for (int q = 0; q < 3; ++q) {
+        uint4 v;
+        memcpy(&v, part[q], 16);
+        *(uint4*)(to + q * plane + e) = v;
+      }
+    } else {
+      StepVec<DT, 8> v;
+      v.w = 0;
+      if (from >= 0) {
+        if (e + 8u <= dim) v.load(row, e);
+        else {
+          uint16_t x[8];
+          for (int j = 0; j < 8; ++j) x[j] = e + j < dim ? *((const STEP_GLOBAL uint16_t*)row + e + j) : (uint16_t)0;
+          memcpy(&v.w, x, 16);
+        }
+      }
+      *(uint4*)(to + e) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+    }
+  }
+}
+
+// A tile's part of each row: (m, S), and the target's logit where it lies here.
+struct VocabStats {
+  float2* parts;
+  float* zt;
+  const int32_t* target;
+  uint32_t rp, left, v0, tile0;          // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile
+  float k;
+  template <class TILE>
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
+    const uint32_t lane = threadIdx.x % kStepWave, wave = threadIdx.x / kStepWave;
+    if (tile.m0 + TILE::M > left) {
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (tile.m(i) + e >= left)
+#pragma unroll
+            for (int j = 0; j < TILE::NT; ++j) acc[i][j][e] = -INFINITY;
+    }
+    float2* part = (float2*)lds;         // [WM][N]
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) {
+      const uint32_t n = tile.n(j), t = (uint32_t)target[n] - v0;      // (none: far beyond)
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float base = vocab_base(top);
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s += vocab_exp(acc[i][j][e], base, k);
+          if (tile.m(i) + e == t && t < left) zt[n] = acc[i][j][e];
+        }
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      if (lane < 16) part[wave / TILE::WN * TILE::N + (n - tile.n0)] = make_float2(top, s);
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < TILE::N; i += TILE::THREADS) {
+      float2 p[TILE::WM];
+      float top = -INFINITY, s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < TILE::WM; ++w) {
+        p[w] = part[w * TILE::N + i];
+        top = fmaxf(top, p[w].x);
+      }
+#pragma unroll
+      for (int w = 0; w < TILE::WM; ++w) s += p[w].y * vocab_exp(p[w].x, vocab_base(top), k);
+      parts[(size_t)(tile0 + at.m) * rp + tile.n0 + i] = make_float2(top, s);
+    }
+  }
+};
+
+// The tiles' parts of a row joined, and what it comes to.  Eight threads to a row.
+__global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
+  __shared__ float2 lds[8][32];
+  const uint32_t i = threadIdx.x % 32u, slice = threadIdx.x / 32u, n = blockIdx.x * 32u + i, count = a.state->count;
+  float top = -INFINITY, s = 0.0f;
+  if (n < count)
+    for (uint32_t t = slice; t < a.tiles; t += 32u) {
+      float2 p[4];
+#pragma unroll
+      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * 8u < a.tiles ? a.parts[(size_t)(t + u * 8u) * a.rp + n] : make_float2(-INFINITY, 0.0f);
+      float more = top;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) more = fmaxf(more, p[u].x);
+      const float base = vocab_base(more);
+      s *= vocab_exp(top, base, a.k);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s += p[u].y * vocab_exp(p[u].x, base, a.k);
+      top = more;
+    }
+  lds[slice][i] = make_float2(top, s);
+  __syncthreads();
+  if (slice) return;
+  for (int k = 1; k < 8; ++k) top = fmaxf(top, lds[k][i].x);
+  const float base = vocab_base(top);
+  s = 0.0f;
+  for (int k = 0; k < 8; ++k) s += lds[k][i].y * vocab_exp(lds[k][i].x, base, a.k);
+  VocabRow r = {0.0f, 0.0f, 0.0f, -1};
+  float logp = 0.0f, loss = 0.0f, w = 0.0f;
+  if (n < count && s != 0.0f) {          // (0: no logit above -infinity)
+    int two;
+    const float f = frexpf(s, &two);
+    w = a.weight[n];
+    logp = (float)(a.c * ((double)a.zt[n] - (double)base) - ((double)two + (double)__builtin_amdgcn_logf(f)) * kVLog2);
+    loss = -w * logp;
+    const float relative = w / *a.top_weight * kDzScale;
+    r = {base, relative / s, relative, a.target[n]};
+  }
+  if (n >= a.rp) return;
+  a.row[n] = r;
+  a.row_loss[n] = loss;
+  a.row_w[n] = w;
+  if (n < count) {
+    if (a.logp) a.logp[a.idx[n]] = logp;
+    if (a.loss) a.loss[a.idx[n]] = loss;
+  }
+}
+
+// sums over the rows, in an order that is always the same
+__global__ void __launch_bounds__(256) dfx_vocab_sums_kernel(VocabArgs a) {
+  __shared__ double lds[2][4];
+  double s = 0.0, w = 0.0;
+  for (uint32_t i = threadIdx.x, n = a.state->count; i < n; i += 256u) {
+    s += (double)a.row_loss[i];
+    w += (double)a.row_w[i];
+  }
+  s = wave_sum(s); w = wave_sum(w);
+  if (threadIdx.x % kStepWave == 0) {
+    lds[0][threadIdx.x / kStepWave] = s;
+    lds[1][threadIdx.x / kStepWave] = w;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) a.sums[threadIdx.x] = (float)(lds[threadIdx.x][0] + lds[threadIdx.x][1] + lds[threadIdx.x][2] + lds[threadIdx.x][3]);
+}
+
+// dz of a tile, to the type of the products
+template <int DT>
+struct VocabDz {
+  const VocabRow* row;
+  uint16_t* dz;                          // [Rp][pitch], planes of them
+  size_t plane;
+  uint32_t pitch, left, v0;
+  float k;
+  template <class TILE>
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) {
+      const uint32_t n = tile.n(j);
+      const VocabRow r = row[n];
+      const uint32_t t = (uint32_t)r.t - v0;
+      uint16_t* to = dz + (size_t)n * pitch;
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i) {
+        const uint32_t m = tile.m(i);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = r.f * vocab_exp(acc[i][j][e], r.m, k);
+          if (m + e == t) v[e] -= r.w;
+          if (m + e >= left) v[e] = 0.0f;
+        }
+        if constexpr (DT == DFX_F32) {
+          uint16_t p[4][3];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) gemm_cut(v[e], p[e]);
+#pragma unroll
+          for (int q = 0; q < 3; ++q) *(uint2*)(to + q * plane + m) = make_uint2(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16);
+        } else {
+          StepVec<DT, 4> o;
+          o.put(v);
+          *(uint2*)(to + m) = make_uint2(o.w[0], o.w[1]);
+        }
+      }
+    }
+  }
+};
+
+// a part of dX, in 32 bits: [splits][rows][pitch]
+struct VocabDx {
+  float* part;
+  uint32_t rows, pitch;
+  bool more;                             // not the first piece
+  template <class TILE>
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) {
+      float* to = part + ((size_t)at.split * rows + tile.n(j)) * pitch;
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i) {
+        const uint32_t m = tile.m(i);
+        if (m >= pitch) continue;
+        GemmAcc* p = (GemmAcc*)(to + m);
+        *p = more ? *p + acc[i][j] : acc[i][j];
+      }
+    }
+  }
+};
+
+// rows of dW
+template <int OUT>
+struct VocabDw {
+  void* grad;
+  size_t stride;
+  const VocabState* state;
+  uint32_t dim, left;                    // elements of a row; rows from grad's first on
+  bool accumulate;
+  template <class TILE>
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
+    const float g = state->g;
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) {
+      const uint32_t n = tile.n(j);
+      if (n >= left) continue;
+      typedef typename StepElem<OUT>::raw raw;
+      raw* to = (raw*)grad + (size_t)n * stride;
+#pragma unroll
+      for (int i = 0; i < TILE::MT; ++i) {
+        const uint32_t m = tile.m(i);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = g * acc[i][j][e];
+        if (m + 4 <= dim) {
+          StepVec<OUT, 4> o;
+          if (accumulate) {
+            o.load(to, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o.get(e);
+          }
+          o.put(v);
+          *(STEP_GLOBAL typename StepVec<OUT, 4>::words*)((STEP_GLOBAL raw*)to + m) = o.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + e < dim) step_put<OUT>(to, m + e, accumulate ? v[e] + step_get<OUT>(to, m + e) : v[e]);
+        }
+      }
+    }
+  }
+};
+
+// dX: the splits' parts, in their order; rows that do not count are 0
+template <int DT>
+__global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const float* part, uint32_t splits, uint32_t split_rows, uint32_t pitch, void* grad, size_t stride, uint32_t dim) {
+  const uint32_t row = blockIdx.x;
+  const int32_t n = a.map[row];
+  const float g = a.state->g;
+  typedef typename StepElem<DT>::raw raw;
+  raw* to = (raw*)grad + (size_t)row * stride;
+  for (uint32_t e = threadIdx.x * 4u; e < dim; e += 256u * 4u) {
+    float v[4] = {0, 0, 0, 0};
+    if (n >= 0) {
+      GemmAcc sum = *(const GemmAcc*)(part + (size_t)n * pitch + e);
+      for (uint32_t s = 1; s < splits; ++s) sum += *(const GemmAcc*)(part + ((size_t)s * split_rows + n) * pitch + e);
+      for (int q = 0; q < 4; ++q) v[q] = g * sum[q];
+    }
+    if (e + 4u <= dim) {
+      StepVec<DT, 4> o;
+      o.put(v);
+      *(STEP_GLOBAL typename StepVec<DT, 4>::words*)((STEP_GLOBAL raw*)to + e) = o.w;
+    } else {
+      for (int q = 0; q < 4; ++q)
+        if (e + q < dim) step_put<DT>(to, e + q, v[q]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// how a call is laid out
+// ------------------------------------------------------------------------------------------
+size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
+
+struct VocabPlan {
+  size_t rp, dp, dq, vp, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, tiles of the vocabulary, splits of dX and a split's rows
+  bool flat;
+  size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, dx, bytes;      // places in the workspace
+};
+
+// Splits of dX along the vocabulary: as many workgroups as compute units.  What depends on the number of rows has room for any smaller number.
+VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad, size_t piece) {
+  VocabPlan p;
+  const size_t planes = gemm_planes(dtype);
+  p.flat = rows <= kFewRows;
+  p.rp = std::max(kTileRows, up(rows, kTileRows));
+  p.dp = up(dim, kGemmK);
+  p.dq = up(dim, 4);
+  p.tiles = (vocab + kTileRows - 1) / kTileRows;
+  const size_t whole = std::max(kTileRows, p.tiles * kTileRows);
+  size_t most = std::min(whole, piece ? piece : kPieceMost), dz_rows = p.rp * most;
+  p.vp = most;
+  if (!piece) {                          // pieces of equal length
+    const size_t length = std::min(most, std::max(kPieceLeast, kPieceElems / p.rp / kTileRows * kTileRows)), pieces = (whole + length - 1) / length;
+    p.vp = up((whole + pieces - 1) / pieces, kTileRows);
+    dz_rows = std::min(dz_rows, std::max(kPieceElems, p.rp * kPieceLeast));
+  }
+  const size_t tile = p.flat ? 64 : 256, across = up(std::max<size_t>(rows, 1), tile) / tile, along = up(dim, 256) / 256;
+  p.splits = std::max<size_t>(1, std::min(256 / (across * along), p.vp / 256));
+  p.split_rows = across * tile;
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
+  p.state = take(sizeof(VocabState) + 4);
+  p.idx = take(4 * p.rp); p.target = take(4 * p.rp); p.map = take(4 * p.rp); p.weight = take(4 * p.rp); p.zt = take(4 * p.rp);
+  p.row_loss = take(4 * p.rp); p.row_w = take(4 * p.rp); p.row = take(sizeof(VocabRow) * p.rp);
+  p.parts = take(sizeof(float2) * p.rp * p.tiles);
+  p.x = take(planes * p.rp * p.dp * 2);
+  p.w = take(planes * most * p.dp * 2);
+  p.dz = grad ? take(planes * dz_rows * 2) : at;
+  p.dx = grad ? take(std::max(256 / along, across) * tile * p.dq * 4) : at;
+  p.bytes = at;
+  return p;
+}
+
+template <int DT, bool TA, bool TB, class EPI>
+int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, hipStream_t stream) {
+  s.mtiles = (uint32_t)((m + 255) / 256);
+  s.ntiles = (uint32_t)(few ? (n + 63) / 64 : (n + 255) / 256);
+  if (!s.mtiles || !s.ntiles) return DFX_OK;
+  if constexpr (!(TA && TB))
+    if (few) return step_launch(dfx_gemm_kernel<DT, GemmFlat, TA, TB, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
+  return step_launch(dfx_gemm_kernel<DT, GemmWide, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
+}
+
+#define VOCAB_TRY(call) do { const int rc_ = (call); if (rc_ != DFX_OK) return rc_; } while (0)
+
+template <int DT>
+int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stream) {
+  unsigned char* ws = (unsigned char*)u.workspace;
+  VocabArgs a;
+  memset(&a, 0, sizeof(a));
+  a.targets = u.targets; a.row_weight = u.row_weight; a.scale = u.scale; a.logp = u.logp; a.loss = u.loss; a.sums = u.sums;
+  a.state = (VocabState*)(ws + p.state); a.top_weight = (float*)(a.state + 1);
+  a.idx = (int32_t*)(ws + p.idx); a.target = (int32_t*)(ws + p.target); a.map = (int32_t*)(ws + p.map); a.weight = (float*)(ws + p.weight);
+  a.zt = (float*)(ws + p.zt); a.row_loss = (float*)(ws + p.row_loss); a.row_w = (float*)(ws + p.row_w); a.row = (VocabRow*)(ws + p.row);
+  a.parts = (float2*)(ws + p.parts);
+  a.rows = (uint32_t)u.rows; a.rp = (uint32_t)p.rp; a.vocab = (uint32_t)u.vocab; a.tiles = (uint32_t)p.tiles;
+  a.c = u.inv_temperature; a.k = (float)(u.inv_temperature * kVLog2e);
+  const size_t eb = step_elem_bytes(DT), ws_stride = u.weight_stride ? u.weight_stride : u.dim;
+  const uint32_t* count = &a.state->count;
+  uint16_t *x = (uint16_t*)(ws + p.x), *w = (uint16_t*)(ws + p.w), *dz = (uint16_t*)(ws + p.dz);
+  float* dx = (float*)(ws + p.dx);
+
+  VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
+  VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, u.hidden_stride ? u.hidden_stride : u.dim, (const int32_t*)a.idx, (uint32_t)u.dim,
+                        (uint32_t)p.dp, x, p.rp * p.dp));
+  // The weight is read where it lies if its rows are whole steps at multiples of 16 bytes; otherwise a piece at a time is laid out.
+  const bool direct = DT != DFX_F32 && u.dim % kGemmK == 0 && (uintptr_t)u.weight % 16 == 0 && ws_stride * eb % 16 == 0;
+  const GemmOperand ox = {x, p.rp * p.dp, (uint32_t)p.dp, (uint32_t)p.rp, (uint32_t)p.dp};
+  const size_t pieces = (u.vocab + p.vp - 1) / p.vp;
+  GemmOperand ow = {};
+  auto take_piece = [&](size_t v0, size_t left) -> int {
+    if (direct) {
+      ow = {(const uint16_t*)u.weight + v0 * ws_stride, 0, (uint32_t)ws_stride, (uint32_t)left, (uint32_t)u.dim};
+      return DFX_OK;
+    }
+    ow = {w, p.vp * p.dp, (uint32_t)p.dp, (uint32_t)left, (uint32_t)p.dp};
+    return step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)left), 256, stream, (const void*)((const unsigned char*)u.weight + v0 * ws_stride * eb), ws_stride, (const int32_t*)nullptr,
+                       (uint32_t)u.dim, (uint32_t)p.dp, w, p.vp * p.dp);
+  };
+  const GemmShape by_rows = {0, 0, 1, (uint32_t)(p.dp / kGemmK), count, false};
+  for (size_t v0 = 0; v0 < u.vocab; v0 += direct ? u.vocab : p.vp) {
+    const size_t left = direct ? u.vocab : std::min(p.vp, u.vocab - v0);
+    VOCAB_TRY(take_piece(v0, left));
+    const VocabStats epi = {a.parts, a.zt, a.target, a.rp, (uint32_t)left, (uint32_t)v0, (uint32_t)(v0 / kTileRows), a.k};
+    VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
+  }
+  VOCAB_TRY(step_launch(dfx_vocab_join_kernel, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
+  if (u.sums) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
+  if (!u.grad_hidden && !u.grad_weight) return DFX_OK;
+  for (size_t v0 = 0; v0 < u.vocab; v0 += p.vp) {
+    const size_t left = std::min(p.vp, u.vocab - v0);
+    if (pieces > 1 || direct) VOCAB_TRY(take_piece(v0, left));
+    const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
+    VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
+    const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.rp, (uint32_t)p.vp};
+    if (u.grad_hidden) {
+      const GemmShape s = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false};
+      const VocabDx to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != 0};
+      VOCAB_TRY((vocab_gemm<DT, true, false>(p.flat, ow, oz, s, u.dim, u.rows, to, stream)));
+    }
+    if (u.grad_weight) {
+      const GemmShape s = {0, 0, 1, 0, count, true};
+      const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
+      if (u.grad_dtype == DFX_F32) {
+        const VocabDw<DFX_F32> to = {(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0};
+        VOCAB_TRY((vocab_gemm<DT, true, true>(false, ox, oz, s, u.dim, left, to, stream)));
+      } else if constexpr (DT != DFX_F32) {
+        const VocabDw<DT> to = {(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0};
+        VOCAB_TRY((vocab_gemm<DT, true, true>(false, ox, oz, s, u.dim, left, to, stream)));
+      }
+    }
+  }
+  if (u.grad_hidden && u.rows)
+    VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
+                          u.grad_hidden_stride ? u.grad_hidden_stride : u.dim, (uint32_t)u.dim));
+  return DFX_OK;
+}
+
+constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
+
+}  // namespace
+
+extern "C" {
+
+size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece) {
+  if (rows >= kMostRows || vocab >= kMostRows || dim >= kMostStride || piece % kTileRows) return 0;
+  return vocab_plan(rows, dim, vocab, dtype, grad != 0, piece).bytes;
+}
+
+int dfx_vocab_loss(const dfx_vocab_loss_args* u, void* hip_stream) {
+  if (!u || u->struct_bytes != sizeof(*u)) return DFX_ERR_INVALID_ARG;
+  if (u->dtype != DFX_F32 && u->dtype != DFX_BF16 && u->dtype != DFX_F16) return DFX_ERR_INVALID_ARG;
+  if (u->grad_dtype != u->dtype && u->grad_dtype != DFX_F32) return DFX_ERR_INVALID_ARG;
+  if (u->rows >= kMostRows || u->vocab >= kMostRows || u->dim >= kMostStride) return DFX_ERR_TOO_LARGE;
+  const size_t eb = step_elem_bytes(u->dtype), gb = step_elem_bytes(u->grad_dtype);
+  const size_t hs = u->hidden_stride ? u->hidden_stride : u->dim, ws = u->weight_stride ? u->weight_stride : u->dim;
+  const size_t ghs = u->grad_hidden_stride ? u->grad_hidden_stride : u->dim, gws = u->grad_weight_stride ? u->grad_weight_stride : u->dim;
+  for (size_t s : {hs, ws, ghs, gws}) {
+    if (s >= kMostStride) return DFX_ERR_TOO_LARGE;
+    if (s < u->dim) return DFX_ERR_INVALID_ARG;
+  }
+  if (!u->dim || u->piece % kTileRows) return DFX_ERR_INVALID_ARG;
+  if (!(u->inv_temperature * kVLog2e >= (double)FLT_MIN && u->inv_temperature * kVLog2e <= (double)FLT_MAX)) return DFX_ERR_INVALID_ARG;
+  if ((u->rows && (!u->hidden || !u->targets)) || (u->vocab && !u->weight)) return DFX_ERR_INVALID_ARG;
+  if ((uintptr_t)u->hidden % eb || (uintptr_t)u->weight % eb || (uintptr_t)u->grad_hidden % eb || (uintptr_t)u->grad_weight % gb || (uintptr_t)u->targets % 8) return DFX_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)u->row_weight, (const void*)u->scale, (const void*)u->logp, (const void*)u->loss, (const void*)u->sums})
+    if ((uintptr_t)p % 4) return DFX_ERR_INVALID_ARG;
+  const VocabPlan p = vocab_plan(u->rows, u->dim, u->vocab, u->dtype, u->grad_hidden || u->grad_weight, u->piece);
+  if (!u->workspace || (uintptr_t)u->workspace % 256 || u->workspace_bytes < p.bytes) return DFX_ERR_INVALID_ARG;
+  auto matrix = [](const void* at, size_t rows, size_t stride, size_t dim, size_t bytes) { return flat(at, rows ? ((rows - 1) * stride + dim) * bytes : 0); };
+  const Span reads[] = {matrix(u->hidden, u->rows, hs, u->dim, eb), matrix(u->weight, u->vocab, ws, u->dim, eb), flat(u->targets, 8 * u->rows), flat(u->row_weight, 4 * u->rows), flat(u->scale, 4)};
+  const Span writes[] = {flat(u->logp, 4 * u->rows), flat(u->loss, 4 * u->rows), flat(u->sums, 8), matrix(u->grad_hidden, u->rows, ghs, u->dim, eb),
+                         matrix(u->grad_weight, u->vocab, gws, u->dim, gb), flat(u->workspace, p.bytes)};
+  for (const Span& w : writes) {
+    for (const Span& r : reads)
+      if (meet(w, r)) return DFX_ERR_INVALID_ARG;
+    for (const Span* o = writes; o != &w; ++o)
+      if (meet(w, *o)) return DFX_ERR_INVALID_ARG;
+  }
+  if (u->dtype == DFX_F32) return vocab_run<DFX_F32>(*u, p, (hipStream_t)hip_stream);
+  if (u->dtype == DFX_BF16) return vocab_run<DFX_BF16>(*u, p, (hipStream_t)hip_stream);
+  return vocab_run<DFX_F16>(*u, p, (hipStream_t)hip_stream);
+}
+
+}  // extern "C"
