@@ -102,6 +102,40 @@ __device__ __forceinline__ GemmShort8 gemm_read(const unsigned char* lds, uint32
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// The same of COUNT tiles of 16 rows at once and both kk, of a turned half tile of 128: the reads and the wait for them are one block of assembly, because the compiler,
+// which does not know what of LDS a load writes, waits for every load to LDS before a transposing read.
+__device__ __forceinline__ uint32_t gemm_turned_at(const unsigned char* lds, uint32_t first) {
+  const uint32_t lane = threadIdx.x % kStepWave, l = lane % 16u, k = 8u * (lane / 16u) + l / 4u;
+  return (uint32_t)(uintptr_t)(GemmLds*)lds + k * 256u + (((first / 16u) ^ gemm_turned_swap(k)) * 32u) + (l & 3u) * 8u;
+}
+template <int COUNT>
+__device__ __forceinline__ void gemm_read_turned(const unsigned char* lds, uint32_t first, GemmShort8 (*to)[2]) {
+  GemmShort4 r[COUNT][4];
+  if constexpr (COUNT == 4)
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:1024\n\tds_read_b64_tr_b16 %2, %16 offset:8192\n\tds_read_b64_tr_b16 %3, %16 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:1024\n\tds_read_b64_tr_b16 %6, %17 offset:8192\n\tds_read_b64_tr_b16 %7, %17 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:1024\n\tds_read_b64_tr_b16 %10, %18 offset:8192\n\tds_read_b64_tr_b16 %11, %18 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:1024\n\tds_read_b64_tr_b16 %14, %19 offset:8192\n\tds_read_b64_tr_b16 %15, %19 offset:9216\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[1][2]), "=&v"(r[1][3]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[2][2]),
+          "=&v"(r[2][3]), "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(r[3][2]), "=&v"(r[3][3])
+        : "v"(gemm_turned_at(lds, first)), "v"(gemm_turned_at(lds, first + 16u)), "v"(gemm_turned_at(lds, first + 32u)), "v"(gemm_turned_at(lds, first + 48u))
+        : "memory");
+  else
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:1024\n\tds_read_b64_tr_b16 %2, %8 offset:8192\n\tds_read_b64_tr_b16 %3, %8 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:1024\n\tds_read_b64_tr_b16 %6, %9 offset:8192\n\tds_read_b64_tr_b16 %7, %9 offset:9216\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[1][2]), "=&v"(r[1][3])
+        : "v"(gemm_turned_at(lds, first)), "v"(gemm_turned_at(lds, first + 16u))
+        : "memory");
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) to[i][kk] = __builtin_shufflevector(r[i][2 * kk], r[i][2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 template <int DT>
 __device__ __forceinline__ GemmAcc gemm_mac(GemmShort8 a, GemmShort8 b, GemmAcc c) {
   if (DT == DFX_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(GemmF16x8, a), __builtin_bit_cast(GemmF16x8, b), c, 0, 0, 0);
@@ -120,8 +154,18 @@ struct GemmTile {
   __device__ __forceinline__ uint32_t n(int nt) const { return n0 + wave_n() + nt * 16 + threadIdx.x % 16; }
 };
 
-typedef GemmTile<2, 4, 8, 4> GemmWide;   // 256 m by 256 n, 512 threads
 typedef GemmTile<4, 1, 4, 4> GemmFlat;   // 256 m by 64 n, 256 threads: few rows
+
+// A tile of 256 m by 256 n by 8 waves, in halves of 128 by 128 in which each wave has 64 m by 32 n.
+struct GemmWide {
+  static constexpr int WM = 2, WN = 4, MT = 8, NT = 4, M = 256, N = 256, THREADS = 512;
+  static constexpr int HALF = 128 * kGemmK * 2, STAGE = 4 * HALF, LDS = 2 * STAGE;
+  uint32_t m0, n0;
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave / WN * 64u; }
+  __device__ __forceinline__ uint32_t wave_n() const { return threadIdx.x / kStepWave % WN * 32u; }
+  __device__ __forceinline__ uint32_t m(int mt) const { return m0 + mt / 4 * 128u + wave_m() + mt % 4 * 16u + threadIdx.x % kStepWave / 16 * 4; }
+  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt / 2 * 128u + wave_n() + nt % 2 * 16u + threadIdx.x % 16; }
+};
 
 template <int DT, class TILE, bool TA, bool TB, class EPI>
 __global__ void __launch_bounds__(TILE::THREADS) dfx_gemm_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
@@ -171,6 +215,129 @@ __global__ void __launch_bounds__(TILE::THREADS) dfx_gemm_kernel(GemmOperand a, 
 #pragma unroll
         for (int j = 0; j < TILE::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i], fb[j], acc[i][j]);
     }
+  }
+  epi(tile, at, acc, gemm_lds);
+}
+
+// A wave's waits: at most so many of its loads to LDS under way, none of its reads from LDS
+template <int LOADS>
+__device__ __forceinline__ void gemm_wait() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((LOADS & 15) | 0x70 | (LOADS >> 4) << 14);
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void gemm_meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// The wide tile.  Two waves share a SIMD, and while one of them has the matrix core the other fetches: a step is four turns, one for each quarter of a wave's
+// products, and a turn is a part that reads LDS and starts loads, and a part of 16 products; waves 4 to 7 run one part behind waves 0 to 3.  Halves of the
+// tiles are read in the order n0, m0, n1, m1, and as soon as both sets of waves have read one, the loads of the step after next may begin to overwrite it: a
+// load has seven turns to arrive, 12 younger ones of a wave under way behind it.
+template <int DT, bool TA, bool TB, class EPI>
+__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  __shared__ __align__(1024) unsigned char gemm_lds[GemmWide::LDS];
+  const GemmPlace at = gemm_place(s);
+  if (!at.any) return;
+  GemmWide tile;
+  tile.m0 = at.m * GemmWide::M; tile.n0 = at.n * GemmWide::N;
+  uint32_t steps = s.ksteps;
+  if (s.count) {
+    const uint32_t count = *s.count;
+    if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
+    else if (tile.n0 >= count) return;
+  }
+  const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
+  GemmAcc acc[GemmWide::MT][GemmWide::NT];
+#pragma unroll
+  for (int i = 0; i < GemmWide::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < GemmWide::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  const uint32_t total = (end - begin) * gemm_pairs(DT);
+  if (total) {
+    const uint32_t wm = tile.wave_m(), wn = tile.wave_n();
+    // what is loaded next: step k of a pair of planes.  Behind the last step it is loaded again, and not used.
+    uint32_t k = begin, left = total;
+    int pair = 0;
+    auto next = [&]() {
+      if (--left == 0) { left = 1; return; }
+      if (++k == end) { k = begin; ++pair; }
+    };
+    auto load_a = [&](uint32_t stage, int half) {
+      gemm_fetch<128, GemmWide::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(pair), tile.m0 + half * 128u, k * kGemmK, gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF);
+    };
+    auto load_b = [&](uint32_t stage, int half) {
+      gemm_fetch<128, GemmWide::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(pair), tile.n0 + half * 128u, k * kGemmK, gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF);
+    };
+    GemmShort8 fa[4][2], fb[3][2][2];    // of n0 in an even step, n1, n0 in an odd one
+    auto read_a = [&](uint32_t stage, int half) {
+      if constexpr (TA) return gemm_read_turned<4>(gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF, wm, fa);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) fa[i][kk] = gemm_read<128, TA>(gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF, wm + i * 16, kk);
+    };
+    auto read_b = [&](uint32_t stage, int half, int to) {
+      if constexpr (TB) return gemm_read_turned<2>(gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF, wn, fb[to]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) fb[to][j][kk] = gemm_read<128, TB>(gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF, wn + j * 16, kk);
+    };
+    auto products = [&](int mh, int nh, int from) {
+      gemm_meet();
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[mh * 4 + i][nh * 2 + j] = gemm_mac<DT>(fa[i][kk], fb[from][j][kk], acc[mh * 4 + i][nh * 2 + j]);
+      __builtin_amdgcn_s_setprio(0);
+      gemm_meet();
+    };
+    for (uint32_t q = 0; q < 2; ++q) {
+      load_b(q, 0); load_a(q, 0); load_b(q, 1); load_a(q, 1);
+      next();
+    }
+    auto step = [&](uint32_t stage) {
+      load_b(stage, 0);
+      read_a(stage, 0);
+      gemm_wait<12>();
+      products(0, 0, 2 * stage);
+      load_a(stage, 0);
+      read_b(stage, 1, 1);
+      gemm_wait<12>();
+      products(0, 1, 1);
+      load_b(stage, 1);
+      read_a(stage, 1);
+      gemm_wait<12>();
+      products(1, 1, 1);
+      load_a(stage, 1);
+      next();
+      read_b(stage ^ 1u, 0, 2 - 2 * stage);
+      gemm_wait<12>();
+      products(1, 0, 2 * stage);
+    };
+    gemm_wait<14>();
+    gemm_meet();
+    read_b(0, 0, 0);
+    gemm_wait<12>();
+    gemm_meet();
+    if (threadIdx.x >= 256) gemm_meet();       // one part behind
+    for (uint32_t q = 0; q < total; q += 2) {
+      step(0);
+      if (q + 1 < total) step(1);
+    }
+    if (threadIdx.x < 256) gemm_meet();
+    gemm_wait<0>();
+    gemm_meet();
   }
   epi(tile, at, acc, gemm_lds);
 }

@@ -443,7 +443,7 @@ int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s
   if (!s.mtiles || !s.ntiles) return DFX_OK;
   if constexpr (!(TA && TB))
     if (few) return step_launch(dfx_gemm_kernel<DT, GemmFlat, TA, TB, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
-  return step_launch(dfx_gemm_kernel<DT, GemmWide, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
+  return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
 }
 
 #define VOCAB_TRY(call) do { const int rc_ = (call); if (rc_ != DFX_OK) return rc_; } while (0)
