@@ -42,15 +42,16 @@ struct GemmShape {
   bool k_counted;
 };
 
-// Workgroups go round the 8 XCDs; each XCD gets tiles that lie together, so that what it reads is in its own L2: kGroup tiles of n, then the next of m.
+// Workgroups go round the 8 XCDs; each XCD gets as many tiles as the others, which lie together, so that what it reads is in its own L2: kGroup tiles of n,
+// then the next of m.
 struct GemmPlace { uint32_t m, n, split; bool any; };
-__device__ __forceinline__ GemmPlace gemm_place(const GemmShape& s) {
+__device__ __forceinline__ GemmPlace gemm_place(const GemmShape& s, uint32_t ntiles, uint32_t block) {
   constexpr uint32_t kGroup = 8;
-  const uint32_t tiles = s.mtiles * s.ntiles, total = tiles * s.splits, each = (total + 7u) / 8u;
-  const uint32_t j = (blockIdx.x & 7u) * each + (blockIdx.x >> 3);
-  if (j >= total || (blockIdx.x >> 3) >= each) return {0, 0, 0, false};
+  const uint32_t tiles = s.mtiles * ntiles, total = tiles * s.splits, each = (total + 7u) / 8u;
+  const uint32_t j = (block & 7u) * each + (block >> 3);
+  if (j >= total || (block >> 3) >= each) return {0, 0, 0, false};
   const uint32_t split = j / tiles, t = j % tiles, group = t / (kGroup * s.mtiles), in = t % (kGroup * s.mtiles);
-  const uint32_t width = min(kGroup, s.ntiles - group * kGroup);
+  const uint32_t width = min(kGroup, ntiles - group * kGroup);
   return {in / width, group * kGroup + in % width, split, true};
 }
 inline uint32_t gemm_groups(const GemmShape& s) { return (uint32_t)(((uint64_t)s.mtiles * s.ntiles * s.splits + 7) / 8 * 8); }
@@ -170,16 +171,16 @@ struct GemmWide {
 template <int DT, class TILE, bool TA, bool TB, class EPI>
 __global__ void __launch_bounds__(TILE::THREADS) dfx_gemm_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
   __shared__ __align__(1024) unsigned char gemm_lds[TILE::LDS];
-  const GemmPlace at = gemm_place(s);
-  if (!at.any) return;
-  TILE tile;
-  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
-  uint32_t steps = s.ksteps;
+  uint32_t steps = s.ksteps, ntiles = s.ntiles;
   if (s.count) {
     const uint32_t count = *s.count;
     if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
-    else if (tile.n0 >= count) return;
+    else ntiles = (count + TILE::N - 1) / TILE::N;
   }
+  const GemmPlace at = gemm_place(s, ntiles, blockIdx.x);
+  if (!at.any) return;
+  TILE tile;
+  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
   const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
   GemmAcc acc[TILE::MT][TILE::NT];
 #pragma unroll
@@ -241,18 +242,17 @@ __device__ __forceinline__ void gemm_meet() {
 // tiles are read in the order n0, m0, n1, m1, and as soon as both sets of waves have read one, the loads of the step after next may begin to overwrite it: a
 // load has seven turns to arrive, 12 younger ones of a wave under way behind it.
 template <int DT, bool TA, bool TB, class EPI>
-__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
-  __shared__ __align__(1024) unsigned char gemm_lds[GemmWide::LDS];
-  const GemmPlace at = gemm_place(s);
-  if (!at.any) return;
-  GemmWide tile;
-  tile.m0 = at.m * GemmWide::M; tile.n0 = at.n * GemmWide::N;
-  uint32_t steps = s.ksteps;
+__device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const EPI& epi, uint32_t block, unsigned char* gemm_lds) {
+  uint32_t steps = s.ksteps, ntiles = s.ntiles;
   if (s.count) {
     const uint32_t count = *s.count;
     if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
-    else if (tile.n0 >= count) return;
+    else ntiles = (count + GemmWide::N - 1) / GemmWide::N;
   }
+  const GemmPlace at = gemm_place(s, ntiles, block);
+  if (!at.any) return;
+  GemmWide tile;
+  tile.m0 = at.m * GemmWide::M; tile.n0 = at.n * GemmWide::N;
   const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
   GemmAcc acc[GemmWide::MT][GemmWide::NT];
 #pragma unroll
@@ -340,6 +340,20 @@ __global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(Gem
     gemm_meet();
   }
   epi(tile, at, acc, gemm_lds);
+}
+
+template <int DT, bool TA, bool TB, class EPI>
+__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  __shared__ __align__(1024) unsigned char lds[GemmWide::LDS];
+  gemm_wide<DT, TA, TB>(a, b, s, epi, blockIdx.x, lds);
+}
+
+// Two products in one launch, the one of the longer sums first: the short ones' tiles fill the compute units that its last round leaves idle.
+template <int DT, bool TA, bool TB, class EPI, bool TA2, bool TB2, class EPI2>
+__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_two_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi, uint32_t first, GemmOperand a2, GemmOperand b2, GemmShape s2, EPI2 epi2) {
+  __shared__ __align__(1024) unsigned char lds[GemmWide::LDS];
+  if (blockIdx.x < first) gemm_wide<DT, TA, TB>(a, b, s, epi, blockIdx.x, lds);
+  else gemm_wide<DT, TA2, TB2>(a2, b2, s2, epi2, blockIdx.x - first, lds);
 }
 
 // The three planes of a 32-bit value, each the nearest bf16 to what is left of it (the largest values' first: towards zero, since the nearest is

@@ -26,7 +26,7 @@ constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
 constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles
-constexpr size_t kPieceElems = 64ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
+constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
 
 // what is known of a call on the device; first in the workspace
 struct VocabState { uint32_t count; float g; };       // rows that count; scale * largest weight * c / 2^15
@@ -446,6 +446,16 @@ int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s
   return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
 }
 
+// dX and dW of a piece in one launch (dX's tiles of many rows are the wide ones)
+template <int DT, class DW>
+int vocab_gemm_two(const GemmOperand& w, const GemmOperand& z, GemmShape sx, size_t dim, size_t rows, const VocabDx& dx, const GemmOperand& x, GemmShape sw, size_t vocab, const DW& dw, hipStream_t stream) {
+  sx.mtiles = sw.mtiles = (uint32_t)((dim + 255) / 256);
+  sx.ntiles = (uint32_t)((rows + 255) / 256);
+  sw.ntiles = (uint32_t)((vocab + 255) / 256);
+  const uint32_t first = gemm_groups(sx);
+  return step_launch(dfx_gemm_two_kernel<DT, true, false, VocabDx, true, true, DW>, dim3(first + gemm_groups(sw)), GemmWide::THREADS, stream, w, z, sx, dx, first, x, z, sw, dw);
+}
+
 #define VOCAB_TRY(call) do { const int rc_ = (call); if (rc_ != DFX_OK) return rc_; } while (0)
 
 template <int DT>
@@ -498,22 +508,16 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
     VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
     const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.rp, (uint32_t)p.vp};
-    if (u.grad_hidden) {
-      const GemmShape s = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false};
-      const VocabDx to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != 0};
-      VOCAB_TRY((vocab_gemm<DT, true, false>(p.flat, ow, oz, s, u.dim, u.rows, to, stream)));
-    }
-    if (u.grad_weight) {
-      const GemmShape s = {0, 0, 1, 0, count, true};
-      const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
-      if (u.grad_dtype == DFX_F32) {
-        const VocabDw<DFX_F32> to = {(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0};
-        VOCAB_TRY((vocab_gemm<DT, true, true>(false, ox, oz, s, u.dim, left, to, stream)));
-      } else if constexpr (DT != DFX_F32) {
-        const VocabDw<DT> to = {(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0};
-        VOCAB_TRY((vocab_gemm<DT, true, true>(false, ox, oz, s, u.dim, left, to, stream)));
-      }
-    }
+    const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false}, sw = {0, 0, 1, 0, count, true};
+    const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != 0};
+    const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
+    auto both = [&](const auto& dw_to) -> int {
+      if (u.grad_hidden && u.grad_weight && !p.flat && u.rows) return vocab_gemm_two<DT>(ow, oz, sx, u.dim, u.rows, dx_to, ox, sw, left, dw_to, stream);
+      if (u.grad_hidden) VOCAB_TRY((vocab_gemm<DT, true, false>(p.flat, ow, oz, sx, u.dim, u.rows, dx_to, stream)));
+      return u.grad_weight ? vocab_gemm<DT, true, true>(false, ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
+    };
+    if (u.grad_dtype == DFX_F32) VOCAB_TRY(both(VocabDw<DFX_F32>{(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
+    else if constexpr (DT != DFX_F32) VOCAB_TRY(both(VocabDw<DT>{(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
   }
   if (u.grad_hidden && u.rows)
     VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
