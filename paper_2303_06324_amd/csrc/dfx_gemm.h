@@ -57,8 +57,10 @@ __device__ __forceinline__ GemmPlace gemm_place(const GemmShape& s, uint32_t nti
 inline uint32_t gemm_groups(const GemmShape& s) { return (uint32_t)(((uint64_t)s.mtiles * s.ntiles * s.splits + 7) / 8 * 8); }
 
 // Tiles in LDS.  k along the rows: a row's 128 bytes, whose 16-byte parts are exchanged by the row's number, so that 16 rows' parts of one k lie in
-// different banks.  Turned: a k's 2 COLS bytes, whose 32-byte parts (16 elements, a tile of the matrix instruction) are exchanged by k.
-__device__ __forceinline__ uint32_t gemm_turned_swap(uint32_t k) { return (k & 3u) | ((k >> 1) & 4u); }
+// different banks.  Turned: a k's 2 COLS bytes, whose 32-byte parts (16 elements, a tile of the matrix instruction) are exchanged by k, so that those of four k's
+// that are read at once do.
+template <int COLS>
+__device__ __forceinline__ uint32_t gemm_turned_swap(uint32_t k) { return COLS >= 128 ? (k & 3u) | ((k >> 1) & 4u) : ((k >> 1) & 1u) | ((k >> 2) & 2u); }
 
 template <int COLS, int THREADS, bool TURNED>
 __device__ __forceinline__ void gemm_fetch(const GemmOperand& o, int plane, uint32_t first, uint32_t k0, unsigned char* lds) {
@@ -81,7 +83,7 @@ __device__ __forceinline__ void gemm_fetch(const GemmOperand& o, int plane, uint
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const uint32_t k = j * (THREADS / PARTS) + t / PARTS, slot = t % PARTS;
-      const uint32_t part = (((slot >> 1) ^ gemm_turned_swap(k)) << 1) | (slot & 1u);
+      const uint32_t part = (((slot >> 1) ^ gemm_turned_swap<COLS>(k)) << 1) | (slot & 1u);
       const uint32_t col = min(first + part * 8u, o.cols - 8u);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)((min(k, last) * o.stride + col) * 2u), 0, 0, 0);
     }
@@ -89,52 +91,72 @@ __device__ __forceinline__ void gemm_fetch(const GemmOperand& o, int plane, uint
 }
 
 // what a lane holds of 16 rows and 32 k's: row lane % 16, k's 8 (lane / 16) on
-template <int COLS, bool TURNED>
 __device__ __forceinline__ GemmShort8 gemm_read(const unsigned char* lds, uint32_t first, int kk) {
-  const uint32_t lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u;
-  if (!TURNED) {
-    const uint32_t row = first + l;
-    return *(const __attribute__((address_space(3))) GemmShort8*)((GemmLds*)lds + row * 128u + (((uint32_t)kk * 4u + g) ^ ((l >> 1) & 7u)) * 16u);
-  }
-  const uint32_t k = kk * 32u + 8u * g + l / 4u;
-  GemmLds* at = (GemmLds*)lds + k * (COLS * 2u) + (((first / 16u) ^ gemm_turned_swap(k)) * 32u) + (l & 3u) * 8u;
-  const GemmShort4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)at);
-  const GemmShort4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)(at + 4u * COLS * 2u));
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  const uint32_t lane = threadIdx.x % kStepWave, l = lane % 16u;
+  return *(const __attribute__((address_space(3))) GemmShort8*)((GemmLds*)lds + (first + l) * 128u + (((uint32_t)kk * 4u + lane / 16u) ^ ((l >> 1) & 7u)) * 16u);
 }
 
-// The same of COUNT tiles of 16 rows at once and both kk, of a turned half tile of 128: the reads and the wait for them are one block of assembly, because the compiler,
+// The same of COUNT tiles of 16 rows at once and both kk, of a turned tile: the reads and the wait for them are one block of assembly, because the compiler,
 // which does not know what of LDS a load writes, waits for every load to LDS before a transposing read.
+template <int COLS>
 __device__ __forceinline__ uint32_t gemm_turned_at(const unsigned char* lds, uint32_t first) {
   const uint32_t lane = threadIdx.x % kStepWave, l = lane % 16u, k = 8u * (lane / 16u) + l / 4u;
-  return (uint32_t)(uintptr_t)(GemmLds*)lds + k * 256u + (((first / 16u) ^ gemm_turned_swap(k)) * 32u) + (l & 3u) * 8u;
+  return (uint32_t)(uintptr_t)(GemmLds*)lds + k * (COLS * 2u) + (((first / 16u) ^ gemm_turned_swap<COLS>(k)) * 32u) + (l & 3u) * 8u;
 }
-template <int COUNT>
+template <int COUNT, int COLS>
 __device__ __forceinline__ void gemm_read_turned(const unsigned char* lds, uint32_t first, GemmShort8 (*to)[2]) {
-  GemmShort4 r[COUNT][4];
+  GemmShort4 r[COUNT][4];                // (4 k's further: COLS 8 bytes, 32: COLS 64)
   if constexpr (COUNT == 4)
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:1024\n\tds_read_b64_tr_b16 %2, %16 offset:8192\n\tds_read_b64_tr_b16 %3, %16 offset:9216\n\t"
-        "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:1024\n\tds_read_b64_tr_b16 %6, %17 offset:8192\n\tds_read_b64_tr_b16 %7, %17 offset:9216\n\t"
-        "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:1024\n\tds_read_b64_tr_b16 %10, %18 offset:8192\n\tds_read_b64_tr_b16 %11, %18 offset:9216\n\t"
-        "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:1024\n\tds_read_b64_tr_b16 %14, %19 offset:8192\n\tds_read_b64_tr_b16 %15, %19 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %0, %16\n\t"
+        "ds_read_b64_tr_b16 %1, %16 offset:%20\n\t"
+        "ds_read_b64_tr_b16 %2, %16 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %3, %16 offset:%22\n\t"
+        "ds_read_b64_tr_b16 %4, %17\n\t"
+        "ds_read_b64_tr_b16 %5, %17 offset:%20\n\t"
+        "ds_read_b64_tr_b16 %6, %17 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %7, %17 offset:%22\n\t"
+        "ds_read_b64_tr_b16 %8, %18\n\t"
+        "ds_read_b64_tr_b16 %9, %18 offset:%20\n\t"
+        "ds_read_b64_tr_b16 %10, %18 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %11, %18 offset:%22\n\t"
+        "ds_read_b64_tr_b16 %12, %19\n\t"
+        "ds_read_b64_tr_b16 %13, %19 offset:%20\n\t"
+        "ds_read_b64_tr_b16 %14, %19 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %15, %19 offset:%22\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[1][2]), "=&v"(r[1][3]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[2][2]),
-          "=&v"(r[2][3]), "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(r[3][2]), "=&v"(r[3][3])
-        : "v"(gemm_turned_at(lds, first)), "v"(gemm_turned_at(lds, first + 16u)), "v"(gemm_turned_at(lds, first + 32u)), "v"(gemm_turned_at(lds, first + 48u))
+        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[1][2]), "=&v"(r[1][3]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[2][2]), "=&v"(r[2][3]), "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(r[3][2]), "=&v"(r[3][3])
+        : "v"(gemm_turned_at<COLS>(lds, first + 0u)), "v"(gemm_turned_at<COLS>(lds, first + 16u)), "v"(gemm_turned_at<COLS>(lds, first + 32u)), "v"(gemm_turned_at<COLS>(lds, first + 48u)), "i"(COLS * 8), "i"(COLS * 64), "i"(COLS * 72)
         : "memory");
   else
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:1024\n\tds_read_b64_tr_b16 %2, %8 offset:8192\n\tds_read_b64_tr_b16 %3, %8 offset:9216\n\t"
-        "ds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:1024\n\tds_read_b64_tr_b16 %6, %9 offset:8192\n\tds_read_b64_tr_b16 %7, %9 offset:9216\n\t"
+        "ds_read_b64_tr_b16 %0, %8\n\t"
+        "ds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %9\n\t"
+        "ds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %6, %9 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[1][2]), "=&v"(r[1][3])
-        : "v"(gemm_turned_at(lds, first)), "v"(gemm_turned_at(lds, first + 16u))
+        : "v"(gemm_turned_at<COLS>(lds, first + 0u)), "v"(gemm_turned_at<COLS>(lds, first + 16u)), "i"(COLS * 8), "i"(COLS * 64), "i"(COLS * 72)
         : "memory");
 #pragma unroll
   for (int i = 0; i < COUNT; ++i)
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) to[i][kk] = __builtin_shufflevector(r[i][2 * kk], r[i][2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// COUNT tiles of 16 rows and 64 k's, either way
+template <int COUNT, int COLS, bool TURNED>
+__device__ __forceinline__ void gemm_take(const unsigned char* lds, uint32_t first, GemmShort8 (*to)[2]) {
+  if constexpr (TURNED) gemm_read_turned<COUNT, COLS>(lds, first, to);
+  else
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) to[i][kk] = gemm_read(lds, first + i * 16, kk);
 }
 
 template <int DT>
@@ -143,19 +165,15 @@ __device__ __forceinline__ GemmAcc gemm_mac(GemmShort8 a, GemmShort8 b, GemmAcc 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(GemmBf16x8, a), __builtin_bit_cast(GemmBf16x8, b), c, 0, 0, 0);
 }
 
-// A tile of 256 m and WN NT 16 n by WM WN waves; a lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
-template <int WM_, int WN_, int MT_, int NT_>
-struct GemmTile {
-  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, M = WM * MT * 16, N = WN * NT * 16, THREADS = WM * WN * kStepWave;
-  static constexpr int STAGE = (M + N) * kGemmK * 2, LDS = 2 * STAGE;
+// Few rows: a tile of 128 m by 64 n by 4 waves of 32 m each.  A lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
+struct GemmFlat {
+  static constexpr int WM = 4, WN = 1, MT = 2, NT = 4, M = 128, N = 64, THREADS = 256;
+  static constexpr int STAGE = (M + N) * kGemmK * 2, STAGES = 3, LOADS = (M + N) * 8 / THREADS;
   uint32_t m0, n0;                       // of the workgroup's tile
-  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave / WN * (MT * 16); }
-  __device__ __forceinline__ uint32_t wave_n() const { return threadIdx.x / kStepWave % WN * (NT * 16); }
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave * 32u; }
   __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16 + threadIdx.x % kStepWave / 16 * 4; }
-  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + wave_n() + nt * 16 + threadIdx.x % 16; }
+  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt * 16 + threadIdx.x % 16; }
 };
-
-typedef GemmTile<4, 1, 4, 4> GemmFlat;   // 256 m by 64 n, 256 threads: few rows
 
 // A tile of 256 m by 256 n by 8 waves, in halves of 128 by 128 in which each wave has 64 m by 32 n.
 struct GemmWide {
@@ -167,58 +185,6 @@ struct GemmWide {
   __device__ __forceinline__ uint32_t m(int mt) const { return m0 + mt / 4 * 128u + wave_m() + mt % 4 * 16u + threadIdx.x % kStepWave / 16 * 4; }
   __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt / 2 * 128u + wave_n() + nt % 2 * 16u + threadIdx.x % 16; }
 };
-
-template <int DT, class TILE, bool TA, bool TB, class EPI>
-__global__ void __launch_bounds__(TILE::THREADS) dfx_gemm_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
-  __shared__ __align__(1024) unsigned char gemm_lds[TILE::LDS];
-  uint32_t steps = s.ksteps, ntiles = s.ntiles;
-  if (s.count) {
-    const uint32_t count = *s.count;
-    if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
-    else ntiles = (count + TILE::N - 1) / TILE::N;
-  }
-  const GemmPlace at = gemm_place(s, ntiles, blockIdx.x);
-  if (!at.any) return;
-  TILE tile;
-  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
-  const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
-  GemmAcc acc[TILE::MT][TILE::NT];
-#pragma unroll
-  for (int i = 0; i < TILE::MT; ++i)
-#pragma unroll
-    for (int j = 0; j < TILE::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
-  const uint32_t span = end - begin, total = span * gemm_pairs(DT);
-  const uint32_t wm = tile.wave_m(), wn = tile.wave_n();
-  uint32_t k = begin;
-  int pair = 0;
-  auto fetch = [&](uint32_t stage) {
-    const int pa = gemm_planes(DT) == 1 ? 0 : gemm_plane_a(pair), pb = gemm_planes(DT) == 1 ? 0 : gemm_plane_b(pair);
-    unsigned char* lds = gemm_lds + stage * TILE::STAGE;
-    gemm_fetch<TILE::M, TILE::THREADS, TA>(a, pa, tile.m0, k * kGemmK, lds);
-    gemm_fetch<TILE::N, TILE::THREADS, TB>(b, pb, tile.n0, k * kGemmK, lds + TILE::M * kGemmK * 2);
-    if (++k == end) { k = begin; ++pair; }
-  };
-  if (total) fetch(0);
-  for (uint32_t q = 0; q < total; ++q) {
-    __syncthreads();                     // this step's tiles have arrived, and nobody reads the other stage any more
-    if (q + 1 < total) fetch((q + 1) & 1u);
-    const unsigned char* la = gemm_lds + (q & 1u) * TILE::STAGE;
-    const unsigned char* lb = la + TILE::M * kGemmK * 2;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      GemmShort8 fa[TILE::MT], fb[TILE::NT];
-#pragma unroll
-      for (int j = 0; j < TILE::NT; ++j) fb[j] = gemm_read<TILE::N, TB>(lb, wn + j * 16, kk);
-#pragma unroll
-      for (int i = 0; i < TILE::MT; ++i) fa[i] = gemm_read<TILE::M, TA>(la, wm + i * 16, kk);
-#pragma unroll
-      for (int i = 0; i < TILE::MT; ++i)
-#pragma unroll
-        for (int j = 0; j < TILE::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i], fb[j], acc[i][j]);
-    }
-  }
-  epi(tile, at, acc, gemm_lds);
-}
 
 // A wave's waits: at most so many of its loads to LDS under way, none of its reads from LDS
 template <int LOADS>
@@ -237,23 +203,91 @@ __device__ __forceinline__ void gemm_meet() {
   asm volatile("" ::: "memory");
 }
 
+// What a workgroup has to do: its tile, and steps of k for each pair of planes
+template <class TILE>
+__device__ __forceinline__ GemmPlace gemm_work(const GemmShape& s, uint32_t block, TILE& tile, uint32_t& begin, uint32_t& end) {
+  uint32_t steps = s.ksteps, ntiles = s.ntiles;
+  if (s.count) {
+    const uint32_t count = *s.count;
+    if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
+    else ntiles = (count + TILE::N - 1) / TILE::N;
+  }
+  const GemmPlace at = gemm_place(s, ntiles, block);
+  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
+  const uint32_t each = (steps + s.splits - 1) / s.splits;
+  begin = min(at.split * each, steps); end = min(begin + each, steps);
+  return at;
+}
+
+// The step of k that is loaded next.  Behind the last one it is loaded again, and not used.
+struct GemmNext {
+  uint32_t k, begin, end, left;
+  int pair;
+  __device__ __forceinline__ GemmNext(uint32_t begin_, uint32_t end_, uint32_t total) : k(begin_), begin(begin_), end(end_), left(total), pair(0) {}
+  __device__ __forceinline__ void advance() {
+    if (--left == 0) left = 1;
+    else if (++k == end) { k = begin; ++pair; }
+  }
+};
+
+// The flat tile streams A, the larger matrix, through the chip once: three stages, two of which are under way while one is used, and two workgroups to a
+// compute unit.
+template <int DT, bool TA, bool TB, class EPI>
+__global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  __shared__ __align__(1024) unsigned char lds[GemmFlat::STAGE * GemmFlat::STAGES];
+  GemmFlat tile;
+  uint32_t begin, end;
+  const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
+  if (!at.any) return;
+  GemmAcc acc[GemmFlat::MT][GemmFlat::NT];
+#pragma unroll
+  for (int i = 0; i < GemmFlat::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  const uint32_t total = (end - begin) * gemm_pairs(DT), wm = tile.wave_m();
+  if (total) {
+    GemmNext next(begin, end, total);
+    auto load = [&](uint32_t stage) {
+      unsigned char* to = lds + stage * GemmFlat::STAGE;
+      gemm_fetch<GemmFlat::M, GemmFlat::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(next.pair), tile.m0, next.k * kGemmK, to);
+      gemm_fetch<GemmFlat::N, GemmFlat::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(next.pair), tile.n0, next.k * kGemmK, to + GemmFlat::M * kGemmK * 2);
+      next.advance();
+    };
+    load(0);
+    load(1);
+    uint32_t stage = 0;
+    for (uint32_t q = 0; q < total; ++q) {
+      gemm_wait<GemmFlat::LOADS>();      // (of the stage that comes next)
+      gemm_meet();                       // this one has arrived for all, and nobody reads the one before it any more
+      load(stage ? stage - 1u : GemmFlat::STAGES - 1u);
+      const unsigned char* la = lds + stage * GemmFlat::STAGE;
+      GemmShort8 fa[GemmFlat::MT][2], fb[GemmFlat::NT][2];
+      gemm_take<GemmFlat::NT, GemmFlat::N, TB>(la + GemmFlat::M * kGemmK * 2, 0, fb);
+      gemm_take<GemmFlat::MT, GemmFlat::M, TA>(la, wm, fa);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < GemmFlat::MT; ++i)
+#pragma unroll
+          for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i][kk], fb[j][kk], acc[i][j]);
+      stage = stage + 1u == GemmFlat::STAGES ? 0u : stage + 1u;
+    }
+    gemm_wait<0>();
+    gemm_meet();
+  }
+  epi(tile, at, acc, lds);
+}
+
 // The wide tile.  Two waves share a SIMD, and while one of them has the matrix core the other fetches: a step is four turns, one for each quarter of a wave's
 // products, and a turn is a part that reads LDS and starts loads, and a part of 16 products; waves 4 to 7 run one part behind waves 0 to 3.  Halves of the
 // tiles are read in the order n0, m0, n1, m1, and as soon as both sets of waves have read one, the loads of the step after next may begin to overwrite it: a
 // load has seven turns to arrive, 12 younger ones of a wave under way behind it.
 template <int DT, bool TA, bool TB, class EPI>
 __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const EPI& epi, uint32_t block, unsigned char* gemm_lds) {
-  uint32_t steps = s.ksteps, ntiles = s.ntiles;
-  if (s.count) {
-    const uint32_t count = *s.count;
-    if (s.k_counted) steps = (count + kGemmK - 1) / kGemmK;
-    else ntiles = (count + GemmWide::N - 1) / GemmWide::N;
-  }
-  const GemmPlace at = gemm_place(s, ntiles, block);
-  if (!at.any) return;
   GemmWide tile;
-  tile.m0 = at.m * GemmWide::M; tile.n0 = at.n * GemmWide::N;
-  const uint32_t each = (steps + s.splits - 1) / s.splits, begin = min(at.split * each, steps), end = min(begin + each, steps);
+  uint32_t begin, end;
+  const GemmPlace at = gemm_work(s, block, tile, begin, end);
+  if (!at.any) return;
   GemmAcc acc[GemmWide::MT][GemmWide::NT];
 #pragma unroll
   for (int i = 0; i < GemmWide::MT; ++i)
@@ -262,34 +296,16 @@ __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperan
   const uint32_t total = (end - begin) * gemm_pairs(DT);
   if (total) {
     const uint32_t wm = tile.wave_m(), wn = tile.wave_n();
-    // what is loaded next: step k of a pair of planes.  Behind the last step it is loaded again, and not used.
-    uint32_t k = begin, left = total;
-    int pair = 0;
-    auto next = [&]() {
-      if (--left == 0) { left = 1; return; }
-      if (++k == end) { k = begin; ++pair; }
-    };
+    GemmNext next(begin, end, total);
     auto load_a = [&](uint32_t stage, int half) {
-      gemm_fetch<128, GemmWide::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(pair), tile.m0 + half * 128u, k * kGemmK, gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF);
+      gemm_fetch<128, GemmWide::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(next.pair), tile.m0 + half * 128u, next.k * kGemmK, gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF);
     };
     auto load_b = [&](uint32_t stage, int half) {
-      gemm_fetch<128, GemmWide::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(pair), tile.n0 + half * 128u, k * kGemmK, gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF);
+      gemm_fetch<128, GemmWide::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(next.pair), tile.n0 + half * 128u, next.k * kGemmK, gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF);
     };
     GemmShort8 fa[4][2], fb[3][2][2];    // of n0 in an even step, n1, n0 in an odd one
-    auto read_a = [&](uint32_t stage, int half) {
-      if constexpr (TA) return gemm_read_turned<4>(gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF, wm, fa);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) fa[i][kk] = gemm_read<128, TA>(gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF, wm + i * 16, kk);
-    };
-    auto read_b = [&](uint32_t stage, int half, int to) {
-      if constexpr (TB) return gemm_read_turned<2>(gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF, wn, fb[to]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) fb[to][j][kk] = gemm_read<128, TB>(gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF, wn + j * 16, kk);
-    };
+    auto read_a = [&](uint32_t stage, int half) { gemm_take<4, 128, TA>(gemm_lds + stage * GemmWide::STAGE + half * GemmWide::HALF, wm, fa); };
+    auto read_b = [&](uint32_t stage, int half, int to) { gemm_take<2, 128, TB>(gemm_lds + stage * GemmWide::STAGE + (2 + half) * GemmWide::HALF, wn, fb[to]); };
     auto products = [&](int mh, int nh, int from) {
       gemm_meet();
       __builtin_amdgcn_s_setprio(1);
@@ -304,7 +320,7 @@ __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperan
     };
     for (uint32_t q = 0; q < 2; ++q) {
       load_b(q, 0); load_a(q, 0); load_b(q, 1); load_a(q, 1);
-      next();
+      next.advance();
     }
     auto step = [&](uint32_t stage) {
       load_b(stage, 0);
@@ -320,7 +336,7 @@ __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperan
       gemm_wait<12>();
       products(1, 1, 1);
       load_a(stage, 1);
-      next();
+      next.advance();
       read_b(stage ^ 1u, 0, 2 - 2 * stage);
       gemm_wait<12>();
       products(1, 0, 2 * stage);

@@ -27,6 +27,7 @@ constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
 constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
+constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
 // what is known of a call on the device; first in the workspace
 struct VocabState { uint32_t count; float g; };       // rows that count; scale * largest weight * c / 2^15
@@ -42,8 +43,8 @@ struct VocabArgs {
   float *weight, *zt, *row_loss, *row_w; // [Rp]
   float* top_weight;                     // largest |weight|
   VocabRow* row;                         // [Rp]
-  float2* parts;                         // [tiles of the vocabulary][Rp]: (m, S) of a tile's part of a row
-  uint32_t rows, rp, vocab, tiles;
+  float2* parts;                         // [tiles of the vocabulary][pitch]: (m, S) of a tile's part of a row
+  uint32_t rows, rp, pitch, vocab, tiles;
   double c;
   float k;                               // c / log 2
 };
@@ -136,12 +137,12 @@ __global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, si
   }
 }
 
-// A tile's part of each row: (m, S), and the target's logit where it lies here.
+// A tile's part of each row: (m, S), and the target's logit where it lies here; for the last piece of a call with gradients the logits as well.
 struct VocabStats {
   float2* parts;
-  float* zt;
+  float *zt, *z;                         // z: [pitch][z_pitch], may be null
   const int32_t* target;
-  uint32_t rp, left, v0, tile0;          // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile
+  uint32_t pitch, z_pitch, left, v0;     // left: rows of the vocabulary from the first of this launch, v0, on
   float k;
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
@@ -155,6 +156,13 @@ struct VocabStats {
 #pragma unroll
             for (int j = 0; j < TILE::NT; ++j) acc[i][j][e] = -INFINITY;
     }
+    if (z)
+#pragma unroll
+      for (int j = 0; j < TILE::NT; ++j) {
+        float* to = z + (size_t)tile.n(j) * z_pitch;
+#pragma unroll
+        for (int i = 0; i < TILE::MT; ++i) *(GemmAcc*)(to + tile.m(i)) = acc[i][j];
+      }
     float2* part = (float2*)lds;         // [WM][N]
     __syncthreads();
 #pragma unroll
@@ -191,7 +199,7 @@ struct VocabStats {
       }
 #pragma unroll
       for (int w = 0; w < TILE::WM; ++w) s += p[w].y * vocab_exp(p[w].x, vocab_base(top), k);
-      parts[(size_t)(tile0 + at.m) * rp + tile.n0 + i] = make_float2(top, s);
+      parts[(size_t)(v0 / TILE::M + at.m) * pitch + tile.n0 + i] = make_float2(top, s);
     }
   }
 };
@@ -205,7 +213,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
     for (uint32_t t = slice; t < a.tiles; t += 32u) {
       float2 p[4];
 #pragma unroll
-      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * 8u < a.tiles ? a.parts[(size_t)(t + u * 8u) * a.rp + n] : make_float2(-INFINITY, 0.0f);
+      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * 8u < a.tiles ? a.parts[(size_t)(t + u * 8u) * a.pitch + n] : make_float2(-INFINITY, 0.0f);
       float more = top;
 #pragma unroll
       for (int u = 0; u < 4; ++u) more = fmaxf(more, p[u].x);
@@ -268,39 +276,50 @@ struct VocabDz {
   size_t plane;
   uint32_t pitch, left, v0;
   float k;
+  // of four logits of a row
+  __device__ __forceinline__ void put(uint32_t n, const VocabRow& r, uint32_t m, GemmAcc z) const {
+    const uint32_t t = (uint32_t)r.t - v0;
+    uint16_t* to = dz + (size_t)n * pitch + m;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = r.f * vocab_exp(z[e], r.m, k);
+      if (m + e == t) v[e] -= r.w;
+      if (m + e >= left) v[e] = 0.0f;
+    }
+    if constexpr (DT == DFX_F32) {
+      uint16_t p[4][3];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gemm_cut(v[e], p[e]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *(uint2*)(to + q * plane) = make_uint2(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16);
+    } else {
+      StepVec<DT, 4> o;
+      o.put(v);
+      *(uint2*)to = make_uint2(o.w[0], o.w[1]);
+    }
+  }
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
 #pragma unroll
     for (int j = 0; j < TILE::NT; ++j) {
       const uint32_t n = tile.n(j);
       const VocabRow r = row[n];
-      const uint32_t t = (uint32_t)r.t - v0;
-      uint16_t* to = dz + (size_t)n * pitch;
 #pragma unroll
-      for (int i = 0; i < TILE::MT; ++i) {
-        const uint32_t m = tile.m(i);
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = r.f * vocab_exp(acc[i][j][e], r.m, k);
-          if (m + e == t) v[e] -= r.w;
-          if (m + e >= left) v[e] = 0.0f;
-        }
-        if constexpr (DT == DFX_F32) {
-          uint16_t p[4][3];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) gemm_cut(v[e], p[e]);
-#pragma unroll
-          for (int q = 0; q < 3; ++q) *(uint2*)(to + q * plane + m) = make_uint2(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16);
-        } else {
-          StepVec<DT, 4> o;
-          o.put(v);
-          *(uint2*)(to + m) = make_uint2(o.w[0], o.w[1]);
-        }
-      }
+      for (int i = 0; i < TILE::MT; ++i) put(n, r, tile.m(i), acc[i][j]);
     }
   }
 };
+
+// dz of a piece whose logits were kept: a workgroup to 1024 logits of a row.  Rows behind those that count are 0 as far as the products take them.
+template <int DT>
+__global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabDz<DT> d, const float* z, const uint32_t* count) {
+  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 4u, rows = *count;
+  if (n >= (rows + kGemmK - 1) / kGemmK * kGemmK || m >= d.pitch) return;
+  GemmAcc v = {0, 0, 0, 0};
+  if (n < rows) v = *(const GemmAcc*)(z + (size_t)n * d.pitch + m);
+  d.put(n, n < rows ? d.row[n] : VocabRow{0.0f, 0.0f, 0.0f, -1}, m, v);
+}
 
 // a part of dX, in 32 bits: [splits][rows][pitch]
 struct VocabDx {
@@ -368,26 +387,26 @@ struct VocabDw {
 // dX: the splits' parts, in their order; rows that do not count are 0
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const float* part, uint32_t splits, uint32_t split_rows, uint32_t pitch, void* grad, size_t stride, uint32_t dim) {
-  const uint32_t row = blockIdx.x;
+  const uint32_t row = blockIdx.x, e = (blockIdx.y * 256u + threadIdx.x) * 4u;
+  if (e >= dim) return;
   const int32_t n = a.map[row];
   const float g = a.state->g;
   typedef typename StepElem<DT>::raw raw;
   raw* to = (raw*)grad + (size_t)row * stride;
-  for (uint32_t e = threadIdx.x * 4u; e < dim; e += 256u * 4u) {
-    float v[4] = {0, 0, 0, 0};
-    if (n >= 0) {
-      GemmAcc sum = *(const GemmAcc*)(part + (size_t)n * pitch + e);
-      for (uint32_t s = 1; s < splits; ++s) sum += *(const GemmAcc*)(part + ((size_t)s * split_rows + n) * pitch + e);
-      for (int q = 0; q < 4; ++q) v[q] = g * sum[q];
-    }
-    if (e + 4u <= dim) {
-      StepVec<DT, 4> o;
-      o.put(v);
-      *(STEP_GLOBAL typename StepVec<DT, 4>::words*)((STEP_GLOBAL raw*)to + e) = o.w;
-    } else {
-      for (int q = 0; q < 4; ++q)
-        if (e + q < dim) step_put<DT>(to, e + q, v[q]);
-    }
+  float v[4] = {0, 0, 0, 0};
+  if (n >= 0) {
+    GemmAcc sum = *(const GemmAcc*)(part + (size_t)n * pitch + e);
+#pragma unroll 8
+    for (uint32_t s = 1; s < splits; ++s) sum += *(const GemmAcc*)(part + ((size_t)s * split_rows + n) * pitch + e);
+    for (int q = 0; q < 4; ++q) v[q] = g * sum[q];
+  }
+  if (e + 4u <= dim) {
+    StepVec<DT, 4> o;
+    o.put(v);
+    *(STEP_GLOBAL typename StepVec<DT, 4>::words*)((STEP_GLOBAL raw*)to + e) = o.w;
+  } else {
+    for (int q = 0; q < 4; ++q)
+      if (e + q < dim) step_put<DT>(to, e + q, v[q]);
   }
 }
 
@@ -397,12 +416,12 @@ __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const fl
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
 struct VocabPlan {
-  size_t rp, dp, dq, vp, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, tiles of the vocabulary, splits of dX and a split's rows
-  bool flat;
-  size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, dx, bytes;      // places in the workspace
+  size_t rp, dp, dq, vp, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, tiles of the vocabulary, splits of dX and the tiles' rows
+  bool flat, keep;                       // keep: the logits of the last piece
+  size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
 };
 
-// Splits of dX along the vocabulary: as many workgroups as compute units.  What depends on the number of rows has room for any smaller number.
+// Splits of dX along the vocabulary: as many workgroups as compute units, of the flat tiles twice as many.  What depends on the number of rows has room for any smaller number.
 VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad, size_t piece) {
   VocabPlan p;
   const size_t planes = gemm_planes(dtype);
@@ -419,30 +438,34 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
     p.vp = up((whole + pieces - 1) / pieces, kTileRows);
     dz_rows = std::min(dz_rows, std::max(kPieceElems, p.rp * kPieceLeast));
   }
-  const size_t tile = p.flat ? 64 : 256, across = up(std::max<size_t>(rows, 1), tile) / tile, along = up(dim, 256) / 256;
-  p.splits = std::max<size_t>(1, std::min(256 / (across * along), p.vp / 256));
+  const size_t tile = p.flat ? GemmFlat::N : GemmWide::N, wide = p.flat ? GemmFlat::M : GemmWide::M, across = up(std::max<size_t>(rows, 1), tile) / tile, along = up(dim, wide) / wide;
+  const size_t groups = p.flat ? 512 : 256;
+  p.splits = std::max<size_t>(1, std::min(groups / (across * along), p.vp / 256));
+  if (p.flat) p.tiles = (vocab + GemmFlat::M - 1) / GemmFlat::M;
+  p.keep = grad && dim >= (dtype == DFX_F32 ? kKeepDimF32 : kKeepDim);
   p.split_rows = across * tile;
+  const size_t across256 = p.rp / 256, along256 = up(dim, 256) / 256;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
   p.state = take(sizeof(VocabState) + 4);
   p.idx = take(4 * p.rp); p.target = take(4 * p.rp); p.map = take(4 * p.rp); p.weight = take(4 * p.rp); p.zt = take(4 * p.rp);
   p.row_loss = take(4 * p.rp); p.row_w = take(4 * p.rp); p.row = take(sizeof(VocabRow) * p.rp);
-  p.parts = take(sizeof(float2) * p.rp * p.tiles);
+  p.parts = take(sizeof(float2) * p.rp * (whole / kTileRows));
   p.x = take(planes * p.rp * p.dp * 2);
   p.w = take(planes * most * p.dp * 2);
   p.dz = grad ? take(planes * dz_rows * 2) : at;
-  p.dx = grad ? take(std::max(256 / along, across) * tile * p.dq * 4) : at;
+  p.z = p.keep ? take(dz_rows * 4) : at;
+  p.dx = grad ? take(std::max(256 / along256, across256) * 256 * p.dq * 4) : at;
   p.bytes = at;
   return p;
 }
 
 template <int DT, bool TA, bool TB, class EPI>
 int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, hipStream_t stream) {
-  s.mtiles = (uint32_t)((m + 255) / 256);
-  s.ntiles = (uint32_t)(few ? (n + 63) / 64 : (n + 255) / 256);
+  s.mtiles = (uint32_t)(few ? (m + GemmFlat::M - 1) / GemmFlat::M : (m + GemmWide::M - 1) / GemmWide::M);
+  s.ntiles = (uint32_t)(few ? (n + GemmFlat::N - 1) / GemmFlat::N : (n + GemmWide::N - 1) / GemmWide::N);
   if (!s.mtiles || !s.ntiles) return DFX_OK;
-  if constexpr (!(TA && TB))
-    if (few) return step_launch(dfx_gemm_kernel<DT, GemmFlat, TA, TB, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
+  if (few) return step_launch(dfx_gemm_flat_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
   return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
 }
 
@@ -468,7 +491,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   a.idx = (int32_t*)(ws + p.idx); a.target = (int32_t*)(ws + p.target); a.map = (int32_t*)(ws + p.map); a.weight = (float*)(ws + p.weight);
   a.zt = (float*)(ws + p.zt); a.row_loss = (float*)(ws + p.row_loss); a.row_w = (float*)(ws + p.row_w); a.row = (VocabRow*)(ws + p.row);
   a.parts = (float2*)(ws + p.parts);
-  a.rows = (uint32_t)u.rows; a.rp = (uint32_t)p.rp; a.vocab = (uint32_t)u.vocab; a.tiles = (uint32_t)p.tiles;
+  a.rows = (uint32_t)u.rows; a.rp = (uint32_t)p.rp; a.pitch = (uint32_t)p.split_rows; a.vocab = (uint32_t)u.vocab; a.tiles = (uint32_t)p.tiles;
   a.c = u.inv_temperature; a.k = (float)(u.inv_temperature * kVLog2e);
   const size_t eb = step_elem_bytes(DT), ws_stride = u.weight_stride ? u.weight_stride : u.dim;
   const uint32_t* count = &a.state->count;
@@ -493,34 +516,37 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
                        (uint32_t)u.dim, (uint32_t)p.dp, w, p.vp * p.dp);
   };
   const GemmShape by_rows = {0, 0, 1, (uint32_t)(p.dp / kGemmK), count, false};
-  for (size_t v0 = 0; v0 < u.vocab; v0 += direct ? u.vocab : p.vp) {
-    const size_t left = direct ? u.vocab : std::min(p.vp, u.vocab - v0);
+  const size_t last = pieces ? (pieces - 1) * p.vp : 0;
+  float* z = p.keep ? (float*)(ws + p.z) : nullptr;
+  for (size_t v0 = 0, left; v0 < u.vocab; v0 += left) {      // what lies where it is in one launch, but for a piece whose logits are kept
+    left = direct ? (z && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
     VOCAB_TRY(take_piece(v0, left));
-    const VocabStats epi = {a.parts, a.zt, a.target, a.rp, (uint32_t)left, (uint32_t)v0, (uint32_t)(v0 / kTileRows), a.k};
+    const VocabStats epi = {a.parts, a.zt, v0 == last ? z : nullptr, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
     VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
   }
   VOCAB_TRY(step_launch(dfx_vocab_join_kernel, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
   if (u.sums) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
   if (!u.grad_hidden && !u.grad_weight) return DFX_OK;
-  for (size_t v0 = 0; v0 < u.vocab; v0 += p.vp) {
-    const size_t left = std::min(p.vp, u.vocab - v0);
-    if (pieces > 1 || direct) VOCAB_TRY(take_piece(v0, left));
+  for (size_t q = pieces; q-- != 0;) {   // the last one first
+    const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
+    if (direct || v0 != last) VOCAB_TRY(take_piece(v0, left));
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
-    VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
+    if (z && v0 == last) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 4 + 255) / 256), 256, stream, epi, (const float*)z, count));
+    else VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
     const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.rp, (uint32_t)p.vp};
     const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false}, sw = {0, 0, 1, 0, count, true};
-    const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != 0};
+    const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != last};
     const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
     auto both = [&](const auto& dw_to) -> int {
       if (u.grad_hidden && u.grad_weight && !p.flat && u.rows) return vocab_gemm_two<DT>(ow, oz, sx, u.dim, u.rows, dx_to, ox, sw, left, dw_to, stream);
       if (u.grad_hidden) VOCAB_TRY((vocab_gemm<DT, true, false>(p.flat, ow, oz, sx, u.dim, u.rows, dx_to, stream)));
-      return u.grad_weight ? vocab_gemm<DT, true, true>(false, ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
+      return u.grad_weight ? vocab_gemm<DT, true, true>(p.flat, ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
     };
     if (u.grad_dtype == DFX_F32) VOCAB_TRY(both(VocabDw<DFX_F32>{(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
     else if constexpr (DT != DFX_F32) VOCAB_TRY(both(VocabDw<DT>{(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
   }
   if (u.grad_hidden && u.rows)
-    VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
+    VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows, (uint32_t)((u.dim + 1023) / 1024)), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
                           u.grad_hidden_stride ? u.grad_hidden_stride : u.dim, (uint32_t)u.dim));
   return DFX_OK;
 }
