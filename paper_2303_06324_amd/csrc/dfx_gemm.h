@@ -168,11 +168,13 @@ __device__ __forceinline__ GemmAcc gemm_mac(GemmShort8 a, GemmShort8 b, GemmAcc 
 // Few rows: a tile of 128 m by 64 n by 4 waves of 32 m each.  A lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
 struct GemmFlat {
   static constexpr int WM = 4, WN = 1, MT = 2, NT = 4, M = 128, N = 64, THREADS = 256;
-  static constexpr int STAGE = (M + N) * kGemmK * 2, STAGES = 3, LOADS = (M + N) * 8 / THREADS;
+  static constexpr int STAGE = (M + N) * kGemmK * 2, LOADS = (M + N) * 8 / THREADS;
   uint32_t m0, n0;                       // of the workgroup's tile
   __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave * 32u; }
   __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16 + threadIdx.x % kStepWave / 16 * 4; }
   __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt * 16 + threadIdx.x % 16; }
+  __device__ __forceinline__ uint32_t row(int nt, uint32_t r) const { return n0 + nt * 16 + r; }
+  __device__ __forceinline__ uint32_t row_of_pass() const { return threadIdx.x % 16; }
 };
 
 // A tile of 256 m by 256 n by 8 waves, in halves of 128 by 128 in which each wave has 64 m by 32 n.
@@ -184,6 +186,8 @@ struct GemmWide {
   __device__ __forceinline__ uint32_t wave_n() const { return threadIdx.x / kStepWave % WN * 32u; }
   __device__ __forceinline__ uint32_t m(int mt) const { return m0 + mt / 4 * 128u + wave_m() + mt % 4 * 16u + threadIdx.x % kStepWave / 16 * 4; }
   __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt / 2 * 128u + wave_n() + nt % 2 * 16u + threadIdx.x % 16; }
+  __device__ __forceinline__ uint32_t row(int nt, uint32_t r) const { return n0 + nt / 2 * 128u + r / 16u * 32u + nt % 2 * 16u + r % 16u; }
+  __device__ __forceinline__ uint32_t row_of_pass() const { return wave_n() / 2u + threadIdx.x % 16; }
 };
 
 // A wave's waits: at most so many of its loads to LDS under way, none of its reads from LDS
@@ -230,11 +234,11 @@ struct GemmNext {
   }
 };
 
-// The flat tile streams A, the larger matrix, through the chip once: three stages, two of which are under way while one is used, and two workgroups to a
-// compute unit.
-template <int DT, bool TA, bool TB, class EPI>
-__global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
-  __shared__ __align__(1024) unsigned char lds[GemmFlat::STAGE * GemmFlat::STAGES];
+// The flat tile.  Where it streams the larger matrix through the chip once: three stages, two of which are under way while one is used, and two workgroups to a
+// compute unit.  Where few rows are summed over (a step or two) and the result is what takes the time: two stages, three workgroups.
+template <int DT, bool TA, bool TB, class EPI, int STAGES>
+__global__ void __launch_bounds__(GemmFlat::THREADS, STAGES == 2 ? 3 : 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  __shared__ __align__(1024) unsigned char lds[GemmFlat::STAGE * STAGES];
   GemmFlat tile;
   uint32_t begin, end;
   const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
@@ -254,12 +258,12 @@ __global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(Gem
       next.advance();
     };
     load(0);
-    load(1);
+    if (STAGES == 3) load(1);
     uint32_t stage = 0;
     for (uint32_t q = 0; q < total; ++q) {
-      gemm_wait<GemmFlat::LOADS>();      // (of the stage that comes next)
-      gemm_meet();                       // this one has arrived for all, and nobody reads the one before it any more
-      load(stage ? stage - 1u : GemmFlat::STAGES - 1u);
+      gemm_wait<GemmFlat::LOADS * (STAGES - 2)>();
+      gemm_meet();                       // this stage has arrived for all, and nobody reads the one before it any more
+      if (STAGES == 3 || q + 1 < total) load(stage ? stage - 1u : STAGES - 1u);
       const unsigned char* la = lds + stage * GemmFlat::STAGE;
       GemmShort8 fa[GemmFlat::MT][2], fb[GemmFlat::NT][2];
       gemm_take<GemmFlat::NT, GemmFlat::N, TB>(la + GemmFlat::M * kGemmK * 2, 0, fb);
@@ -270,12 +274,39 @@ __global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(Gem
         for (int i = 0; i < GemmFlat::MT; ++i)
 #pragma unroll
           for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i][kk], fb[j][kk], acc[i][j]);
-      stage = stage + 1u == GemmFlat::STAGES ? 0u : stage + 1u;
+      stage = stage + 1u == STAGES ? 0u : stage + 1u;
     }
     gemm_wait<0>();
     gemm_meet();
   }
   epi(tile, at, acc, lds);
+}
+
+// A tile by its rows of n: f(n, m, v) for E elements that follow one another from m on, of one row by threads beside each other, so that what they write lies
+// together.  Through LDS, WN 16 rows at a time, which lie 16 bytes further in the banks each.
+template <int E, class TILE, class F>
+__device__ __forceinline__ void gemm_by_rows(const TILE& tile, const GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds, const F& f) {
+  constexpr uint32_t ROWS = TILE::WN * 16, PITCH = TILE::M + 4, PARTS = TILE::M / E;
+  float* at = (float*)lds;
+#pragma unroll
+  for (int j = 0; j < TILE::NT; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TILE::MT; ++i) *(GemmAcc*)(at + tile.row_of_pass() * PITCH + tile.m(i) - tile.m0) = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (uint32_t q = threadIdx.x; q < ROWS * PARTS; q += TILE::THREADS) {
+      const uint32_t r = q / PARTS, m = q % PARTS * E;
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const GemmAcc four = *(const GemmAcc*)(at + r * PITCH + m + e);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[e + x] = four[x];
+      }
+      f(tile.row(j, r), tile.m0 + m, v);
+    }
+  }
 }
 
 // The wide tile.  Two waves share a SIMD, and while one of them has the matrix core the other fetches: a step is four turns, one for each quarter of a wave's

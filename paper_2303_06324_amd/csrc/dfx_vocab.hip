@@ -25,7 +25,7 @@ constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.442695040888963407
 constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
-constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles
+constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles (at most 256: dfx_vocab_few_kernel has a thread for each)
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
 constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
@@ -51,6 +51,12 @@ struct VocabArgs {
 
 __device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
 __device__ __forceinline__ float vocab_exp(float z, float base, float k) { return __builtin_amdgcn_exp2f((z - base) * k); }
+
+__device__ __forceinline__ void vocab_state(const VocabArgs& a, uint32_t count, float top) {
+  a.state->count = count;
+  a.state->g = count ? (float)((a.scale ? (double)a.scale[0] : 1.0) * (double)top * a.c / (double)kDzScale) : 0.0f;
+  *a.top_weight = top;
+}
 
 // The rows that count, in their order, by one workgroup; logp and loss of the others.
 __global__ void __launch_bounds__(kRowsThreads) dfx_vocab_rows_kernel(VocabArgs a) {
@@ -95,39 +101,42 @@ __global__ void __launch_bounds__(kRowsThreads) dfx_vocab_rows_kernel(VocabArgs 
   if (me == 0) {
     for (uint32_t k = 1; k < W; ++k) top = fmaxf(top, tops[k]);
     top = fmaxf(top, tops[0]);
-    a.state->count = done;
-    a.state->g = done ? (float)((a.scale ? (double)a.scale[0] : 1.0) * (double)top * a.c / (double)kDzScale) : 0.0f;
-    *a.top_weight = top;
+    vocab_state(a, done, top);
   }
 }
 
-// Rows of a matrix for the products: padded with zeros to whole steps, 32 bits cut into planes; idx: which rows (-1: zeros), or null: row for row.
+// A row of a matrix for the products, by a workgroup: padded with zeros to whole steps, 32 bits cut into planes.  null: zeros.
 template <int DT>
-__global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, size_t stride, const int32_t* idx, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
-  const uint32_t r = blockIdx.x;
-  const int64_t from = idx ? (int64_t)idx[r] : (int64_t)r;
-  const unsigned char* row = (const unsigned char*)src + (from < 0 ? 0 : (size_t)from) * stride * step_elem_bytes(DT);
-  uint16_t* to = dst + (size_t)r * padded;
+__device__ __forceinline__ void pack_row(const void* row, uint32_t dim, uint32_t padded, uint16_t* to, size_t plane) {
   for (uint32_t e = threadIdx.x * 8u; e < padded; e += 256u * 8u) {
     if constexpr (DT == DFX_F32) {
-      uint16_t part[3][8];
-      for (int j = 0; j < 8; ++j) {
-        uint16_t p[3] = {0, 0, 0};
-        if (from >= 0 && e + j < dim) gemm_cut(step_get<DT>(row, e + j), p);
-        for (int q = 0; q < 3; ++q) part[q][j] = p[q];
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (row) {
+        if (e + 8u <= dim) {
+          StepVec<DT, 4> lo, hi;
+          lo.load(row, e); hi.load(row, e + 4u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { v[j] = lo.get(j); v[4 + j] = hi.get(j); }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (e + j < dim) v[j] = step_get<DT>(row, e + j);
+        }
       }
-      for (int q = 0; q < 3; ++q) {
-        uint4 v;
-        memcpy(&v, part[q], 16);
-        *(uint4*)(to + q * plane + e) = v;
-      }
+      uint16_t p[8][3];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) gemm_cut(v[j], p[j]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        *(uint4*)(to + q * plane + e) = make_uint4(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16, p[4][q] | (uint32_t)p[5][q] << 16, p[6][q] | (uint32_t)p[7][q] << 16);
     } else {
       StepVec<DT, 8> v;
       v.w = 0;
-      if (from >= 0) {
+      if (row) {
         if (e + 8u <= dim) v.load(row, e);
         else {
           uint16_t x[8];
+#pragma unroll
           for (int j = 0; j < 8; ++j) x[j] = e + j < dim ? *((const STEP_GLOBAL uint16_t*)row + e + j) : (uint16_t)0;
           memcpy(&v.w, x, 16);
         }
@@ -135,6 +144,56 @@ __global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, si
       *(uint4*)(to + e) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
     }
   }
+}
+
+// idx: which rows (-1: zeros), or null: row for row
+template <int DT>
+__global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, size_t stride, const int32_t* idx, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
+  const uint32_t r = blockIdx.x;
+  const int64_t from = idx ? (int64_t)idx[r] : (int64_t)r;
+  pack_row<DT>(from < 0 ? nullptr : (const unsigned char*)src + (size_t)from * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)r * padded, plane);
+}
+
+// The same for few rows in one launch with what dfx_vocab_rows_kernel does: every workgroup finds the rows that count, and lays out the one of its number.
+template <int DT>
+__global__ void __launch_bounds__(256) dfx_vocab_few_kernel(VocabArgs a, const void* src, size_t stride, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
+  __shared__ uint32_t counts[4];
+  __shared__ float tops[4];
+  __shared__ int32_t mine;
+  const uint32_t me = threadIdx.x, wave = me / kStepWave, lane = me % kStepWave;
+  const int64_t t = me < a.rows ? a.targets[me] : -1;
+  const float w = me < a.rows && a.row_weight ? a.row_weight[me] : 1.0f;
+  const bool counts_here = t >= 0 && t < (int64_t)a.vocab && w != 0.0f;
+  const uint64_t mask = __ballot(counts_here);
+  const float top = __uint_as_float(wave_max(__float_as_uint(counts_here ? fmaxf(fabsf(w), 0.0f) : 0.0f)));
+  if (lane == 0) { counts[wave] = (uint32_t)__popcll(mask); tops[wave] = top; }
+  if (me == 0) mine = -1;
+  __syncthreads();
+  uint32_t place = (uint32_t)__popcll(mask & ((1ull << lane) - 1ull)), done = 0;
+  float most = 0.0f;
+  for (uint32_t k = 0; k < 4; ++k) {
+    place += k < wave ? counts[k] : 0u;
+    done += counts[k];
+    most = fmaxf(most, tops[k]);
+  }
+  if (counts_here && place == blockIdx.x) mine = (int32_t)me;
+  if (blockIdx.x == 0) {
+    if (me < a.rows) {
+      a.map[me] = counts_here ? (int32_t)place : -1;
+      if (counts_here) {
+        a.idx[place] = (int32_t)me; a.target[place] = (int32_t)t; a.weight[place] = w;
+      } else {
+        if (a.logp) a.logp[me] = 0.0f;
+        if (a.loss) a.loss[me] = 0.0f;
+      }
+    }
+    if (me >= done && me < a.rp) {
+      a.idx[me] = -1; a.target[me] = -1; a.weight[me] = 0.0f;
+    }
+    if (me == 0) vocab_state(a, done, most);
+  }
+  __syncthreads();
+  pack_row<DT>(mine < 0 ? nullptr : (const unsigned char*)src + (size_t)mine * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)blockIdx.x * padded, plane);
 }
 
 // A tile's part of each row: (m, S), and the target's logit where it lies here; for the last piece of a call with gradients the logits as well.
@@ -204,16 +263,18 @@ struct VocabStats {
   }
 };
 
-// The tiles' parts of a row joined, and what it comes to.  Eight threads to a row.
+// The tiles' parts of a row joined, and what it comes to.  S threads to a row: few where there are many rows.
+template <uint32_t S>
 __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
-  __shared__ float2 lds[8][32];
-  const uint32_t i = threadIdx.x % 32u, slice = threadIdx.x / 32u, n = blockIdx.x * 32u + i, count = a.state->count;
+  constexpr uint32_t R = 256 / S;
+  __shared__ float2 lds[S][R];
+  const uint32_t i = threadIdx.x % R, slice = threadIdx.x / R, n = blockIdx.x * R + i, count = a.state->count;
   float top = -INFINITY, s = 0.0f;
   if (n < count)
-    for (uint32_t t = slice; t < a.tiles; t += 32u) {
+    for (uint32_t t = slice; t < a.tiles; t += 4u * S) {
       float2 p[4];
 #pragma unroll
-      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * 8u < a.tiles ? a.parts[(size_t)(t + u * 8u) * a.pitch + n] : make_float2(-INFINITY, 0.0f);
+      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * S < a.tiles ? a.parts[(size_t)(t + u * S) * a.pitch + n] : make_float2(-INFINITY, 0.0f);
       float more = top;
 #pragma unroll
       for (int u = 0; u < 4; ++u) more = fmaxf(more, p[u].x);
@@ -225,11 +286,11 @@ __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
     }
   lds[slice][i] = make_float2(top, s);
   __syncthreads();
-  if (slice) return;
-  for (int k = 1; k < 8; ++k) top = fmaxf(top, lds[k][i].x);
+  if (slice || n >= a.rp) return;
+  for (uint32_t k = 1; k < S; ++k) top = fmaxf(top, lds[k][i].x);
   const float base = vocab_base(top);
   s = 0.0f;
-  for (int k = 0; k < 8; ++k) s += lds[k][i].y * vocab_exp(lds[k][i].x, base, a.k);
+  for (uint32_t k = 0; k < S; ++k) s += lds[k][i].y * vocab_exp(lds[k][i].x, base, a.k);
   VocabRow r = {0.0f, 0.0f, 0.0f, -1};
   float logp = 0.0f, loss = 0.0f, w = 0.0f;
   if (n < count && s != 0.0f) {          // (0: no logit above -infinity)
@@ -241,7 +302,6 @@ __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
     const float relative = w / *a.top_weight * kDzScale;
     r = {base, relative / s, relative, a.target[n]};
   }
-  if (n >= a.rp) return;
   a.row[n] = r;
   a.row_loss[n] = loss;
   a.row_w[n] = w;
@@ -276,48 +336,43 @@ struct VocabDz {
   size_t plane;
   uint32_t pitch, left, v0;
   float k;
-  // of four logits of a row
-  __device__ __forceinline__ void put(uint32_t n, const VocabRow& r, uint32_t m, GemmAcc z) const {
+  // of eight logits of a row
+  __device__ __forceinline__ void put(uint32_t n, const VocabRow& r, uint32_t m, const float* z) const {
     const uint32_t t = (uint32_t)r.t - v0;
     uint16_t* to = dz + (size_t)n * pitch + m;
-    float v[4];
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
       v[e] = r.f * vocab_exp(z[e], r.m, k);
       if (m + e == t) v[e] -= r.w;
       if (m + e >= left) v[e] = 0.0f;
     }
     if constexpr (DT == DFX_F32) {
-      uint16_t p[4][3];
+      uint16_t p[8][3];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) gemm_cut(v[e], p[e]);
+      for (int e = 0; e < 8; ++e) gemm_cut(v[e], p[e]);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) *(uint2*)(to + q * plane) = make_uint2(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16);
+      for (int q = 0; q < 3; ++q)
+        *(uint4*)(to + q * plane) = make_uint4(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16, p[4][q] | (uint32_t)p[5][q] << 16, p[6][q] | (uint32_t)p[7][q] << 16);
     } else {
-      StepVec<DT, 4> o;
+      StepVec<DT, 8> o;
       o.put(v);
-      *(uint2*)to = make_uint2(o.w[0], o.w[1]);
+      *(uint4*)to = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
     }
   }
   template <class TILE>
-  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
-#pragma unroll
-    for (int j = 0; j < TILE::NT; ++j) {
-      const uint32_t n = tile.n(j);
-      const VocabRow r = row[n];
-#pragma unroll
-      for (int i = 0; i < TILE::MT; ++i) put(n, r, tile.m(i), acc[i][j]);
-    }
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
+    gemm_by_rows<8>(tile, acc, lds, [&](uint32_t n, uint32_t m, const float* z) { put(n, row[n], m, z); });
   }
 };
 
-// dz of a piece whose logits were kept: a workgroup to 1024 logits of a row.  Rows behind those that count are 0 as far as the products take them.
+// dz of a piece whose logits were kept: a workgroup to 2048 logits of a row.  Rows behind those that count are 0 as far as the products take them.
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabDz<DT> d, const float* z, const uint32_t* count) {
-  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 4u, rows = *count;
+  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 8u, rows = *count;
   if (n >= (rows + kGemmK - 1) / kGemmK * kGemmK || m >= d.pitch) return;
-  GemmAcc v = {0, 0, 0, 0};
-  if (n < rows) v = *(const GemmAcc*)(z + (size_t)n * d.pitch + m);
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (n < rows) memcpy(v, __builtin_assume_aligned(z + (size_t)n * d.pitch + m, 16), 32);
   d.put(n, n < rows ? d.row[n] : VocabRow{0.0f, 0.0f, 0.0f, -1}, m, v);
 }
 
@@ -351,36 +406,30 @@ struct VocabDw {
   uint32_t dim, left;                    // elements of a row; rows from grad's first on
   bool accumulate;
   template <class TILE>
-  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char*) const {
+  __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
+    typedef typename StepElem<OUT>::raw raw;
+    constexpr int E = 16 / (int)sizeof(raw);
     const float g = state->g;
-#pragma unroll
-    for (int j = 0; j < TILE::NT; ++j) {
-      const uint32_t n = tile.n(j);
-      if (n >= left) continue;
-      typedef typename StepElem<OUT>::raw raw;
+    gemm_by_rows<E>(tile, acc, lds, [&](uint32_t n, uint32_t m, float* v) {
+      if (n >= left || m >= dim) return;
       raw* to = (raw*)grad + (size_t)n * stride;
 #pragma unroll
-      for (int i = 0; i < TILE::MT; ++i) {
-        const uint32_t m = tile.m(i);
-        float v[4];
+      for (int e = 0; e < E; ++e) v[e] *= g;
+      if (m + E <= dim) {
+        StepVec<OUT, E> o;
+        if (accumulate) {
+          o.load(to, m);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = g * acc[i][j][e];
-        if (m + 4 <= dim) {
-          StepVec<OUT, 4> o;
-          if (accumulate) {
-            o.load(to, m);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o.get(e);
-          }
-          o.put(v);
-          *(STEP_GLOBAL typename StepVec<OUT, 4>::words*)((STEP_GLOBAL raw*)to + m) = o.w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < dim) step_put<OUT>(to, m + e, accumulate ? v[e] + step_get<OUT>(to, m + e) : v[e]);
+          for (int e = 0; e < E; ++e) v[e] += o.get(e);
         }
+        o.put(v);
+        *(STEP_GLOBAL typename StepVec<OUT, E>::words*)((STEP_GLOBAL raw*)to + m) = o.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (m + e < dim) step_put<OUT>(to, m + e, accumulate ? v[e] + step_get<OUT>(to, m + e) : v[e]);
       }
-    }
+    });
   }
 };
 
@@ -442,7 +491,8 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   const size_t groups = p.flat ? 512 : 256;
   p.splits = std::max<size_t>(1, std::min(groups / (across * along), p.vp / 256));
   if (p.flat) p.tiles = (vocab + GemmFlat::M - 1) / GemmFlat::M;
-  p.keep = grad && dim >= (dtype == DFX_F32 ? kKeepDimF32 : kKeepDim);
+  const bool long_rows = dim >= (dtype == DFX_F32 ? kKeepDimF32 : kKeepDim);
+  p.keep = grad && (p.flat || long_rows);
   p.split_rows = across * tile;
   const size_t across256 = p.rp / 256, along256 = up(dim, 256) / 256;
   size_t at = 0;
@@ -454,7 +504,7 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   p.x = take(planes * p.rp * p.dp * 2);
   p.w = take(planes * most * p.dp * 2);
   p.dz = grad ? take(planes * dz_rows * 2) : at;
-  p.z = p.keep ? take(dz_rows * 4) : at;
+  p.z = grad ? take((long_rows ? dz_rows : kTileRows * most) * 4) : at;
   p.dx = grad ? take(std::max(256 / along256, across256) * 256 * p.dq * 4) : at;
   p.bytes = at;
   return p;
@@ -465,7 +515,7 @@ int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s
   s.mtiles = (uint32_t)(few ? (m + GemmFlat::M - 1) / GemmFlat::M : (m + GemmWide::M - 1) / GemmWide::M);
   s.ntiles = (uint32_t)(few ? (n + GemmFlat::N - 1) / GemmFlat::N : (n + GemmWide::N - 1) / GemmWide::N);
   if (!s.mtiles || !s.ntiles) return DFX_OK;
-  if (few) return step_launch(dfx_gemm_flat_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
+  if (few) return step_launch(dfx_gemm_flat_kernel<DT, TA, TB, EPI, TA && TB ? 2 : 3>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
   return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
 }
 
@@ -498,12 +548,15 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   uint16_t *x = (uint16_t*)(ws + p.x), *w = (uint16_t*)(ws + p.w), *dz = (uint16_t*)(ws + p.dz);
   float* dx = (float*)(ws + p.dx);
 
-  VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
-  VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, u.hidden_stride ? u.hidden_stride : u.dim, (const int32_t*)a.idx, (uint32_t)u.dim,
-                        (uint32_t)p.dp, x, p.rp * p.dp));
+  const size_t hs = u.hidden_stride ? u.hidden_stride : u.dim;
+  if (p.flat) VOCAB_TRY(step_launch(dfx_vocab_few_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+  else {
+    VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
+    VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, hs, (const int32_t*)a.idx, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+  }
   // The weight is read where it lies if its rows are whole steps at multiples of 16 bytes; otherwise a piece at a time is laid out.
   const bool direct = DT != DFX_F32 && u.dim % kGemmK == 0 && (uintptr_t)u.weight % 16 == 0 && ws_stride * eb % 16 == 0;
-  const GemmOperand ox = {x, p.rp * p.dp, (uint32_t)p.dp, (uint32_t)p.rp, (uint32_t)p.dp};
+  const GemmOperand ox = {x, p.rp * p.dp, (uint32_t)p.dp, (uint32_t)p.split_rows, (uint32_t)p.dp};
   const size_t pieces = (u.vocab + p.vp - 1) / p.vp;
   GemmOperand ow = {};
   auto take_piece = [&](size_t v0, size_t left) -> int {
@@ -524,16 +577,17 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     const VocabStats epi = {a.parts, a.zt, v0 == last ? z : nullptr, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
     VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
   }
-  VOCAB_TRY(step_launch(dfx_vocab_join_kernel, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
+  if (p.flat) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
+  else VOCAB_TRY(step_launch(dfx_vocab_join_kernel<8>, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
   if (u.sums) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
   if (!u.grad_hidden && !u.grad_weight) return DFX_OK;
   for (size_t q = pieces; q-- != 0;) {   // the last one first
     const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
     if (direct || v0 != last) VOCAB_TRY(take_piece(v0, left));
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
-    if (z && v0 == last) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 4 + 255) / 256), 256, stream, epi, (const float*)z, count));
+    if (z && v0 == last) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, epi, (const float*)z, count));
     else VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
-    const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.rp, (uint32_t)p.vp};
+    const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
     const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false}, sw = {0, 0, 1, 0, count, true};
     const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != last};
     const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
