@@ -18,7 +18,7 @@ namespace {
 constexpr int kEmbedThreads = 256;
 constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / kStepWave, kSortChunks = 256, kSortChunk = 2048;      // chunks at most, places of one at least
 constexpr uint32_t kDigitBits = 10;      // at most
-constexpr uint32_t kSumMost = 64, kSumBlocks = 1024;      // places of a block of the sums at most; blocks, where they are fewer
+constexpr uint32_t kSumMost = 64, kSumBlocks = 512;      // places of a block of the sums at most; blocks, where they are fewer
 
 struct EmbedArgs {
   const int64_t* tokens;
@@ -42,7 +42,7 @@ __device__ __forceinline__ void part_take(const void* row, uint32_t e, uint32_t 
     for (int k = 0; k < N; ++k) v[k] = e + k < dim ? step_get<DT>(row, e + k) : 0.0f;
   }
 }
-template <int DT, int N>
+template <int DT, int N, bool STREAM = false>
 __device__ __forceinline__ void part_put(void* row, uint32_t e, uint32_t dim, const float* v) {
   if (e + N <= dim) {
     if constexpr (N * (DT == DFX_F32 ? 4 : 2) == 32) {
@@ -54,7 +54,8 @@ __device__ __forceinline__ void part_put(void* row, uint32_t e, uint32_t dim, co
     } else {
       StepVec<DT, N> a;
       a.put(v);
-      *(STEP_GLOBAL typename StepVec<DT, N>::words*)((STEP_GLOBAL typename StepElem<DT>::raw*)row + e) = a.w;
+      if (STREAM) a.stream(row, e);
+      else *(STEP_GLOBAL typename StepVec<DT, N>::words*)((STEP_GLOBAL typename StepElem<DT>::raw*)row + e) = a.w;
     }
   } else {
 #pragma unroll
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_kernel(EmbedArgs a) {
 #pragma unroll
       for (int k = 0; k < (int)N; ++k) v[k] = 0.0f;
     }
-    part_put<DT, N>(to, e, a.dim, v);
+    part_put<DT, N, true>(to, e, a.dim, v);
   }
 }
 
@@ -182,6 +183,103 @@ __global__ void __launch_bounds__(kSortThreads) dfx_embed_move_kernel(SortArgs a
   }
 }
 
+// The same in one launch where there are few places and not very many tokens: a workgroup has the tokens of one remainder by kOwners.  It looks at all places, counts those
+// of smaller remainders, which come first, keeps its own in LDS in their order, and sorts them by the quotient: places of a quotient are counted, and one wave moves them, 64
+// at a time.  The workgroups behind clear the table's gradient meanwhile.
+constexpr uint32_t kOwnMost = 16384, kOwnBits = 7, kOwners = 1u << kOwnBits, kOwnThreads = 1024, kOwnWaves = kOwnThreads / kStepWave, kOwnQuotients = 2 * kOwnThreads;
+
+template <int OUT>
+__device__ __forceinline__ void clear_row(void* out, size_t stride, uint32_t dim, uint32_t row) {
+  constexpr uint32_t N = 16 / sizeof(typename StepElem<OUT>::raw);
+  typename StepElem<OUT>::raw* at = (typename StepElem<OUT>::raw*)out + (size_t)row * stride;
+  float zero[N];
+#pragma unroll
+  for (int k = 0; k < (int)N; ++k) zero[k] = 0.0f;
+  for (uint32_t e = threadIdx.x * N; e < dim; e += blockDim.x * N) part_put<OUT, N, true>(at, e, dim, zero);
+}
+
+template <int OUT>
+__global__ void __launch_bounds__(kOwnThreads) dfx_embed_own_kernel(SortArgs a, void* out, size_t stride, uint32_t dim) {
+  constexpr uint32_t U = kOwnMost / kOwnThreads;
+  __shared__ uint16_t quotient[kOwnMost], place[kOwnMost];
+  __shared__ uint32_t bin[kOwnQuotients], sums[kOwnWaves];
+  __shared__ uint32_t counts[3][kOwnWaves];      // of smaller remainders, of this one, without a token
+  const uint32_t me = threadIdx.x, wave = me / kStepWave, lane = me % kStepWave;
+  if (blockIdx.x >= kOwners) {
+    for (uint32_t row = blockIdx.x - kOwners; row < a.vocab; row += gridDim.x - kOwners) clear_row<OUT>(out, stride, dim, row);
+    return;
+  }
+  bin[2u * me] = bin[2u * me + 1u] = 0;
+  // a wave has places that follow one another
+  const uint32_t each = ((a.n + kOwnWaves - 1u) / kOwnWaves + kStepWave - 1u) / kStepWave * kStepWave;
+  const uint32_t begin = min(a.n, wave * each), end = min(a.n, begin + each);
+  uint32_t t[U], smaller = 0, here = 0, none = 0;
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t i = begin + u * kStepWave + lane;
+    t[u] = i < end ? sort_take(a, i).x : ~0u;
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t own = t[u] < a.vocab ? t[u] % kOwners : kOwners;
+    smaller += (uint32_t)__popcll(__ballot(own < blockIdx.x));
+    here += (uint32_t)__popcll(__ballot(own == blockIdx.x));
+    none += (uint32_t)__popcll(__ballot(t[u] == a.vocab));
+  }
+  if (lane == 0) { counts[0][wave] = smaller; counts[1][wave] = here; counts[2][wave] = none; }
+  __syncthreads();
+  uint32_t base = 0, at = 0, all = 0, left = 0;
+  for (uint32_t w = 0; w < kOwnWaves; ++w) {
+    base += counts[0][w];
+    at += w < wave ? counts[1][w] : 0u;
+    all += counts[1][w];
+    left += counts[2][w];
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    const bool mine = t[u] < a.vocab && t[u] % kOwners == blockIdx.x;
+    const uint64_t mask = __ballot(mine);
+    if (mine) {
+      const uint32_t to = at + (uint32_t)__popcll(mask & ((1ull << lane) - 1ull));
+      quotient[to] = (uint16_t)(t[u] / kOwners);
+      place[to] = (uint16_t)(begin + u * kStepWave + lane);
+      atomicAdd(&bin[t[u] / kOwners], 1u);
+    }
+    at += (uint32_t)__popcll(mask);
+  }
+  __syncthreads();
+  const uint32_t one = bin[2u * me], two = one + bin[2u * me + 1u];
+  uint32_t sum = two;
+#pragma unroll
+  for (uint32_t d = 1; d < kStepWave; d <<= 1) {
+    const uint32_t more = __shfl_up(sum, d);
+    if (lane >= d) sum += more;
+  }
+  if (lane == kStepWave - 1u) sums[wave] = sum;
+  __syncthreads();
+  uint32_t before = base + sum - two;
+  for (uint32_t w = 0; w < wave; ++w) before += sums[w];
+  bin[2u * me] = before; bin[2u * me + 1u] = before + one;
+  __syncthreads();
+  if (wave == 0)
+    for (uint32_t first = 0; first < all; first += kStepWave) {
+      const uint32_t i = first + lane, q = i < all ? quotient[i] : 0u;
+      uint64_t same = __ballot(i < all);
+#pragma unroll
+      for (uint32_t b = 0; b < 11; ++b) {
+        const uint64_t set = __ballot((q >> b) & 1u);
+        same &= (q >> b) & 1u ? set : ~set;
+      }
+      if (i < all) {
+        const uint32_t to = bin[q];
+        a.to[to + (uint32_t)__popcll(same & ((1ull << lane) - 1ull))] = make_uint2(q << kOwnBits | blockIdx.x, place[i]);
+        if (lane == (uint32_t)__ffsll((long long)same) - 1u) bin[q] = to + (uint32_t)__popcll(same);      // (behind every lane's read)
+      }
+    }
+  if (blockIdx.x == 0)                   // behind all tokens: as many places without one
+    for (uint32_t i = me; i < left; i += kOwnThreads) a.to[a.n - 1u - i] = make_uint2(a.vocab, 0u);
+}
+
 // ------------------------------------------------------------------------------------------
 // sums along the sorted places
 // ------------------------------------------------------------------------------------------
@@ -216,7 +314,7 @@ __device__ __forceinline__ void sum_put(const SumArgs& a, uint32_t token, uint32
 template <int DT, int OUT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_sum_kernel(SumArgs a) {
   typedef typename StepElem<DT>::raw raw;
-  constexpr int N = 16 / (int)sizeof(raw), U = 4;
+  constexpr int N = 16 / (int)sizeof(raw), U = 8;
   const uint32_t b = blockIdx.x * (kEmbedThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
   const uint32_t e = (blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1u))) * N;
   if (b >= a.blocks || e >= a.dim) return;
@@ -273,23 +371,106 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_join_kernel(SumArgs a
   if (a.sorted[begin].x == token && begin > 0 && a.sorted[begin - 1u].x == token) return;      // (began before)
   float s[N];
   part_take<DFX_F32, N>(a.part + ((size_t)b * 2u + 1u) * a.dim, e, a.dim, s);
-  for (uint32_t c = b + 1u; c < a.blocks && a.sorted[c * a.block].x == token; ++c) {
-    float v[N];
-    part_take<DFX_F32, N>(a.part + (size_t)c * 2u * a.dim, e, a.dim, v);
+  constexpr uint32_t U = 16;             // blocks at once
+  bool on = true;
+  for (uint32_t c = b + 1u; on; c += U) {
+    bool has[U];
+    float v[U][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) s[k] += v[k];
+    for (uint32_t u = 0; u < U; ++u) has[u] = c + u < a.blocks && a.sorted[(size_t)(c + u) * a.block].x == token;
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (has[u]) part_take<DFX_F32, N>(a.part + (size_t)(c + u) * 2u * a.dim, e, a.dim, v[u]);
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (has[u])
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] += v[u][k];
+    on = has[U - 1u];
   }
   sum_put<OUT, N>(a, token, e, s);
 }
 
+// ------------------------------------------------------------------------------------------
+// few places: no sort.  A workgroup finds the places of its rows of the table among all of them, in their order.  Onto the gradient that is there: a workgroup to a
+// place, which does nothing if its token stood before; otherwise a workgroup to eight rows of the table.
+// ------------------------------------------------------------------------------------------
+constexpr uint32_t kFewPlaces = 512, kFewTable = 8;
+
+template <int DT, int OUT>
+__global__ void __launch_bounds__(kEmbedThreads) dfx_embed_few_kernel(SumArgs a, const int64_t* tokens) {
+  typedef typename StepElem<DT>::raw raw;
+  constexpr int N = 16 / (int)sizeof(raw), U = 64 / N;
+  constexpr uint32_t W = kFewPlaces / kStepWave, R = kFewPlaces / kEmbedThreads;      // groups of 64 places; a thread's places
+  __shared__ uint32_t place[kFewPlaces], counts[kFewTable][W], start[kFewTable + 1];
+  const uint32_t me = threadIdx.x, lane = me % kStepWave;
+  int64_t first = (int64_t)blockIdx.x * kFewTable;
+  uint32_t table = kFewTable;
+  if (a.accumulate) {
+    first = tokens[blockIdx.x]; table = 1;
+    if (first < 0 || first >= (int64_t)a.vocab) return;
+  }
+  uint64_t same[R];                      // lanes whose places have this one's token
+  uint32_t row[R];
+  bool stood = false;
+#pragma unroll
+  for (uint32_t r = 0; r < R; ++r) {
+    const uint32_t i = r * kEmbedThreads + me;
+    const int64_t t = i < a.n ? tokens[i] : -1;
+    row[r] = t >= first && t < first + table && t < (int64_t)a.vocab ? (uint32_t)(t - first) : kFewTable;
+    stood = stood || (a.accumulate && row[r] < kFewTable && i < blockIdx.x);
+    for (uint32_t q = 0; q < table; ++q) {
+      const uint64_t mask = __ballot(row[r] == q);
+      if (row[r] == q) same[r] = mask;
+      if (lane == 0) counts[q][i / kStepWave] = (uint32_t)__popcll(mask);
+    }
+  }
+  if (__syncthreads_or(stood)) return;
+  if (me <= table) {
+    uint32_t before = 0;
+    for (uint32_t q = 0; q < me; ++q)
+      for (uint32_t w = 0; w < W; ++w) before += counts[q][w];
+    start[me] = before;
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t r = 0; r < R; ++r)
+    if (row[r] < kFewTable) {
+      uint32_t to = start[row[r]] + (uint32_t)__popcll(same[r] & ((1ull << lane) - 1ull));
+      for (uint32_t w = 0; w < (r * kEmbedThreads + me) / kStepWave; ++w) to += counts[row[r]][w];
+      place[to] = r * kEmbedThreads + me;
+    }
+  __syncthreads();
+  for (uint32_t q = 0; q < table; ++q) {
+    const int64_t v = first + q;
+    if (v >= (int64_t)a.vocab) return;
+    const uint32_t begin = start[q], end = start[q + 1];
+    for (uint32_t e = me * N; e < a.dim; e += kEmbedThreads * N) {
+      float s[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) s[k] = 0.0f;
+      for (uint32_t i = begin; i < end; i += U) {
+        float x[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (i + u < end) part_take<DT, N>((const raw*)a.grad + (size_t)place[i + u] * a.grad_stride, e, a.dim, x[u]);
+          else
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[u][k] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < N; ++k) s[k] += x[u][k];
+      }
+      sum_put<OUT, N>(a, (uint32_t)v, e, s);
+    }
+  }
+}
+
 template <int OUT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_clear_kernel(void* out, size_t stride, uint32_t dim) {
-  constexpr uint32_t N = 16 / sizeof(typename StepElem<OUT>::raw);
-  typename StepElem<OUT>::raw* row = (typename StepElem<OUT>::raw*)out + (size_t)blockIdx.x * stride;
-  float zero[N];
-#pragma unroll
-  for (int k = 0; k < (int)N; ++k) zero[k] = 0.0f;
-  for (uint32_t e = threadIdx.x * N; e < dim; e += kEmbedThreads * N) part_put<OUT, N>(row, e, dim, zero);
+  clear_row<OUT>(out, stride, dim, blockIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -393,23 +574,40 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
   if (meet(out, tokens) || meet(out, grad) || meet(out, work) || meet(work, tokens) || meet(work, grad)) return DFX_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)hip_stream;
   unsigned char* ws = (unsigned char*)u->workspace;
-  if (!u->accumulate) {
+  SumArgs a;
+  memset(&a, 0, sizeof(a));
+  a.grad = u->grad; a.out = u->table_grad; a.part = (float*)(ws + p.part); a.grad_stride = gs; a.out_stride = os;
+  a.n = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.vocab = (uint32_t)u->vocab; a.block = p.block; a.blocks = p.blocks; a.scale = (float)u->scale; a.accumulate = u->accumulate != 0;
+  if (u->rows && u->rows <= kFewPlaces) {
+    const dim3 grid(u->accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable));
+    const bool wide = u->out_dtype == DFX_F32;
+    auto k = u->dtype == DFX_F32 ? dfx_embed_few_kernel<DFX_F32, DFX_F32> : u->dtype == DFX_BF16 ? (wide ? dfx_embed_few_kernel<DFX_BF16, DFX_F32> : dfx_embed_few_kernel<DFX_BF16, DFX_BF16>)
+                                                                        : (wide ? dfx_embed_few_kernel<DFX_F16, DFX_F32> : dfx_embed_few_kernel<DFX_F16, DFX_F16>);
+    return step_launch(k, grid, kEmbedThreads, s, a, u->tokens);
+  }
+  uint2* pairs[2] = {(uint2*)(ws + p.pairs[0]), (uint2*)(ws + p.pairs[1])};
+  const bool few = u->rows && u->rows <= kOwnMost && u->vocab <= (size_t)kOwnQuotients * kOwners;
+  if (few) {
+    auto k = u->out_dtype == DFX_F32 ? dfx_embed_own_kernel<DFX_F32> : u->out_dtype == DFX_BF16 ? dfx_embed_own_kernel<DFX_BF16> : dfx_embed_own_kernel<DFX_F16>;
+    const SortArgs x = {u->tokens, nullptr, pairs[0], nullptr, (uint32_t)u->rows, (uint32_t)u->vocab, 0, 0, 0};
+    const int rc = step_launch(k, dim3(kOwners + (u->accumulate ? 0u : (uint32_t)std::min<size_t>(u->vocab, 4096))), kOwnThreads, s, x, u->table_grad, os, (uint32_t)u->dim);
+    if (rc != DFX_OK) return rc;
+    a.sorted = pairs[0];
+  } else if (!u->accumulate) {
     auto k = u->out_dtype == DFX_F32 ? dfx_embed_clear_kernel<DFX_F32> : u->out_dtype == DFX_BF16 ? dfx_embed_clear_kernel<DFX_BF16> : dfx_embed_clear_kernel<DFX_F16>;
     const int rc = step_launch(k, dim3((uint32_t)u->vocab), kEmbedThreads, s, u->table_grad, os, (uint32_t)u->dim);
     if (rc != DFX_OK) return rc;
   }
   if (!u->rows) return DFX_OK;
-  uint2* pairs[2] = {(uint2*)(ws + p.pairs[0]), (uint2*)(ws + p.pairs[1])};
-  for (uint32_t k = 0; k < p.passes; ++k) {
-    const SortArgs a = {k ? nullptr : u->tokens, k ? pairs[(k - 1) & 1] : nullptr, pairs[k & 1], (uint32_t*)(ws + p.counts), (uint32_t)u->rows, (uint32_t)u->vocab, p.chunk, k * p.bits, p.bits};
-    int rc = step_launch(dfx_embed_count_kernel, dim3(p.chunks), kSortThreads, s, a);
-    if (rc == DFX_OK) rc = step_launch(dfx_embed_move_kernel, dim3(p.chunks), kSortThreads, s, a);
-    if (rc != DFX_OK) return rc;
+  if (!few) {
+    for (uint32_t k = 0; k < p.passes; ++k) {
+      const SortArgs x = {k ? nullptr : u->tokens, k ? pairs[(k - 1) & 1] : nullptr, pairs[k & 1], (uint32_t*)(ws + p.counts), (uint32_t)u->rows, (uint32_t)u->vocab, p.chunk, k * p.bits, p.bits};
+      int rc = step_launch(dfx_embed_count_kernel, dim3(p.chunks), kSortThreads, s, x);
+      if (rc == DFX_OK) rc = step_launch(dfx_embed_move_kernel, dim3(p.chunks), kSortThreads, s, x);
+      if (rc != DFX_OK) return rc;
+    }
+    a.sorted = pairs[(p.passes - 1) & 1];
   }
-  SumArgs a;
-  memset(&a, 0, sizeof(a));
-  a.sorted = pairs[(p.passes - 1) & 1]; a.grad = u->grad; a.out = u->table_grad; a.part = (float*)(ws + p.part); a.grad_stride = gs; a.out_stride = os;
-  a.n = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.vocab = (uint32_t)u->vocab; a.block = p.block; a.blocks = p.blocks; a.scale = (float)u->scale; a.accumulate = u->accumulate != 0;
   if (u->dtype == DFX_F32) return embed_sums<DFX_F32, DFX_F32>(a, s);
   if (u->dtype == DFX_BF16) return u->out_dtype == DFX_F32 ? embed_sums<DFX_BF16, DFX_F32>(a, s) : embed_sums<DFX_BF16, DFX_BF16>(a, s);
   return u->out_dtype == DFX_F32 ? embed_sums<DFX_F16, DFX_F32>(a, s) : embed_sums<DFX_F16, DFX_F16>(a, s);

@@ -78,9 +78,7 @@ __device__ __forceinline__ void* row_of(void* p, size_t stride, uint32_t row) { 
 template <int T, int THREADS, int NUM>
 __device__ __forceinline__ void row_sum(float (&s)[NUM], float (*lds)[2][THREADS / kStepWave], uint32_t& turn) {
 #pragma unroll
-  for (int d = kStepWave / 2; d; d >>= 1)
-#pragma unroll
-    for (int q = 0; q < NUM; ++q) s[q] += __shfl_xor(s[q], d);
+  for (int q = 0; q < NUM; ++q) s[q] = wave_sum(s[q]);
   if constexpr (T > kStepWave) {
     constexpr int W = T / kStepWave;
     const uint32_t wave = threadIdx.x / kStepWave;
@@ -140,71 +138,122 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_kernel(NormArgs a)
   }
 }
 
-// The same for the gradients.  A thread's columns are the same in every row, so that the sums over rows stay in its registers.
+// A row as it is loaded: U vectors a thread, the last of them perhaps of fewer elements.
 template <int DT, int T, int U>
-__global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_grad_kernel(NormArgs a) {
-  constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+struct NormRow {
+  static constexpr int N = 16 / (int)sizeof(typename StepElem<DT>::raw);
+  StepVec<DT, N> r[U];
+  __device__ __forceinline__ void take(const void* row, uint32_t me, uint32_t dim) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t e = (u * T + me) * N;
+      if (e + N <= dim) r[u].load(row, e);
+      else {
+        float v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = e + k < dim ? step_get<DT>(row, e + k) : 0.0f;
+        r[u].put(v);                     // (values of the type: nothing is rounded)
+      }
+    }
+  }
+  __device__ __forceinline__ void again() {
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u].again();
+  }
+};
+
+// The same for the gradients.  A thread's columns are the same in every row, so that the weight and the sums over rows stay in its registers, and the next
+// row is on its way while one is worked on.  With d = x - mean, mean(g h) = r mean(g d): two rounds of sums over a row, (x, g) and (d^2, g d).
+// That takes 128 registers of workgroups of 512, two to a compute unit; rows above 8192 16-bit elements (4096 of 32 bits) have a workgroup of 1024, and no room for either (AHEAD).
+template <int DT, int T, int U, int THREADS, bool AHEAD>
+__global__ void __launch_bounds__(THREADS, 4) dfx_norm_grad_kernel(NormArgs a) {
+  constexpr int ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
   __shared__ float lds[2][2][THREADS / kStepWave];
-  const uint32_t me = threadIdx.x % T, sub = threadIdx.x / T;
+  const uint32_t me = threadIdx.x % T, sub = threadIdx.x / T, step = gridDim.x * ROWS;
+  const float per = 1.0f / (float)a.dim;
   uint32_t turn = 0;
-  float dw[U][N], db[U][N];
+  float dw[U][N], db[U][N], w[U][N];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < U; ++u) {
+    const uint32_t e = (u * T + me) * N;
 #pragma unroll
-    for (int k = 0; k < N; ++k) dw[u][k] = db[u][k] = 0.0f;
-  for (uint32_t row0 = blockIdx.x * ROWS; row0 < a.rows; row0 += gridDim.x * ROWS) {
-    const uint32_t row = row0 + sub;
-    if (ROWS > 1 && row >= a.rows) break;  // (a wave or more of one)
-    const void *x = row_of<DT>(a.x, a.x_stride, row), *dy = row_of<DT>(a.dy, a.dy_stride, row);
-    float v[U][N], g[U][N], s[1] = {0.0f};
+    for (int k = 0; k < N; ++k) dw[u][k] = db[u][k] = w[u][k] = 0.0f;
+    if (AHEAD && e < a.dim) param_take<DT, N>(a.weight, a.param_f32, e, a.dim, w[u], 1.0f);
+  }
+  auto weights = [&](int u, float* v) {
+    const uint32_t e = (u * T + me) * N;
 #pragma unroll
-    for (int u = 0; u < U; ++u) row_take<DT, N>(x, (u * T + me) * N, a.dim, v[u], 0.0f);
+    for (int k = 0; k < N; ++k) v[k] = w[u][k];
+    if (!AHEAD && e < a.dim) param_take<DT, N>(a.weight, a.param_f32, e, a.dim, v, 1.0f);
+    if (!AHEAD) __builtin_amdgcn_sched_barrier(0);      // (one vector's at a time)
+  };
+  NormRow<DT, T, U> x, y;
+  uint32_t row = blockIdx.x * ROWS + sub;
+  if (AHEAD && row < a.rows) {
+    x.take(row_of<DT>(a.x, a.x_stride, row), me, a.dim);
+    y.take(row_of<DT>(a.dy, a.dy_stride, row), me, a.dim);
+  }
+  for (uint32_t row0 = blockIdx.x * ROWS; row0 < a.rows; row0 += step, row += step) {      // (all of the workgroup as often)
+    const bool any = row < a.rows, more = AHEAD && row < a.rows && a.rows - row > step;
+    NormRow<DT, T, U> x1, y1;
+    if (more) {
+      x1.take(row_of<DT>(a.x, a.x_stride, row + step), me, a.dim);
+      y1.take(row_of<DT>(a.dy, a.dy_stride, row + step), me, a.dim);
+    }
+    if (!AHEAD && any) {
+      x.take(row_of<DT>(a.x, a.x_stride, row), me, a.dim);
+      y.take(row_of<DT>(a.dy, a.dy_stride, row), me, a.dim);
+    }
+    float s[2] = {0.0f, 0.0f};
+    if (any)
 #pragma unroll
-    for (int u = 0; u < U; ++u) row_take<DT, N>(dy, (u * T + me) * N, a.dim, g[u], 0.0f);
+      for (int u = 0; u < U; ++u) {
+        float wu[N];
+        weights(u, wu);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < N; ++k) s[0] += v[u][k];
-    row_sum<T, THREADS, 1>(s, lds, turn);
-    const float mean = s[0] / (float)a.dim;
-    s[0] = 0.0f;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        v[u][k] = (u * T + me) * N + k < a.dim ? v[u][k] - mean : 0.0f;
-        s[0] = fmaf(v[u][k], v[u][k], s[0]);
+        for (int k = 0; k < N; ++k) {
+          s[0] += x.r[u].get(k);
+          s[1] = fmaf(y.r[u].get(k), wu[k], s[1]);
+        }
       }
-    row_sum<T, THREADS, 1>(s, lds, turn);
-    const float r = 1.0f / sqrtf(s[0] / (float)a.dim + a.eps);
-    float c[2] = {0.0f, 0.0f};
+    row_sum<T, THREADS, 2>(s, lds, turn);
+    const float mean = s[0] * per, c0 = s[1] * per;
+    x.again(); y.again();
+    s[0] = s[1] = 0.0f;
+    if (any)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t e = (u * T + me) * N;
-      float w[N];
-      if (e < a.dim) param_take<DT, N>(a.weight, a.param_f32, e, a.dim, w, 1.0f);
+      for (int u = 0; u < U; ++u) {
+        float wu[N];
+        weights(u, wu);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        v[u][k] *= r;
-        dw[u][k] = fmaf(g[u][k], v[u][k], dw[u][k]);
-        db[u][k] += g[u][k];
-        if (e < a.dim) g[u][k] *= w[k];
-        c[0] += g[u][k];
-        c[1] = fmaf(g[u][k], v[u][k], c[1]);
+        for (int k = 0; k < N; ++k) {
+          const float d = (u * T + me) * N + k < a.dim ? x.r[u].get(k) - mean : 0.0f;
+          s[0] = fmaf(d, d, s[0]);
+          s[1] = fmaf(y.r[u].get(k) * wu[k], d, s[1]);
+        }
+      }
+    row_sum<T, THREADS, 2>(s, lds, turn);
+    const float r = 1.0f / sqrtf(s[0] * per + a.eps), c1 = s[1] * per * r;
+    x.again(); y.again();
+    if (any) {
+      void* dx = a.dx ? row_of<DT>(a.dx, a.dx_stride, row) : nullptr;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t e = (u * T + me) * N;
+        float wu[N];
+        weights(u, wu);
+        float out[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float h = (x.r[u].get(k) - mean) * r, dy = y.r[u].get(k);
+          dw[u][k] = fmaf(dy, h, dw[u][k]);
+          db[u][k] += dy;
+          out[k] = r * (fmaf(dy, wu[k], -c0) - h * c1);
+        }
+        if (dx && e < a.dim) row_put<DT, N>(dx, e, a.dim, out);
       }
     }
-    if (!a.dx) continue;                 // (all alike)
-    row_sum<T, THREADS, 2>(c, lds, turn);
-    c[0] /= (float)a.dim; c[1] /= (float)a.dim;
-    void* dx = row_of<DT>(a.dx, a.dx_stride, row);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t e = (u * T + me) * N;
-      if (e >= a.dim) break;
-#pragma unroll
-      for (int k = 0; k < N; ++k) g[u][k] = r * (g[u][k] - c[0] - v[u][k] * c[1]);
-      row_put<DT, N>(dx, e, a.dim, g[u]);
-    }
+    if (more) { x = x1; y = y1; }
   }
   if (!a.part) return;
   // the rows of a workgroup at once: one behind the other through LDS
@@ -229,16 +278,22 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_grad_kernel(NormAr
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const uint32_t e = (u * T + me) * N;
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (e + k < a.dim) { part[e + k] = dw[u][k]; part[a.dim + e + k] = db[u][k]; }
+    if (e < a.dim) {
+      row_put<DFX_F32, 4>(part, e, a.dim, dw[u]);
+      row_put<DFX_F32, 4>(part + a.dim, e, a.dim, db[u]);
+      if constexpr (N == 8)
+        if (e + 4u < a.dim) {
+          row_put<DFX_F32, 4>(part, e + 4u, a.dim, dw[u] + 4);
+          row_put<DFX_F32, 4>(part + a.dim, e + 4u, a.dim, db[u] + 4);
+        }
+    }
   }
 }
 
-// The workgroups' shares of a column, in their order: 32 columns of a workgroup, 8 threads to each.
+// The workgroups' shares of a column, in their order: 32 columns of a workgroup, 32 threads to each.
 template <int OUT>
-__global__ void __launch_bounds__(256) dfx_norm_sums_kernel(const float* part, uint32_t groups, uint32_t dim, void* grad_weight, void* grad_bias, bool accumulate) {
-  __shared__ float lds[8][32];
+__global__ void __launch_bounds__(1024) dfx_norm_sums_kernel(const float* part, uint32_t groups, uint32_t dim, void* grad_weight, void* grad_bias, bool accumulate) {
+  __shared__ float lds[32][32];
   const uint32_t i = threadIdx.x % 32u, slice = threadIdx.x / 32u, col = blockIdx.x * 32u + i;
   const bool bias = blockIdx.y != 0;
   void* to = bias ? grad_bias : grad_weight;
@@ -246,14 +301,14 @@ __global__ void __launch_bounds__(256) dfx_norm_sums_kernel(const float* part, u
   float s = 0.0f;
   if (col < dim) {
     const float* p = part + (bias ? dim : 0u) + col;
-    const uint32_t each = (groups + 7u) / 8u, end = min((slice + 1u) * each, groups);
+    const uint32_t each = (groups + 31u) / 32u, end = min((slice + 1u) * each, groups);
 #pragma unroll 8
     for (uint32_t g = slice * each; g < end; ++g) s += p[(size_t)g * 2u * dim];
   }
   lds[slice][i] = s;
   __syncthreads();
   if (slice || col >= dim) return;
-  for (int k = 1; k < 8; ++k) s += lds[k][i];
+  for (int k = 1; k < 32; ++k) s += lds[k][i];
   if (accumulate) s += step_get<OUT>(to, col);
   step_put<OUT>(to, col, s);
 }
@@ -281,16 +336,16 @@ template <int DT>
 int norm_grad_launch(const NormArgs& a, uint32_t groups, hipStream_t s) {
   constexpr uint32_t N = 16 / (DT == DFX_F32 ? 4 : 2);
   const uint32_t nvec = (a.dim + N - 1) / N;
-#define NORM(T, U) return step_launch(dfx_norm_grad_kernel<DT, T, U>, dim3(groups), T < 256 ? 256 : T, s, a)
-  if (nvec <= 64) NORM(64, 1);
-  if (nvec <= 128) NORM(64, 2);
-  if (nvec <= 256) NORM(256, 1);
-  if (nvec <= 512) NORM(256, 2);
-  if (nvec <= 1024) NORM(256, 4);
-  if (nvec <= 2048) NORM(1024, 2);
+#define NORM(T, U, THREADS) return step_launch(dfx_norm_grad_kernel<DT, T, U, THREADS, (U < 4)>, dim3(groups), THREADS, s, a)
+  if (nvec <= 64) NORM(64, 1, 256);
+  if (nvec <= 128) NORM(128, 1, 256);
+  if (nvec <= 256) NORM(256, 1, 256);
+  if (nvec <= 512) NORM(512, 1, 512);
+  if (nvec <= 1024) NORM(1024, 1, 1024);
+  if (nvec <= 2048) NORM(1024, 2, 1024);
   if constexpr (DT == DFX_F32)
-    if (nvec > 4096) NORM(1024, 8);
-  NORM(1024, 4);
+    if (nvec > 4096) NORM(1024, 8, 1024);
+  NORM(1024, 4, 1024);
 #undef NORM
 }
 
@@ -368,7 +423,7 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* u, void* hip_stream) {
   if (!sums) return DFX_OK;
   const dim3 grid((a.dim + 31u) / 32u, 2);
   auto k = u->grad_dtype == DFX_F32 ? dfx_norm_sums_kernel<DFX_F32> : u->grad_dtype == DFX_BF16 ? dfx_norm_sums_kernel<DFX_BF16> : dfx_norm_sums_kernel<DFX_F16>;
-  return step_launch(k, grid, 256, s, (const float*)a.part, groups, a.dim, u->grad_weight, u->grad_bias, u->accumulate != 0);
+  return step_launch(k, grid, 1024, s, (const float*)a.part, groups, a.dim, u->grad_weight, u->grad_bias, u->accumulate != 0);
 }
 
 }  // extern "C"

@@ -147,6 +147,20 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int d = kStepWave / 2; d; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
+// A sum over the wave's lanes for all of them, by moves between lanes that need no LDS: within rows of 16, then a row's total into the next, then half a wave's.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float lanes_add(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = lanes_add<0x111, 0xf>(v);          // from 1, 2, 4, 8 lanes before
+  v = lanes_add<0x112, 0xf>(v);
+  v = lanes_add<0x114, 0xf>(v);
+  v = lanes_add<0x118, 0xf>(v);
+  v = lanes_add<0x142, 0xa>(v);          // the last lane of a row, to all of the next
+  v = lanes_add<0x143, 0xc>(v);          // of the first half, to all of the second
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 #pragma unroll
   for (int d = kStepWave / 2; d; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
