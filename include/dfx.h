@@ -578,7 +578,7 @@ int dfx_policy_loss(const dfx_policy_loss_args* args, void* hip_stream);
  * from a matrix's first to its last row counts as that matrix's.
  * Tokens and targets outside [0, vocab) stand for none: padding, a prompt.
  * Errors of all: INVALID_ARG (NULL or misaligned memory, types, strides, overlap, workspace too small, numbers that are not finite in 32 bits), TOO_LARGE
- * (rows or vocab of 2^31 - 2^10 and more, dim or a stride of 2^20 and more, memory beyond 2^62 bytes), HIP.
+ * (rows or vocab of 2^31 - 2^10 and more, dim or a stride of 2^20 and more; what else a call says), HIP.
  */
 
 /* out[i] = scale * table[tokens[i]]; zeros where there is no token. */
@@ -620,7 +620,7 @@ int dfx_embed_grad(const dfx_embed_grad_args* args, void* hip_stream);
 
 /*
  * Layer norm of rows: h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps);  y = h weight + bias.  y may take x's place (same memory and stride).
- * A row with an infinity or NaN is NaN.
+ * A row with an infinity or NaN is NaN.  TOO_LARGE above 32768 elements of a row.
  */
 typedef struct {
   uint32_t struct_bytes;
@@ -672,8 +672,8 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* args, void* hip_stream);
  *   logp = log softmax(z)[target];  loss = -row_weight logp;  dz = scale inv_temperature row_weight (softmax(z) - [j = target])
  *   grad_hidden = dz weight;  grad_weight = dz^T hidden
  * The products are made on the matrix cores in pieces of the vocabulary, and their sums in 32 bits; 32-bit inputs are taken as three terms of 8 bits of
- * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time, piece by piece, and dz is rounded
- * to the type of the inputs on its way into the products (32-bit inputs: to three such terms).
+ * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time, piece by piece (but for those of the last piece, which are
+ * kept where that takes less time), and dz is rounded to the type of the inputs on its way into the products (32-bit inputs: to three such terms).
  * A row of weight 0 or without a target has nothing to learn from: it takes no part in the products, its hidden state is not looked at, its
  * logp, loss and grad_hidden are 0.  So has a row with no logit above -infinity.  A logit of NaN or +infinity makes its row NaN, and with it
  * grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of rows are finite.
@@ -699,11 +699,11 @@ typedef struct {
   void* grad_weight;         /* may be NULL */
   size_t grad_weight_stride;
   double inv_temperature;    /* > 0, and 1.45 times it a normal number in 32 bits */
-  size_t piece;              /* rows of weight whose dz is held at a time, a multiple of 256; 0 = the library's choice */
+  size_t piece;              /* rows of weight whose dz is held at a time (at most 2^22), a multiple of 256; 0 = the library's choice: 2^28 elements of dz, 65536 rows */
   void* workspace;           /* dfx_vocab_loss_workspace bytes, 256-byte aligned */
   size_t workspace_bytes;
 } dfx_vocab_loss_args;
-/* grad: whether a gradient is asked for.  A call of fewer rows has room in it as well. */
+/* grad: whether a gradient is asked for.  A call of fewer rows has room in it as well.  0 for what is refused. */
 size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece);
 int dfx_vocab_loss(const dfx_vocab_loss_args* args, void* hip_stream);
 

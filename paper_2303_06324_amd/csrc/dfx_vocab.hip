@@ -26,7 +26,7 @@ constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
 constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles (at most 256: dfx_vocab_few_kernel has a thread for each)
-constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536;
+constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
 constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
 // what is known of a call on the device; first in the workspace
@@ -480,7 +480,8 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   p.dq = up(dim, 4);
   p.tiles = (vocab + kTileRows - 1) / kTileRows;
   const size_t whole = std::max(kTileRows, p.tiles * kTileRows);
-  size_t most = std::min(whole, piece ? piece : kPieceMost), dz_rows = p.rp * most;
+  const size_t most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceMost);
+  size_t dz_rows = p.rp * most;
   p.vp = most;
   if (!piece) {                          // pieces of equal length
     const size_t length = std::min(most, std::max(kPieceLeast, kPieceElems / p.rp / kTileRows * kTileRows)), pieces = (whole + length - 1) / length;
@@ -607,13 +608,17 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
 
 constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
 
+// tiles of rows by the vocabulary are counted in 32 bits
+bool vocab_too_large(const VocabPlan& p) { return p.rp / GemmFlat::N > (1ull << 31) / std::max<size_t>(p.tiles, 1); }
+
 }  // namespace
 
 extern "C" {
 
 size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece) {
   if (rows >= kMostRows || vocab >= kMostRows || dim >= kMostStride || piece % kTileRows) return 0;
-  return vocab_plan(rows, dim, vocab, dtype, grad != 0, piece).bytes;
+  const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, grad != 0, piece);
+  return vocab_too_large(p) ? 0 : p.bytes;
 }
 
 int dfx_vocab_loss(const dfx_vocab_loss_args* u, void* hip_stream) {
@@ -635,6 +640,7 @@ int dfx_vocab_loss(const dfx_vocab_loss_args* u, void* hip_stream) {
   for (const void* p : {(const void*)u->row_weight, (const void*)u->scale, (const void*)u->logp, (const void*)u->loss, (const void*)u->sums})
     if ((uintptr_t)p % 4) return DFX_ERR_INVALID_ARG;
   const VocabPlan p = vocab_plan(u->rows, u->dim, u->vocab, u->dtype, u->grad_hidden || u->grad_weight, u->piece);
+  if (vocab_too_large(p)) return DFX_ERR_TOO_LARGE;
   if (!u->workspace || (uintptr_t)u->workspace % 256 || u->workspace_bytes < p.bytes) return DFX_ERR_INVALID_ARG;
   auto matrix = [](const void* at, size_t rows, size_t stride, size_t dim, size_t bytes) { return flat(at, rows ? ((rows - 1) * stride + dim) * bytes : 0); };
   const Span reads[] = {matrix(u->hidden, u->rows, hs, u->dim, eb), matrix(u->weight, u->vocab, ws, u->dim, eb), flat(u->targets, 8 * u->rows), flat(u->row_weight, 4 * u->rows), flat(u->scale, 4)};
