@@ -38,6 +38,7 @@ struct GemmOperand {
 struct GemmShape {
   uint32_t mtiles, ntiles, splits;       // workgroups; splits along k
   uint32_t ksteps;                       // (or of what count says)
+  uint32_t height;                       // rows of m from one tile to the next, where they are not all of a tile; otherwise 0
   const uint32_t* count;                 // device, may be null: what it holds bounds n (n_counted), or k
   bool k_counted;
 };
@@ -165,6 +166,28 @@ __device__ __forceinline__ GemmAcc gemm_mac(GemmShort8 a, GemmShort8 b, GemmAcc 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(GemmBf16x8, a), __builtin_bit_cast(GemmBf16x8, b), c, 0, 0, 0);
 }
 
+// The three planes of two 32-bit values, side by side in a word each, every one the nearest bf16 to what is left (the largest values' first: the largest bf16, where the
+// nearest would be infinite).  Of an infinity or NaN one of them is NaN.
+__device__ __forceinline__ void gemm_cut(float x, float y, uint32_t* part) {
+  const float most = 3.3895313892515355e38f;
+  StepPair v = {__builtin_amdgcn_fmed3f(x, -most, most), __builtin_amdgcn_fmed3f(y, -most, most)};
+  part[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, StepBf16Pair));
+  v[0] = x - __uint_as_float(part[0] << 16); v[1] = y - __uint_as_float(part[0] & 0xffff0000u);
+  part[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, StepBf16Pair));
+  v[0] -= __uint_as_float(part[1] << 16); v[1] -= __uint_as_float(part[1] & 0xffff0000u);
+  part[2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, StepBf16Pair));
+}
+// ... of eight, as four words of each plane
+__device__ __forceinline__ void gemm_cut8(const float* v, uint32_t (*part)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t p[3];
+    gemm_cut(v[2 * e], v[2 * e + 1], p);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) part[q][e] = p[q];
+  }
+}
+
 // Few rows: a tile of 128 m by 64 n by 4 waves of 32 m each.  A lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
 struct GemmFlat {
   static constexpr int WM = 4, WN = 1, MT = 2, NT = 4, M = 128, N = 64, THREADS = 256;
@@ -217,7 +240,7 @@ __device__ __forceinline__ GemmPlace gemm_work(const GemmShape& s, uint32_t bloc
     else ntiles = (count + TILE::N - 1) / TILE::N;
   }
   const GemmPlace at = gemm_place(s, ntiles, block);
-  tile.m0 = at.m * TILE::M; tile.n0 = at.n * TILE::N;
+  tile.m0 = at.m * (s.height ? s.height : TILE::M); tile.n0 = at.n * TILE::N;
   const uint32_t each = (steps + s.splits - 1) / s.splits;
   begin = min(at.split * each, steps); end = min(begin + each, steps);
   return at;
@@ -234,40 +257,42 @@ struct GemmNext {
   }
 };
 
-// The flat tile.  Where it streams the larger matrix through the chip once: three stages, two of which are under way while one is used, and two workgroups to a
-// compute unit.  Where few rows are summed over (a step or two) and the result is what takes the time: two stages, three workgroups.
-template <int DT, bool TA, bool TB, class EPI, int STAGES>
-__global__ void __launch_bounds__(GemmFlat::THREADS, STAGES == 2 ? 3 : 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+// The flat tile: it streams a 16-bit matrix of rows at multiples of 16 bytes through the chip once.  Three stages, two of which are under way while one is used, and two
+// workgroups to a compute unit.
+template <int DT, class EPI>
+__global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  constexpr uint32_t STAGES = 3;
   __shared__ __align__(1024) unsigned char lds[GemmFlat::STAGE * STAGES];
   GemmFlat tile;
   uint32_t begin, end;
   const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
   if (!at.any) return;
+  if (s.height) a.rows = min(a.rows, tile.m0 + s.height);
   GemmAcc acc[GemmFlat::MT][GemmFlat::NT];
 #pragma unroll
   for (int i = 0; i < GemmFlat::MT; ++i)
 #pragma unroll
     for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
-  const uint32_t total = (end - begin) * gemm_pairs(DT), wm = tile.wave_m();
+  const uint32_t total = end - begin, wm = tile.wave_m();
   if (total) {
     GemmNext next(begin, end, total);
     auto load = [&](uint32_t stage) {
       unsigned char* to = lds + stage * GemmFlat::STAGE;
-      gemm_fetch<GemmFlat::M, GemmFlat::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(next.pair), tile.m0, next.k * kGemmK, to);
-      gemm_fetch<GemmFlat::N, GemmFlat::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(next.pair), tile.n0, next.k * kGemmK, to + GemmFlat::M * kGemmK * 2);
+      gemm_fetch<GemmFlat::M, GemmFlat::THREADS, false>(a, 0, tile.m0, next.k * kGemmK, to);
+      gemm_fetch<GemmFlat::N, GemmFlat::THREADS, false>(b, 0, tile.n0, next.k * kGemmK, to + GemmFlat::M * kGemmK * 2);
       next.advance();
     };
     load(0);
-    if (STAGES == 3) load(1);
+    load(1);
     uint32_t stage = 0;
     for (uint32_t q = 0; q < total; ++q) {
-      gemm_wait<GemmFlat::LOADS * (STAGES - 2)>();
+      gemm_wait<GemmFlat::LOADS>();
       gemm_meet();                       // this stage has arrived for all, and nobody reads the one before it any more
-      if (STAGES == 3 || q + 1 < total) load(stage ? stage - 1u : STAGES - 1u);
+      load(stage ? stage - 1u : STAGES - 1u);
       const unsigned char* la = lds + stage * GemmFlat::STAGE;
       GemmShort8 fa[GemmFlat::MT][2], fb[GemmFlat::NT][2];
-      gemm_take<GemmFlat::NT, GemmFlat::N, TB>(la + GemmFlat::M * kGemmK * 2, 0, fb);
-      gemm_take<GemmFlat::MT, GemmFlat::M, TA>(la, wm, fa);
+      gemm_take<GemmFlat::NT, GemmFlat::N, false>(la + GemmFlat::M * kGemmK * 2, 0, fb);
+      gemm_take<GemmFlat::MT, GemmFlat::M, false>(la, wm, fa);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -403,17 +428,331 @@ __global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_two_kernel(Gemm
   else gemm_wide<DT, TA2, TB2>(a2, b2, s2, epi2, blockIdx.x - first, lds);
 }
 
-// The three planes of a 32-bit value, each the nearest bf16 to what is left of it (the largest values' first: towards zero, since the nearest is
-// infinite).  Of an infinity or NaN the first is one, the others 0.
-__device__ __forceinline__ void gemm_cut(float v, uint16_t* part) {
-  const uint32_t b = __float_as_uint(v);
-  part[0] = StepElem<DFX_BF16>::put(v);
-  part[1] = part[2] = 0;
-  if ((b & 0x7f800000u) == 0x7f800000u) return;
-  if ((part[0] & 0x7f80u) == 0x7f80u) part[0] = (uint16_t)(b >> 16);
-  const float rest = v - StepElem<DFX_BF16>::get(part[0]);
-  part[1] = StepElem<DFX_BF16>::put(rest);
-  part[2] = StepElem<DFX_BF16>::put(rest - StepElem<DFX_BF16>::get(part[1]));
+// ------------------------------------------------------------------------------------------
+// Few rows: the larger matrix, W, goes through the chip once and past LDS, from its own type at any alignment straight into the registers that the matrix
+// instructions take, steps ahead; the other operand, small and in planes, comes through LDS.  HBM bounds these.
+// ------------------------------------------------------------------------------------------
+// A matrix as the caller has it.  dim >= 64 elements of a row.
+struct GemmSource {
+  const void* p;
+  size_t stride;
+  uint32_t rows, dim;
+};
+
+// 16 bytes of a row from element e on, or the last 16 bytes of the row where it ends before: `over` elements further on
+template <int DT>
+__device__ __forceinline__ StepVec<DT, 16 / (int)sizeof(typename StepElem<DT>::raw)> gemm_row_part(const void* row, uint32_t e, uint32_t dim) {
+  constexpr uint32_t N = 16 / sizeof(typename StepElem<DT>::raw);
+  StepVec<DT, (int)N> v;
+  v.load(row, min(e, dim - N));
+  return v;
+}
+// ... put right: elements that lie behind the row's end are 0
+template <int DT, int N>
+__device__ __forceinline__ void gemm_row_end(StepVec<DT, N>& v, uint32_t e, uint32_t dim) {
+  constexpr uint32_t BITS = 8 * sizeof(typename StepElem<DT>::raw), WORDS = sizeof(v.w) / 4;
+  const uint32_t over = e + N > dim ? min(e + N - dim, (uint32_t)N) : 0u, words = over * BITS / 32u, half = over * BITS % 32u;
+  uint32_t x[WORDS + 1];
+#pragma unroll
+  for (uint32_t k = 0; k < WORDS; ++k) {
+    x[k] = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < WORDS; ++j)
+      if (k + words == j) x[k] = v.w[j];
+  }
+  x[WORDS] = 0;
+#pragma unroll
+  for (uint32_t k = 0; k < WORDS; ++k) v.w[k] = half ? x[k] >> 16 | x[k + 1] << 16 : x[k];
+}
+
+template <int NT_, int MT_>
+struct GemmFew {
+  static constexpr int WM = 4, WN = 1, MT = MT_, NT = NT_, M = 64 * MT, N = 16 * NT, THREADS = 256;
+  uint32_t m0, n0;
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave * (MT * 16); }
+  __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16 + threadIdx.x % kStepWave / 16 * 4; }
+  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt * 16 + threadIdx.x % 16; }
+  __device__ __forceinline__ uint32_t row(int nt, uint32_t r) const { return n0 + nt * 16 + r; }
+  __device__ __forceinline__ uint32_t row_of_pass() const { return threadIdx.x % 16; }
+};
+
+// planes of eight 32-bit values, or eight 16-bit ones as they are
+template <int DT>
+__device__ __forceinline__ void gemm_parts(const StepVec<DT, 16 / (int)sizeof(typename StepElem<DT>::raw)>* v, GemmShort8* to) {
+  if constexpr (DT == DFX_F32) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = v[e / 4].get(e % 4);
+    uint32_t p[3][4];
+    gemm_cut8(x, p);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) to[q] = __builtin_bit_cast(GemmShort8, p[q]);
+  } else to[0] = __builtin_bit_cast(GemmShort8, v[0].w);
+}
+
+// Logits: M rows of W by N rows of x, along both.
+template <int DT, int NT, int MT, int DEPTH, class EPI>
+__global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, GemmOperand b, GemmShape s, EPI epi) {
+  typedef GemmFew<NT, MT> TILE;
+  constexpr int P = gemm_planes(DT), V = DT == DFX_F32 ? 2 : 1, N = 16 / (int)sizeof(typename StepElem<DT>::raw), PLANE = TILE::N * kGemmK * 2, STAGE = P * PLANE, LOADS = MT * 2 * V + P * NT / 2;
+  constexpr int STAGES = DEPTH + 1;
+  __shared__ __align__(1024) unsigned char lds[STAGES * STAGE > 16 * (TILE::M + 4) * 4 ? STAGES * STAGE : 16 * (TILE::M + 4) * 4];
+  TILE tile;
+  uint32_t begin, end;
+  const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
+  if (!at.any) return;
+  GemmAcc acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  if (s.height) w.rows = min(w.rows, tile.m0 + s.height);
+  const uint32_t lane = threadIdx.x % kStepWave, g = lane / 16u;
+  const void* row[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) row[i] = (const typename StepElem<DT>::raw*)w.p + (size_t)min(tile.m0 + tile.wave_m() + i * 16u + lane % 16u, w.rows - 1u) * w.stride;
+  StepVec<DT, N> raw[DEPTH][MT][2][V];
+  GemmNext next(begin, end, end - begin);
+  auto load = [&](int set, uint32_t stage) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[set][i][kk][v] = gemm_row_part<DT>(row[i], next.k * kGemmK + kk * 32u + g * 8u + v * N, w.dim);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int p = 0; p < P; ++p) gemm_fetch<TILE::N, 256, false>(b, p, tile.n0, next.k * kGemmK, lds + stage * STAGE + p * PLANE);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    next.advance();
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) load(d, d);
+  uint32_t stage = 0;
+  auto step = [&](int set, uint32_t k) {
+    gemm_wait<LOADS * (DEPTH - 1)>();
+    gemm_meet();                         // this step's operands have arrived, and nobody reads the stage of the one before any more
+    GemmShort8 fa[MT][2][P];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        if ((k + 1u) * kGemmK > w.dim)
+#pragma unroll
+          for (int v = 0; v < V; ++v) gemm_row_end(raw[set][i][kk][v], k * kGemmK + kk * 32u + g * 8u + v * N, w.dim);
+        gemm_parts<DT>(raw[set][i][kk], fa[i][kk]);
+      }
+    load(set, stage ? stage - 1u : STAGES - 1u);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      GemmShort8 fb[P][2];
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) fb[p][kk] = gemm_read(lds + stage * STAGE + p * PLANE, j * 16, kk);
+#pragma unroll
+      for (int pair = 0; pair < gemm_pairs(DT); ++pair)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[i][j] = gemm_mac<DT>(fa[i][kk][P == 1 ? 0 : gemm_plane_a(pair)], fb[P == 1 ? 0 : gemm_plane_b(pair)][kk], acc[i][j]);
+    }
+    stage = stage + 1u == STAGES ? 0u : stage + 1u;
+  };
+  for (uint32_t k = begin; k < end; k += DEPTH)
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (k + d < end) step(d, k + d);
+  gemm_wait<0>();
+  gemm_meet();
+  epi(tile, at, acc, lds);
+}
+
+// A part of dX: 16 E elements of a row of W, by N rows of dz, summed over rows of W, 32 of each 128 by each of four waves.  A lane reads E elements of eight rows, and
+// so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes so many registers that it is slower: 48 x 1024 x 32000 22.5 us and 16.6.)
+constexpr uint32_t kFewK = 128;
+constexpr int kFewE = 4;
+template <int DT, int NT>
+__global__ void __launch_bounds__(256, DT == DFX_F32 && NT == 4 ? 1 : 2) dfx_gemm_few_dx_kernel(GemmSource w, GemmOperand b, GemmShape s, float* part, uint32_t rows, uint32_t pitch, bool more) {
+  constexpr int E = kFewE;
+  GemmFew<NT, E / 4> tile;
+  constexpr int P = gemm_planes(DT), PLANE = 16 * NT * kGemmK * 2, STAGE = 2 * P * PLANE, PITCH = 16 * E + 4, SUMS = 4 * 16 * PITCH * 4;
+  __shared__ __align__(1024) unsigned char lds[2 * STAGE > SUMS ? 2 * STAGE : SUMS];
+  uint32_t begin, end;
+  const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
+  if (!at.any) return;
+  GemmAcc acc[E][NT];
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, g = lane / 16u, l = lane % 16u, e = tile.m0 + E * l;
+  StepVec<DT, E> raw[2][8];
+  GemmNext next(begin, end, end - begin);
+  auto load_w = [&](int set) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t v = min(next.k * kFewK + wave * 32u + g * 8u + j, w.rows - 1u);
+      raw[set][j].load((const typename StepElem<DT>::raw*)w.p + (size_t)v * w.stride, min(e, w.dim - E));
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto load_b = [&](uint32_t k, uint32_t stage) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int p = 0; p < P; ++p) gemm_fetch<16 * NT, 256, false>(b, p, tile.n0, k * kFewK + half * kGemmK, lds + stage * STAGE + (half * P + p) * PLANE);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto step = [&](int set, uint32_t k) {
+    gemm_wait<8>();                      // dz of this step and its part of W; the next one's rows of W are under way
+    gemm_meet();
+    if (tile.m0 + 16u * E > w.dim)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) gemm_row_end(raw[set][j], e, w.dim);
+    GemmShort8 fa[E][P];
+#pragma unroll
+    for (int t = 0; t < E; ++t) {
+      if constexpr (DT == DFX_F32) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = raw[set][j].get(t);
+        uint32_t p[3][4];
+        gemm_cut8(x, p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) fa[t][q] = __builtin_bit_cast(GemmShort8, p[q]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) fa[t][0][j] = (short)(raw[set][j].w[t / 2] >> (t % 2 * 16));
+      }
+    }
+    load_b(min(k + 1u, end - 1u), set ^ 1);
+    load_w(set);
+    next.advance();
+    const unsigned char* lb = lds + set * STAGE + wave / 2u * P * PLANE;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      GemmShort8 fb[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) fb[p] = gemm_read(lb + p * PLANE, j * 16, wave % 2u);
+#pragma unroll
+      for (int pair = 0; pair < gemm_pairs(DT); ++pair)
+#pragma unroll
+        for (int t = 0; t < E; ++t) acc[t][j] = gemm_mac<DT>(fa[t][P == 1 ? 0 : gemm_plane_a(pair)], fb[P == 1 ? 0 : gemm_plane_b(pair)], acc[t][j]);
+    }
+  };
+  if (begin < end) {
+    load_w(0);
+    next.advance();
+    load_b(begin, 0);
+    load_w(1);
+    next.advance();
+    for (uint32_t k = begin; k < end; k += 2) {
+      step(0, k);
+      if (k + 1u < end) step(1, k + 1u);
+    }
+    gemm_wait<0>();
+    gemm_meet();
+  }
+  float* sums = (float*)lds;             // [wave][n][PITCH]
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int t = 0; t < E; t += 4) {
+        const GemmAcc four = {acc[t][j][x], acc[t + 1][j][x], acc[t + 2][j][x], acc[t + 3][j][x]};
+        *(GemmAcc*)(sums + (wave * 16u + l) * PITCH + E * (4u * g + x) + t) = four;
+      }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t q = threadIdx.x; q < 16u * 4u * E; q += 256u) {
+      const uint32_t n = q / (4u * E), d = q % (4u * E) * 4u;
+      GemmAcc sum = *(const GemmAcc*)(sums + n * PITCH + d);
+#pragma unroll
+      for (uint32_t x = 1; x < 4; ++x) sum += *(const GemmAcc*)(sums + (x * 16u + n) * PITCH + d);
+      if (tile.m0 + d < pitch) {
+        GemmAcc* to = (GemmAcc*)(part + ((size_t)at.split * rows + tile.n0 + j * 16 + n) * pitch + tile.m0 + d);
+        *to = more ? *to + sum : sum;
+      }
+    }
+  }
+}
+
+// dW of few rows, whose sums are a step or two long: writing it is what takes the time.  A wave has 32 elements of x's rows in registers, all the sums' length, and goes from
+// 64 rows of dW to others; the next ones' dz is on its way meanwhile.  Its two tiles' rows are exchanged in fours, so that a lane has eight elements of dW side by side.
+template <int DT, int STEPS, class OUT>
+__global__ void __launch_bounds__(256, DT == DFX_F32 ? 1 : 3) dfx_gemm_few_dw_kernel(GemmOperand x, GemmOperand z, const uint32_t* count, uint32_t mtiles, uint32_t ntiles, uint32_t each, OUT out) {
+  constexpr int P = gemm_planes(DT), PLANE = 64 * kGemmK * 2, STAGE = STEPS * P * PLANE, WIDE = 128, NT = 4;
+  constexpr int LDS = 2 * STAGE > WIDE * kGemmK * 2 ? 2 * STAGE : WIDE * kGemmK * 2;
+  __shared__ __align__(1024) unsigned char lds[LDS];
+  const uint32_t m0 = blockIdx.x % mtiles * WIDE, first = blockIdx.x / mtiles, wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u;
+  const uint32_t steps = min((*count + kGemmK - 1) / kGemmK, (uint32_t)STEPS);
+  GemmShort8 fa[2][STEPS][2][P];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if ((uint32_t)s < steps) gemm_fetch<WIDE, 256, true>(x, p, m0, s * kGemmK, lds);
+      __syncthreads();
+      const uint32_t k = 8u * g + l / 4u, q = l & 3u;
+      GemmLds* at = (GemmLds*)lds + k * (WIDE * 2u) + (((wave * 2u + q / 2u) ^ gemm_turned_swap<WIDE>(k)) * 32u) + (q & 1u) * 16u;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const GemmShort4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)(at + kk * 32 * WIDE * 2 + t * 8));
+          const GemmShort4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) GemmShort4*)(at + kk * 32 * WIDE * 2 + 4 * WIDE * 2 + t * 8));
+          fa[t][s][kk][p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+      __syncthreads();
+    }
+  auto load = [&](uint32_t n, uint32_t stage) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+      if ((uint32_t)s < steps)
+#pragma unroll
+        for (int p = 0; p < P; ++p) gemm_fetch<64, 256, true>(z, p, n * 64u, s * kGemmK, lds + stage * STAGE + (s * P + p) * PLANE);
+  };
+  if (first < ntiles) load(first, 0);
+  uint32_t stage = 0;
+  for (uint32_t n = first; n < ntiles; n += each, stage ^= 1u) {
+    gemm_wait<0>();
+    gemm_meet();
+    if (n + each < ntiles) load(n + each, stage ^ 1u);
+    GemmAcc acc[2][NT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[t][j] = GemmAcc{0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+      if ((uint32_t)s < steps) {
+        GemmShort8 fb[P][NT][2];
+#pragma unroll
+        for (int p = 0; p < P; ++p) gemm_read_turned<NT, 64>(lds + stage * STAGE + (s * P + p) * PLANE, 0, fb[p]);
+#pragma unroll
+        for (int pair = 0; pair < gemm_pairs(DT); ++pair)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int t = 0; t < 2; ++t) acc[t][j] = gemm_mac<DT>(fa[t][s][kk][P == 1 ? 0 : gemm_plane_a(pair)], fb[P == 1 ? 0 : gemm_plane_b(pair)][j][kk], acc[t][j]);
+      }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = acc[e / 4][j][e % 4];
+      out.put8(n * 64u + j * 16u + l, m0 + wave * 32u + g * 8u, v);
+    }
+  }
 }
 
 }  // namespace

@@ -25,8 +25,10 @@ constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.442695040888963407
 constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
-constexpr uint32_t kFewRows = 128;       // up to so many rows take flat tiles (at most 256: dfx_vocab_few_kernel has a thread for each)
-constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
+constexpr uint32_t kFewRows = 128, kFewDim = 64;      // up to so many rows of at least so many elements go by the products for few rows (at most 256 rows: dfx_vocab_few_kernel has a thread for each)
+constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
+constexpr size_t kFewWide = 65536;       // from so long a vocabulary on, few rows' logits are made by twice as many rows of weight to a workgroup
+constexpr uint32_t kDwGroups = 1024;     // workgroups of dW of few rows
 constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
 // what is known of a call on the device; first in the workspace
@@ -123,12 +125,10 @@ __device__ __forceinline__ void pack_row(const void* row, uint32_t dim, uint32_t
             if (e + j < dim) v[j] = step_get<DT>(row, e + j);
         }
       }
-      uint16_t p[8][3];
+      uint32_t p[3][4];
+      gemm_cut8(v, p);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) gemm_cut(v[j], p[j]);
-#pragma unroll
-      for (int q = 0; q < 3; ++q)
-        *(uint4*)(to + q * plane + e) = make_uint4(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16, p[4][q] | (uint32_t)p[5][q] << 16, p[6][q] | (uint32_t)p[7][q] << 16);
+      for (int q = 0; q < 3; ++q) *(uint4*)(to + q * plane + e) = make_uint4(p[q][0], p[q][1], p[q][2], p[q][3]);
     } else {
       StepVec<DT, 8> v;
       v.w = 0;
@@ -201,17 +201,18 @@ struct VocabStats {
   float2* parts;
   float *zt, *z;                         // z: [pitch][z_pitch], may be null
   const int32_t* target;
-  uint32_t pitch, z_pitch, left, v0;     // left: rows of the vocabulary from the first of this launch, v0, on
+  uint32_t pitch, z_pitch, left, v0, tile0, height;      // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile; height: of a tile
   float k;
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
     const uint32_t lane = threadIdx.x % kStepWave, wave = threadIdx.x / kStepWave;
-    if (tile.m0 + TILE::M > left) {
+    const uint32_t end = min(left, tile.m0 + height);
+    if (tile.m0 + TILE::M > end) {
 #pragma unroll
       for (int i = 0; i < TILE::MT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (tile.m(i) + e >= left)
+          if (tile.m(i) + e >= end)
 #pragma unroll
             for (int j = 0; j < TILE::NT; ++j) acc[i][j][e] = -INFINITY;
     }
@@ -220,8 +221,10 @@ struct VocabStats {
       for (int j = 0; j < TILE::NT; ++j) {
         float* to = z + (size_t)tile.n(j) * z_pitch;
 #pragma unroll
-        for (int i = 0; i < TILE::MT; ++i) *(GemmAcc*)(to + tile.m(i)) = acc[i][j];
+        for (int i = 0; i < TILE::MT; ++i)
+          if (tile.m(i) < end) *(GemmAcc*)(to + tile.m(i)) = acc[i][j];      // (heights are multiples of 4, and what is behind the vocabulary is not looked at)
       }
+    if (!parts) return;                  // (they are known: the logits alone)
     float2* part = (float2*)lds;         // [WM][N]
     __syncthreads();
 #pragma unroll
@@ -241,7 +244,7 @@ struct VocabStats {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           s += vocab_exp(acc[i][j][e], base, k);
-          if (tile.m(i) + e == t && t < left) zt[n] = acc[i][j][e];
+          if (tile.m(i) + e == t && t < end) zt[n] = acc[i][j][e];
         }
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
@@ -258,7 +261,7 @@ struct VocabStats {
       }
 #pragma unroll
       for (int w = 0; w < TILE::WM; ++w) s += p[w].y * vocab_exp(p[w].x, vocab_base(top), k);
-      parts[(size_t)(v0 / TILE::M + at.m) * pitch + tile.n0 + i] = make_float2(top, s);
+      parts[(size_t)(tile0 + at.m) * pitch + tile.n0 + i] = make_float2(top, s);
     }
   }
 };
@@ -348,12 +351,10 @@ struct VocabDz {
       if (m + e >= left) v[e] = 0.0f;
     }
     if constexpr (DT == DFX_F32) {
-      uint16_t p[8][3];
+      uint32_t p[3][4];
+      gemm_cut8(v, p);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gemm_cut(v[e], p[e]);
-#pragma unroll
-      for (int q = 0; q < 3; ++q)
-        *(uint4*)(to + q * plane) = make_uint4(p[0][q] | (uint32_t)p[1][q] << 16, p[2][q] | (uint32_t)p[3][q] << 16, p[4][q] | (uint32_t)p[5][q] << 16, p[6][q] | (uint32_t)p[7][q] << 16);
+      for (int q = 0; q < 3; ++q) *(uint4*)(to + q * plane) = make_uint4(p[q][0], p[q][1], p[q][2], p[q][3]);
     } else {
       StepVec<DT, 8> o;
       o.put(v);
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabDz<DT> d, const 
   const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 8u, rows = *count;
   if (n >= (rows + kGemmK - 1) / kGemmK * kGemmK || m >= d.pitch) return;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (n < rows) memcpy(v, __builtin_assume_aligned(z + (size_t)n * d.pitch + m, 16), 32);
+  if (n < rows && m < d.left) memcpy(v, __builtin_assume_aligned(z + (size_t)n * d.pitch + m, 16), 32);      // (left is rounded up to a multiple of 4 at most)
   d.put(n, n < rows ? d.row[n] : VocabRow{0.0f, 0.0f, 0.0f, -1}, m, v);
 }
 
@@ -405,31 +406,39 @@ struct VocabDw {
   const VocabState* state;
   uint32_t dim, left;                    // elements of a row; rows from grad's first on
   bool accumulate;
+  template <int E>
+  __device__ __forceinline__ void put(uint32_t n, uint32_t m, float* v, float g) const {
+    if (n >= left || m >= dim) return;
+    typedef typename StepElem<OUT>::raw raw;
+    raw* to = (raw*)grad + (size_t)n * stride;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] *= g;
+    if (m + E <= dim) {
+      StepVec<OUT, E> o;
+      if (accumulate) {
+        o.load(to, m);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] += o.get(e);
+      }
+      o.put(v);
+      *(STEP_GLOBAL typename StepVec<OUT, E>::words*)((STEP_GLOBAL raw*)to + m) = o.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (m + e < dim) step_put<OUT>(to, m + e, accumulate ? v[e] + step_get<OUT>(to, m + e) : v[e]);
+    }
+  }
+  __device__ __forceinline__ void put8(uint32_t n, uint32_t m, float* v) const {
+    if constexpr (OUT == DFX_F32) {
+      put<4>(n, m, v, state->g);
+      put<4>(n, m + 4u, v + 4, state->g);
+    } else put<8>(n, m, v, state->g);
+  }
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace&, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
-    typedef typename StepElem<OUT>::raw raw;
-    constexpr int E = 16 / (int)sizeof(raw);
+    constexpr int E = 16 / (int)sizeof(typename StepElem<OUT>::raw);
     const float g = state->g;
-    gemm_by_rows<E>(tile, acc, lds, [&](uint32_t n, uint32_t m, float* v) {
-      if (n >= left || m >= dim) return;
-      raw* to = (raw*)grad + (size_t)n * stride;
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= g;
-      if (m + E <= dim) {
-        StepVec<OUT, E> o;
-        if (accumulate) {
-          o.load(to, m);
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[e] += o.get(e);
-        }
-        o.put(v);
-        *(STEP_GLOBAL typename StepVec<OUT, E>::words*)((STEP_GLOBAL raw*)to + m) = o.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (m + e < dim) step_put<OUT>(to, m + e, accumulate ? v[e] + step_get<OUT>(to, m + e) : v[e]);
-      }
-    });
+    gemm_by_rows<E>(tile, acc, lds, [&](uint32_t n, uint32_t m, float* v) { put<E>(n, m, v, g); });
   }
 };
 
@@ -464,60 +473,112 @@ __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const fl
 // ------------------------------------------------------------------------------------------
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
+// Whether the weight can be read where it lies by loads to LDS: 16-bit rows of whole steps at multiples of 16 bytes.
+bool vocab_aligned(const dfx_vocab_loss_args& u) {
+  return u.dtype != DFX_F32 && u.dim % kGemmK == 0 && (uintptr_t)u.weight % 16 == 0 && (u.weight_stride ? u.weight_stride : u.dim) % 8 == 0;
+}
+
 struct VocabPlan {
-  size_t rp, dp, dq, vp, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, tiles of the vocabulary, splits of dX and the tiles' rows
-  bool flat, keep;                       // keep: the logits of the last piece
+  size_t rp, dp, dq, vp, pieces, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, pieces, tiles of the vocabulary, splits of dX and the tiles' rows
+  bool few, keep;                        // keep: the logits of the last piece
+  int nt, mt;                            // tiles of the products for few rows
+  size_t height;                         // of a tile of the vocabulary
   size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
 };
 
-// Splits of dX along the vocabulary: as many workgroups as compute units, of the flat tiles twice as many.  What depends on the number of rows has room for any smaller number.
-VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad, size_t piece) {
+// Splits of dX along the vocabulary: as many workgroups as compute units, of the products for few rows three times as many.  What depends on the number of rows has room for
+// any smaller number.  aligned: rows of weight lie at multiples of 16 bytes (which changes nothing of the space).
+VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad, size_t piece, bool aligned) {
   VocabPlan p;
   const size_t planes = gemm_planes(dtype);
-  p.flat = rows <= kFewRows;
+  p.few = rows <= kFewRows && dim >= kFewDim;
   p.rp = std::max(kTileRows, up(rows, kTileRows));
   p.dp = up(dim, kGemmK);
   p.dq = up(dim, 4);
-  p.tiles = (vocab + kTileRows - 1) / kTileRows;
-  const size_t whole = std::max(kTileRows, p.tiles * kTileRows);
-  const size_t most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceMost);
-  size_t dz_rows = p.rp * most;
-  p.vp = most;
-  if (!piece) {                          // pieces of equal length
-    const size_t length = std::min(most, std::max(kPieceLeast, kPieceElems / p.rp / kTileRows * kTileRows)), pieces = (whole + length - 1) / length;
-    p.vp = up((whole + pieces - 1) / pieces, kTileRows);
-    dz_rows = std::min(dz_rows, std::max(kPieceElems, p.rp * kPieceLeast));
-  }
-  const size_t tile = p.flat ? GemmFlat::N : GemmWide::N, wide = p.flat ? GemmFlat::M : GemmWide::M, across = up(std::max<size_t>(rows, 1), tile) / tile, along = up(dim, wide) / wide;
-  const size_t groups = p.flat ? 512 : 256;
-  p.splits = std::max<size_t>(1, std::min(groups / (across * along), p.vp / 256));
-  if (p.flat) p.tiles = (vocab + GemmFlat::M - 1) / GemmFlat::M;
+  const size_t whole = std::max(kTileRows, up(vocab, kTileRows));
+  const size_t most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceMost), few_most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceFew);
   const bool long_rows = dim >= (dtype == DFX_F32 ? kKeepDimF32 : kKeepDim);
-  p.keep = grad && (p.flat || long_rows);
-  p.split_rows = across * tile;
-  const size_t across256 = p.rp / 256, along256 = up(dim, 256) / 256;
+  size_t length = most, dz = p.rp * most;
+  if (!piece) {
+    length = std::min(most, std::max(kPieceLeast, kPieceElems / p.rp / kTileRows * kTileRows));
+    dz = std::min(dz, std::max(kPieceElems, p.rp * kPieceLeast));
+  }
+  if (p.few) length = few_most;
+  p.pieces = (whole + length - 1) / length;
+  p.vp = piece ? length : up((whole + p.pieces - 1) / p.pieces, kTileRows);      // (of equal length)
+  p.keep = grad && (p.few || long_rows);
+  if (p.few) {
+    p.nt = rows <= 32 ? 2 : 4;
+    p.mt = aligned || vocab >= kFewWide ? 2 : 1;
+    // so many tiles that whole rounds of workgroups, two to a compute unit, have them all
+    const size_t rounds = std::max<size_t>(1, (vocab + 512 * 64 * p.mt - 1) / (512 * 64 * p.mt));
+    p.height = std::max<size_t>(16, up((vocab + 512 * rounds - 1) / (512 * rounds), 4));
+    p.tiles = (vocab + p.height - 1) / p.height + p.pieces;      // (of each piece by itself)
+    p.split_rows = up(std::max<size_t>(rows, 1), 64);
+    const size_t dx_wide = 16 * kFewE, groups = up(std::max<size_t>(rows, 1), 16 * p.nt) / (16 * p.nt) * (up(dim, dx_wide) / dx_wide);
+    p.splits = std::max<size_t>(1, std::min(768 / groups, p.vp / kFewK));
+  } else {
+    p.height = kTileRows;
+    p.tiles = (vocab + kTileRows - 1) / kTileRows;
+    p.split_rows = p.rp;
+    p.splits = std::max<size_t>(1, std::min(256 / (p.rp / 256 * (up(dim, 256) / 256)), p.vp / 256));
+  }
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
   p.state = take(sizeof(VocabState) + 4);
   p.idx = take(4 * p.rp); p.target = take(4 * p.rp); p.map = take(4 * p.rp); p.weight = take(4 * p.rp); p.zt = take(4 * p.rp);
   p.row_loss = take(4 * p.rp); p.row_w = take(4 * p.rp); p.row = take(sizeof(VocabRow) * p.rp);
-  p.parts = take(sizeof(float2) * p.rp * (whole / kTileRows));
+  p.parts = take(sizeof(float2) * std::max<size_t>(p.rp * (whole / kTileRows), kFewRows * std::min(whole / 4, whole / 32 + 520)));
   p.x = take(planes * p.rp * p.dp * 2);
-  p.w = take(planes * most * p.dp * 2);
-  p.dz = grad ? take(planes * dz_rows * 2) : at;
-  p.z = grad ? take((long_rows ? dz_rows : kTileRows * most) * 4) : at;
-  p.dx = grad ? take(std::max(256 / along256, across256) * 256 * p.dq * 4) : at;
+  p.w = p.few ? at : take(planes * most * p.dp * 2);
+  p.dz = grad ? take(planes * std::max(dz, kFewRows * few_most) * 2) : at;
+  p.z = grad ? take(std::max(long_rows ? dz : 0, kFewRows * few_most) * 4) : at;
+  p.dx = grad ? take(std::max(std::max(256 / (up(dim, 256) / 256), p.rp / 256) * 256, std::max<size_t>(768 / (up(dim, 64) / 64), 1) * kFewRows) * p.dq * 4) : at;
   p.bytes = at;
   return p;
 }
 
 template <int DT, bool TA, bool TB, class EPI>
-int vocab_gemm(bool few, const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, hipStream_t stream) {
-  s.mtiles = (uint32_t)(few ? (m + GemmFlat::M - 1) / GemmFlat::M : (m + GemmWide::M - 1) / GemmWide::M);
-  s.ntiles = (uint32_t)(few ? (n + GemmFlat::N - 1) / GemmFlat::N : (n + GemmWide::N - 1) / GemmWide::N);
+int vocab_gemm(const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, hipStream_t stream) {
+  s.mtiles = (uint32_t)((m + GemmWide::M - 1) / GemmWide::M);
+  s.ntiles = (uint32_t)((n + GemmWide::N - 1) / GemmWide::N);
   if (!s.mtiles || !s.ntiles) return DFX_OK;
-  if (few) return step_launch(dfx_gemm_flat_kernel<DT, TA, TB, EPI, TA && TB ? 2 : 3>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, b, s, epi);
   return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
+}
+
+// the products for few rows: logits, dX, dW
+template <int DT, class EPI>
+int vocab_few(const VocabPlan& p, bool aligned, const GemmSource& w, const GemmOperand& x, GemmShape s, size_t rows, const EPI& epi, hipStream_t stream) {
+  s.mtiles = (uint32_t)((w.rows + p.height - 1) / p.height);
+  s.height = (uint32_t)p.height;
+  if constexpr (DT != DFX_F32)
+    if (aligned) {
+      s.ntiles = (uint32_t)((rows + GemmFlat::N - 1) / GemmFlat::N);
+      const GemmOperand a = {(const uint16_t*)w.p, 0, (uint32_t)w.stride, w.rows, w.dim};
+      return s.mtiles && s.ntiles ? step_launch(dfx_gemm_flat_kernel<DT, EPI>, dim3(gemm_groups(s)), GemmFlat::THREADS, stream, a, x, s, epi) : DFX_OK;
+    }
+  s.ntiles = (uint32_t)((rows + 16 * p.nt - 1) / (16 * p.nt));
+  if (!s.mtiles || !s.ntiles) return DFX_OK;
+  constexpr int D2 = DT == DFX_F32 ? 3 : 4, D4 = DT == DFX_F32 ? 2 : 4;
+  auto k = p.nt == 2 ? (p.mt == 2 ? dfx_gemm_few_kernel<DT, 2, 2, D2, EPI> : dfx_gemm_few_kernel<DT, 2, 1, D2, EPI>)
+                     : (p.mt == 2 ? dfx_gemm_few_kernel<DT, 4, 2, D4, EPI> : dfx_gemm_few_kernel<DT, 4, 1, D4, EPI>);
+  return step_launch(k, dim3(gemm_groups(s)), 256, stream, w, x, s, epi);
+}
+
+template <int DT>
+int vocab_few_dx(const VocabPlan& p, const GemmSource& w, const GemmOperand& z, GemmShape s, size_t rows, float* dx, bool more, hipStream_t stream) {
+  constexpr uint32_t wide = 16 * kFewE;
+  s.mtiles = (w.dim + wide - 1) / wide;
+  s.ntiles = (uint32_t)((rows + 16 * p.nt - 1) / (16 * p.nt));
+  s.ksteps = (w.rows + kFewK - 1) / kFewK;
+  if (!s.ntiles) return DFX_OK;
+  return step_launch(p.nt == 2 ? dfx_gemm_few_dx_kernel<DT, 2> : dfx_gemm_few_dx_kernel<DT, 4>, dim3(gemm_groups(s)), 256, stream, w, z, s, dx, (uint32_t)p.split_rows, (uint32_t)p.dq, more);
+}
+
+template <int DT, class OUT>
+int vocab_few_dw(const GemmOperand& x, const GemmOperand& z, const uint32_t* count, size_t rows, size_t dim, size_t vocab, const OUT& out, hipStream_t stream) {
+  const uint32_t mtiles = (uint32_t)((dim + 127) / 128), ntiles = (uint32_t)((vocab + 63) / 64), each = std::min(ntiles, std::max(1u, kDwGroups / mtiles));
+  return step_launch(rows <= kGemmK ? dfx_gemm_few_dw_kernel<DT, 1, OUT> : dfx_gemm_few_dw_kernel<DT, 2, OUT>, dim3(mtiles * each), 256, stream, x, z, count, mtiles, ntiles, each, out);
 }
 
 // dX and dW of a piece in one launch (dX's tiles of many rows are the wide ones)
@@ -550,13 +611,14 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   float* dx = (float*)(ws + p.dx);
 
   const size_t hs = u.hidden_stride ? u.hidden_stride : u.dim;
-  if (p.flat) VOCAB_TRY(step_launch(dfx_vocab_few_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+  if (p.few) VOCAB_TRY(step_launch(dfx_vocab_few_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
   else {
     VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
     VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, hs, (const int32_t*)a.idx, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
   }
   // The weight is read where it lies if its rows are whole steps at multiples of 16 bytes; otherwise a piece at a time is laid out.
-  const bool direct = DT != DFX_F32 && u.dim % kGemmK == 0 && (uintptr_t)u.weight % 16 == 0 && ws_stride * eb % 16 == 0;
+  // (The products for few rows take it as it is.)
+  const bool direct = !p.few && vocab_aligned(u);
   const GemmOperand ox = {x, p.rp * p.dp, (uint32_t)p.dp, (uint32_t)p.split_rows, (uint32_t)p.dp};
   const size_t pieces = (u.vocab + p.vp - 1) / p.vp;
   GemmOperand ow = {};
@@ -569,33 +631,52 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     return step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)left), 256, stream, (const void*)((const unsigned char*)u.weight + v0 * ws_stride * eb), ws_stride, (const int32_t*)nullptr,
                        (uint32_t)u.dim, (uint32_t)p.dp, w, p.vp * p.dp);
   };
-  const GemmShape by_rows = {0, 0, 1, (uint32_t)(p.dp / kGemmK), count, false};
+  const GemmShape by_rows = {0, 0, 1, (uint32_t)(p.dp / kGemmK), 0, count, false};
   const size_t last = pieces ? (pieces - 1) * p.vp : 0;
   float* z = p.keep ? (float*)(ws + p.z) : nullptr;
+  size_t tile0 = 0;
+  auto stats = [&](size_t v0, size_t left, float* keep, size_t tile, float2* parts) {
+    return VocabStats{parts, a.zt, keep, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, (uint32_t)tile, (uint32_t)p.height, a.k};
+  };
+  GemmSource few_w = {};
+  auto logits = [&](size_t v0, size_t left, const auto& epi) -> int {      // of rows of weight from v0 on
+    if (p.few) {
+      few_w = {(const unsigned char*)u.weight + v0 * ws_stride * eb, ws_stride, (uint32_t)left, (uint32_t)u.dim};
+      return vocab_few<DT>(p, vocab_aligned(u), few_w, ox, by_rows, u.rows, epi, stream);
+    }
+    return vocab_gemm<DT, false, false>(ow, ox, by_rows, left, u.rows, epi, stream);
+  };
   for (size_t v0 = 0, left; v0 < u.vocab; v0 += left) {      // what lies where it is in one launch, but for a piece whose logits are kept
-    left = direct ? (z && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
-    VOCAB_TRY(take_piece(v0, left));
-    const VocabStats epi = {a.parts, a.zt, v0 == last ? z : nullptr, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
-    VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
+    left = direct || p.few ? (z && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
+    if (!p.few) VOCAB_TRY(take_piece(v0, left));
+    VOCAB_TRY(logits(v0, left, stats(v0, left, v0 == last ? z : nullptr, tile0, a.parts)));
+    tile0 += (left + p.height - 1) / p.height;
   }
-  if (p.flat) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
+  a.tiles = (uint32_t)tile0;
+  if (p.few) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
   else VOCAB_TRY(step_launch(dfx_vocab_join_kernel<8>, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
   if (u.sums) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
   if (!u.grad_hidden && !u.grad_weight) return DFX_OK;
   for (size_t q = pieces; q-- != 0;) {   // the last one first
     const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
-    if (direct || v0 != last) VOCAB_TRY(take_piece(v0, left));
+    if (direct || (!p.few && v0 != last)) VOCAB_TRY(take_piece(v0, left));
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
-    if (z && v0 == last) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, epi, (const float*)z, count));
-    else VOCAB_TRY((vocab_gemm<DT, false, false>(p.flat, ow, ox, by_rows, left, u.rows, epi, stream)));
+    if (p.few && v0 != last) VOCAB_TRY(logits(v0, left, stats(v0, left, z, 0, nullptr)));
+    if (p.few || (z && v0 == last)) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, epi, (const float*)z, count));
+    else VOCAB_TRY((vocab_gemm<DT, false, false>(ow, ox, by_rows, left, u.rows, epi, stream)));
     const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
-    const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), count, false}, sw = {0, 0, 1, 0, count, true};
+    const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), 0, count, false}, sw = {0, 0, 1, 0, 0, count, true};
     const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != last};
     const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
     auto both = [&](const auto& dw_to) -> int {
-      if (u.grad_hidden && u.grad_weight && !p.flat && u.rows) return vocab_gemm_two<DT>(ow, oz, sx, u.dim, u.rows, dx_to, ox, sw, left, dw_to, stream);
-      if (u.grad_hidden) VOCAB_TRY((vocab_gemm<DT, true, false>(p.flat, ow, oz, sx, u.dim, u.rows, dx_to, stream)));
-      return u.grad_weight ? vocab_gemm<DT, true, true>(p.flat, ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
+      if (p.few) {
+        few_w = {(const unsigned char*)u.weight + v0 * ws_stride * eb, ws_stride, (uint32_t)left, (uint32_t)u.dim};
+        if (u.grad_hidden) VOCAB_TRY((vocab_few_dx<DT>(p, few_w, oz, sx, u.rows, dx, v0 != last, stream)));
+        return u.grad_weight ? vocab_few_dw<DT>(ox, oz, count, u.rows, u.dim, left, dw_to, stream) : DFX_OK;
+      }
+      if (u.grad_hidden && u.grad_weight && u.rows) return vocab_gemm_two<DT>(ow, oz, sx, u.dim, u.rows, dx_to, ox, sw, left, dw_to, stream);
+      if (u.grad_hidden) VOCAB_TRY((vocab_gemm<DT, true, false>(ow, oz, sx, u.dim, u.rows, dx_to, stream)));
+      return u.grad_weight ? vocab_gemm<DT, true, true>(ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
     };
     if (u.grad_dtype == DFX_F32) VOCAB_TRY(both(VocabDw<DFX_F32>{(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
     else if constexpr (DT != DFX_F32) VOCAB_TRY(both(VocabDw<DT>{(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
@@ -609,7 +690,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
 constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
 
 // tiles of rows by the vocabulary are counted in 32 bits
-bool vocab_too_large(const VocabPlan& p) { return p.rp / GemmFlat::N > (1ull << 31) / std::max<size_t>(p.tiles, 1); }
+bool vocab_too_large(const VocabPlan& p) { return p.rp / 64 > (1ull << 31) / std::max<size_t>(p.tiles, 1); }
 
 }  // namespace
 
@@ -617,7 +698,7 @@ extern "C" {
 
 size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece) {
   if (rows >= kMostRows || vocab >= kMostRows || dim >= kMostStride || piece % kTileRows) return 0;
-  const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, grad != 0, piece);
+  const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, grad != 0, piece, true);
   return vocab_too_large(p) ? 0 : p.bytes;
 }
 
@@ -639,7 +720,7 @@ int dfx_vocab_loss(const dfx_vocab_loss_args* u, void* hip_stream) {
   if ((uintptr_t)u->hidden % eb || (uintptr_t)u->weight % eb || (uintptr_t)u->grad_hidden % eb || (uintptr_t)u->grad_weight % gb || (uintptr_t)u->targets % 8) return DFX_ERR_INVALID_ARG;
   for (const void* p : {(const void*)u->row_weight, (const void*)u->scale, (const void*)u->logp, (const void*)u->loss, (const void*)u->sums})
     if ((uintptr_t)p % 4) return DFX_ERR_INVALID_ARG;
-  const VocabPlan p = vocab_plan(u->rows, u->dim, u->vocab, u->dtype, u->grad_hidden || u->grad_weight, u->piece);
+  const VocabPlan p = vocab_plan(u->rows, u->dim, u->vocab, u->dtype, u->grad_hidden || u->grad_weight, u->piece, vocab_aligned(*u));
   if (vocab_too_large(p)) return DFX_ERR_TOO_LARGE;
   if (!u->workspace || (uintptr_t)u->workspace % 256 || u->workspace_bytes < p.bytes) return DFX_ERR_INVALID_ARG;
   auto matrix = [](const void* at, size_t rows, size_t stride, size_t dim, size_t bytes) { return flat(at, rows ? ((rows - 1) * stride + dim) * bytes : 0); };
