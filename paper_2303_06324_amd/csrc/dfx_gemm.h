@@ -9,6 +9,7 @@
 #define DFX_GEMM_H
 
 #include "dfx_step.h"
+#include "dfx_tiles.h"
 
 namespace {
 
@@ -68,25 +69,24 @@ __device__ __forceinline__ void gemm_fetch(const GemmOperand& o, int plane, uint
   constexpr int LOADS = COLS * 8 / THREADS;
   const uint32_t t = threadIdx.x, wave = t / kStepWave;
   if (!TURNED) {
-    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)first * o.stride + k0;
+    const uint32_t from = tile_base(first, o.rows);      // (half a tile may lie behind the last row)
+    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)from * o.stride + k0;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, -1, 0x00020000);
-    const uint32_t last = o.rows - 1u - first;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const uint32_t row = j * (THREADS / 8) + t / 8, part = (t & 7u) ^ ((row >> 1) & 7u);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)(min(row, last) * o.stride * 2u + part * 16u), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)(tile_row(first, row, o.rows) * o.stride * 2u + part * 16u), 0, 0, 0);
     }
   } else {
     constexpr int PARTS = COLS / 8;      // of 16 bytes in a k's row
-    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)k0 * o.stride;
+    const uint16_t* base = o.p + (size_t)plane * o.plane + (size_t)tile_base(k0, o.rows) * o.stride;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, -1, 0x00020000);
-    const uint32_t last = o.rows - 1u - k0;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const uint32_t k = j * (THREADS / PARTS) + t / PARTS, slot = t % PARTS;
       const uint32_t part = (((slot >> 1) ^ gemm_turned_swap<COLS>(k)) << 1) | (slot & 1u);
-      const uint32_t col = min(first + part * 8u, o.cols - 8u);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)((min(k, last) * o.stride + col) * 2u), 0, 0, 0);
+      const uint32_t col = tile_col(first, part, o.cols);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * kStepWave) * 16), 16, (int)((tile_row(k0, k, o.rows) * o.stride + col) * 2u), 0, 0, 0);
     }
   }
 }
@@ -570,13 +570,78 @@ __global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, Gemm
   epi(tile, at, acc, lds);
 }
 
+// Logits of 16 NT rows at most: x stays in registers, of each of eight waves 32 KK elements of all rows.  A wave reads so much of a row of W at a time, which lies together (the
+// memory is quicker at that than at 128 bytes of each of many rows), a tile of 16 rows ahead; the waves' sums meet in LDS at the end of 64 rows.
+template <int DT, int NT, int KK, class EPI>
+__global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, GemmOperand x, uint32_t height, EPI epi) {
+  constexpr int P = gemm_planes(DT), V = DT == DFX_F32 ? 2 : 1, N = 16 / (int)sizeof(typename StepElem<DT>::raw), ROWS = 16 * NT, PITCH = ROWS + 1;
+  __shared__ __align__(16) float sums[8 * 64 * PITCH];
+  __shared__ float2 pairs[16 * ROWS];
+  const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u, k0 = wave * KK * 32u + g * 8u;
+  const uint32_t m0 = blockIdx.x * height, end = min(w.rows, m0 + height);
+  StepVec<DT, N> raw[2][KK][V];
+  auto load = [&](int set, int i) {
+    const void* row = (const typename StepElem<DT>::raw*)w.p + (size_t)min(m0 + i * 16u + l, end - 1u) * w.stride;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw[set][kk][v] = gemm_row_part<DT>(row, k0 + kk * 32u + v * N, w.dim);
+  };
+  load(0, 0);
+  GemmShort8 fx[NT][KK][P];              // (x is 0 from dim to its padded length, and here behind that)
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const uint32_t e = k0 + kk * 32u;
+        fx[j][kk][p] = GemmShort8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (e < x.cols) fx[j][kk][p] = *(const STEP_GLOBAL GemmShort8*)(x.p + (size_t)p * x.plane + (size_t)(j * 16 + l) * x.stride + e);
+      }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < 3) load((i + 1) & 1, i + 1);
+    GemmAcc acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = GemmAcc{0, 0, 0, 0};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      if ((wave + 1u) * KK * 32u > w.dim)
+#pragma unroll
+        for (int v = 0; v < V; ++v) gemm_row_end(raw[i & 1][kk][v], k0 + kk * 32u + v * N, w.dim);
+      GemmShort8 fa[P];
+      gemm_parts<DT>(raw[i & 1][kk], fa);
+#pragma unroll
+      for (int pair = 0; pair < gemm_pairs(DT); ++pair)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j] = gemm_mac<DT>(fa[P == 1 ? 0 : gemm_plane_a(pair)], fx[j][kk][P == 1 ? 0 : gemm_plane_b(pair)], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[(wave * 64u + i * 16u + 4u * g + e) * PITCH + j * 16 + l] = acc[j][e];
+  }
+  __syncthreads();
+  GemmAcc v = {0, 0, 0, 0};
+  const uint32_t n = threadIdx.x % ROWS, four = threadIdx.x / ROWS;
+  if (four < 16u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = sums[(four * 4u + e) * PITCH + n];
+#pragma unroll
+      for (uint32_t q = 1; q < 8; ++q) v[e] += sums[(q * 64u + four * 4u + e) * PITCH + n];
+    }
+  epi.template of_fours<ROWS>(blockIdx.x, m0, end, v, pairs);
+}
+
 // A part of dX: 16 E elements of a row of W, by N rows of dz, summed over rows of W, 32 of each 128 by each of four waves.  A lane reads E elements of eight rows, and
-// so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes so many registers that it is slower: 48 x 1024 x 32000 22.5 us and 16.6.)
+// so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes too many registers by 64 rows: 48 x 1024 x 32000 22.5 us and 16.6.)
 constexpr uint32_t kFewK = 128;
-constexpr int kFewE = 4;
+__host__ __device__ constexpr int gemm_few_e(int dt, int nt) { return dt != DFX_F32 && nt == 2 ? 8 : 4; }
 template <int DT, int NT>
 __global__ void __launch_bounds__(256, DT == DFX_F32 && NT == 4 ? 1 : 2) dfx_gemm_few_dx_kernel(GemmSource w, GemmOperand b, GemmShape s, float* part, uint32_t rows, uint32_t pitch, bool more) {
-  constexpr int E = kFewE;
+  constexpr int E = gemm_few_e(DT, NT);
   GemmFew<NT, E / 4> tile;
   constexpr int P = gemm_planes(DT), PLANE = 16 * NT * kGemmK * 2, STAGE = 2 * P * PLANE, PITCH = 16 * E + 4, SUMS = 4 * 16 * PITCH * 4;
   __shared__ __align__(1024) unsigned char lds[2 * STAGE > SUMS ? 2 * STAGE : SUMS];

@@ -25,10 +25,12 @@ constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.442695040888963407
 constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
-constexpr uint32_t kFewRows = 128, kFewDim = 64;      // up to so many rows of at least so many elements go by the products for few rows (at most 256 rows: dfx_vocab_few_kernel has a thread for each)
+constexpr uint32_t kFewRows = 128, kFewDim = 64;      // up to so many rows of at least so many elements go by the products for few rows
+constexpr uint32_t kLayRows = 1024;      // up to so many rows are found by every workgroup that lays one out
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
 constexpr size_t kFewWide = 65536;       // from so long a vocabulary on, few rows' logits are made by twice as many rows of weight to a workgroup
 constexpr uint32_t kDwGroups = 1024;     // workgroups of dW of few rows
+constexpr size_t kKeepElems = 32ull << 20, kJoinMost = 16384;      // logits that are kept in any case; rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, of dz where there is one
 constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
 // what is known of a call on the device; first in the workspace
@@ -154,43 +156,60 @@ __global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, si
   pack_row<DT>(from < 0 ? nullptr : (const unsigned char*)src + (size_t)from * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)r * padded, plane);
 }
 
-// The same for few rows in one launch with what dfx_vocab_rows_kernel does: every workgroup finds the rows that count, and lays out the one of its number.
+// The same for up to kLayRows rows in one launch with what dfx_vocab_rows_kernel does: every workgroup finds the rows that count, and lays out the one of its number.
 template <int DT>
-__global__ void __launch_bounds__(256) dfx_vocab_few_kernel(VocabArgs a, const void* src, size_t stride, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
-  __shared__ uint32_t counts[4];
+__global__ void __launch_bounds__(256) dfx_vocab_lay_kernel(VocabArgs a, const void* src, size_t stride, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
+  constexpr uint32_t R = kLayRows / 256u;
+  __shared__ uint32_t counts[R][4];
   __shared__ float tops[4];
   __shared__ int32_t mine;
   const uint32_t me = threadIdx.x, wave = me / kStepWave, lane = me % kStepWave;
-  const int64_t t = me < a.rows ? a.targets[me] : -1;
-  const float w = me < a.rows && a.row_weight ? a.row_weight[me] : 1.0f;
-  const bool counts_here = t >= 0 && t < (int64_t)a.vocab && w != 0.0f;
-  const uint64_t mask = __ballot(counts_here);
-  const float top = __uint_as_float(wave_max(__float_as_uint(counts_here ? fmaxf(fabsf(w), 0.0f) : 0.0f)));
-  if (lane == 0) { counts[wave] = (uint32_t)__popcll(mask); tops[wave] = top; }
+  int64_t t[R];
+  float w[R], top = 0.0f;
+  uint64_t mask[R];
+#pragma unroll
+  for (uint32_t r = 0; r < R; ++r) {
+    const uint32_t i = r * 256u + me;
+    t[r] = i < a.rows ? a.targets[i] : -1;
+    w[r] = i < a.rows && a.row_weight ? a.row_weight[i] : 1.0f;
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < R; ++r) {
+    const bool counts_here = t[r] >= 0 && t[r] < (int64_t)a.vocab && w[r] != 0.0f;
+    mask[r] = __ballot(counts_here);
+    if (counts_here) top = fmaxf(top, fabsf(w[r]));
+    if (lane == 0) counts[r][wave] = (uint32_t)__popcll(mask[r]);
+  }
+  top = __uint_as_float(wave_max(__float_as_uint(top)));
+  if (lane == 0) tops[wave] = top;
   if (me == 0) mine = -1;
   __syncthreads();
-  uint32_t place = (uint32_t)__popcll(mask & ((1ull << lane) - 1ull)), done = 0;
-  float most = 0.0f;
-  for (uint32_t k = 0; k < 4; ++k) {
-    place += k < wave ? counts[k] : 0u;
-    done += counts[k];
-    most = fmaxf(most, tops[k]);
-  }
-  if (counts_here && place == blockIdx.x) mine = (int32_t)me;
-  if (blockIdx.x == 0) {
-    if (me < a.rows) {
-      a.map[me] = counts_here ? (int32_t)place : -1;
+  uint32_t done = 0;
+#pragma unroll
+  for (uint32_t r = 0; r < R; ++r) {
+    uint32_t place = done + (uint32_t)__popcll(mask[r] & ((1ull << lane) - 1ull));
+    for (uint32_t k = 0; k < 4; ++k) {
+      place += k < wave ? counts[r][k] : 0u;
+      done += counts[r][k];
+    }
+    const bool counts_here = mask[r] >> lane & 1u;
+    const uint32_t i = r * 256u + me;
+    if (counts_here && place == blockIdx.x) mine = (int32_t)i;
+    if (blockIdx.x == 0 && i < a.rows) {
+      a.map[i] = counts_here ? (int32_t)place : -1;
       if (counts_here) {
-        a.idx[place] = (int32_t)me; a.target[place] = (int32_t)t; a.weight[place] = w;
+        a.idx[place] = (int32_t)i; a.target[place] = (int32_t)t[r]; a.weight[place] = w[r];
       } else {
-        if (a.logp) a.logp[me] = 0.0f;
-        if (a.loss) a.loss[me] = 0.0f;
+        if (a.logp) a.logp[i] = 0.0f;
+        if (a.loss) a.loss[i] = 0.0f;
       }
     }
-    if (me >= done && me < a.rp) {
-      a.idx[me] = -1; a.target[me] = -1; a.weight[me] = 0.0f;
+  }
+  if (blockIdx.x == 0) {
+    for (uint32_t i = done + me; i < a.rp; i += 256u) {
+      a.idx[i] = -1; a.target[i] = -1; a.weight[i] = 0.0f;
     }
-    if (me == 0) vocab_state(a, done, most);
+    if (me == 0) vocab_state(a, done, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
   }
   __syncthreads();
   pack_row<DT>(mine < 0 ? nullptr : (const unsigned char*)src + (size_t)mine * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)blockIdx.x * padded, plane);
@@ -264,7 +283,89 @@ struct VocabStats {
       parts[(size_t)(tile0 + at.m) * pitch + tile.n0 + i] = make_float2(top, s);
     }
   }
+  // of 64 logits of N rows, four of a row in each of N 16 threads (thread i: row i % N, logits 4 (i / N) on); lds: 16 N pairs
+  template <int N>
+  __device__ __forceinline__ void of_fours(uint32_t tile, uint32_t m0, uint32_t end, GemmAcc v, float2* lds) const {
+    const uint32_t n = threadIdx.x % N, four = threadIdx.x / N, m = m0 + four * 4u;
+    float top = -INFINITY, s = 0.0f;
+    if (four < 16u) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (m + e >= end) v[e] = -INFINITY;
+      if (z && m < end) *(GemmAcc*)(z + (size_t)n * z_pitch + m) = v;
+      const uint32_t t = (uint32_t)target[n] - v0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        top = fmaxf(top, v[e]);
+        if (m + e == t && t < end) zt[n] = v[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += vocab_exp(v[e], vocab_base(top), k);
+      lds[four * N + n] = make_float2(top, s);
+    }
+    if (!parts) return;
+    __syncthreads();
+    if (threadIdx.x >= N) return;
+    for (uint32_t q = 1; q < 16; ++q) top = fmaxf(top, lds[q * N + n].x);
+    s = 0.0f;
+    for (uint32_t q = 0; q < 16; ++q) s += lds[q * N + n].y * vocab_exp(lds[q * N + n].x, vocab_base(top), k);
+    parts[(size_t)(tile0 + tile) * pitch + n] = make_float2(top, s);
+  }
 };
+
+// What the n-th of the rows that count comes to, of its largest logit and the sum around it; behind them: nothing.
+__device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint32_t count, float top, float s, bool writes) {
+  VocabRow r = {0.0f, 0.0f, 0.0f, -1};
+  float logp = 0.0f, loss = 0.0f, w = 0.0f;
+  if (n < count && s != 0.0f) {          // (0: no logit above -infinity)
+    int two;
+    const float f = frexpf(s, &two), base = vocab_base(top);
+    w = a.weight[n];
+    logp = (float)(a.c * ((double)a.zt[n] - (double)base) - ((double)two + (double)__builtin_amdgcn_logf(f)) * kVLog2);
+    loss = -w * logp;
+    const float relative = w / *a.top_weight * kDzScale;
+    r = {base, relative / s, relative, a.target[n]};
+  }
+  if (!writes) return r;
+  a.row[n] = r;
+  a.row_loss[n] = loss;
+  a.row_w[n] = w;
+  if (n < count) {
+    if (a.logp) a.logp[a.idx[n]] = logp;
+    if (a.loss) a.loss[a.idx[n]] = loss;
+  }
+  return r;
+}
+
+// The tiles' parts of a row joined by a workgroup of 256: where they are few.  (Which way they are joined goes by the vocabulary alone, so that a row's logp is the same with
+// gradients and without.)
+__device__ __forceinline__ float2 join_row(const VocabArgs& a, uint32_t n, bool any) {
+  __shared__ float2 lds[4];
+  float top = -INFINITY, s = 0.0f;
+  if (any)
+    for (uint32_t t = threadIdx.x; t < a.tiles; t += 256u) {
+      const float2 p = a.parts[(size_t)t * a.pitch + n];
+      const float more = fmaxf(top, p.x), base = vocab_base(more);
+      s = s * vocab_exp(top, base, a.k) + p.y * vocab_exp(p.x, base, a.k);
+      top = more;
+    }
+  float most = top;
+#pragma unroll
+  for (uint32_t x = kStepWave / 2; x; x >>= 1) most = fmaxf(most, __shfl_xor(most, (int)x));
+  s = wave_sum(s * vocab_exp(top, vocab_base(most), a.k));
+  if (threadIdx.x % kStepWave == 0) lds[threadIdx.x / kStepWave] = make_float2(most, s);
+  __syncthreads();
+  top = fmaxf(fmaxf(lds[0].x, lds[1].x), fmaxf(lds[2].x, lds[3].x));
+  s = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) s += lds[k].y * vocab_exp(lds[k].x, vocab_base(top), a.k);
+  return make_float2(top, s);
+}
+__global__ void __launch_bounds__(256) dfx_vocab_row_kernel(VocabArgs a) {
+  const uint32_t n = blockIdx.x, count = a.state->count;
+  const float2 all = join_row(a, n, n < count);
+  if (threadIdx.x == 0) row_end(a, n, count, all.x, all.y, true);
+}
 
 // The tiles' parts of a row joined, and what it comes to.  S threads to a row: few where there are many rows.
 template <uint32_t S>
@@ -291,31 +392,13 @@ __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
   __syncthreads();
   if (slice || n >= a.rp) return;
   for (uint32_t k = 1; k < S; ++k) top = fmaxf(top, lds[k][i].x);
-  const float base = vocab_base(top);
   s = 0.0f;
-  for (uint32_t k = 0; k < S; ++k) s += lds[k][i].y * vocab_exp(lds[k][i].x, base, a.k);
-  VocabRow r = {0.0f, 0.0f, 0.0f, -1};
-  float logp = 0.0f, loss = 0.0f, w = 0.0f;
-  if (n < count && s != 0.0f) {          // (0: no logit above -infinity)
-    int two;
-    const float f = frexpf(s, &two);
-    w = a.weight[n];
-    logp = (float)(a.c * ((double)a.zt[n] - (double)base) - ((double)two + (double)__builtin_amdgcn_logf(f)) * kVLog2);
-    loss = -w * logp;
-    const float relative = w / *a.top_weight * kDzScale;
-    r = {base, relative / s, relative, a.target[n]};
-  }
-  a.row[n] = r;
-  a.row_loss[n] = loss;
-  a.row_w[n] = w;
-  if (n < count) {
-    if (a.logp) a.logp[a.idx[n]] = logp;
-    if (a.loss) a.loss[a.idx[n]] = loss;
-  }
+  for (uint32_t k = 0; k < S; ++k) s += lds[k][i].y * vocab_exp(lds[k][i].x, vocab_base(top), a.k);
+  row_end(a, n, count, top, s, true);
 }
 
-// sums over the rows, in an order that is always the same
-__global__ void __launch_bounds__(256) dfx_vocab_sums_kernel(VocabArgs a) {
+// sums over the rows, in an order that is always the same, by a workgroup of 256
+__device__ __forceinline__ void vocab_sums(const VocabArgs& a) {
   __shared__ double lds[2][4];
   double s = 0.0, w = 0.0;
   for (uint32_t i = threadIdx.x, n = a.state->count; i < n; i += 256u) {
@@ -330,6 +413,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_sums_kernel(VocabArgs a) {
   __syncthreads();
   if (threadIdx.x < 2) a.sums[threadIdx.x] = (float)(lds[threadIdx.x][0] + lds[threadIdx.x][1] + lds[threadIdx.x][2] + lds[threadIdx.x][3]);
 }
+__global__ void __launch_bounds__(256) dfx_vocab_sums_kernel(VocabArgs a) { vocab_sums(a); }
 
 // dz of a tile, to the type of the products
 template <int DT>
@@ -367,14 +451,20 @@ struct VocabDz {
   }
 };
 
-// dz of a piece whose logits were kept: a workgroup to 2048 logits of a row.  Rows behind those that count are 0 as far as the products take them.
-template <int DT>
-__global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabDz<DT> d, const float* z, const uint32_t* count) {
-  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 8u, rows = *count;
-  if (n >= (rows + kGemmK - 1) / kGemmK * kGemmK || m >= d.pitch) return;
+// dz of a piece whose logits were kept: a workgroup to 2048 logits of a row.  Rows behind those that count are 0 as far as the products take them.  JOIN: the row's parts are
+// joined by each of its workgroups, which spares a launch where they are few.
+template <int DT, bool JOIN>
+__global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabArgs a, VocabDz<DT> d, const float* z) {
+  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 8u, count = a.state->count;
+  const bool in = m < d.pitch, any = n < count;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (n < rows && m < d.left) memcpy(v, __builtin_assume_aligned(z + (size_t)n * d.pitch + m, 16), 32);      // (left is rounded up to a multiple of 4 at most)
-  d.put(n, n < rows ? d.row[n] : VocabRow{0.0f, 0.0f, 0.0f, -1}, m, v);
+  if (any && in && m < d.left) memcpy(v, __builtin_assume_aligned(z + (size_t)n * d.pitch + m, 16), 32);      // (left is rounded up to a multiple of 4 at most)
+  VocabRow r = {0.0f, 0.0f, 0.0f, -1};
+  if constexpr (JOIN) {
+    const float2 all = join_row(a, n, any);
+    r = row_end(a, n, count, all.x, all.y, blockIdx.y == 0 && threadIdx.x == 0);
+  } else if (any) r = d.row[n];
+  if (in && n < (count + kGemmK - 1) / kGemmK * kGemmK) d.put(n, r, m, v);
 }
 
 // a part of dX, in 32 bits: [splits][rows][pitch]
@@ -442,10 +532,14 @@ struct VocabDw {
   }
 };
 
-// dX: the splits' parts, in their order; rows that do not count are 0
+// dX: the splits' parts, in their order; rows that do not count are 0.  A workgroup behind them makes the sums, where they are asked for.
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const float* part, uint32_t splits, uint32_t split_rows, uint32_t pitch, void* grad, size_t stride, uint32_t dim) {
   const uint32_t row = blockIdx.x, e = (blockIdx.y * 256u + threadIdx.x) * 4u;
+  if (row == a.rows) {                   // one more, for the sums
+    if (blockIdx.y == 0) vocab_sums(a);
+    return;
+  }
   if (e >= dim) return;
   const int32_t n = a.map[row];
   const float g = a.state->g;
@@ -480,7 +574,7 @@ bool vocab_aligned(const dfx_vocab_loss_args& u) {
 
 struct VocabPlan {
   size_t rp, dp, dq, vp, pieces, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, pieces, tiles of the vocabulary, splits of dX and the tiles' rows
-  bool few, keep;                        // keep: the logits of the last piece
+  bool few, lone, keep;                  // lone: x stays in registers; keep: the logits of the last piece
   int nt, mt;                            // tiles of the products for few rows
   size_t height;                         // of a tile of the vocabulary
   size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
@@ -492,6 +586,7 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   VocabPlan p;
   const size_t planes = gemm_planes(dtype);
   p.few = rows <= kFewRows && dim >= kFewDim;
+  p.lone = false;
   p.rp = std::max(kTileRows, up(rows, kTileRows));
   p.dp = up(dim, kGemmK);
   p.dq = up(dim, 4);
@@ -506,16 +601,17 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   if (p.few) length = few_most;
   p.pieces = (whole + length - 1) / length;
   p.vp = piece ? length : up((whole + p.pieces - 1) / p.pieces, kTileRows);      // (of equal length)
-  p.keep = grad && (p.few || long_rows);
+  p.keep = grad && (p.few || long_rows || p.rp * p.vp <= kKeepElems);
   if (p.few) {
     p.nt = rows <= 32 ? 2 : 4;
-    p.mt = aligned || vocab >= kFewWide ? 2 : 1;
+    p.lone = rows <= (dtype == DFX_F32 ? 16 : 32) && dim <= (rows <= 16 && dtype != DFX_F32 ? 4096 : 2048);
+    p.mt = !p.lone && (aligned || vocab >= kFewWide) ? 2 : 1;
     // so many tiles that whole rounds of workgroups, two to a compute unit, have them all
     const size_t rounds = std::max<size_t>(1, (vocab + 512 * 64 * p.mt - 1) / (512 * 64 * p.mt));
     p.height = std::max<size_t>(16, up((vocab + 512 * rounds - 1) / (512 * rounds), 4));
     p.tiles = (vocab + p.height - 1) / p.height + p.pieces;      // (of each piece by itself)
     p.split_rows = up(std::max<size_t>(rows, 1), 64);
-    const size_t dx_wide = 16 * kFewE, groups = up(std::max<size_t>(rows, 1), 16 * p.nt) / (16 * p.nt) * (up(dim, dx_wide) / dx_wide);
+    const size_t dx_wide = 16 * gemm_few_e(dtype, p.nt), groups = up(std::max<size_t>(rows, 1), 16 * p.nt) / (16 * p.nt) * (up(dim, dx_wide) / dx_wide);
     p.splits = std::max<size_t>(1, std::min(768 / groups, p.vp / kFewK));
   } else {
     p.height = kTileRows;
@@ -532,8 +628,8 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   p.x = take(planes * p.rp * p.dp * 2);
   p.w = p.few ? at : take(planes * most * p.dp * 2);
   p.dz = grad ? take(planes * std::max(dz, kFewRows * few_most) * 2) : at;
-  p.z = grad ? take(std::max(long_rows ? dz : 0, kFewRows * few_most) * 4) : at;
-  p.dx = grad ? take(std::max(std::max(256 / (up(dim, 256) / 256), p.rp / 256) * 256, std::max<size_t>(768 / (up(dim, 64) / 64), 1) * kFewRows) * p.dq * 4) : at;
+  p.z = grad ? take(std::max(long_rows ? dz : std::min(dz, kKeepElems), kFewRows * few_most) * 4) : at;
+  p.dx = grad ? take(std::max(std::max(256 / (up(dim, 256) / 256), p.rp / 256) * 256, std::max<size_t>(768 / (up(dim, 128) / 128), 1) * kFewRows) * p.dq * 4) : at;
   p.bytes = at;
   return p;
 }
@@ -551,6 +647,16 @@ template <int DT, class EPI>
 int vocab_few(const VocabPlan& p, bool aligned, const GemmSource& w, const GemmOperand& x, GemmShape s, size_t rows, const EPI& epi, hipStream_t stream) {
   s.mtiles = (uint32_t)((w.rows + p.height - 1) / p.height);
   s.height = (uint32_t)p.height;
+  if (p.lone) {
+    if (!s.mtiles || !rows) return DFX_OK;
+    auto go = [&](auto k) { return step_launch(k, dim3(s.mtiles), 512, stream, w, x, s.height, epi); };
+    if (rows > 16) {
+      if constexpr (DT != DFX_F32) return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 2, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 2, 8, EPI>);
+    }
+    if constexpr (DT != DFX_F32)
+      if (w.dim > 2048) return go(dfx_gemm_lone_kernel<DT, 1, 16, EPI>);
+    return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 1, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 1, 8, EPI>);
+  }
   if constexpr (DT != DFX_F32)
     if (aligned) {
       s.ntiles = (uint32_t)((rows + GemmFlat::N - 1) / GemmFlat::N);
@@ -567,7 +673,7 @@ int vocab_few(const VocabPlan& p, bool aligned, const GemmSource& w, const GemmO
 
 template <int DT>
 int vocab_few_dx(const VocabPlan& p, const GemmSource& w, const GemmOperand& z, GemmShape s, size_t rows, float* dx, bool more, hipStream_t stream) {
-  constexpr uint32_t wide = 16 * kFewE;
+  const uint32_t wide = 16 * gemm_few_e(DT, p.nt);
   s.mtiles = (w.dim + wide - 1) / wide;
   s.ntiles = (uint32_t)((rows + 16 * p.nt - 1) / (16 * p.nt));
   s.ksteps = (w.rows + kFewK - 1) / kFewK;
@@ -611,7 +717,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   float* dx = (float*)(ws + p.dx);
 
   const size_t hs = u.hidden_stride ? u.hidden_stride : u.dim;
-  if (p.few) VOCAB_TRY(step_launch(dfx_vocab_few_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+  if (u.rows <= kLayRows) VOCAB_TRY(step_launch(dfx_vocab_lay_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
   else {
     VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
     VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, hs, (const int32_t*)a.idx, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
@@ -653,16 +759,22 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     tile0 += (left + p.height - 1) / p.height;
   }
   a.tiles = (uint32_t)tile0;
-  if (p.few) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
-  else VOCAB_TRY(step_launch(dfx_vocab_join_kernel<8>, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
-  if (u.sums) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
-  if (!u.grad_hidden && !u.grad_weight) return DFX_OK;
+  const bool grad = u.grad_hidden || u.grad_weight, by_row = u.vocab <= kJoinMost, join = grad && z && pieces && by_row;
+  if (!join) {
+    if (by_row) VOCAB_TRY(step_launch(dfx_vocab_row_kernel, dim3((uint32_t)p.rp), 256, stream, a));
+    else if (p.few) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
+    else VOCAB_TRY(step_launch(dfx_vocab_join_kernel<8>, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
+  }
+  const bool sums_last = u.sums && u.grad_hidden && u.rows;
+  if (u.sums && !sums_last && !join) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
+  if (!grad) return DFX_OK;
   for (size_t q = pieces; q-- != 0;) {   // the last one first
     const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
     if (direct || (!p.few && v0 != last)) VOCAB_TRY(take_piece(v0, left));
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
     if (p.few && v0 != last) VOCAB_TRY(logits(v0, left, stats(v0, left, z, 0, nullptr)));
-    if (p.few || (z && v0 == last)) VOCAB_TRY(step_launch(dfx_vocab_dz_kernel<DT>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, epi, (const float*)z, count));
+    if (p.few || (z && v0 == last))
+      VOCAB_TRY(step_launch(join && v0 == last ? dfx_vocab_dz_kernel<DT, true> : dfx_vocab_dz_kernel<DT, false>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, a, epi, (const float*)z));
     else VOCAB_TRY((vocab_gemm<DT, false, false>(ow, ox, by_rows, left, u.rows, epi, stream)));
     const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
     const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), 0, count, false}, sw = {0, 0, 1, 0, 0, count, true};
@@ -681,8 +793,9 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     if (u.grad_dtype == DFX_F32) VOCAB_TRY(both(VocabDw<DFX_F32>{(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
     else if constexpr (DT != DFX_F32) VOCAB_TRY(both(VocabDw<DT>{(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
   }
+  if (u.sums && !sums_last && join) VOCAB_TRY(step_launch(dfx_vocab_sums_kernel, dim3(1), 256, stream, a));
   if (u.grad_hidden && u.rows)
-    VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows, (uint32_t)((u.dim + 1023) / 1024)), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
+    VOCAB_TRY(step_launch(dfx_vocab_dx_kernel<DT>, dim3((uint32_t)u.rows + (sums_last ? 1u : 0u), (uint32_t)((u.dim + 1023) / 1024)), 256, stream, a, (const float*)dx, (uint32_t)p.splits, (uint32_t)p.split_rows, (uint32_t)p.dq, u.grad_hidden,
                           u.grad_hidden_stride ? u.grad_hidden_stride : u.dim, (uint32_t)u.dim));
   return DFX_OK;
 }

@@ -323,7 +323,8 @@ class Vocab:
 
 
 VOCAB = [(1, 1, 1), (1, 64, 257), (2, 7, 5), (48, 128, 1000), (64, 64, 256), (65, 192, 513), (130, 100, 777), (200, 256, 1025), (257, 65, 300), (300, 320, 3000), (600, 64, 512),
-         (1, 77, 300), (20, 1001, 700), (33, 66, 1000), (100, 130, 515), (128, 200, 900), (129, 64, 400), (5, 63, 300), (3, 64, 65600), (70, 71, 66001)]
+         (1, 77, 300), (20, 1001, 700), (33, 66, 1000), (100, 130, 515), (128, 200, 900), (129, 64, 400), (5, 63, 300), (3, 64, 65600), (70, 71, 66001),
+         (16, 1024, 300), (17, 1025, 300), (9, 2048, 520), (31, 2040, 260), (3, 2047, 300), (12, 4095, 270), (16, 4096, 260), (33, 4096, 260), (1000, 96, 600), (1025, 70, 300)]
 
 
 @pytest.mark.parametrize("dt", TYPES)
