@@ -1,6 +1,8 @@
 // Walks the rows and elements that a tile's loads read: all of them lie inside the matrix, and those of the tile that the matrix has are the tile's own.
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "../../paper_2303_06324_amd/csrc/dfx_tiles.h"
 
 int main() {
