@@ -56,7 +56,7 @@ __device__ __forceinline__ GemmPlace gemm_place(const GemmShape& s, uint32_t nti
   const uint32_t width = min(kGroup, ntiles - group * kGroup);
   return {in / width, group * kGroup + in % width, split, true};
 }
-inline uint32_t gemm_groups(const GemmShape& s) { return (uint32_t)(((uint64_t)s.mtiles * s.ntiles * s.splits + 7) / 8 * 8); }
+inline __host__ __device__ uint32_t gemm_groups(const GemmShape& s) { return (uint32_t)(((uint64_t)s.mtiles * s.ntiles * s.splits + 7) / 8 * 8); }
 
 // Tiles in LDS.  k along the rows: a row's 128 bytes, whose 16-byte parts are exchanged by the row's number, so that 16 rows' parts of one k lie in
 // different banks.  Turned: a k's 2 COLS bytes, whose 32-byte parts (16 elements, a tile of the matrix instruction) are exchanged by k, so that those of four k's
@@ -414,18 +414,93 @@ __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperan
   epi(tile, at, acc, gemm_lds);
 }
 
+// A quarter of it: 128 by 128, of which each of the eight waves has 64 by 32.
+struct GemmQuarter {
+  static constexpr int WM = 2, WN = 4, MT = 4, NT = 2, M = 128, N = 128, THREADS = 512;
+  static constexpr int HALF = 128 * kGemmK * 2, STAGE = 2 * HALF, STAGES = 4, LOADS = 4;
+  uint32_t m0, n0;
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave / WN * 64u; }
+  __device__ __forceinline__ uint32_t wave_n() const { return threadIdx.x / kStepWave % WN * 32u; }
+  __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16u + threadIdx.x % kStepWave / 16 * 4; }
+  __device__ __forceinline__ uint32_t n(int nt) const { return n0 + wave_n() + nt * 16u + threadIdx.x % 16; }
+  __device__ __forceinline__ uint32_t row(int nt, uint32_t r) const { return n0 + r / 16u * 32u + nt * 16u + r % 16u; }
+  __device__ __forceinline__ uint32_t row_of_pass() const { return wave_n() / 2u + threadIdx.x % 16; }
+};
+static_assert(GemmQuarter::STAGES * GemmQuarter::STAGE <= GemmWide::LDS, "a workgroup takes either tile");
+
+// Where wide tiles would leave compute units idle.  Four stages, three of which are under way; the waves of a SIMD fill each other's waits.
 template <int DT, bool TA, bool TB, class EPI>
-__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
-  __shared__ __align__(1024) unsigned char lds[GemmWide::LDS];
-  gemm_wide<DT, TA, TB>(a, b, s, epi, blockIdx.x, lds);
+__device__ __forceinline__ void gemm_quarter(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const EPI& epi, uint32_t block, unsigned char* lds) {
+  typedef GemmQuarter TILE;
+  TILE tile;
+  uint32_t begin, end;
+  const GemmPlace at = gemm_work(s, block, tile, begin, end);
+  if (!at.any) return;
+  GemmAcc acc[TILE::MT][TILE::NT];
+#pragma unroll
+  for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < TILE::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+  const uint32_t total = (end - begin) * gemm_pairs(DT);
+  if (total) {
+    GemmNext next(begin, end, total);
+    auto load = [&](uint32_t stage) {
+      gemm_fetch<128, TILE::THREADS, TA>(a, gemm_planes(DT) == 1 ? 0 : gemm_plane_a(next.pair), tile.m0, next.k * kGemmK, lds + stage * TILE::STAGE);
+      gemm_fetch<128, TILE::THREADS, TB>(b, gemm_planes(DT) == 1 ? 0 : gemm_plane_b(next.pair), tile.n0, next.k * kGemmK, lds + stage * TILE::STAGE + TILE::HALF);
+      next.advance();
+    };
+    for (uint32_t q = 0; q < 3; ++q) load(q);
+    for (uint32_t q = 0; q < total; ++q) {
+      gemm_wait<2 * TILE::LOADS>();
+      gemm_meet();                       // this stage has arrived for all, and nobody reads the one before it any more
+      load((q + 3u) & 3u);
+      const unsigned char* at_a = lds + (q & 3u) * TILE::STAGE;
+      GemmShort8 fa[TILE::MT][2], fb[TILE::NT][2];
+      gemm_take<TILE::NT, 128, TB>(at_a + TILE::HALF, tile.wave_n(), fb);
+      gemm_take<TILE::MT, 128, TA>(at_a, tile.wave_m(), fa);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+          for (int j = 0; j < TILE::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i][kk], fb[j][kk], acc[i][j]);
+    }
+    gemm_wait<0>();
+    gemm_meet();
+  }
+  epi(tile, at, acc, lds);
 }
 
-// Two products in one launch, the one of the longer sums first: the short ones' tiles fill the compute units that its last round leaves idle.
+// What the workgroups of a launch from `from` on do: a product by wide tiles or by quarters
+template <class EPI>
+struct GemmTask {
+  GemmOperand a, b;
+  GemmShape s;
+  uint32_t from;
+  bool quarters;
+  EPI epi;
+};
+template <int DT, bool TA, bool TB, class EPI>
+__device__ __forceinline__ bool gemm_task(const GemmTask<EPI>& t, unsigned char* lds) {
+  const uint32_t block = blockIdx.x - t.from;
+  if (block >= gemm_groups(t.s)) return false;
+  if (t.quarters) gemm_quarter<DT, TA, TB>(t.a, t.b, t.s, t.epi, block, lds);
+  else gemm_wide<DT, TA, TB>(t.a, t.b, t.s, t.epi, block, lds);
+  return true;
+}
+
+// Two products in one launch, the one of the longer sums first: the other's tiles fill the compute units that its last round leaves idle.
 template <int DT, bool TA, bool TB, class EPI, bool TA2, bool TB2, class EPI2>
-__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_two_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi, uint32_t first, GemmOperand a2, GemmOperand b2, GemmShape s2, EPI2 epi2) {
+__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_two_kernel(GemmTask<EPI> one, GemmTask<EPI2> two) {
   __shared__ __align__(1024) unsigned char lds[GemmWide::LDS];
-  if (blockIdx.x < first) gemm_wide<DT, TA, TB>(a, b, s, epi, blockIdx.x, lds);
-  else gemm_wide<DT, TA2, TB2>(a2, b2, s2, epi2, blockIdx.x - first, lds);
+  if (!gemm_task<DT, TA, TB>(one, lds)) gemm_task<DT, TA2, TB2>(two, lds);
+}
+// ... of which both are one, some of its tiles wide
+template <int DT, bool TA, bool TB, class EPI>
+__global__ void __launch_bounds__(GemmWide::THREADS, 2) dfx_gemm_wide_kernel(GemmTask<EPI> wide, GemmTask<EPI> quarters) {
+  __shared__ __align__(1024) unsigned char lds[GemmWide::LDS];
+  if (blockIdx.x < quarters.from) gemm_wide<DT, TA, TB>(wide.a, wide.b, wide.s, wide.epi, blockIdx.x, lds);
+  else gemm_quarter<DT, TA, TB>(quarters.a, quarters.b, quarters.s, quarters.epi, blockIdx.x - quarters.from, lds);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -220,12 +220,12 @@ struct VocabStats {
   float2* parts;
   float *zt, *z;                         // z: [pitch][z_pitch], may be null
   const int32_t* target;
-  uint32_t pitch, z_pitch, left, v0, tile0, height;      // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile; height: of a tile
+  uint32_t pitch, z_pitch, left, v0, tile0, height;      // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile; height: of a tile, 0: all of it
   float k;
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
     const uint32_t lane = threadIdx.x % kStepWave, wave = threadIdx.x / kStepWave;
-    const uint32_t end = min(left, tile.m0 + height);
+    const uint32_t end = min(left, tile.m0 + (height ? height : (uint32_t)TILE::M));
     if (tile.m0 + TILE::M > end) {
 #pragma unroll
       for (int i = 0; i < TILE::MT; ++i)
@@ -576,9 +576,51 @@ struct VocabPlan {
   size_t rp, dp, dq, vp, pieces, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, pieces, tiles of the vocabulary, splits of dX and the tiles' rows
   bool few, lone, keep;                  // lone: x stays in registers; keep: the logits of the last piece
   int nt, mt;                            // tiles of the products for few rows
-  size_t height;                         // of a tile of the vocabulary
+  size_t height;                         // of a tile of the vocabulary, for few rows
+  size_t wide;                           // otherwise: rows of the vocabulary whose logits go by wide tiles, the others' by quarters
+  bool dx_quarters, dw_quarters;         // whether the gradients' products do
   size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
 };
+
+// How long a launch takes of workgroups, one to a compute unit, of two kinds: n of length l each, the longer ones first.
+double vocab_time(size_t n, double l, size_t n2, double l2) {
+  if (l2 > l) { std::swap(n, n2); std::swap(l, l2); }
+  const size_t some = n % 256;           // compute units that have one more of the long ones
+  const double early = (double)(n / 256) * l, late = some ? early + l : early;
+  if (!n2) return late;
+  auto done = [&](double t) { return (double)(256 - some) * floor((t - early) / l2 + 1e-9) + (t > late ? (double)some * floor((t - late) / l2 + 1e-9) : 0.0); };
+  double k = std::max(1.0, std::max(floor((double)n2 / 256), std::min(ceil((double)n2 / (double)(256 - some)), floor((late - early) / l2))));
+  while (done(early + k * l2) < (double)n2) k += 1;
+  const double t = early + k * l2, other = t > late ? late + floor((t - late) / l2) * l2 : late;      // (those that come behind the late ones may be the last)
+  return std::max(late, other < t && done(other) >= (double)n2 ? other : t);
+}
+
+// Tiles of the products of many rows, and splits of dX: what takes the shortest time where a wide tile takes a unit for a step of k and as long as 8 steps (logits; a part
+// of dX 4, of dW 5) besides, and a quarter of it 0.3 of both.
+constexpr double kQuarter = 0.3;
+void vocab_tiles(VocabPlan& p, size_t rows, size_t dim, size_t vocab, size_t pairs) {
+  auto over = [](size_t n, size_t by) { return (n + by - 1) / by; };
+  const size_t n4 = over(rows, 256), n1 = over(rows, 128), v4 = over(vocab, 256), m4 = over(dim, 256), m1 = over(dim, 128);
+  const double logits = (double)(p.dp / kGemmK * pairs) + 8;
+  double best = 1e300;
+  for (size_t wide : {v4, v4 * n4 / 256 * 256 / n4, (size_t)0}) {
+    const double t = vocab_time(wide * n4, logits, n1 * (wide < v4 ? over(vocab - wide * 256, 128) : 0), kQuarter * logits);
+    if (t < best) { best = t; p.wide = wide * 256; }
+  }
+  p.tiles = p.wide / 256 + over(vocab > p.wide ? vocab - p.wide : 0, 128);
+  const size_t most = std::max<size_t>(1, std::min(256 / (p.rp / 256 * m4), p.vp / 256)), steps = p.vp / kGemmK;
+  const double dw = (double)(over(rows, kGemmK) * pairs) + 5;
+  best = 1e300;
+  for (int kind = 0; kind < 4; ++kind) {
+    const bool xq = kind & 1, wq = kind >> 1;
+    for (size_t part = 1; part <= 16; ++part) {
+      const size_t splits = over(most * part, 16);
+      const double dx = (double)(over(steps, splits) * pairs) + 4;
+      const double t = vocab_time(splits * (xq ? n1 * m1 : n4 * m4), xq ? kQuarter * dx : dx, wq ? m1 * over(p.vp, 128) : m4 * (p.vp / 256), wq ? kQuarter * dw : dw) + (double)(splits * rows * dim) * 0.5e-6;
+      if (t < best) { best = t; p.splits = splits; p.dx_quarters = xq; p.dw_quarters = wq; }
+    }
+  }
+}
 
 // Splits of dX along the vocabulary: as many workgroups as compute units, of the products for few rows three times as many.  What depends on the number of rows has room for
 // any smaller number.  aligned: rows of weight lie at multiples of 16 bytes (which changes nothing of the space).
@@ -614,17 +656,16 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
     const size_t dx_wide = 16 * gemm_few_e(dtype, p.nt), groups = up(std::max<size_t>(rows, 1), 16 * p.nt) / (16 * p.nt) * (up(dim, dx_wide) / dx_wide);
     p.splits = std::max<size_t>(1, std::min(768 / groups, p.vp / kFewK));
   } else {
-    p.height = kTileRows;
-    p.tiles = (vocab + kTileRows - 1) / kTileRows;
+    p.height = 0;
     p.split_rows = p.rp;
-    p.splits = std::max<size_t>(1, std::min(256 / (p.rp / 256 * (up(dim, 256) / 256)), p.vp / 256));
+    vocab_tiles(p, std::max<size_t>(rows, 1), dim, vocab, gemm_pairs(dtype));
   }
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
   p.state = take(sizeof(VocabState) + 4);
   p.idx = take(4 * p.rp); p.target = take(4 * p.rp); p.map = take(4 * p.rp); p.weight = take(4 * p.rp); p.zt = take(4 * p.rp);
   p.row_loss = take(4 * p.rp); p.row_w = take(4 * p.rp); p.row = take(sizeof(VocabRow) * p.rp);
-  p.parts = take(sizeof(float2) * std::max<size_t>(p.rp * (whole / kTileRows), kFewRows * std::min(whole / 4, whole / 32 + 520)));
+  p.parts = take(sizeof(float2) * std::max<size_t>(p.rp * (whole / 128), kFewRows * std::min(whole / 4, whole / 32 + 520)));
   p.x = take(planes * p.rp * p.dp * 2);
   p.w = p.few ? at : take(planes * most * p.dp * 2);
   p.dz = grad ? take(planes * std::max(dz, kFewRows * few_most) * 2) : at;
@@ -634,12 +675,24 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   return p;
 }
 
-template <int DT, bool TA, bool TB, class EPI>
-int vocab_gemm(const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, hipStream_t stream) {
-  s.mtiles = (uint32_t)((m + GemmWide::M - 1) / GemmWide::M);
-  s.ntiles = (uint32_t)((n + GemmWide::N - 1) / GemmWide::N);
-  if (!s.mtiles || !s.ntiles) return DFX_OK;
-  return step_launch(dfx_gemm_wide_kernel<DT, TA, TB, EPI>, dim3(gemm_groups(s)), GemmWide::THREADS, stream, a, b, s, epi);
+// a product as workgroups of a launch from `from` on, of m by n elements
+template <class EPI>
+GemmTask<EPI> vocab_task(const GemmOperand& a, const GemmOperand& b, GemmShape s, size_t m, size_t n, const EPI& epi, bool quarters, uint32_t from) {
+  const size_t tile = quarters ? 128 : 256;
+  s.mtiles = (uint32_t)((m + tile - 1) / tile);
+  s.ntiles = (uint32_t)((n + tile - 1) / tile);
+  return {a, b, s, from, quarters, epi};
+}
+
+// what is made of logits, with wide tiles and with quarters
+template <int DT, class EPI>
+int vocab_logits(const GemmOperand& w, const GemmOperand& x, const GemmShape& s, size_t wide, size_t vocab, size_t rows, const EPI& epi, const EPI& epi_quarters, hipStream_t stream) {
+  GemmOperand rest = w;
+  rest.p += wide * w.stride; rest.rows = (uint32_t)(vocab - wide);
+  const auto one = vocab_task(w, x, s, wide, rows, epi, false, 0);
+  const auto two = vocab_task(rest, x, s, vocab - wide, rows, epi_quarters, true, gemm_groups(one.s));
+  const uint32_t groups = two.from + gemm_groups(two.s);
+  return groups ? step_launch(dfx_gemm_wide_kernel<DT, false, false, EPI>, dim3(groups), GemmWide::THREADS, stream, one, two) : DFX_OK;
 }
 
 // the products for few rows: logits, dX, dW
@@ -687,14 +740,17 @@ int vocab_few_dw(const GemmOperand& x, const GemmOperand& z, const uint32_t* cou
   return step_launch(rows <= kGemmK ? dfx_gemm_few_dw_kernel<DT, 1, OUT> : dfx_gemm_few_dw_kernel<DT, 2, OUT>, dim3(mtiles * each), 256, stream, x, z, count, mtiles, ntiles, each, out);
 }
 
-// dX and dW of a piece in one launch (dX's tiles of many rows are the wide ones)
+// dX and dW of a piece, or one of them, in one launch: the longer ones first
 template <int DT, class DW>
-int vocab_gemm_two(const GemmOperand& w, const GemmOperand& z, GemmShape sx, size_t dim, size_t rows, const VocabDx& dx, const GemmOperand& x, GemmShape sw, size_t vocab, const DW& dw, hipStream_t stream) {
-  sx.mtiles = sw.mtiles = (uint32_t)((dim + 255) / 256);
-  sx.ntiles = (uint32_t)((rows + 255) / 256);
-  sw.ntiles = (uint32_t)((vocab + 255) / 256);
-  const uint32_t first = gemm_groups(sx);
-  return step_launch(dfx_gemm_two_kernel<DT, true, false, VocabDx, true, true, DW>, dim3(first + gemm_groups(sw)), GemmWide::THREADS, stream, w, z, sx, dx, first, x, z, sw, dw);
+int vocab_grads(const VocabPlan& p, const GemmOperand& w, const GemmOperand& z, const GemmShape& sx, size_t dim, size_t rows, const VocabDx* dx, const GemmOperand& x, const GemmShape& sw, size_t vocab, const DW* dw,
+                hipStream_t stream) {
+  auto one = vocab_task(w, z, sx, dx ? dim : 0, rows, dx ? *dx : VocabDx{}, p.dx_quarters, 0);
+  auto two = vocab_task(x, z, sw, dw ? dim : 0, vocab, dw ? *dw : DW{}, p.dw_quarters, 0);
+  const uint32_t n1 = gemm_groups(one.s), n2 = gemm_groups(two.s);
+  const bool dw_first = (p.dw_quarters ? kQuarter : 1.0) * (double)((rows + kGemmK - 1) / kGemmK) > (p.dx_quarters ? kQuarter : 1.0) * (double)(sx.ksteps / sx.splits);
+  if (dw_first) one.from = n2;
+  else two.from = n1;
+  return n1 + n2 ? step_launch(dfx_gemm_two_kernel<DT, true, false, VocabDx, true, true, DW>, dim3(n1 + n2), GemmWide::THREADS, stream, one, two) : DFX_OK;
 }
 
 #define VOCAB_TRY(call) do { const int rc_ = (call); if (rc_ != DFX_OK) return rc_; } while (0)
@@ -745,20 +801,24 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     return VocabStats{parts, a.zt, keep, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, (uint32_t)tile, (uint32_t)p.height, a.k};
   };
   GemmSource few_w = {};
-  auto logits = [&](size_t v0, size_t left, const auto& epi) -> int {      // of rows of weight from v0 on
-    if (p.few) {
-      few_w = {(const unsigned char*)u.weight + v0 * ws_stride * eb, ws_stride, (uint32_t)left, (uint32_t)u.dim};
-      return vocab_few<DT>(p, vocab_aligned(u), few_w, ox, by_rows, u.rows, epi, stream);
-    }
-    return vocab_gemm<DT, false, false>(ow, ox, by_rows, left, u.rows, epi, stream);
+  auto few_logits = [&](size_t v0, size_t left, const VocabStats& epi) -> int {      // of rows of weight from v0 on
+    few_w = {(const unsigned char*)u.weight + v0 * ws_stride * eb, ws_stride, (uint32_t)left, (uint32_t)u.dim};
+    return vocab_few<DT>(p, vocab_aligned(u), few_w, ox, by_rows, u.rows, epi, stream);
   };
+  auto wide_of = [&](size_t v0, size_t left) { return p.wide > v0 ? std::min(p.wide - v0, left) : 0; };      // rows of a piece that go by wide tiles
   for (size_t v0 = 0, left; v0 < u.vocab; v0 += left) {      // what lies where it is in one launch, but for a piece whose logits are kept
     left = direct || p.few ? (z && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
     if (!p.few) VOCAB_TRY(take_piece(v0, left));
-    VOCAB_TRY(logits(v0, left, stats(v0, left, v0 == last ? z : nullptr, tile0, a.parts)));
-    tile0 += (left + p.height - 1) / p.height;
+    float* keep = v0 == last ? z : nullptr;
+    if (p.few) {
+      VOCAB_TRY(few_logits(v0, left, stats(v0, left, keep, tile0, a.parts)));
+      tile0 += (left + p.height - 1) / p.height;
+    } else {
+      const size_t wide = wide_of(v0, left), v1 = v0 + wide;
+      VOCAB_TRY((vocab_logits<DT>(ow, ox, by_rows, wide, left, u.rows, stats(v0, wide, keep, v0 / 256, a.parts), stats(v1, left - wide, keep ? keep + wide : nullptr, p.wide / 256 + (v1 - std::min(v1, p.wide)) / 128, a.parts), stream)));
+    }
   }
-  a.tiles = (uint32_t)tile0;
+  a.tiles = (uint32_t)(p.few ? tile0 : p.tiles);
   const bool grad = u.grad_hidden || u.grad_weight, by_row = u.vocab <= kJoinMost, join = grad && z && pieces && by_row;
   if (!join) {
     if (by_row) VOCAB_TRY(step_launch(dfx_vocab_row_kernel, dim3((uint32_t)p.rp), 256, stream, a));
@@ -772,10 +832,13 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
     if (direct || (!p.few && v0 != last)) VOCAB_TRY(take_piece(v0, left));
     const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
-    if (p.few && v0 != last) VOCAB_TRY(logits(v0, left, stats(v0, left, z, 0, nullptr)));
+    if (p.few && v0 != last) VOCAB_TRY(few_logits(v0, left, stats(v0, left, z, 0, nullptr)));
     if (p.few || (z && v0 == last))
       VOCAB_TRY(step_launch(join && v0 == last ? dfx_vocab_dz_kernel<DT, true> : dfx_vocab_dz_kernel<DT, false>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, a, epi, (const float*)z));
-    else VOCAB_TRY((vocab_gemm<DT, false, false>(ow, ox, by_rows, left, u.rows, epi, stream)));
+    else {
+      const size_t wide = wide_of(v0, left);
+      VOCAB_TRY((vocab_logits<DT>(ow, ox, by_rows, wide, left, u.rows, epi, VocabDz<DT>{a.row, dz + wide, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)(left - wide), (uint32_t)(v0 + wide), a.k}, stream)));
+    }
     const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
     const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), 0, count, false}, sw = {0, 0, 1, 0, 0, count, true};
     const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != last};
@@ -786,9 +849,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
         if (u.grad_hidden) VOCAB_TRY((vocab_few_dx<DT>(p, few_w, oz, sx, u.rows, dx, v0 != last, stream)));
         return u.grad_weight ? vocab_few_dw<DT>(ox, oz, count, u.rows, u.dim, left, dw_to, stream) : DFX_OK;
       }
-      if (u.grad_hidden && u.grad_weight && u.rows) return vocab_gemm_two<DT>(ow, oz, sx, u.dim, u.rows, dx_to, ox, sw, left, dw_to, stream);
-      if (u.grad_hidden) VOCAB_TRY((vocab_gemm<DT, true, false>(ow, oz, sx, u.dim, u.rows, dx_to, stream)));
-      return u.grad_weight ? vocab_gemm<DT, true, true>(ox, oz, sw, u.dim, left, dw_to, stream) : DFX_OK;
+      return vocab_grads<DT>(p, ow, oz, sx, u.dim, u.rows, u.grad_hidden && u.rows ? &dx_to : nullptr, ox, sw, left, u.grad_weight ? &dw_to : nullptr, stream);
     };
     if (u.grad_dtype == DFX_F32) VOCAB_TRY(both(VocabDw<DFX_F32>{(float*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
     else if constexpr (DT != DFX_F32) VOCAB_TRY(both(VocabDw<DT>{(uint16_t*)u.grad_weight + v0 * gs, gs, a.state, (uint32_t)u.dim, (uint32_t)left, u.accumulate != 0}));
