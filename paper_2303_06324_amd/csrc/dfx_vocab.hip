@@ -261,10 +261,13 @@ struct VocabStats {
 #pragma unroll
       for (int i = 0; i < TILE::MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s += vocab_exp(acc[i][j][e], base, k);
-          if (tile.m(i) + e == t && t < end) zt[n] = acc[i][j][e];
-        }
+        for (int e = 0; e < 4; ++e) s += vocab_exp(acc[i][j][e], base, k);
+      if (t >= tile.m0 && t < end)       // (few rows of a tile have their target in it)
+#pragma unroll
+        for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (tile.m(i) + e == t) zt[n] = acc[i][j][e];
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
       if (lane < 16) part[wave / TILE::WN * TILE::N + (n - tile.n0)] = make_float2(top, s);
