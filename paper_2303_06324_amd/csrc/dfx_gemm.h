@@ -188,12 +188,13 @@ __device__ __forceinline__ void gemm_cut8(const float* v, uint32_t (*part)[4]) {
   }
 }
 
-// Few rows: a tile of 128 m by 64 n by 4 waves of 32 m each.  A lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
+// Few rows: a tile of 64 MT m by 64 n by 4 waves of 16 MT m each.  A lane holds, of each of its wave's MT NT products of 16 x 16, n = lane % 16 and m = 4 (lane / 16) on.
+template <int MT_>
 struct GemmFlat {
-  static constexpr int WM = 4, WN = 1, MT = 2, NT = 4, M = 128, N = 64, THREADS = 256;
+  static constexpr int WM = 4, WN = 1, MT = MT_, NT = 4, M = 64 * MT, N = 64, THREADS = 256;
   static constexpr int STAGE = (M + N) * kGemmK * 2, LOADS = (M + N) * 8 / THREADS;
   uint32_t m0, n0;                       // of the workgroup's tile
-  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave * 32u; }
+  __device__ __forceinline__ uint32_t wave_m() const { return threadIdx.x / kStepWave * (16u * MT); }
   __device__ __forceinline__ uint32_t m(int mt) const { return m0 + wave_m() + mt * 16 + threadIdx.x % kStepWave / 16 * 4; }
   __device__ __forceinline__ uint32_t n(int nt) const { return n0 + nt * 16 + threadIdx.x % 16; }
   __device__ __forceinline__ uint32_t row(int nt, uint32_t r) const { return n0 + nt * 16 + r; }
@@ -259,46 +260,47 @@ struct GemmNext {
 
 // The flat tile: it streams a 16-bit matrix of rows at multiples of 16 bytes through the chip once.  Three stages, two of which are under way while one is used, and two
 // workgroups to a compute unit.
-template <int DT, class EPI>
-__global__ void __launch_bounds__(GemmFlat::THREADS, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
-  constexpr uint32_t STAGES = 3;
-  __shared__ __align__(1024) unsigned char lds[GemmFlat::STAGE * STAGES];
-  GemmFlat tile;
+template <int DT, int MT, class EPI>
+__global__ void __launch_bounds__(256, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
+  typedef GemmFlat<MT> TILE;
+  constexpr uint32_t STAGES = MT == 1 ? 4 : 3;
+  __shared__ __align__(1024) unsigned char lds[TILE::STAGE * STAGES];
+  TILE tile;
   uint32_t begin, end;
   const GemmPlace at = gemm_work(s, blockIdx.x, tile, begin, end);
   if (!at.any) return;
   if (s.height) a.rows = min(a.rows, tile.m0 + s.height);
-  GemmAcc acc[GemmFlat::MT][GemmFlat::NT];
+  GemmAcc acc[TILE::MT][TILE::NT];
 #pragma unroll
-  for (int i = 0; i < GemmFlat::MT; ++i)
+  for (int i = 0; i < TILE::MT; ++i)
 #pragma unroll
-    for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
+    for (int j = 0; j < TILE::NT; ++j) acc[i][j] = GemmAcc{0, 0, 0, 0};
   const uint32_t total = end - begin, wm = tile.wave_m();
   if (total) {
     GemmNext next(begin, end, total);
     auto load = [&](uint32_t stage) {
-      unsigned char* to = lds + stage * GemmFlat::STAGE;
-      gemm_fetch<GemmFlat::M, GemmFlat::THREADS, false>(a, 0, tile.m0, next.k * kGemmK, to);
-      gemm_fetch<GemmFlat::N, GemmFlat::THREADS, false>(b, 0, tile.n0, next.k * kGemmK, to + GemmFlat::M * kGemmK * 2);
+      unsigned char* to = lds + stage * TILE::STAGE;
+      gemm_fetch<TILE::M, TILE::THREADS, false>(a, 0, tile.m0, next.k * kGemmK, to);
+      gemm_fetch<TILE::N, TILE::THREADS, false>(b, 0, tile.n0, next.k * kGemmK, to + TILE::M * kGemmK * 2);
       next.advance();
     };
-    load(0);
-    load(1);
+#pragma unroll
+    for (uint32_t q = 0; q < STAGES - 1; ++q) load(q);
     uint32_t stage = 0;
     for (uint32_t q = 0; q < total; ++q) {
-      gemm_wait<GemmFlat::LOADS>();
+      gemm_wait<(STAGES - 2) * TILE::LOADS>();
       gemm_meet();                       // this stage has arrived for all, and nobody reads the one before it any more
       load(stage ? stage - 1u : STAGES - 1u);
-      const unsigned char* la = lds + stage * GemmFlat::STAGE;
-      GemmShort8 fa[GemmFlat::MT][2], fb[GemmFlat::NT][2];
-      gemm_take<GemmFlat::NT, GemmFlat::N, false>(la + GemmFlat::M * kGemmK * 2, 0, fb);
-      gemm_take<GemmFlat::MT, GemmFlat::M, false>(la, wm, fa);
+      const unsigned char* la = lds + stage * TILE::STAGE;
+      GemmShort8 fa[TILE::MT][2], fb[TILE::NT][2];
+      gemm_take<TILE::NT, TILE::N, false>(la + TILE::M * kGemmK * 2, 0, fb);
+      gemm_take<TILE::MT, TILE::M, false>(la, wm, fa);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int i = 0; i < GemmFlat::MT; ++i)
+        for (int i = 0; i < TILE::MT; ++i)
 #pragma unroll
-          for (int j = 0; j < GemmFlat::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i][kk], fb[j][kk], acc[i][j]);
+          for (int j = 0; j < TILE::NT; ++j) acc[i][j] = gemm_mac<DT>(fa[i][kk], fb[j][kk], acc[i][j]);
       stage = stage + 1u == STAGES ? 0u : stage + 1u;
     }
     gemm_wait<0>();
@@ -646,14 +648,16 @@ __global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, Gemm
 }
 
 // Logits of 16 NT rows at most: x stays in registers, of each of eight waves 32 KK elements of all rows.  A wave reads so much of a row of W at a time, which lies together (the
-// memory is quicker at that than at 128 bytes of each of many rows), a tile of 16 rows ahead; the waves' sums meet in LDS at the end of 64 rows.
+// memory is quicker at that than at 128 bytes of each of many rows), a tile of 16 rows ahead, also where the next tile of 64 rows begins: as many workgroups as fit at once go
+// through all of W.  The waves' sums meet in LDS at the end of 64 rows.  HBM bounds it: 1 row of bf16, 2048 x 50257, 43 us (4.8 TB/s; a workgroup for each 64 rows 47, by 128 bytes
+// of 64 rows past LDS 47; 2000 elements 39 and 52); 32-bit rows of 1024 elements 49 and 55, of 2048, whose planes take too many registers, 153 and 102.
 template <int DT, int NT, int KK, class EPI>
 __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, GemmOperand x, uint32_t height, EPI epi) {
   constexpr int P = gemm_planes(DT), V = DT == DFX_F32 ? 2 : 1, N = 16 / (int)sizeof(typename StepElem<DT>::raw), ROWS = 16 * NT, PITCH = ROWS + 1;
   __shared__ __align__(16) float sums[8 * 64 * PITCH];
   __shared__ float2 pairs[16 * ROWS];
   const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u, k0 = wave * KK * 32u + g * 8u;
-  const uint32_t m0 = blockIdx.x * height, end = min(w.rows, m0 + height);
+  uint32_t m0 = blockIdx.x * height, end = min(w.rows, m0 + height);
   StepVec<DT, N> raw[2][KK][V];
   auto load = [&](int set, int i) {
     const void* row = (const typename StepElem<DT>::raw*)w.p + (size_t)min(m0 + i * 16u + l, end - 1u) * w.stride;
@@ -674,40 +678,49 @@ __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, Gem
         fx[j][kk][p] = GemmShort8{0, 0, 0, 0, 0, 0, 0, 0};
         if (e < x.cols) fx[j][kk][p] = *(const STEP_GLOBAL GemmShort8*)(x.p + (size_t)p * x.plane + (size_t)(j * 16 + l) * x.stride + e);
       }
+  for (uint32_t tile = blockIdx.x;;) {
+    const uint32_t here = m0, till = end;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < 3) load((i + 1) & 1, i + 1);
-    GemmAcc acc[NT];
+    for (int i = 0; i < 4; ++i) {
+      if (i == 3) {                        // the next tile's first rows
+        m0 = min(m0 + gridDim.x * height, w.rows - 1u); end = min(w.rows, m0 + height);
+      }
+      load((i + 1) & 1, (i + 1) & 3);
+      GemmAcc acc[NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = GemmAcc{0, 0, 0, 0};
+      for (int j = 0; j < NT; ++j) acc[j] = GemmAcc{0, 0, 0, 0};
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      if ((wave + 1u) * KK * 32u > w.dim)
+      for (int kk = 0; kk < KK; ++kk) {
+        if ((wave + 1u) * KK * 32u > w.dim)
 #pragma unroll
-        for (int v = 0; v < V; ++v) gemm_row_end(raw[i & 1][kk][v], k0 + kk * 32u + v * N, w.dim);
-      GemmShort8 fa[P];
-      gemm_parts<DT>(raw[i & 1][kk], fa);
+          for (int v = 0; v < V; ++v) gemm_row_end(raw[i & 1][kk][v], k0 + kk * 32u + v * N, w.dim);
+        GemmShort8 fa[P];
+        gemm_parts<DT>(raw[i & 1][kk], fa);
 #pragma unroll
-      for (int pair = 0; pair < gemm_pairs(DT); ++pair)
+        for (int pair = 0; pair < gemm_pairs(DT); ++pair)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j] = gemm_mac<DT>(fa[P == 1 ? 0 : gemm_plane_a(pair)], fx[j][kk][P == 1 ? 0 : gemm_plane_b(pair)], acc[j]);
+          for (int j = 0; j < NT; ++j) acc[j] = gemm_mac<DT>(fa[P == 1 ? 0 : gemm_plane_a(pair)], fx[j][kk][P == 1 ? 0 : gemm_plane_b(pair)], acc[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[(wave * 64u + i * 16u + 4u * g + e) * PITCH + j * 16 + l] = acc[j][e];
     }
+    __syncthreads();
+    GemmAcc v = {0, 0, 0, 0};
+    const uint32_t n = threadIdx.x % ROWS, four = threadIdx.x / ROWS;
+    if (four < 16u)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int e = 0; e < 4; ++e) {
+        v[e] = sums[(four * 4u + e) * PITCH + n];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sums[(wave * 64u + i * 16u + 4u * g + e) * PITCH + j * 16 + l] = acc[j][e];
+        for (uint32_t q = 1; q < 8; ++q) v[e] += sums[(q * 64u + four * 4u + e) * PITCH + n];
+      }
+    epi.template of_fours<ROWS>(tile, here, till, v, pairs);
+    tile += gridDim.x;
+    if (tile * height >= w.rows) break;
+    __syncthreads();
   }
-  __syncthreads();
-  GemmAcc v = {0, 0, 0, 0};
-  const uint32_t n = threadIdx.x % ROWS, four = threadIdx.x / ROWS;
-  if (four < 16u)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = sums[(four * 4u + e) * PITCH + n];
-#pragma unroll
-      for (uint32_t q = 1; q < 8; ++q) v[e] += sums[(q * 64u + four * 4u + e) * PITCH + n];
-    }
-  epi.template of_fours<ROWS>(blockIdx.x, m0, end, v, pairs);
 }
 
 // A part of dX: 16 E elements of a row of W, by N rows of dz, summed over rows of W, 32 of each 128 by each of four waves.  A lane reads E elements of eight rows, and
