@@ -650,23 +650,24 @@ __global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, Gemm
 // Logits of 16 NT rows at most: x stays in registers, of each of eight waves 32 KK elements of all rows.  A wave reads so much of a row of W at a time, which lies together (the
 // memory is quicker at that than at 128 bytes of each of many rows), a tile of 16 rows ahead, also where the next tile of 64 rows begins: as many workgroups as fit at once go
 // through all of W.  The waves' sums meet in LDS at the end of 64 rows.  HBM bounds it: 1 row of bf16, 2048 x 50257, 43 us (4.8 TB/s; a workgroup for each 64 rows 47, by 128 bytes
-// of 64 rows past LDS 47; 2000 elements 39 and 52); 32-bit rows of 1024 elements 49 and 55, of 2048, whose planes take too many registers, 153 and 102.
+// of 64 rows past LDS 47; 2000 elements 39 and 52; 4096 x 32000 47 and 53); 32-bit rows of 1024 elements 49 and 55, of 2048 79 and 102.
 template <int DT, int NT, int KK, class EPI>
 __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, GemmOperand x, uint32_t height, EPI epi) {
   constexpr int P = gemm_planes(DT), V = DT == DFX_F32 ? 2 : 1, N = 16 / (int)sizeof(typename StepElem<DT>::raw), ROWS = 16 * NT, PITCH = ROWS + 1;
+  constexpr int PART = DT == DFX_F32 ? 4 : 8, H = KK > PART ? KK / PART : 1, CK = KK / H;      // a row's elements are taken in H parts, which the registers hold twice
   __shared__ __align__(16) float sums[8 * 64 * PITCH];
   __shared__ float2 pairs[16 * ROWS];
   const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u, k0 = wave * KK * 32u + g * 8u;
   uint32_t m0 = blockIdx.x * height, end = min(w.rows, m0 + height);
-  StepVec<DT, N> raw[2][KK][V];
-  auto load = [&](int set, int i) {
+  StepVec<DT, N> raw[2][CK][V];
+  auto load = [&](int set, int i, int h) {
     const void* row = (const typename StepElem<DT>::raw*)w.p + (size_t)min(m0 + i * 16u + l, end - 1u) * w.stride;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
+    for (int kk = 0; kk < CK; ++kk)
 #pragma unroll
-      for (int v = 0; v < V; ++v) raw[set][kk][v] = gemm_row_part<DT>(row, k0 + kk * 32u + v * N, w.dim);
+      for (int v = 0; v < V; ++v) raw[set][kk][v] = gemm_row_part<DT>(row, k0 + (h * CK + kk) * 32u + v * N, w.dim);
   };
-  load(0, 0);
+  load(0, 0, 0);
   GemmShort8 fx[NT][KK][P];              // (x is 0 from dim to its padded length, and here behind that)
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -680,31 +681,34 @@ __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, Gem
       }
   for (uint32_t tile = blockIdx.x;;) {
     const uint32_t here = m0, till = end;
+    GemmAcc acc[NT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i == 3) {                        // the next tile's first rows
+    for (int q = 0; q < 4 * H; ++q) {
+      const int i = q / H, h = q % H, set = q & 1;
+      if (q == 4 * H - 1) {              // the next tile's first rows
         m0 = min(m0 + gridDim.x * height, w.rows - 1u); end = min(w.rows, m0 + height);
       }
-      load((i + 1) & 1, (i + 1) & 3);
-      GemmAcc acc[NT];
+      load(set ^ 1, (q + 1) / H & 3, (q + 1) % H);
+      if (h == 0)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j] = GemmAcc{0, 0, 0, 0};
+        for (int j = 0; j < NT; ++j) acc[j] = GemmAcc{0, 0, 0, 0};
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
+      for (int kk = 0; kk < CK; ++kk) {
         if ((wave + 1u) * KK * 32u > w.dim)
 #pragma unroll
-          for (int v = 0; v < V; ++v) gemm_row_end(raw[i & 1][kk][v], k0 + kk * 32u + v * N, w.dim);
+          for (int v = 0; v < V; ++v) gemm_row_end(raw[set][kk][v], k0 + (h * CK + kk) * 32u + v * N, w.dim);
         GemmShort8 fa[P];
-        gemm_parts<DT>(raw[i & 1][kk], fa);
+        gemm_parts<DT>(raw[set][kk], fa);
 #pragma unroll
         for (int pair = 0; pair < gemm_pairs(DT); ++pair)
 #pragma unroll
-          for (int j = 0; j < NT; ++j) acc[j] = gemm_mac<DT>(fa[P == 1 ? 0 : gemm_plane_a(pair)], fx[j][kk][P == 1 ? 0 : gemm_plane_b(pair)], acc[j]);
+          for (int j = 0; j < NT; ++j) acc[j] = gemm_mac<DT>(fa[P == 1 ? 0 : gemm_plane_a(pair)], fx[j][h * CK + kk][P == 1 ? 0 : gemm_plane_b(pair)], acc[j]);
       }
+      if (h == H - 1)
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sums[(wave * 64u + i * 16u + 4u * g + e) * PITCH + j * 16 + l] = acc[j][e];
+          for (int e = 0; e < 4; ++e) sums[(wave * 64u + i * 16u + 4u * g + e) * PITCH + j * 16 + l] = acc[j][e];
     }
     __syncthreads();
     GemmAcc v = {0, 0, 0, 0};

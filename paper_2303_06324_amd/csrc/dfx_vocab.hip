@@ -649,7 +649,7 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   p.keep = grad && (p.few || long_rows || p.rp * p.vp <= kKeepElems);
   if (p.few) {
     p.nt = rows <= 32 ? 2 : 4;
-    p.lone = dtype == DFX_F32 ? rows <= 16 && dim <= 1024 : rows <= 32 && dim <= 2048;
+    p.lone = rows <= (dtype == DFX_F32 ? 16 : 32) && dim <= (dtype == DFX_F32 || rows > 16 ? 2048 : 4096);
     p.mt = !p.lone && (aligned || vocab >= kFewWide) ? 2 : 1;
     // so many tiles that whole rounds of workgroups, two to a compute unit, have them all
     const size_t rounds = std::max<size_t>(1, (vocab + 512 * 64 * p.mt - 1) / (512 * 64 * p.mt));
@@ -708,9 +708,9 @@ int vocab_few(const VocabPlan& p, bool aligned, const GemmSource& w, const GemmO
     auto go = [&](auto k) { return step_launch(k, dim3(std::min(s.mtiles, w.dim <= 1024 ? 512u : 256u)), 512, stream, w, x, s.height, epi); };      // (what fits at once)
     if constexpr (DT != DFX_F32) {
       if (rows > 16) return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 2, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 2, 8, EPI>);
-      if (w.dim > 1024) return go(dfx_gemm_lone_kernel<DT, 1, 8, EPI>);
+      if (w.dim > 2048) return go(dfx_gemm_lone_kernel<DT, 1, 16, EPI>);
     }
-    return go(dfx_gemm_lone_kernel<DT, 1, 4, EPI>);
+    return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 1, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 1, 8, EPI>);
   }
   if constexpr (DT != DFX_F32)
     if (aligned) {
