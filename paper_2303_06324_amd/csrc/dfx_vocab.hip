@@ -30,7 +30,7 @@ constexpr uint32_t kLayRows = 1024;      // up to so many rows are found by ever
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
 constexpr size_t kFewWide = 65536;       // from so long a vocabulary on, few rows' logits are made by twice as many rows of weight to a workgroup
 constexpr uint32_t kDwGroups = 1024;     // workgroups of dW of few rows
-constexpr size_t kKeepElems = 32ull << 20, kJoinMost = 16384;      // logits that are kept in any case; rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, of dz where there is one
+constexpr size_t kKeepElems = 32ull << 20, kJoinMost = 16384, kJoinFew = 65536;      // logits that are kept in any case; rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, of dz where there is one
 constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
 
 // what is known of a call on the device; first in the workspace
@@ -47,8 +47,8 @@ struct VocabArgs {
   float *weight, *zt, *row_loss, *row_w; // [Rp]
   float* top_weight;                     // largest |weight|
   VocabRow* row;                         // [Rp]
-  float2* parts;                         // [tiles of the vocabulary][pitch]: (m, S) of a tile's part of a row
-  uint32_t rows, rp, pitch, vocab, tiles;
+  float2* parts;                         // (m, S) of a tile's part of a row, at tile * tile_step + row * row_step: of many rows beside each other as a tile has them, of few a row's tiles
+  uint32_t rows, rp, tile_step, row_step, vocab, tiles;
   double c;
   float k;                               // c / log 2
 };
@@ -218,9 +218,9 @@ __global__ void __launch_bounds__(256) dfx_vocab_lay_kernel(VocabArgs a, const v
 // A tile's part of each row: (m, S), and the target's logit where it lies here; for the last piece of a call with gradients the logits as well.
 struct VocabStats {
   float2* parts;
-  float *zt, *z;                         // z: [pitch][z_pitch], may be null
+  float *zt, *z;                         // z: rows of z_pitch, may be null
   const int32_t* target;
-  uint32_t pitch, z_pitch, left, v0, tile0, height;      // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile; height: of a tile, 0: all of it
+  uint32_t tile_step, row_step, z_pitch, left, v0, tile0, height;      // left: rows of the vocabulary from the first of this launch, v0, on; tile0: its first tile; height: of a tile, 0: all of it
   float k;
   template <class TILE>
   __device__ __forceinline__ void operator()(const TILE& tile, const GemmPlace& at, GemmAcc (&acc)[TILE::MT][TILE::NT], unsigned char* lds) const {
@@ -283,7 +283,7 @@ struct VocabStats {
       }
 #pragma unroll
       for (int w = 0; w < TILE::WM; ++w) s += p[w].y * vocab_exp(p[w].x, vocab_base(top), k);
-      parts[(size_t)(tile0 + at.m) * pitch + tile.n0 + i] = make_float2(top, s);
+      parts[(size_t)(tile0 + at.m) * tile_step + (size_t)(tile.n0 + i) * row_step] = make_float2(top, s);
     }
   }
   // of 64 logits of N rows, four of a row in each of N 16 threads (thread i: row i % N, logits 4 (i / N) on); lds: 16 N pairs
@@ -312,7 +312,7 @@ struct VocabStats {
     for (uint32_t q = 1; q < 16; ++q) top = fmaxf(top, lds[q * N + n].x);
     s = 0.0f;
     for (uint32_t q = 0; q < 16; ++q) s += lds[q * N + n].y * vocab_exp(lds[q * N + n].x, vocab_base(top), k);
-    parts[(size_t)(tile0 + tile) * pitch + n] = make_float2(top, s);
+    parts[(size_t)(tile0 + tile) * tile_step + (size_t)n * row_step] = make_float2(top, s);
   }
 };
 
@@ -347,7 +347,7 @@ __device__ __forceinline__ float2 join_row(const VocabArgs& a, uint32_t n, bool 
   float top = -INFINITY, s = 0.0f;
   if (any)
     for (uint32_t t = threadIdx.x; t < a.tiles; t += 256u) {
-      const float2 p = a.parts[(size_t)t * a.pitch + n];
+      const float2 p = a.parts[(size_t)t * a.tile_step + (size_t)n * a.row_step];
       const float more = fmaxf(top, p.x), base = vocab_base(more);
       s = s * vocab_exp(top, base, a.k) + p.y * vocab_exp(p.x, base, a.k);
       top = more;
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
     for (uint32_t t = slice; t < a.tiles; t += 4u * S) {
       float2 p[4];
 #pragma unroll
-      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * S < a.tiles ? a.parts[(size_t)(t + u * S) * a.pitch + n] : make_float2(-INFINITY, 0.0f);
+      for (uint32_t u = 0; u < 4; ++u) p[u] = t + u * S < a.tiles ? a.parts[(size_t)(t + u * S) * a.tile_step + (size_t)n * a.row_step] : make_float2(-INFINITY, 0.0f);
       float more = top;
 #pragma unroll
       for (int u = 0; u < 4; ++u) more = fmaxf(more, p[u].x);
@@ -767,7 +767,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   a.idx = (int32_t*)(ws + p.idx); a.target = (int32_t*)(ws + p.target); a.map = (int32_t*)(ws + p.map); a.weight = (float*)(ws + p.weight);
   a.zt = (float*)(ws + p.zt); a.row_loss = (float*)(ws + p.row_loss); a.row_w = (float*)(ws + p.row_w); a.row = (VocabRow*)(ws + p.row);
   a.parts = (float2*)(ws + p.parts);
-  a.rows = (uint32_t)u.rows; a.rp = (uint32_t)p.rp; a.pitch = (uint32_t)p.split_rows; a.vocab = (uint32_t)u.vocab; a.tiles = (uint32_t)p.tiles;
+  a.rows = (uint32_t)u.rows; a.rp = (uint32_t)p.rp; a.tile_step = p.few ? 1u : (uint32_t)p.split_rows; a.row_step = p.few ? (uint32_t)p.tiles : 1u; a.vocab = (uint32_t)u.vocab; a.tiles = (uint32_t)p.tiles;
   a.c = u.inv_temperature; a.k = (float)(u.inv_temperature * kVLog2e);
   const size_t eb = step_elem_bytes(DT), ws_stride = u.weight_stride ? u.weight_stride : u.dim;
   const uint32_t* count = &a.state->count;
@@ -800,7 +800,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   float* z = p.keep ? (float*)(ws + p.z) : nullptr;
   size_t tile0 = 0;
   auto stats = [&](size_t v0, size_t left, float* keep, size_t tile, float2* parts) {
-    return VocabStats{parts, a.zt, keep, a.target, a.pitch, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, (uint32_t)tile, (uint32_t)p.height, a.k};
+    return VocabStats{parts, a.zt, keep, a.target, a.tile_step, a.row_step, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, (uint32_t)tile, (uint32_t)p.height, a.k};
   };
   GemmSource few_w = {};
   auto few_logits = [&](size_t v0, size_t left, const VocabStats& epi) -> int {      // of rows of weight from v0 on
@@ -821,9 +821,9 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     }
   }
   a.tiles = (uint32_t)(p.few ? tile0 : p.tiles);
-  const bool grad = u.grad_hidden || u.grad_weight, by_row = u.vocab <= kJoinMost, join = grad && z && pieces && by_row;
+  const bool grad = u.grad_hidden || u.grad_weight, by_row = u.vocab <= (p.few ? kJoinFew : kJoinMost), join = grad && z && pieces && by_row;
   if (!join) {
-    if (by_row) VOCAB_TRY(step_launch(dfx_vocab_row_kernel, dim3((uint32_t)p.rp), 256, stream, a));
+    if (by_row) VOCAB_TRY(step_launch(dfx_vocab_row_kernel, dim3((uint32_t)p.split_rows), 256, stream, a));
     else if (p.few) VOCAB_TRY(step_launch(dfx_vocab_join_kernel<64>, dim3((uint32_t)(p.rp / 4)), 256, stream, a));
     else VOCAB_TRY(step_launch(dfx_vocab_join_kernel<8>, dim3((uint32_t)(p.rp / 32)), 256, stream, a));
   }
