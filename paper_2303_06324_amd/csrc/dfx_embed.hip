@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_few_kernel(SumArgs a,
     const int64_t v = first + q;
     if (v >= (int64_t)a.vocab) return;
     const uint32_t begin = start[q], end = start[q + 1];
-    for (uint32_t e = me * N; e < a.dim; e += kEmbedThreads * N) {
+    for (uint32_t e = (blockIdx.y * kEmbedThreads + me) * N; e < a.dim; e += gridDim.y * kEmbedThreads * N) {
       float s[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) s[k] = 0.0f;
@@ -579,7 +579,8 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
   a.grad = u->grad; a.out = u->table_grad; a.part = (float*)(ws + p.part); a.grad_stride = gs; a.out_stride = os;
   a.n = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.vocab = (uint32_t)u->vocab; a.block = p.block; a.blocks = p.blocks; a.scale = (float)u->scale; a.accumulate = u->accumulate != 0;
   if (u->rows && u->rows <= kFewPlaces) {
-    const dim3 grid(u->accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable));
+    const uint32_t at_once = kEmbedThreads * 16 / (uint32_t)eb;      // elements of a row that a workgroup has
+    const dim3 grid(u->accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable), std::min(8u, (a.dim + at_once - 1) / at_once));
     const bool wide = u->out_dtype == DFX_F32;
     auto k = u->dtype == DFX_F32 ? dfx_embed_few_kernel<DFX_F32, DFX_F32> : u->dtype == DFX_BF16 ? (wide ? dfx_embed_few_kernel<DFX_BF16, DFX_F32> : dfx_embed_few_kernel<DFX_BF16, DFX_BF16>)
                                                                         : (wide ? dfx_embed_few_kernel<DFX_F16, DFX_F32> : dfx_embed_few_kernel<DFX_F16, DFX_F16>);
