@@ -25,13 +25,25 @@ constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.442695040888963407
 constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
-constexpr uint32_t kFewRows = 128, kFewDim = 64;      // up to so many rows of at least so many elements go by the products for few rows
-constexpr uint32_t kLayRows = 1024;      // up to so many rows are found by every workgroup that lays one out
-constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;      // (offsets within a tile of dz have 32 bits)
+
+// Up to so many rows of at least so many elements go by the products for few rows, which read the weight as it lies (us, by them and by wide tiles with gradients: 64 x 2048 x 32000
+// bf16 97 and 117, 64 x 1024 x 32000 in 32 bits 153 and 277; 128 rows 126 and 127, 252 and 295; between 65 and 128 bf16 rows -10 % to +19 %, the better the longer the vocabulary).
+constexpr uint32_t kFewRows = 128, kFewDim = 64;
+// Up to so many rows are found by every workgroup that lays one out, which spares a launch (1024 x 1024 x 2000: 23.4 us and 24.1).
+constexpr uint32_t kLayRows = 1024;
+// Elements of dz that are held at a time, and with them the logits of the last piece in 32 bits (8192 x 4096 x 131072: 2^26 24.1 ms, 2^27 23.8, 2^28 23.5: 1.6 GB; all of it, 2^30 and 6.4 GB, a
+// seventh less); rows of a piece at least, at most, of few rows, and where the caller says (offsets within a tile of dz have 32 bits).
+constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;
 constexpr size_t kFewWide = 65536;       // from so long a vocabulary on, few rows' logits are made by twice as many rows of weight to a workgroup
-constexpr uint32_t kDwGroups = 1024;     // workgroups of dW of few rows
-constexpr size_t kKeepElems = 32ull << 20, kJoinMost = 16384, kJoinFew = 65536;      // logits that are kept in any case; rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, of dz where there is one
-constexpr size_t kKeepDim = 1536, kKeepDimF32 = 256;
+// Workgroups of dW of few rows (48 x 1024 x 32000 f16 and 8 x 3840 x 72397 bf16: 768 20.3 and 142 us, 1024 20.0 and 141, 2048 20.0 and 150).
+constexpr uint32_t kDwGroups = 1024;
+// The last piece's logits are kept, in 32 bits, where making them again takes longer than writing and reading them: of long rows (us, kept and not: 8192 x 512 x 32768 bf16 1255 and 1143,
+// x 1024 1820 and 1931, x 2048 2998 and 3433; 4096 x 128 x 16384 in 32 bits 576 and 552, x 256 810 and 855), and of so few that a launch counts
+// (256 elements: 1024 x 8192 55 and 57, 2048 x 16000 146 and 131).
+constexpr size_t kKeepDim = 1024, kKeepDimF32 = 256, kKeepElems = 16ull << 20;
+// Rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, with gradients by each of dz's, which spares a launch (200 x 512 x 8000 43.9 us and 46.0, 1024 x 512 x 16000 level);
+// of few rows, whose parts lie together (8 x 512 x 60000 78.7 and 81.4, 128 rows 92.3 and 94.0).
+constexpr size_t kJoinMost = 16384, kJoinFew = 65536;
 
 // what is known of a call on the device; first in the workspace
 struct VocabState { uint32_t count; float g; };       // rows that count; scale * largest weight * c / 2^15
