@@ -654,7 +654,7 @@ __global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, Gemm
 template <int DT, int NT, int KK, class EPI>
 __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, GemmOperand x, uint32_t height, EPI epi) {
   constexpr int P = gemm_planes(DT), V = DT == DFX_F32 ? 2 : 1, N = 16 / (int)sizeof(typename StepElem<DT>::raw), ROWS = 16 * NT, PITCH = ROWS + 1;
-  constexpr int PART = DT == DFX_F32 ? 4 : 8, H = KK > PART ? KK / PART : 1, CK = KK / H;      // a row's elements are taken in H parts, which the registers hold twice
+  constexpr int PART = DT == DFX_F32 ? 4 : 8, H = (KK + PART - 1) / PART, CK = KK / H;      // a row's elements are taken in H parts, which the registers hold twice
   __shared__ __align__(16) float sums[8 * 64 * PITCH];
   __shared__ float2 pairs[16 * ROWS];
   const uint32_t wave = threadIdx.x / kStepWave, lane = threadIdx.x % kStepWave, l = lane % 16u, g = lane / 16u, k0 = wave * KK * 32u + g * 8u;

@@ -34,7 +34,9 @@ constexpr uint32_t kLayRows = 1024;
 // Elements of dz that are held at a time, and with them the logits of the last piece in 32 bits (8192 x 4096 x 131072: 2^26 24.1 ms, 2^27 23.8, 2^28 23.5: 1.6 GB; all of it, 2^30 and 6.4 GB, a
 // seventh less); rows of a piece at least, at most, of few rows, and where the caller says (offsets within a tile of dz have 32 bits).
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;
-constexpr size_t kFewWide = 65536;       // from so long a vocabulary on, few rows' logits are made by twice as many rows of weight to a workgroup
+// From so long a vocabulary on, few rows' logits are made by twice as many rows of an unaligned or 32-bit weight to a workgroup (40 x 2001 x 100000 bf16 184 us and 195 by half as many, but 66 x
+// 1789 x 30000 in 32 bits 140 and 94).
+constexpr size_t kFewWide = 65536;
 // Workgroups of dW of few rows (48 x 1024 x 32000 f16 and 8 x 3840 x 72397 bf16: 768 20.3 and 142 us, 1024 20.0 and 141, 2048 20.0 and 150).
 constexpr uint32_t kDwGroups = 1024;
 // The last piece's logits are kept, in 32 bits, where making them again takes longer than writing and reading them: of long rows (us, kept and not: 8192 x 512 x 32768 bf16 1255 and 1143,
@@ -589,13 +591,27 @@ bool vocab_aligned(const dfx_vocab_loss_args& u) {
 
 struct VocabPlan {
   size_t rp, dp, dq, vp, pieces, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, pieces, tiles of the vocabulary, splits of dX and the tiles' rows
-  bool few, lone, keep;                  // lone: x stays in registers; keep: the logits of the last piece
+  bool few, keep;                        // keep: the logits of the last piece
+  int lone;                              // x stays in registers, 32 times so many elements of a wave; or 0
   int nt, mt;                            // tiles of the products for few rows
   size_t height;                         // of a tile of the vocabulary, for few rows
   size_t wide;                           // otherwise: rows of the vocabulary whose logits go by wide tiles, the others' by quarters
   bool dx_quarters, dw_quarters;         // whether the gradients' products do
   size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
 };
+
+// Whether logits go by workgroups that keep x, and 32 times how many elements of it each of the eight waves has: not where an eighth of those would lie behind a row's end (us by
+// them and by the others, bf16 of 1 row by 32000, the weight in the caches: 1024 elements 19.6 and 20.9, 1001 28.1 and 31.8, 1531 42.3 and 46.2, but 1600 28.2 and 26.4, 3200 45.2 and 40.5; from
+// HBM, by 50257: 2000 49 and 62, 2048 53 and 57).
+int vocab_lone(size_t rows, size_t dim, int dtype) {
+  if (rows > (dtype == DFX_F32 ? 16 : 32)) return 0;
+  for (int kk : {4, 6, 8, 12, 16}) {
+    if (kk > (dtype == DFX_F32 || rows > 16 ? 8 : 16)) break;
+    const size_t all = 256 * (size_t)kk;
+    if (dim <= all) return dim * 8 > all * 7 ? kk : 0;
+  }
+  return 0;
+}
 
 // How long a launch takes of workgroups, one to a compute unit, of two kinds: n of length l each, the longer ones first.
 double vocab_time(size_t n, double l, size_t n2, double l2) {
@@ -643,7 +659,7 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   VocabPlan p;
   const size_t planes = gemm_planes(dtype);
   p.few = rows <= kFewRows && dim >= kFewDim;
-  p.lone = false;
+  p.lone = 0;
   p.rp = std::max(kTileRows, up(rows, kTileRows));
   p.dp = up(dim, kGemmK);
   p.dq = up(dim, 4);
@@ -661,7 +677,7 @@ VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad
   p.keep = grad && (p.few || long_rows || p.rp * p.vp <= kKeepElems);
   if (p.few) {
     p.nt = rows <= 32 ? 2 : 4;
-    p.lone = rows <= (dtype == DFX_F32 ? 16 : 32) && dim <= (dtype == DFX_F32 || rows > 16 ? 2048 : 4096);
+    p.lone = vocab_lone(rows, dim, dtype);
     p.mt = !p.lone && (aligned || vocab >= kFewWide) ? 2 : 1;
     // so many tiles that whole rounds of workgroups, two to a compute unit, have them all
     const size_t rounds = std::max<size_t>(1, (vocab + 512 * 64 * p.mt - 1) / (512 * 64 * p.mt));
@@ -717,12 +733,12 @@ int vocab_few(const VocabPlan& p, bool aligned, const GemmSource& w, const GemmO
   s.height = (uint32_t)p.height;
   if (p.lone) {
     if (!s.mtiles || !rows) return DFX_OK;
-    auto go = [&](auto k) { return step_launch(k, dim3(std::min(s.mtiles, w.dim <= 1024 ? 512u : 256u)), 512, stream, w, x, s.height, epi); };      // (what fits at once)
+    auto go = [&](auto k) { return step_launch(k, dim3(std::min(s.mtiles, p.lone == 4 ? 512u : 256u)), 512, stream, w, x, s.height, epi); };      // (what fits at once)
     if constexpr (DT != DFX_F32) {
-      if (rows > 16) return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 2, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 2, 8, EPI>);
-      if (w.dim > 2048) return go(dfx_gemm_lone_kernel<DT, 1, 16, EPI>);
+      if (rows > 16) return p.lone == 4 ? go(dfx_gemm_lone_kernel<DT, 2, 4, EPI>) : p.lone == 6 ? go(dfx_gemm_lone_kernel<DT, 2, 6, EPI>) : go(dfx_gemm_lone_kernel<DT, 2, 8, EPI>);
+      if (p.lone > 8) return p.lone == 12 ? go(dfx_gemm_lone_kernel<DT, 1, 12, EPI>) : go(dfx_gemm_lone_kernel<DT, 1, 16, EPI>);
     }
-    return w.dim <= 1024 ? go(dfx_gemm_lone_kernel<DT, 1, 4, EPI>) : go(dfx_gemm_lone_kernel<DT, 1, 8, EPI>);
+    return p.lone == 4 ? go(dfx_gemm_lone_kernel<DT, 1, 4, EPI>) : p.lone == 6 ? go(dfx_gemm_lone_kernel<DT, 1, 6, EPI>) : go(dfx_gemm_lone_kernel<DT, 1, 8, EPI>);
   }
   if constexpr (DT != DFX_F32)
     if (aligned) {
