@@ -672,8 +672,9 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* args, void* hip_stream);
  *   logp = log softmax(z)[target];  loss = -row_weight logp;  dz = scale inv_temperature row_weight (softmax(z) - [j = target])
  *   grad_hidden = dz weight;  grad_weight = dz^T hidden
  * The products are made on the matrix cores in pieces of the vocabulary, and their sums in 32 bits; 32-bit inputs are taken as three terms of 8 bits of
- * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time, piece by piece (but for those of the last piece, which are
- * kept where that takes less time), and dz is rounded to the type of the inputs on its way into the products (32-bit inputs: to three such terms).
+ * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time,
+ * piece by piece (one piece's are kept in 32 bits where that takes less time), and dz is rounded to the type of the inputs on its way into the products (of
+ * 32-bit inputs: to three such terms).  A row's numbers are the same with gradients and without (of one piece's length).
  * A row of weight 0 or without a target has nothing to learn from: it takes no part in the products, its hidden state is not looked at, its
  * logp, loss and grad_hidden are 0.  So has a row with no logit above -infinity.  A logit of NaN or +infinity makes its row NaN, and with it
  * grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of rows are finite.
@@ -699,7 +700,8 @@ typedef struct {
   void* grad_weight;         /* may be NULL */
   size_t grad_weight_stride;
   double inv_temperature;    /* > 0, and 1.45 times it a normal number in 32 bits */
-  size_t piece;              /* rows of weight whose dz is held at a time (at most 2^22), a multiple of 256; 0 = the library's choice: 2^28 elements of dz, 65536 rows */
+  size_t piece;              /* rows of weight whose dz is held at a time (at most 2^22), a multiple of 256; 0 = the library's choice: at most 2^28
+                                elements of dz.  More save time where there is the memory */
   void* workspace;           /* dfx_vocab_loss_workspace bytes, 256-byte aligned */
   size_t workspace_bytes;
 } dfx_vocab_loss_args;

@@ -18,7 +18,8 @@ namespace {
 constexpr int kEmbedThreads = 256;
 constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / kStepWave, kSortChunks = 256, kSortChunk = 2048;      // chunks at most, places of one at least
 constexpr uint32_t kDigitBits = 10;      // at most
-constexpr uint32_t kSumMost = 64, kSumBlocks = 512;      // places of a block of the sums at most; blocks, where they are fewer
+// places of a block of the sums at most; blocks, where they are fewer (us: 16384 x 4096 bf16 onto 256 98, 512 81, 1024 92; x 1024 86, 64, 57; 4000 x 1024 32, 29, 34)
+constexpr uint32_t kSumMost = 64, kSumBlocks = 512;
 
 struct EmbedArgs {
   const int64_t* tokens;
@@ -64,6 +65,7 @@ __device__ __forceinline__ void part_put(void* row, uint32_t e, uint32_t dim, co
   }
 }
 
+// a.lanes threads to a row; what is written goes past the caches.  HBM's writes bound it: 16384 x 4096 bf16 31 us, 6.1 TB/s; one row 1.7.
 template <int DT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_kernel(EmbedArgs a) {
   typedef typename StepElem<DT>::raw raw;
@@ -185,7 +187,8 @@ __global__ void __launch_bounds__(kSortThreads) dfx_embed_move_kernel(SortArgs a
 
 // The same in one launch where there are few places and not very many tokens: a workgroup has the tokens of one remainder by kOwners.  It looks at all places, counts those
 // of smaller remainders, which come first, keeps its own in LDS in their order, and sorts them by the quotient: places of a quotient are counted, and one wave moves them, 64
-// at a time.  The workgroups behind clear the table's gradient meanwhile.
+// at a time.  The workgroups behind clear the table's gradient meanwhile.  16384 places 19.6 us: the chain of one wave's rounds over its share and the counts before it.  In all, by this and by
+// the passes: 4000 x 1024 29 us and 39, 16384 x 4096 81 and 86.
 constexpr uint32_t kOwnMost = 16384, kOwnBits = 7, kOwners = 1u << kOwnBits, kOwnThreads = 1024, kOwnWaves = kOwnThreads / kStepWave, kOwnQuotients = 2 * kOwnThreads;
 
 template <int OUT>
@@ -281,7 +284,7 @@ __global__ void __launch_bounds__(kOwnThreads) dfx_embed_own_kernel(SortArgs a, 
 }
 
 // ------------------------------------------------------------------------------------------
-// sums along the sorted places
+// sums along the sorted places: 16384 x 4096 bf16 onto 131072 rows 72 us, 0.24 GB; a row onto the table waits for what the table holds, one token after the other
 // ------------------------------------------------------------------------------------------
 struct SumArgs {
   const uint2* sorted;
@@ -359,7 +362,7 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_sum_kernel(SumArgs a)
   close(end < a.n && a.sorted[end].x == token);
 }
 
-// A token whose places go on behind the block that they begin in: its blocks' parts, in their order.
+// A token whose places go on behind the block that they begin in: its blocks' parts, in their order.  15 us of the same.
 template <int OUT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_join_kernel(SumArgs a) {
   constexpr int N = 4;
@@ -394,6 +397,7 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_join_kernel(SumArgs a
 // ------------------------------------------------------------------------------------------
 // few places: no sort.  A workgroup finds the places of its rows of the table among all of them, in their order.  Onto the gradient that is there: a workgroup to a
 // place, which does nothing if its token stood before; otherwise a workgroup to eight rows of the table.
+// In all, by this and by the sort: 300 x 1024 bf16 9 us and 17, 500 x 4096 11.4 and 17.4.
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t kFewPlaces = 512, kFewTable = 8;
 

@@ -258,8 +258,8 @@ struct GemmNext {
   }
 };
 
-// The flat tile: it streams a 16-bit matrix of rows at multiples of 16 bytes through the chip once.  Three stages, two of which are under way while one is used, and two
-// workgroups to a compute unit.
+// The flat tile: it streams a 16-bit matrix of rows at multiples of 16 bytes through the chip once.  Three or four stages, one of which is used while the others are under way, and
+// two workgroups to a compute unit.  HBM bounds it: logits of 64 x 4096 x 131072 bf16 187 us (5.7 TB/s) where the kernel past LDS takes 216, of 48 x 2048 x 32000 30 and 40.
 template <int DT, int MT, class EPI>
 __global__ void __launch_bounds__(256, 2) dfx_gemm_flat_kernel(GemmOperand a, GemmOperand b, GemmShape s, EPI epi) {
   typedef GemmFlat<MT> TILE;
@@ -339,7 +339,8 @@ __device__ __forceinline__ void gemm_by_rows(const TILE& tile, const GemmAcc (&a
 // The wide tile.  Two waves share a SIMD, and while one of them has the matrix core the other fetches: a step is four turns, one for each quarter of a wave's
 // products, and a turn is a part that reads LDS and starts loads, and a part of 16 products; waves 4 to 7 run one part behind waves 0 to 3.  Halves of the
 // tiles are read in the order n0, m0, n1, m1, and as soon as both sets of waves have read one, the loads of the step after next may begin to overwrite it: a
-// load has seven turns to arrive, 12 younger ones of a wave under way behind it.
+// load has seven turns to arrive, 12 younger ones of a wave under way behind it.  The matrix cores' power bounds it: logits of 6700 x 4096 x 131072 bf16 1.30 PFLOP/s, dX with dW 1.21 (as
+// one set of waves 29.4 ms in all, now 22.1); 32-bit ones as six products 1.15 PFLOP/s of bf16.  Products of 32 x 32 x 16 were 6 % slower, a step in two turns 3 %.
 template <int DT, bool TA, bool TB, class EPI>
 __device__ __forceinline__ void gemm_wide(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const EPI& epi, uint32_t block, unsigned char* gemm_lds) {
   GemmWide tile;
@@ -430,7 +431,8 @@ struct GemmQuarter {
 };
 static_assert(GemmQuarter::STAGES * GemmQuarter::STAGE <= GemmWide::LDS, "a workgroup takes either tile");
 
-// Where wide tiles would leave compute units idle.  Four stages, three of which are under way; the waves of a SIMD fill each other's waits.
+// Where wide tiles would leave compute units idle.  Four stages, three of which are under way; the waves of a SIMD fill each other's waits.  It needs twice the bytes from L2 for a
+// product, which bound it (12 TB/s): 0.39 of a wide tile's time for a quarter of its work.  650 x 1984 x 2368 bf16 with gradients: 111 us by wide tiles, 61 by these.
 template <int DT, bool TA, bool TB, class EPI>
 __device__ __forceinline__ void gemm_quarter(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const EPI& epi, uint32_t block, unsigned char* lds) {
   typedef GemmQuarter TILE;
@@ -567,7 +569,7 @@ __device__ __forceinline__ void gemm_parts(const StepVec<DT, 16 / (int)sizeof(ty
   } else to[0] = __builtin_bit_cast(GemmShort8, v[0].w);
 }
 
-// Logits: M rows of W by N rows of x, along both.
+// Logits: M rows of W by N rows of x, along both; loads of W are DEPTH steps ahead.  66 x 1789 x 67561 in 32 bits 171 us (2.8 TB/s; cut into planes and laid out first 548).
 template <int DT, int NT, int MT, int DEPTH, class EPI>
 __global__ void __launch_bounds__(256, 2) dfx_gemm_few_kernel(GemmSource w, GemmOperand b, GemmShape s, EPI epi) {
   typedef GemmFew<NT, MT> TILE;
@@ -728,7 +730,8 @@ __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, Gem
 }
 
 // A part of dX: 16 E elements of a row of W, by N rows of dz, summed over rows of W, 32 of each 128 by each of four waves.  A lane reads E elements of eight rows, and
-// so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes too many registers by 64 rows: 48 x 1024 x 32000 22.5 us and 16.6.)
+// so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes too many registers by 64 rows: 48 x 1024 x 32000 22.5 us and 18.)
+// 8 x 3840 x 72397 bf16 112 us, 5.0 TB/s.
 constexpr uint32_t kFewK = 128;
 __host__ __device__ constexpr int gemm_few_e(int dt, int nt) { return dt != DFX_F32 && nt == 2 ? 8 : 4; }
 template <int DT, int NT>
@@ -843,6 +846,7 @@ __global__ void __launch_bounds__(256, DT == DFX_F32 && NT == 4 ? 1 : 2) dfx_gem
 
 // dW of few rows, whose sums are a step or two long: writing it is what takes the time.  A wave has 32 elements of x's rows in registers, all the sums' length, and goes from
 // 64 rows of dW to others; the next ones' dz is on its way meanwhile.  Its two tiles' rows are exchanged in fours, so that a lane has eight elements of dW side by side.
+// 48 x 1024 x 32000 f16 20 us, 8 x 3840 x 72397 bf16 141 us: 3.3 and 3.9 TB/s, all of it writes.
 template <int DT, int STEPS, class OUT>
 __global__ void __launch_bounds__(256, DT == DFX_F32 ? 1 : 3) dfx_gemm_few_dw_kernel(GemmOperand x, GemmOperand z, const uint32_t* count, uint32_t mtiles, uint32_t ntiles, uint32_t each, OUT out) {
   constexpr int P = gemm_planes(DT), PLANE = 64 * kGemmK * 2, STAGE = STEPS * P * PLANE, WIDE = 128, NT = 4;

