@@ -678,6 +678,8 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* args, void* hip_stream);
  * A row of weight 0 or without a target has nothing to learn from: it takes no part in the products, its hidden state is not looked at, its
  * logp, loss and grad_hidden are 0.  So has a row with no logit above -infinity.  A logit of NaN or +infinity makes its row NaN, and with it
  * grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of rows are finite.
+ * TOO_LARGE from 2^24 - 2^10 rows and from a vocab of 2^28 on, and where rows * vocab is 2^36 or more and a launch would not hold its tiles (at the latest from
+ * 2^38 on).
  */
 typedef struct {
   uint32_t struct_bytes;

@@ -473,12 +473,13 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_few_kernel(SumArgs a,
 }
 
 template <int OUT>
-__global__ void __launch_bounds__(kEmbedThreads) dfx_embed_clear_kernel(void* out, size_t stride, uint32_t dim) {
-  clear_row<OUT>(out, stride, dim, blockIdx.x);
+__global__ void __launch_bounds__(kEmbedThreads) dfx_embed_clear_kernel(void* out, size_t stride, uint32_t dim, uint32_t vocab) {
+  for (uint32_t row = blockIdx.x; row < vocab; row += gridDim.x) clear_row<OUT>(out, stride, dim, row);
 }
 
 // ------------------------------------------------------------------------------------------
 constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
+constexpr size_t kRowsAtOnce = 1ull << 22;      // workgroups of a launch (whose threads are counted in 32 bits)
 
 uint32_t lanes_log2(uint32_t vectors) {
   uint32_t k = 0;
@@ -553,9 +554,14 @@ int dfx_embed(const dfx_embed_args* u, void* hip_stream) {
   const uint32_t N = 16 / (uint32_t)eb, vectors = (a.dim + N - 1) / N;
   a.lanes_log2 = lanes_log2(vectors); a.lanes = 1u << a.lanes_log2;
   const uint32_t groups = kEmbedThreads >> a.lanes_log2;
-  const dim3 grid((a.rows + groups - 1) / groups, std::min(4u, (vectors + a.lanes - 1) / a.lanes));
   auto k = u->dtype == DFX_F32 ? dfx_embed_kernel<DFX_F32> : u->dtype == DFX_BF16 ? dfx_embed_kernel<DFX_BF16> : dfx_embed_kernel<DFX_F16>;
-  return step_launch(k, grid, kEmbedThreads, (hipStream_t)hip_stream, a);
+  for (size_t first = 0; first < u->rows; first += kRowsAtOnce) {
+    a.tokens = u->tokens + first; a.out = (unsigned char*)u->out + first * os * eb;
+    a.rows = (uint32_t)std::min(kRowsAtOnce, u->rows - first);
+    const int rc = step_launch(k, dim3((a.rows + groups - 1) / groups, std::min(4u, (vectors + a.lanes - 1) / a.lanes)), kEmbedThreads, (hipStream_t)hip_stream, a);
+    if (rc != DFX_OK) return rc;
+  }
+  return DFX_OK;
 }
 
 size_t dfx_embed_grad_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype) {
@@ -582,7 +588,7 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
   memset(&a, 0, sizeof(a));
   a.grad = u->grad; a.out = u->table_grad; a.part = (float*)(ws + p.part); a.grad_stride = gs; a.out_stride = os;
   a.n = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.vocab = (uint32_t)u->vocab; a.block = p.block; a.blocks = p.blocks; a.scale = (float)u->scale; a.accumulate = u->accumulate != 0;
-  if (u->rows && u->rows <= kFewPlaces) {
+  if (u->rows && u->rows <= kFewPlaces && (u->accumulate || u->vocab <= kRowsAtOnce)) {
     const uint32_t at_once = kEmbedThreads * 16 / (uint32_t)eb;      // elements of a row that a workgroup has
     const dim3 grid(u->accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable), std::min(8u, (a.dim + at_once - 1) / at_once));
     const bool wide = u->out_dtype == DFX_F32;
@@ -600,7 +606,7 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
     a.sorted = pairs[0];
   } else if (!u->accumulate) {
     auto k = u->out_dtype == DFX_F32 ? dfx_embed_clear_kernel<DFX_F32> : u->out_dtype == DFX_BF16 ? dfx_embed_clear_kernel<DFX_BF16> : dfx_embed_clear_kernel<DFX_F16>;
-    const int rc = step_launch(k, dim3((uint32_t)u->vocab), kEmbedThreads, s, u->table_grad, os, (uint32_t)u->dim);
+    const int rc = step_launch(k, dim3((uint32_t)std::min(u->vocab, kRowsAtOnce)), kEmbedThreads, s, u->table_grad, os, (uint32_t)u->dim, (uint32_t)u->vocab);
     if (rc != DFX_OK) return rc;
   }
   if (!u->rows) return DFX_OK;

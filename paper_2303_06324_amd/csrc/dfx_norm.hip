@@ -352,6 +352,7 @@ int norm_grad_launch(const NormArgs& a, uint32_t groups, hipStream_t s) {
 }
 
 constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
+constexpr size_t kRowsAtOnce = 1ull << 22;      // of a launch of the forward pass (whose threads are counted in 32 bits)
 
 bool norm_types(int dtype, int other) { return (dtype == DFX_F32 || dtype == DFX_BF16 || dtype == DFX_F16) && (other == dtype || other == DFX_F32); }
 
@@ -380,7 +381,13 @@ int dfx_layer_norm(const dfx_layer_norm_args* u, void* hip_stream) {
   a.x = u->x; a.weight = u->weight; a.bias = u->bias; a.y = u->y; a.x_stride = xs; a.y_stride = ys;
   a.rows = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.eps = (float)u->eps; a.param_f32 = u->param_dtype == DFX_F32;
   hipStream_t s = (hipStream_t)hip_stream;
-  return u->dtype == DFX_F32 ? norm_launch<DFX_F32>(a, s) : u->dtype == DFX_BF16 ? norm_launch<DFX_BF16>(a, s) : norm_launch<DFX_F16>(a, s);
+  for (size_t first = 0; first < u->rows; first += kRowsAtOnce) {
+    a.x = (const unsigned char*)u->x + first * xs * eb; a.y = (unsigned char*)u->y + first * ys * eb;
+    a.rows = (uint32_t)std::min(kRowsAtOnce, u->rows - first);
+    const int rc = u->dtype == DFX_F32 ? norm_launch<DFX_F32>(a, s) : u->dtype == DFX_BF16 ? norm_launch<DFX_BF16>(a, s) : norm_launch<DFX_F16>(a, s);
+    if (rc != DFX_OK) return rc;
+  }
+  return DFX_OK;
 }
 
 size_t dfx_layer_norm_grad_workspace(size_t rows, size_t dim, dfx_dtype dtype) {

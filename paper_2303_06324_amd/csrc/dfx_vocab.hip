@@ -891,17 +891,17 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   return DFX_OK;
 }
 
-constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
+constexpr size_t kMostRows = (1ull << 24) - 1024, kMostVocab = 1ull << 28, kMostStride = 1ull << 20;
 
-// tiles of rows by the vocabulary are counted in 32 bits
-bool vocab_too_large(const VocabPlan& p) { return p.rp / 64 > (1ull << 31) / std::max<size_t>(p.tiles, 1); }
+// a launch's threads are counted in 32 bits: workgroups of 512 to each tile of the vocabulary by 128 rows at least
+bool vocab_too_large(const VocabPlan& p) { return p.rp / 128 * p.tiles >= (1ull << 23) - 8; }
 
 }  // namespace
 
 extern "C" {
 
 size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece) {
-  if (rows >= kMostRows || vocab >= kMostRows || dim >= kMostStride || piece % kTileRows) return 0;
+  if (rows >= kMostRows || vocab >= kMostVocab || dim >= kMostStride || piece % kTileRows) return 0;
   const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, grad != 0, piece, true);
   return vocab_too_large(p) ? 0 : p.bytes;
 }
@@ -910,7 +910,7 @@ int dfx_vocab_loss(const dfx_vocab_loss_args* u, void* hip_stream) {
   if (!u || u->struct_bytes != sizeof(*u)) return DFX_ERR_INVALID_ARG;
   if (u->dtype != DFX_F32 && u->dtype != DFX_BF16 && u->dtype != DFX_F16) return DFX_ERR_INVALID_ARG;
   if (u->grad_dtype != u->dtype && u->grad_dtype != DFX_F32) return DFX_ERR_INVALID_ARG;
-  if (u->rows >= kMostRows || u->vocab >= kMostRows || u->dim >= kMostStride) return DFX_ERR_TOO_LARGE;
+  if (u->rows >= kMostRows || u->vocab >= kMostVocab || u->dim >= kMostStride) return DFX_ERR_TOO_LARGE;
   const size_t eb = step_elem_bytes(u->dtype), gb = step_elem_bytes(u->grad_dtype);
   const size_t hs = u->hidden_stride ? u->hidden_stride : u->dim, ws = u->weight_stride ? u->weight_stride : u->dim;
   const size_t ghs = u->grad_hidden_stride ? u->grad_hidden_stride : u->dim, gws = u->grad_weight_stride ? u->grad_weight_stride : u->dim;

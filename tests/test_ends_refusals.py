@@ -87,6 +87,17 @@ def test_too_large(what):
         assert _call(what, kw) == dfx.ERR_TOO_LARGE, kw
 
 
+def test_too_many_tiles_of_a_vocabulary():
+    """A launch's threads are counted in 32 bits."""
+    dfx, _ = _lib()
+    for kw in (dict(rows=(1 << 24) - 1024), dict(vocab=1 << 28), dict(rows=1 << 22, vocab=1 << 16), dict(rows=1 << 23, vocab=50257)):
+        assert _call("vocab_loss", kw) == dfx.ERR_TOO_LARGE, kw
+        size = dict(dict(rows=4, vocab=50), **kw)
+        assert dfx.vocab_loss_workspace(size["rows"], 100, size["vocab"], dfx.BF16) == 0, kw
+    for rows, vocab in ((1 << 20, 1 << 16), (256, (1 << 28) - 1), (1, (1 << 28) - 1)):
+        assert dfx.vocab_loss_workspace(rows, 100, vocab, dfx.BF16) > 0
+
+
 def test_workspaces_have_room_for_fewer_rows():
     dfx, _ = _lib()
     rows = [0, 1, 2, 3, 63, 64, 65, 127, 128, 129, 255, 256, 257, 1000, 1023, 1024, 1025, 4095, 4097, 8191, 8192, 16384, 65535, 65536, 65537, 100000, 300001]

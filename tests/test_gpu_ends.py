@@ -246,6 +246,36 @@ def test_layer_norm_values(dt):
     _near(_np(y)[4:], h, eh + 3 * U * np.abs(h) + HALF[dt] * np.abs(h) + TINY[dt])
 
 
+def test_more_rows_than_a_launch_has():
+    """Short rows, so many that they take several launches; and a table of as many, cleared."""
+    torch, _ = _t()
+    dfx, kinds = _dfx()
+    rows, dim, vocab = (1 << 22) + 5, 8, 1000
+    gen = torch.Generator("cuda").manual_seed(17)
+    tokens = torch.randint(-1, vocab, (rows,), generator=gen, device="cuda")
+    table = torch.randn(vocab, dim, generator=gen, device="cuda").bfloat16()
+    og, out = _rows(rows, dim, "bf16", fill=7.0)
+    dfx.embed(rows, dim, vocab, kinds["bf16"], tokens.data_ptr(), table.data_ptr(), og.ptr(), scale=0.5)
+    og.check()
+    assert torch.equal(out, torch.where(tokens[:, None] >= 0, (table * 0.5)[tokens.clamp(min=0)], torch.zeros((), dtype=torch.bfloat16, device="cuda")))
+    yg, y = _rows(rows, dim, "bf16", fill=7.0)
+    dfx.layer_norm(rows, dim, kinds["bf16"], og.ptr(), yg.ptr(), eps=EPS)
+    yg.check()
+    one, two = _rows(6, dim, "bf16", fill=7.0)
+    last = out[-6:].contiguous()
+    dfx.layer_norm(6, dim, kinds["bf16"], last.data_ptr(), one.ptr(), eps=EPS)
+    assert torch.equal(y[-6:], two)
+    for n, vocab in ((600, (1 << 24) + 3), (600, 1 << 18), (20, (1 << 22) + 9)):
+        t = torch.arange(n, device="cuda") * 7 + vocab - 7 * n
+        g = torch.ones(n, 1, dtype=torch.float16, device="cuda")
+        Gg, G = _rows(vocab, 1, "f16", fill=7.0)
+        nbytes = dfx.embed_grad_workspace(n, 1, vocab, kinds["f16"])
+        work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        dfx.embed_grad(n, 1, vocab, kinds["f16"], t.data_ptr(), g.data_ptr(), Gg.ptr(), workspace=work.data_ptr(), workspace_bytes=nbytes)
+        Gg.check()
+        assert bool((G[t, 0] == 1).all()) and int((G != 0).sum()) == n
+
+
 # ------------------------------------------------------------------------------------------------------------ the vocabulary's loss
 class Vocab:
     """A call's memory, and the check of everything that it gives."""
