@@ -201,6 +201,27 @@ __device__ __forceinline__ void clear_row(void* out, size_t stride, uint32_t dim
   for (uint32_t e = threadIdx.x * N; e < dim; e += blockDim.x * N) part_put<OUT, N, true>(at, e, dim, zero);
 }
 
+// The whole table, by `groups` workgroups of which this one is the group-th: where its rows follow one another as one piece of memory, in vectors at multiples of 16 bytes (35146 rows of
+// 657 bf16: row for row 62 us of the gradient of 758 places, so 30).
+template <int OUT>
+__device__ __forceinline__ void clear_table(void* out, size_t stride, uint32_t dim, uint32_t vocab, uint32_t group, uint32_t groups) {
+  typedef typename StepElem<OUT>::raw raw;
+  if (stride != dim) {
+    for (uint32_t row = group; row < vocab; row += groups) clear_row<OUT>(out, stride, dim, row);
+    return;
+  }
+  constexpr uint32_t N = 16 / sizeof(raw);
+  const size_t all = (size_t)vocab * dim, head = min(all, (size_t)((16u - (uint32_t)((uintptr_t)out & 15u)) & 15u) / sizeof(raw)), vectors = (all - head) / N;
+  StepVec<OUT, (int)N> zero;
+  zero.w = 0;
+  raw* body = (raw*)out + head;
+  for (size_t v = (size_t)group * blockDim.x + threadIdx.x; v < vectors; v += (size_t)groups * blockDim.x) zero.stream(body, v * N);
+  if (group == 0 && threadIdx.x < 2 * N) {
+    const size_t i = threadIdx.x < N ? (size_t)threadIdx.x : head + vectors * N + threadIdx.x - N;      // in front of the vectors, behind them
+    if (threadIdx.x < N ? i < head : i < all) step_put<OUT>(out, i, 0.0f);
+  }
+}
+
 template <int OUT>
 __global__ void __launch_bounds__(kOwnThreads) dfx_embed_own_kernel(SortArgs a, void* out, size_t stride, uint32_t dim) {
   constexpr uint32_t U = kOwnMost / kOwnThreads;
@@ -209,7 +230,7 @@ __global__ void __launch_bounds__(kOwnThreads) dfx_embed_own_kernel(SortArgs a, 
   __shared__ uint32_t counts[3][kOwnWaves];      // of smaller remainders, of this one, without a token
   const uint32_t me = threadIdx.x, wave = me / kStepWave, lane = me % kStepWave;
   if (blockIdx.x >= kOwners) {
-    for (uint32_t row = blockIdx.x - kOwners; row < a.vocab; row += gridDim.x - kOwners) clear_row<OUT>(out, stride, dim, row);
+    clear_table<OUT>(out, stride, dim, a.vocab, blockIdx.x - kOwners, gridDim.x - kOwners);
     return;
   }
   bin[2u * me] = bin[2u * me + 1u] = 0;
@@ -400,6 +421,10 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_join_kernel(SumArgs a
 // In all, by this and by the sort: 300 x 1024 bf16 9 us and 17, 500 x 4096 11.4 and 17.4.
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t kFewPlaces = 512, kFewTable = 8;
+// From so many rows on, the table is cleared first, a launch more, and the sums added onto it (us, cleared first and not: 300 x 368 by 86505 fp32 26 and 47, 129 x 448 by 21904 bf16 12 and 18, 26 x
+// 1001 by 10000 fp32 level, 300 x 1001 by 5003 27 and 23).
+constexpr size_t kFewClear = 16384;
+constexpr size_t kClearGroups = 8192;    // workgroups of the clearing, at most: 86505 x 368 fp32 in some 20 us, 6 TB/s
 
 template <int DT, int OUT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_few_kernel(SumArgs a, const int64_t* tokens) {
@@ -474,7 +499,7 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_few_kernel(SumArgs a,
 
 template <int OUT>
 __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_clear_kernel(void* out, size_t stride, uint32_t dim, uint32_t vocab) {
-  for (uint32_t row = blockIdx.x; row < vocab; row += gridDim.x) clear_row<OUT>(out, stride, dim, row);
+  clear_table<OUT>(out, stride, dim, vocab, blockIdx.x, gridDim.x);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -588,9 +613,19 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
   memset(&a, 0, sizeof(a));
   a.grad = u->grad; a.out = u->table_grad; a.part = (float*)(ws + p.part); a.grad_stride = gs; a.out_stride = os;
   a.n = (uint32_t)u->rows; a.dim = (uint32_t)u->dim; a.vocab = (uint32_t)u->vocab; a.block = p.block; a.blocks = p.blocks; a.scale = (float)u->scale; a.accumulate = u->accumulate != 0;
-  if (u->rows && u->rows <= kFewPlaces && (u->accumulate || u->vocab <= kRowsAtOnce)) {
+  auto clear = [&]() -> int {
+    auto k = u->out_dtype == DFX_F32 ? dfx_embed_clear_kernel<DFX_F32> : u->out_dtype == DFX_BF16 ? dfx_embed_clear_kernel<DFX_BF16> : dfx_embed_clear_kernel<DFX_F16>;
+    const size_t groups = os == u->dim ? u->vocab * u->dim * ob / (16 * kEmbedThreads) + 1 : u->vocab;
+    return step_launch(k, dim3((uint32_t)std::min(groups, kClearGroups)), kEmbedThreads, s, u->table_grad, os, (uint32_t)u->dim, (uint32_t)u->vocab);
+  };
+  if (u->rows && u->rows <= kFewPlaces) {
+    if (!a.accumulate && u->vocab >= kFewClear) {
+      const int rc = clear();
+      if (rc != DFX_OK) return rc;
+      a.accumulate = true;
+    }
     const uint32_t at_once = kEmbedThreads * 16 / (uint32_t)eb;      // elements of a row that a workgroup has
-    const dim3 grid(u->accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable), std::min(8u, (a.dim + at_once - 1) / at_once));
+    const dim3 grid(a.accumulate ? a.n : (uint32_t)((u->vocab + kFewTable - 1) / kFewTable), std::min(8u, (a.dim + at_once - 1) / at_once));
     const bool wide = u->out_dtype == DFX_F32;
     auto k = u->dtype == DFX_F32 ? dfx_embed_few_kernel<DFX_F32, DFX_F32> : u->dtype == DFX_BF16 ? (wide ? dfx_embed_few_kernel<DFX_BF16, DFX_F32> : dfx_embed_few_kernel<DFX_BF16, DFX_BF16>)
                                                                         : (wide ? dfx_embed_few_kernel<DFX_F16, DFX_F32> : dfx_embed_few_kernel<DFX_F16, DFX_F16>);
@@ -605,8 +640,7 @@ int dfx_embed_grad(const dfx_embed_grad_args* u, void* hip_stream) {
     if (rc != DFX_OK) return rc;
     a.sorted = pairs[0];
   } else if (!u->accumulate) {
-    auto k = u->out_dtype == DFX_F32 ? dfx_embed_clear_kernel<DFX_F32> : u->out_dtype == DFX_BF16 ? dfx_embed_clear_kernel<DFX_BF16> : dfx_embed_clear_kernel<DFX_F16>;
-    const int rc = step_launch(k, dim3((uint32_t)std::min(u->vocab, kRowsAtOnce)), kEmbedThreads, s, u->table_grad, os, (uint32_t)u->dim, (uint32_t)u->vocab);
+    const int rc = clear();
     if (rc != DFX_OK) return rc;
   }
   if (!u->rows) return DFX_OK;
