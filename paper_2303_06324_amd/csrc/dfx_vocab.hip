@@ -901,7 +901,8 @@ bool vocab_too_large(const VocabPlan& p) { return p.rp / 128 * p.tiles >= (1ull 
 extern "C" {
 
 size_t dfx_vocab_loss_workspace(size_t rows, size_t dim, size_t vocab, dfx_dtype dtype, int grad, size_t piece) {
-  if (rows >= kMostRows || vocab >= kMostVocab || dim >= kMostStride || piece % kTileRows) return 0;
+  if (dtype != DFX_F32 && dtype != DFX_BF16 && dtype != DFX_F16) return 0;
+  if (rows >= kMostRows || vocab >= kMostVocab || !dim || dim >= kMostStride || piece % kTileRows) return 0;
   const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, grad != 0, piece, true);
   return vocab_too_large(p) ? 0 : p.bytes;
 }
