@@ -10,6 +10,7 @@
 
 #include "dfx_step.h"
 #include "dfx_tiles.h"
+#include "dfx_vocab_plan.h"
 
 namespace {
 
@@ -20,10 +21,6 @@ typedef short GemmShort8 __attribute__((ext_vector_type(8)));
 typedef float GemmAcc __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) unsigned char GemmLds;
 
-constexpr int kGemmK = 64;               // elements of k in a step: 128 bytes of a row
-
-__host__ __device__ constexpr int gemm_planes(int dt) { return dt == DFX_F32 ? 3 : 1; }
-__host__ __device__ constexpr int gemm_pairs(int dt) { return dt == DFX_F32 ? 6 : 1; }
 __device__ __forceinline__ int gemm_plane_a(int pair) { return (0x201100 >> (4 * (5 - pair))) & 0xf; }      // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
 __device__ __forceinline__ int gemm_plane_b(int pair) { return (0x021010 >> (4 * (5 - pair))) & 0xf; }
 
@@ -732,8 +729,6 @@ __global__ void __launch_bounds__(512, 2) dfx_gemm_lone_kernel(GemmSource w, Gem
 // A part of dX: 16 E elements of a row of W, by N rows of dz, summed over rows of W, 32 of each 128 by each of four waves.  A lane reads E elements of eight rows, and
 // so holds eight k's of each of E tiles whose rows are E elements apart.  (E = 8, 16 bytes of 16-bit rows, takes too many registers by 64 rows: 48 x 1024 x 32000 22.5 us and 18.)
 // 8 x 3840 x 72397 bf16 112 us, 5.0 TB/s.
-constexpr uint32_t kFewK = 128;
-__host__ __device__ constexpr int gemm_few_e(int dt, int nt) { return dt != DFX_F32 && nt == 2 ? 8 : 4; }
 template <int DT, int NT>
 __global__ void __launch_bounds__(256, DT == DFX_F32 && NT == 4 ? 1 : 2) dfx_gemm_few_dx_kernel(GemmSource w, GemmOperand b, GemmShape s, float* part, uint32_t rows, uint32_t pitch, bool more) {
   constexpr int E = gemm_few_e(DT, NT);

@@ -18,39 +18,20 @@
 #include <algorithm>
 
 #include "dfx_gemm.h"
+#include "dfx_vocab_plan.h"
 
 namespace {
 
 constexpr double kVLog2 = 0.69314718055994530942, kVLog2e = 1.44269504088896340736;
 constexpr float kDzScale = 32768.0f;
 constexpr uint32_t kRowsThreads = 1024;
-constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
-
-// Up to so many rows of at least so many elements go by the products for few rows, which read the weight as it lies (us, by them and by wide tiles with gradients: 64 x 2048 x 32000
-// bf16 97 and 117, 64 x 1024 x 32000 in 32 bits 153 and 277; 128 rows 126 and 127, 252 and 295; between 65 and 128 bf16 rows -10 % to +19 %, the better the longer the vocabulary).
-constexpr uint32_t kFewRows = 128, kFewDim = 64;
 // Up to so many rows are found by every workgroup that lays one out, which spares a launch (1024 x 1024 x 2000: 23.4 us and 24.1).
 constexpr uint32_t kLayRows = 1024;
-// Elements of dz that are held at a time, and with them the logits of the last piece in 32 bits (8192 x 4096 x 131072: 2^26 24.1 ms, 2^27 23.8, 2^28 23.5: 1.6 GB; all of it, 2^30 and 6.4 GB, a
-// seventh less); rows of a piece at least, at most, of few rows, and where the caller says (offsets within a tile of dz have 32 bits).
-constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;
-// From so long a vocabulary on, few rows' logits are made by twice as many rows of an unaligned or 32-bit weight to a workgroup (40 x 2001 x 100000 bf16 184 us and 195 by half as many, but 66 x
-// 1789 x 30000 in 32 bits 140 and 94).
-constexpr size_t kFewWide = 65536;
 // Workgroups of dW of few rows (48 x 1024 x 32000 f16 and 8 x 3840 x 72397 bf16: 768 20.3 and 142 us, 1024 20.0 and 141, 2048 20.0 and 150).
 constexpr uint32_t kDwGroups = 1024;
-// The last piece's logits are kept, in 32 bits, where making them again takes longer than writing and reading them: of long rows (us, kept and not: 8192 x 512 x 32768 bf16 1255 and 1143,
-// x 1024 1820 and 1931, x 2048 2998 and 3433; 4096 x 128 x 16384 in 32 bits 576 and 552, x 256 810 and 855), and of so few that a launch counts
-// (256 elements: 1024 x 8192 55 and 57, 2048 x 16000 146 and 131).
-constexpr size_t kKeepDim = 1024, kKeepDimF32 = 256, kKeepElems = 16ull << 20;
 // Rows of a vocabulary whose tiles' parts are joined by a workgroup for each row, with gradients by each of dz's, which spares a launch (200 x 512 x 8000 43.9 us and 46.0, 1024 x 512 x 16000 level);
 // of few rows, whose parts lie together (8 x 512 x 60000 78.7 and 81.4, 128 rows 92.3 and 94.0).
 constexpr size_t kJoinMost = 16384, kJoinFew = 65536;
-
-// what is known of a call on the device; first in the workspace
-struct VocabState { uint32_t count; float g; };       // rows that count; scale * largest weight * c / 2^15
-
-struct VocabRow { float m, f, w; int32_t t; };        // largest logit, w / S, weight (relative, times 2^15), target
 
 struct VocabArgs {
   const int64_t* targets;
@@ -582,128 +563,9 @@ __global__ void __launch_bounds__(256) dfx_vocab_dx_kernel(VocabArgs a, const fl
 // ------------------------------------------------------------------------------------------
 // how a call is laid out
 // ------------------------------------------------------------------------------------------
-size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
-
 // Whether the weight can be read where it lies by loads to LDS: 16-bit rows of whole steps at multiples of 16 bytes.
 bool vocab_aligned(const dfx_vocab_loss_args& u) {
   return u.dtype != DFX_F32 && u.dim % kGemmK == 0 && (uintptr_t)u.weight % 16 == 0 && (u.weight_stride ? u.weight_stride : u.dim) % 8 == 0;
-}
-
-struct VocabPlan {
-  size_t rp, dp, dq, vp, pieces, tiles, splits, split_rows;      // rows and elements padded, dX's pitch, rows of a piece, pieces, tiles of the vocabulary, splits of dX and the tiles' rows
-  bool few, keep;                        // keep: the logits of the last piece
-  int lone;                              // x stays in registers, 32 times so many elements of a wave; or 0
-  int nt, mt;                            // tiles of the products for few rows
-  size_t height;                         // of a tile of the vocabulary, for few rows
-  size_t wide;                           // otherwise: rows of the vocabulary whose logits go by wide tiles, the others' by quarters
-  bool dx_quarters, dw_quarters;         // whether the gradients' products do
-  size_t state, idx, target, map, weight, zt, row_loss, row_w, row, parts, x, w, dz, z, dx, bytes;      // places in the workspace
-};
-
-// Whether logits go by workgroups that keep x, and 32 times how many elements of it each of the eight waves has: not where an eighth of those would lie behind a row's end (us by
-// them and by the others, bf16 of 1 row by 32000, the weight in the caches: 1024 elements 19.6 and 20.9, 1001 28.1 and 31.8, 1531 42.3 and 46.2, but 1600 28.2 and 26.4, 3200 45.2 and 40.5; from
-// HBM, by 50257: 2000 49 and 62, 2048 53 and 57).
-int vocab_lone(size_t rows, size_t dim, int dtype) {
-  if (rows > (dtype == DFX_F32 ? 16 : 32)) return 0;
-  for (int kk : {4, 6, 8, 12, 16}) {
-    if (kk > (dtype == DFX_F32 || rows > 16 ? 8 : 16)) break;
-    const size_t all = 256 * (size_t)kk;
-    if (dim <= all) return dim * 8 > all * 7 ? kk : 0;
-  }
-  return 0;
-}
-
-// How long a launch takes of workgroups, one to a compute unit, of two kinds: n of length l each, the longer ones first.
-double vocab_time(size_t n, double l, size_t n2, double l2) {
-  if (l2 > l) { std::swap(n, n2); std::swap(l, l2); }
-  const size_t some = n % 256;           // compute units that have one more of the long ones
-  const double early = (double)(n / 256) * l, late = some ? early + l : early;
-  if (!n2) return late;
-  auto done = [&](double t) { return (double)(256 - some) * floor((t - early) / l2 + 1e-9) + (t > late ? (double)some * floor((t - late) / l2 + 1e-9) : 0.0); };
-  double k = std::max(1.0, std::max(floor((double)n2 / 256), std::min(ceil((double)n2 / (double)(256 - some)), floor((late - early) / l2))));
-  while (done(early + k * l2) < (double)n2) k += 1;
-  const double t = early + k * l2, other = t > late ? late + floor((t - late) / l2) * l2 : late;      // (those that come behind the late ones may be the last)
-  return std::max(late, other < t && done(other) >= (double)n2 ? other : t);
-}
-
-// Tiles of the products of many rows, and splits of dX: what takes the shortest time where a wide tile takes a unit for a step of k and as long as 8 steps besides, and a quarter of it
-// 0.4 of both (4096 x 2048 x 8192, logits: 65 us and 25; dW: 117 and 45).
-constexpr double kQuarter = 0.4;
-void vocab_tiles(VocabPlan& p, size_t rows, size_t dim, size_t vocab, size_t pairs) {
-  auto over = [](size_t n, size_t by) { return (n + by - 1) / by; };
-  const size_t n4 = over(rows, 256), n1 = over(rows, 128), v4 = over(vocab, 256), m4 = over(dim, 256), m1 = over(dim, 128);
-  const double logits = (double)(p.dp / kGemmK * pairs) + 8;
-  double best = 1e300;
-  for (size_t wide : {v4, v4 * n4 / 256 * 256 / n4, (size_t)0}) {
-    const double t = vocab_time(wide * n4, logits, n1 * (wide < v4 ? over(vocab - wide * 256, 128) : 0), kQuarter * logits);
-    if (t < best) { best = t; p.wide = wide * 256; }
-  }
-  p.tiles = p.wide / 256 + over(vocab > p.wide ? vocab - p.wide : 0, 128);
-  const size_t most = std::max<size_t>(1, std::min(256 / (p.rp / 256 * m4), p.vp / 256)), steps = p.vp / kGemmK;
-  const double dw = (double)(over(rows, kGemmK) * pairs) + 8;
-  best = 1e300;
-  for (int kind = 0; kind < 4; ++kind) {
-    const bool xq = kind & 1, wq = kind >> 1;
-    for (size_t part = 1; part <= 16; ++part) {
-      const size_t splits = over(most * part, 16);
-      const double dx = (double)(over(steps, splits) * pairs) + 8;
-      const double t = vocab_time(splits * (xq ? n1 * m1 : n4 * m4), xq ? kQuarter * dx : dx, wq ? m1 * over(p.vp, 128) : m4 * (p.vp / 256), wq ? kQuarter * dw : dw) + (double)(splits * rows * dim) * 0.5e-6;
-      if (t < best) { best = t; p.splits = splits; p.dx_quarters = xq; p.dw_quarters = wq; }
-    }
-  }
-}
-
-// Splits of dX along the vocabulary: as many workgroups as compute units, of the products for few rows three times as many.  What depends on the number of rows has room for
-// any smaller number.  aligned: rows of weight lie at multiples of 16 bytes (which changes nothing of the space).
-VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bool grad, size_t piece, bool aligned) {
-  VocabPlan p;
-  const size_t planes = gemm_planes(dtype);
-  p.few = rows <= kFewRows && dim >= kFewDim;
-  p.lone = 0;
-  p.rp = std::max(kTileRows, up(rows, kTileRows));
-  p.dp = up(dim, kGemmK);
-  p.dq = up(dim, 4);
-  const size_t whole = std::max(kTileRows, up(vocab, kTileRows));
-  const size_t most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceMost), few_most = std::min(whole, piece ? std::min(piece, kPieceEver) : kPieceFew);
-  const bool long_rows = dim >= (dtype == DFX_F32 ? kKeepDimF32 : kKeepDim);
-  size_t length = most, dz = p.rp * most;
-  if (!piece) {
-    length = std::min(most, std::max(kPieceLeast, kPieceElems / p.rp / kTileRows * kTileRows));
-    dz = std::min(dz, std::max(kPieceElems, p.rp * kPieceLeast));
-  }
-  if (p.few) length = few_most;
-  p.pieces = (whole + length - 1) / length;
-  p.vp = piece ? length : up((whole + p.pieces - 1) / p.pieces, kTileRows);      // (of equal length)
-  p.keep = grad && (p.few || long_rows || p.rp * p.vp <= kKeepElems);
-  if (p.few) {
-    p.nt = rows <= 32 ? 2 : 4;
-    p.lone = vocab_lone(rows, dim, dtype);
-    p.mt = !p.lone && (aligned || vocab >= kFewWide) ? 2 : 1;
-    // so many tiles that whole rounds of workgroups, two to a compute unit, have them all
-    const size_t rounds = std::max<size_t>(1, (vocab + 512 * 64 * p.mt - 1) / (512 * 64 * p.mt));
-    p.height = std::max<size_t>(16, up((vocab + 512 * rounds - 1) / (512 * rounds), 4));
-    p.tiles = (vocab + p.height - 1) / p.height + p.pieces;      // (of each piece by itself)
-    p.split_rows = up(std::max<size_t>(rows, 1), 64);
-    const size_t dx_wide = 16 * gemm_few_e(dtype, p.nt), groups = up(std::max<size_t>(rows, 1), 16 * p.nt) / (16 * p.nt) * (up(dim, dx_wide) / dx_wide);
-    p.splits = std::max<size_t>(1, std::min(768 / groups, p.vp / kFewK));
-  } else {
-    p.height = 0;
-    p.split_rows = p.rp;
-    vocab_tiles(p, std::max<size_t>(rows, 1), dim, vocab, gemm_pairs(dtype));
-  }
-  size_t at = 0;
-  auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
-  p.state = take(sizeof(VocabState) + 4);
-  p.idx = take(4 * p.rp); p.target = take(4 * p.rp); p.map = take(4 * p.rp); p.weight = take(4 * p.rp); p.zt = take(4 * p.rp);
-  p.row_loss = take(4 * p.rp); p.row_w = take(4 * p.rp); p.row = take(sizeof(VocabRow) * p.rp);
-  p.parts = take(sizeof(float2) * std::max<size_t>(p.rp * (whole / 128), kFewRows * std::min(whole / 4, whole / 32 + 520)));
-  p.x = take(planes * p.rp * p.dp * 2);
-  p.w = p.few ? at : take(planes * most * p.dp * 2);
-  p.dz = grad ? take(planes * std::max(dz, kFewRows * few_most) * 2) : at;
-  p.z = grad ? take(std::max(long_rows ? dz : std::min(dz, kKeepElems), kFewRows * few_most) * 4) : at;
-  p.dx = grad ? take(std::max(std::max(256 / (up(dim, 256) / 256), p.rp / 256) * 256, std::max<size_t>(768 / (up(dim, 128) / 128), 1) * kFewRows) * p.dq * 4) : at;
-  p.bytes = at;
-  return p;
 }
 
 // a product as workgroups of a launch from `from` on, of m by n elements
@@ -803,15 +665,15 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   float* dx = (float*)(ws + p.dx);
 
   const size_t hs = u.hidden_stride ? u.hidden_stride : u.dim;
-  if (u.rows <= kLayRows) VOCAB_TRY(step_launch(dfx_vocab_lay_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+  if (u.rows <= kLayRows) VOCAB_TRY(step_launch(dfx_vocab_lay_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.x_plane));
   else {
     VOCAB_TRY(step_launch(dfx_vocab_rows_kernel, dim3(1), kRowsThreads, stream, a));
-    VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, hs, (const int32_t*)a.idx, (uint32_t)u.dim, (uint32_t)p.dp, x, p.rp * p.dp));
+    VOCAB_TRY(step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)p.rp), 256, stream, u.hidden, hs, (const int32_t*)a.idx, (uint32_t)u.dim, (uint32_t)p.dp, x, p.x_plane));
   }
   // The weight is read where it lies if its rows are whole steps at multiples of 16 bytes; otherwise a piece at a time is laid out.
   // (The products for few rows take it as it is.)
   const bool direct = !p.few && vocab_aligned(u);
-  const GemmOperand ox = {x, p.rp * p.dp, (uint32_t)p.dp, (uint32_t)p.split_rows, (uint32_t)p.dp};
+  const GemmOperand ox = {x, p.x_plane, (uint32_t)p.dp, (uint32_t)p.split_rows, (uint32_t)p.dp};
   const size_t pieces = (u.vocab + p.vp - 1) / p.vp;
   GemmOperand ow = {};
   auto take_piece = [&](size_t v0, size_t left) -> int {
@@ -819,9 +681,9 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
       ow = {(const uint16_t*)u.weight + v0 * ws_stride, 0, (uint32_t)ws_stride, (uint32_t)left, (uint32_t)u.dim};
       return DFX_OK;
     }
-    ow = {w, p.vp * p.dp, (uint32_t)p.dp, (uint32_t)left, (uint32_t)p.dp};
+    ow = {w, p.w_plane, (uint32_t)p.dp, (uint32_t)left, (uint32_t)p.dp};
     return step_launch(dfx_vocab_pack_kernel<DT>, dim3((uint32_t)left), 256, stream, (const void*)((const unsigned char*)u.weight + v0 * ws_stride * eb), ws_stride, (const int32_t*)nullptr,
-                       (uint32_t)u.dim, (uint32_t)p.dp, w, p.vp * p.dp);
+                       (uint32_t)u.dim, (uint32_t)p.dp, w, p.w_plane);
   };
   const GemmShape by_rows = {0, 0, 1, (uint32_t)(p.dp / kGemmK), 0, count, false};
   const size_t last = pieces ? (pieces - 1) * p.vp : 0;
@@ -861,15 +723,15 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   for (size_t q = pieces; q-- != 0;) {   // the last one first
     const size_t v0 = q * p.vp, left = std::min(p.vp, u.vocab - v0);
     if (direct || (!p.few && v0 != last)) VOCAB_TRY(take_piece(v0, left));
-    const VocabDz<DT> epi = {a.row, dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
+    const VocabDz<DT> epi = {a.row, dz, p.dz_plane, (uint32_t)p.vp, (uint32_t)left, (uint32_t)v0, a.k};
     if (p.few && v0 != last) VOCAB_TRY(few_logits(v0, left, stats(v0, left, z, 0, nullptr)));
     if (p.few || (z && v0 == last))
       VOCAB_TRY(step_launch(join && v0 == last ? dfx_vocab_dz_kernel<DT, true> : dfx_vocab_dz_kernel<DT, false>, dim3((uint32_t)p.split_rows, (uint32_t)(p.vp / 8 + 255) / 256), 256, stream, a, epi, (const float*)z));
     else {
       const size_t wide = wide_of(v0, left);
-      VOCAB_TRY((vocab_logits<DT>(ow, ox, by_rows, wide, left, u.rows, epi, VocabDz<DT>{a.row, dz + wide, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)(left - wide), (uint32_t)(v0 + wide), a.k}, stream)));
+      VOCAB_TRY((vocab_logits<DT>(ow, ox, by_rows, wide, left, u.rows, epi, VocabDz<DT>{a.row, dz + wide, p.dz_plane, (uint32_t)p.vp, (uint32_t)(left - wide), (uint32_t)(v0 + wide), a.k}, stream)));
     }
-    const GemmOperand oz = {dz, p.rp * p.vp, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
+    const GemmOperand oz = {dz, p.dz_plane, (uint32_t)p.vp, (uint32_t)p.split_rows, (uint32_t)p.vp};
     const GemmShape sx = {0, 0, (uint32_t)p.splits, (uint32_t)((left + kGemmK - 1) / kGemmK), 0, count, false}, sw = {0, 0, 1, 0, 0, count, true};
     const VocabDx dx_to = {dx, (uint32_t)p.split_rows, (uint32_t)p.dq, v0 != last};
     const size_t gs = u.grad_weight_stride ? u.grad_weight_stride : u.dim;
@@ -892,9 +754,6 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
 }
 
 constexpr size_t kMostRows = (1ull << 24) - 1024, kMostVocab = 1ull << 28, kMostStride = 1ull << 20;
-
-// a launch's threads are counted in 32 bits: workgroups of 512 to each tile of the vocabulary by 128 rows at least
-bool vocab_too_large(const VocabPlan& p) { return p.rp / 128 * p.tiles >= (1ull << 23) - 8; }
 
 }  // namespace
 
