@@ -146,7 +146,7 @@ inline VocabPlan vocab_plan(size_t rows, size_t dim, size_t vocab, int dtype, bo
   }
   p.x_plane = p.rp * p.dp;
   p.w_plane = p.vp * p.dp;
-  p.dz_plane = p.rp * p.vp;
+  p.dz_plane = p.split_rows * p.vp;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += up(n, 256); return here; };
   p.state = take(sizeof(VocabState) + 4);
