@@ -352,7 +352,7 @@ int norm_grad_launch(const NormArgs& a, uint32_t groups, hipStream_t s) {
 }
 
 constexpr size_t kMostRows = (1ull << 31) - 1024, kMostStride = 1ull << 20;
-constexpr size_t kRowsAtOnce = 1ull << 22;      // of a launch of the forward pass (whose threads are counted in 32 bits)
+constexpr size_t kRowsAtOnce = 1ull << 21;      // of a launch of the forward pass: a row has 1024 threads at most, and a launch's threads are counted in 32 bits
 
 bool norm_types(int dtype, int other) { return (dtype == DFX_F32 || dtype == DFX_BF16 || dtype == DFX_F16) && (other == dtype || other == DFX_F32); }
 
