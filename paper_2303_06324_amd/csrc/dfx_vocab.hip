@@ -430,7 +430,7 @@ struct VocabDz {
     for (int e = 0; e < 8; ++e) {
       v[e] = r.f * vocab_exp(z[e], r.m, k);
       if (m + e == t) v[e] -= r.w;
-      if (m + e >= left) v[e] = 0.0f;
+      if (m + e >= left || r.t < 0) v[e] = 0.0f;      // (a row behind those that count may have NaN for logits: 0 times an infinite weight)
     }
     if constexpr (DT == DFX_F32) {
       uint32_t p[3][4];

@@ -32,3 +32,46 @@ def test_more_long_rows_than_a_launch_has():
     dfx.layer_norm(rows, dim, kinds["bf16"], x.data_ptr(), x.data_ptr())
     assert torch.equal(x[at], want) and bool(want.any())
     assert not x[1:2000].any() and not x[-2000:-2].any()      # (the last two are of the five)
+
+
+# Rows that are few and many, dim and vocab, and a piece (0: the library's): hidden states in registers, through LDS and past it; tiles of one piece, whose logits are kept, and of several
+INFINITE = [(9, 1024, 520, 0), (20, 128, 700, 0), (70, 100, 700, 256), (300, 128, 700, 0), (300, 128, 700, 256), (130, 70, 700, 512)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,dim,vocab,piece", INFINITE)
+def test_a_logit_of_plus_infinity(rows, dim, vocab, piece, dt):
+    """Its row is NaN, and with it the weight's gradient; the other rows' numbers are the same bits as without it."""
+    torch, _ = _t()
+    v = Vocab(rows, dim, vocab, dt, seed=110, weights=None)
+    v.t[5] = 1
+    keep = np.delete(np.arange(rows), 5)
+    v.w[:, 7] = v.w[:, 7].abs() + 0.5
+    v.x[:, 7] = 0.0
+    v.run(piece=piece)
+    before = [v.lg.t.clone(), v.og.t.clone(), v.gh.clone()]
+    v.x[5, 7] = float("inf")
+    v.run(piece=piece)
+    for a, b in zip(before, (v.lg.t, v.og.t, v.gh)):
+        assert torch.equal(a[keep], b[keep])
+    assert bool(v.lg.t[5].isnan()) and bool(v.og.t[5].isnan()) and bool(v.gh[5].isnan().all()) and bool(v.gw.isnan().any()) and bool(v.sg.t[0].isnan())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,dim,vocab,piece", INFINITE)
+def test_a_token_of_minus_infinity(rows, dim, vocab, piece, dt):
+    """A row of the weight whose logits are all -infinity has probability 0, and its gradient is 0 (that of the hidden states, 0 times an infinity, is NaN by its definition)."""
+    v = Vocab(rows, dim, vocab, dt, seed=130, weights=None)
+    v.x[:, 7] = v.x[:, 7].abs() + 0.5
+    off = vocab - 300                          # (not in the last of several pieces)
+    v.t[v.t == off] = off - 1
+    v.w[off] = 0.0
+    v.w[off, 7] = -float("inf")
+    v.run(piece=piece, hidden=False)
+    got = _np(v.gw)
+    assert not np.isnan(v.lg.host()).any() and not np.isnan(got).any() and not got[off].any()
+    # the other tokens: as if that one were not there
+    v.w[off] = 0.0
+    v.w[off, 7] = -1000.0                      # (far below all others: probability 0 as well)
+    v.run(piece=piece, hidden=False)
+    assert np.array_equal(np.delete(_np(v.gw), off, 0), np.delete(got, off, 0))
