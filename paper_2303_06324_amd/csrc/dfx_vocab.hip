@@ -43,7 +43,8 @@ struct VocabArgs {
   float* top_weight;                     // largest |weight|
   VocabRow* row;                         // [Rp]
   float2* parts;                         // (m, S) of a tile's part of a row, at tile * tile_step + row * row_step: of many rows beside each other as a tile has them, of few a row's tiles
-  uint32_t rows, rp, tile_step, row_step, vocab, tiles;
+  uint16_t* x;                           // the rows that count, of 16 bits (null: of 32, whose infinite hidden states give NaN)
+  uint32_t rows, rp, tile_step, row_step, vocab, tiles, dp;      // dp: elements of a row of x
   double c;
   float k;                               // c / log 2
 };
@@ -332,6 +333,8 @@ __device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint
     if (a.logp) a.logp[a.idx[n]] = logp;
     if (a.loss) a.loss[a.idx[n]] = loss;
   }
+  if (n < count && s == 0.0f && a.x)     // its hidden state, which may be infinite, has no part in the products either: 0 times that is NaN
+    for (uint32_t e = 0; e < a.dp; e += 8u) *(uint4*)(a.x + (size_t)n * a.dp + e) = make_uint4(0, 0, 0, 0);
   return r;
 }
 
@@ -663,6 +666,7 @@ int vocab_run(const dfx_vocab_loss_args& u, const VocabPlan& p, hipStream_t stre
   const uint32_t* count = &a.state->count;
   uint16_t *x = (uint16_t*)(ws + p.x), *w = (uint16_t*)(ws + p.w), *dz = (uint16_t*)(ws + p.dz);
   float* dx = (float*)(ws + p.dx);
+  a.x = DT == DFX_F32 ? nullptr : x; a.dp = (uint32_t)p.dp;
 
   const size_t hs = u.hidden_stride ? u.hidden_stride : u.dim;
   if (u.rows <= kLayRows) VOCAB_TRY(step_launch(dfx_vocab_lay_kernel<DT>, dim3((uint32_t)p.split_rows), 256, stream, a, u.hidden, hs, (uint32_t)u.dim, (uint32_t)p.dp, x, p.x_plane));

@@ -38,6 +38,12 @@ def test_more_long_rows_than_a_launch_has():
 INFINITE = [(9, 1024, 520, 0), (20, 128, 700, 0), (70, 100, 700, 256), (300, 128, 700, 0), (300, 128, 700, 256), (130, 70, 700, 512)]
 
 
+def _hide(v, rows):
+    """The call's own arrays without some of its rows, as Vocab.check takes them: no target."""
+    v.t = v.t.copy()
+    v.t[rows] = -1
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows,dim,vocab,piece", INFINITE)
 def test_a_logit_of_plus_infinity(rows, dim, vocab, piece, dt):
@@ -55,6 +61,22 @@ def test_a_logit_of_plus_infinity(rows, dim, vocab, piece, dt):
     for a, b in zip(before, (v.lg.t, v.og.t, v.gh)):
         assert torch.equal(a[keep], b[keep])
     assert bool(v.lg.t[5].isnan()) and bool(v.og.t[5].isnan()) and bool(v.gh[5].isnan().all()) and bool(v.gw.isnan().any()) and bool(v.sg.t[0].isnan())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,dim,vocab,piece", INFINITE)
+def test_a_row_without_a_logit_above_minus_infinity(rows, dim, vocab, piece, dt):
+    """It has nothing to learn from: zeros, no weight in the sums, and no part in the weight's gradient, infinite as its hidden state is."""
+    v = Vocab(rows, dim, vocab, dt, seed=120, weights=None)
+    v.t[5], v.t[6] = 1, 2
+    v.w[:, 7] = -v.w[:, 7].abs() - 0.5
+    v.x[:, 7] = 0.0
+    v.x[5:7, 7] = float("inf")
+    v.run(piece=piece)
+    assert float(v.lg.t[5]) == 0.0 and float(v.og.t[6]) == 0.0 and not v.gh[5:7].any()
+    v.x[5:7, 7] = 0.0
+    _hide(v, [5, 6])
+    v.check()
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
