@@ -356,10 +356,11 @@ constexpr size_t kRowsAtOnce = 1ull << 21;      // of a launch of the forward pa
 
 bool norm_types(int dtype, int other) { return (dtype == DFX_F32 || dtype == DFX_BF16 || dtype == DFX_F16) && (other == dtype || other == DFX_F32); }
 
+// all space from a matrix's first to its last row
+Span rows_of(const void* a, size_t stride, size_t rows, size_t dim, size_t eb) { return flat(a, rows ? ((rows - 1) * stride + dim) * eb : 0); }
 // two matrices of rows: apart, or the same memory with the same stride
-bool rows_lie_well(const void* a, size_t as, const void* b, size_t bs, size_t rows, size_t dim, size_t eb, bool in_place) {
-  if (!rows || !a || !b || (in_place && a == b && as == bs)) return true;
-  return !meet(flat(a, ((rows - 1) * as + dim) * eb), flat(b, ((rows - 1) * bs + dim) * eb));
+bool rows_lie_well(const void* a, size_t as, const void* b, size_t bs, size_t rows, size_t dim, size_t eb) {
+  return (a == b && as == bs) || !meet(rows_of(a, as, rows, dim, eb), rows_of(b, bs, rows, dim, eb));
 }
 
 }  // namespace
@@ -373,8 +374,8 @@ int dfx_layer_norm(const dfx_layer_norm_args* u, void* hip_stream) {
   if (!u->dim || xs < u->dim || ys < u->dim || !(u->eps >= 0.0) || !step_normal(u->eps)) return DFX_ERR_INVALID_ARG;
   if ((u->rows && (!u->x || !u->y)) || (uintptr_t)u->x % eb || (uintptr_t)u->y % eb || (uintptr_t)u->weight % pb || (uintptr_t)u->bias % pb) return DFX_ERR_INVALID_ARG;
   if (!u->rows) return DFX_OK;
-  if (!rows_lie_well(u->x, xs, u->y, ys, u->rows, u->dim, eb, true)) return DFX_ERR_INVALID_ARG;
-  const Span y = {(uintptr_t)u->y, u->rows, u->dim * eb, ys * eb};
+  if (!rows_lie_well(u->x, xs, u->y, ys, u->rows, u->dim, eb)) return DFX_ERR_INVALID_ARG;
+  const Span y = rows_of(u->y, ys, u->rows, u->dim, eb);
   if (meet(flat(u->weight, u->dim * pb), y) || meet(flat(u->bias, u->dim * pb), y)) return DFX_ERR_INVALID_ARG;
   NormArgs a;
   memset(&a, 0, sizeof(a));
@@ -408,9 +409,9 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* u, void* hip_stream) {
   const bool sums = u->grad_weight || u->grad_bias;
   const size_t need = dfx_layer_norm_grad_workspace(u->rows, u->dim, u->dtype);
   if (sums && (!u->workspace || (uintptr_t)u->workspace % 16 || u->workspace_bytes < need)) return DFX_ERR_INVALID_ARG;
-  if (!rows_lie_well(u->x, xs, u->dx, dxs, u->rows, u->dim, eb, true) || !rows_lie_well(u->dy, dys, u->dx, dxs, u->rows, u->dim, eb, true)) return DFX_ERR_INVALID_ARG;
   const size_t rows = u->rows;
-  const Span x = {(uintptr_t)u->x, rows, u->dim * eb, xs * eb}, dy = {(uintptr_t)u->dy, rows, u->dim * eb, dys * eb}, dx = {(uintptr_t)u->dx, u->dx ? rows : 0, u->dim * eb, dxs * eb};
+  if (!rows_lie_well(u->x, xs, u->dx, dxs, rows, u->dim, eb) || !rows_lie_well(u->dy, dys, u->dx, dxs, rows, u->dim, eb)) return DFX_ERR_INVALID_ARG;
+  const Span x = rows_of(u->x, xs, rows, u->dim, eb), dy = rows_of(u->dy, dys, rows, u->dim, eb), dx = rows_of(u->dx, dxs, rows, u->dim, eb);
   const Span w = flat(u->weight, u->dim * pb), writes[] = {flat(u->grad_weight, u->dim * gb), flat(u->grad_bias, u->dim * gb), flat(sums ? u->workspace : nullptr, need)};
   if (meet(w, dx)) return DFX_ERR_INVALID_ARG;
   for (int k = 0; k < 3; ++k) {
