@@ -4,6 +4,7 @@ import pytest
 
 from tests.test_gpu_ends import Vocab, _dfx, _np, _rows, _t
 from tests.test_gpu_step import HALF, TINY, U, Guarded, _near
+from tests.test_vocab_plan import WIDE
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +98,14 @@ def test_a_token_of_minus_infinity(rows, dim, vocab, piece, dt):
     v.w[off, 7] = -1000.0                      # (far below all others: probability 0 as well)
     v.run(piece=piece, hidden=False)
     assert np.array_equal(np.delete(_np(v.gw), off, 0), np.delete(got, off, 0))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "x".join(map(str, c[0])))
+def test_wide_tiles(case, dt):
+    """The weight read in place where its rows are whole steps, by a stride and without one; and at odd places, the gradient in 32 bits and onto what is there."""
+    rows, dim, vocab, piece = case[0]
+    for more, off, onto, gt in ((8 if dim % 64 == 0 else 0, 0, False, dt), (3, 1, True, "f32")):
+        v = Vocab(rows, dim, vocab, dt, gt, more=more, off=off, seed=140)
+        v.run(onto=onto, piece=piece)
+        v.check(onto=onto)
