@@ -598,7 +598,7 @@ int dfx_embed(const dfx_embed_args* args, void* hip_stream);
 /*
  * The gradient of dfx_embed's table: table_grad[v] = scale * sum of grad[i] over the i with tokens[i] = v.  accumulate: that is added to what
  * table_grad holds, and rows that no token names are neither read nor written; otherwise all of it is written.  The rows of a token are
- * added up in 32 bits, in their order.
+ * added up in 32 bits, in an order that the tokens alone decide: blocks of places in theirs, then the blocks.
  */
 typedef struct {
   uint32_t struct_bytes;
@@ -620,7 +620,8 @@ int dfx_embed_grad(const dfx_embed_grad_args* args, void* hip_stream);
 
 /*
  * Layer norm of rows: h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps);  y = h weight + bias.  y may take x's place (same memory and stride).
- * A row with an infinity or NaN is NaN.  TOO_LARGE above 32768 elements of a row.
+ * A row with an infinity or NaN is NaN.  Mean and squares are taken in 32 bits: h is off by the mean's rounding (2^-24 of it, or a few times that) over the deviation, and h of a
+ * row whose mean square does not fit (deviations of 1.8e19 and more) is 0.  TOO_LARGE above 32768 elements of a row.
  */
 typedef struct {
   uint32_t struct_bytes;
@@ -674,10 +675,12 @@ int dfx_layer_norm_grad(const dfx_layer_norm_grad_args* args, void* hip_stream);
  * The products are made on the matrix cores in pieces of the vocabulary, and their sums in 32 bits; 32-bit inputs are taken as three terms of 8 bits of
  * mantissa each, of whose products the smallest are left out (together at most 2^-22 of the whole one).  For the gradients the logits are made a second time,
  * piece by piece (one piece's are kept in 32 bits where that takes less time), and dz is rounded to the type of the inputs on its way into the products (of
- * 32-bit inputs: to three such terms).  A row's numbers are the same with gradients and without (of one piece's length).
+ * 32-bit inputs: to three such terms; of f16 ones in steps of 2^-39 of the largest row weight at least, so that rows of a far smaller weight lose their small probabilities).
+ * dz goes into them times 2^15: sums that 32 bits cannot hold so are infinite.  A row's numbers are the same with gradients and without (of one piece's length).
  * A row of weight 0 or without a target has nothing to learn from: it takes no part in the products, its hidden state is not looked at, its
- * logp, loss and grad_hidden are 0.  So has a row with no logit above -infinity.  A logit of NaN or +infinity makes its row NaN, and with it
- * grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of rows are finite.
+ * logp, loss and grad_hidden are 0.  So are those of a row with no logit above -infinity, which has no part in grad_weight and no weight in the sums either.
+ * A logit of NaN or +infinity makes its row NaN, and with it grad_weight; an infinity in 32-bit hidden or weight makes NaN of the logits that it reaches.  Weights of
+ * rows are finite.
  * TOO_LARGE from 2^24 - 2^10 rows and from a vocab of 2^28 on, and where rows * vocab is 2^36 or more and a launch would not hold its tiles (at the latest from
  * 2^38 on).
  */

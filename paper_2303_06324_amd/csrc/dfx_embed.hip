@@ -18,7 +18,8 @@ namespace {
 constexpr int kEmbedThreads = 256;
 constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / kStepWave, kSortChunks = 256, kSortChunk = 2048;      // chunks at most, places of one at least
 constexpr uint32_t kDigitBits = 10;      // at most
-// places of a block of the sums at most; blocks, where they are fewer (us: 16384 x 4096 bf16 onto 256 98, 512 81, 1024 92; x 1024 86, 64, 57; 4000 x 1024 32, 29, 34)
+// places of a block of the sums at most; blocks, where they are fewer (us, on the same memory each time, some of it in the caches: 16384 x 4096 bf16 onto 131072 rows 256 98, 512 78, 1024 91;
+// x 1024 87, 65, 62; 4000 x 1024 onto 50000 28, 25, 30)
 constexpr uint32_t kSumMost = 64, kSumBlocks = 512;
 
 struct EmbedArgs {
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kSortThreads) dfx_embed_move_kernel(SortArgs a
 // The same in one launch where there are few places and not very many tokens: a workgroup has the tokens of one remainder by kOwners.  It looks at all places, counts those
 // of smaller remainders, which come first, keeps its own in LDS in their order, and sorts them by the quotient: places of a quotient are counted, and one wave moves them, 64
 // at a time.  The workgroups behind clear the table's gradient meanwhile.  16384 places 19.6 us: the chain of one wave's rounds over its share and the counts before it.  In all, by this and by
-// the passes: 4000 x 1024 29 us and 39, 16384 x 4096 81 and 86.
+// the passes, on the same memory each time: 4000 x 1024 28 us and 37, 16384 x 4096 82 and 86 (from HBM 104).
 constexpr uint32_t kOwnMost = 16384, kOwnBits = 7, kOwners = 1u << kOwnBits, kOwnThreads = 1024, kOwnWaves = kOwnThreads / kStepWave, kOwnQuotients = 2 * kOwnThreads;
 
 template <int OUT>
@@ -202,7 +203,7 @@ __device__ __forceinline__ void clear_row(void* out, size_t stride, uint32_t dim
 }
 
 // The whole table, by `groups` workgroups of which this one is the group-th: where its rows follow one another as one piece of memory, in vectors at multiples of 16 bytes (35146 rows of
-// 657 bf16: row for row 62 us of the gradient of 758 places, so 30).
+// 657 bf16: row for row 62 us of the gradient of 758 places, so 28).
 template <int OUT>
 __device__ __forceinline__ void clear_table(void* out, size_t stride, uint32_t dim, uint32_t vocab, uint32_t group, uint32_t groups) {
   typedef typename StepElem<OUT>::raw raw;
@@ -418,11 +419,13 @@ __global__ void __launch_bounds__(kEmbedThreads) dfx_embed_join_kernel(SumArgs a
 // ------------------------------------------------------------------------------------------
 // few places: no sort.  A workgroup finds the places of its rows of the table among all of them, in their order.  Onto the gradient that is there: a workgroup to a
 // place, which does nothing if its token stood before; otherwise a workgroup to eight rows of the table.
-// In all, by this and by the sort: 300 x 1024 bf16 9 us and 17, 500 x 4096 11.4 and 17.4.
+// In all, by this and by the sort: 300 x 1024 bf16 7.0 us and 16.9, 500 x 4096 11.0 and 18.1.  A workgroup that has a frequent token adds up all its places in its part of the row: 300 x 1001 fp32,
+// whole table of 5003 rows, 8.7 us without tokens (20 MB of zeros), 11 with tokens of three places at most, 15 with one of 16, 115 where all are the same (1024 elements, whose vectors lie at
+// multiples of 16 bytes: 8.4, 10.2, 10.5, 37).
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t kFewPlaces = 512, kFewTable = 8;
-// From so many rows on, the table is cleared first, a launch more, and the sums added onto it (us, cleared first and not: 300 x 368 by 86505 fp32 26 and 47, 129 x 448 by 21904 bf16 12 and 18, 26 x
-// 1001 by 10000 fp32 level, 300 x 1001 by 5003 27 and 23).
+// From so many rows on, the table is cleared first, a launch more, and the sums added onto it (us, cleared first and not: 300 x 368 by 86505 fp32 28 and 47, 129 x 448 by 21904 bf16 10 and 15, 26 x
+// 1001 by 10000 fp32 level, 300 x 1001 by 5003 14.7 and 16.2; below, it goes by the launch that it spares).
 constexpr size_t kFewClear = 16384;
 constexpr size_t kClearGroups = 8192;    // workgroups of the clearing, at most: 86505 x 368 fp32 in some 20 us, 6 TB/s
 

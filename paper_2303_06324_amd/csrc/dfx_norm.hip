@@ -1,7 +1,9 @@
 // Layer norm over rows, forward and backward.
 //
 // h = (x - mean) r, r = 1 / sqrt(var + eps), y = h w + b;  with g = dy w:  dx = r (g - mean g - h mean(g h)), dw = sum dy h, db = sum dy.
-// A row stays in registers from its mean to its results: mean and variance are taken one behind the other, so that a large mean costs no digits.
+// A row stays in registers from its mean to its results.  Mean and variance are taken one behind the other, so that a large mean costs the variance nothing; h keeps the mean's own
+// rounding, 2^-24 of it or a few times that, over the deviation (as mean d, d = x - mean, it could be summed and taken out: 16384 x 4096 bf16 42 to 45 us forward, 91 to 113 backward; the sum
+// of x in 64 bits instead 43 and 98).
 // The backward pass makes both again rather than read what the forward pass would have to keep.
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -16,7 +18,7 @@
 namespace {
 
 constexpr uint32_t kNormDim = 32768;     // elements of a row, at most: what a workgroup of 1024 keeps in registers
-// workgroups of the backward pass, at most: each leaves its share of the sums over rows (us: 16384 x 4096 bf16 256 127, 512 104, 1024 106; 4096 x 1024 14.9, 12.9, 14.5)
+// workgroups of the backward pass, at most: each leaves its share of the sums over rows (us: 16384 x 4096 bf16 256 132, 512 94, 1024 102; 4096 x 1024 14.5, 12.4, 14.0)
 constexpr uint32_t kNormGroups = 512;
 
 struct NormArgs {
@@ -165,8 +167,10 @@ struct NormRow {
 
 // The same for the gradients.  A thread's columns are the same in every row, so that the weight and the sums over rows stay in its registers, and the next
 // row is on its way while one is worked on.  With d = x - mean, mean(g h) = r mean(g d): two rounds of sums over a row, (x, g) and (d^2, g d).
-// That takes 128 registers of workgroups of 512, two to a compute unit; rows above 8192 16-bit elements (4096 of 32 bits) have a workgroup of 1024, and no room for either (AHEAD).
-// 16384 x 4096 bf16 92 us, 4.4 TB/s (without the next row on its way 140): HBM, and a workgroup's two rounds of sums for each of its rows.
+// Workgroups of up to 512, two to a compute unit, have room for that in 128 registers, and so has one of 1024 for rows above 4096 16-bit elements (2048 of 32 bits).  From 8193 16-bit elements on they
+// have not: up to 16384 (8192 of 32 bits, which just fit) 25 of them lie in scratch, and above that 40 to 264, where the next row is not fetched and the weight is read again (AHEAD false).
+// 16384 x 4096 bf16 92 us, 4.4 TB/s (without the next row on its way 140): HBM, and a workgroup's two rounds of sums for each of its rows.  Longer rows, bf16: 8192 x 8192 108 us (3.7 TB/s),
+// 4096 x 16384 162, 2048 x 32768 410 (scratch: 1.0 TB/s); fp32: 8192 x 4096 93 and 4096 x 8192 92 (4.4 TB/s), 4096 x 16384 262, 2048 x 32768 750.
 template <int DT, int T, int U, int THREADS, bool AHEAD>
 __global__ void __launch_bounds__(THREADS, 4) dfx_norm_grad_kernel(NormArgs a) {
   constexpr int ROWS = THREADS / T, N = 16 / (int)sizeof(typename StepElem<DT>::raw);

@@ -28,8 +28,8 @@ constexpr size_t kTileRows = 256;        // rows of hidden and of weight are pad
 // Up to so many rows of at least so many elements go by the products for few rows, which read the weight as it lies (us, by them and by wide tiles with gradients: 64 x 2048 x 32000
 // bf16 97 and 117, 64 x 1024 x 32000 in 32 bits 153 and 277; 128 rows 126 and 127, 252 and 295; between 65 and 128 bf16 rows -10 % to +19 %, the better the longer the vocabulary).
 constexpr uint32_t kFewRows = 128, kFewDim = 64;
-// Elements of dz that are held at a time, and with them the logits of the last piece in 32 bits (8192 x 4096 x 131072: 2^26 24.1 ms, 2^27 23.8, 2^28 23.5: 1.6 GB; all of it, 2^30 and 6.4 GB, a
-// seventh less); rows of a piece at least, at most, of few rows, and where the caller says (offsets within a tile of dz have 32 bits).
+// Elements of dz that are held at a time, and with them the logits of the last piece in 32 bits (8192 x 4096 x 131072: 2^26 24.1 ms, 2^27 23.8, 2^28 23.5: 1.6 GB of a
+// workspace of 2.4, which has 0.5 for a weight that cannot be read where it lies; all of it, 2^30, 6.4 of 7.8 GB, a seventh less); rows of a piece at least, at most, of few rows, and where the caller says (offsets within a tile of dz have 32 bits).
 constexpr size_t kPieceElems = 256ull << 20, kPieceLeast = 1024, kPieceMost = 65536, kPieceFew = 1ull << 19, kPieceEver = 1ull << 22;
 // From so long a vocabulary on, few rows' logits are made by twice as many rows of an unaligned or 32-bit weight to a workgroup (40 x 2001 x 100000 bf16 184 us and 195 by half as many, but 66 x
 // 1789 x 30000 in 32 bits 140 and 94).
