@@ -109,3 +109,33 @@ def test_wide_tiles(case, dt):
         v = Vocab(rows, dim, vocab, dt, gt, more=more, off=off, seed=140)
         v.run(onto=onto, piece=piece)
         v.check(onto=onto)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,dim", [(1, 4000), (40, 4000), (40, 4096), (100, 3001)])
+def test_logits_of_few_long_rows(rows, dim, dt):
+    """The error of logp over many rows, by their root mean square: additions on the matrix cores cost up to 2 u of the sum that they meet, evenly spread (2 / sqrt 3 u), and one takes 32
+    products.  Where blocks are added up, of B steps of 64 elements and with P products of each (1, or 6 of 32 bits), the sum grows to Z sqrt(f) over a fraction f of the row: 2 P dim / 64 additions inside
+    of blocks of B / (dim / 64) of the row, and dim / (64 B) of blocks, rounded.  The sum of exponentials costs as much again, its logarithm and the rest 8 u.  (As one sum, the 32-bit rows were beyond.)"""
+    torch, _ = _t()
+    dfx, kinds = _dfx()
+    vocab, errors, sizes = 1000, [], []
+    for seed in range(max(1, 40 // rows)):
+        gen = torch.Generator("cuda").manual_seed(seed)
+        T = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dt]
+        w = (torch.randn(vocab, dim, generator=gen, device="cuda") * (2.5 / dim ** 0.5)).to(T)
+        t = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+        x = (torch.randn(rows, dim, generator=gen, device="cuda") + torch.rand(rows, 1, generator=gen, device="cuda") * 2 * w[t].float()).to(T)
+        logp = torch.empty(rows, device="cuda")
+        nbytes = dfx.vocab_loss_workspace(rows, dim, vocab, kinds[dt])
+        work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        dfx.vocab_loss(rows, dim, vocab, kinds[dt], x.data_ptr(), w.data_ptr(), t.data_ptr(), logp=logp.data_ptr(), workspace=work.data_ptr(), workspace_bytes=nbytes)
+        z = x.double().cpu() @ w.double().cpu().t()
+        zt = z.gather(1, t.cpu()[:, None])[:, 0]
+        errors.append((logp.double().cpu() - (zt - torch.logsumexp(z, 1))).numpy())
+        sizes.append(zt.numpy())
+    rms = lambda a: float(np.sqrt(np.mean(np.concatenate(a) ** 2)))
+    steps, block, products = dim / 64, 3 if dt == "f32" else 8, 6 if dt == "f32" else 1
+    inside = 2 * products * steps * 0.5 * (block / steps) * 4 / 3
+    between = steps / (2 if dt == "f32" else 8) * 0.5 / 3
+    assert rms(errors) <= (2 ** 0.5 * (inside + between) ** 0.5 * rms(sizes) + 8) * U, (rms(errors) / U, rms(sizes))
