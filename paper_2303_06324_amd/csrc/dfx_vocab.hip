@@ -1,7 +1,8 @@
 // Softmax cross entropy over a vocabulary whose logits are never kept, and its gradients: the head of a language model and the loss in one.
 //
-// With z = hidden weight^T and, for a row, m its largest logit and S = sum exp(c (z - m)):  logp = c (z_t - m) - log S.  Tiles of z are made on the matrix
-// cores and reduced to (m, S) of each row where they lie; a second kernel joins the tiles' parts.  For the gradients a piece of the vocabulary at
+// With z = hidden weight^T and, for a row, m its largest logit, R = the sum of exp(c (z - m)) but for the target's and S = R + exp(c (z_t - m)):  logp = c (z_t - m) - log S, or
+// -log(1 + R) where the target's is the largest, and its dz = -R / S: so that a token that is expected keeps the digits of what is missing from 1.  Tiles of z are made on the matrix
+// cores and reduced to (m, R) of each row where they lie; a second kernel joins the tiles' parts.  For the gradients a piece of the vocabulary at
 // a time is made again (the last one's logits may be kept), turned into dz = softmax - [target], and goes as the operand into dX += dz W and dW = dz^T X.
 //
 // Rows that have nothing to learn from are left out first: the others' hidden states are laid one behind the other (and padded to whole steps of
@@ -42,7 +43,7 @@ struct VocabArgs {
   float *weight, *zt, *row_loss, *row_w; // [Rp]
   float* top_weight;                     // largest |weight|
   VocabRow* row;                         // [Rp]
-  float2* parts;                         // (m, S) of a tile's part of a row, at tile * tile_step + row * row_step: of many rows beside each other as a tile has them, of few a row's tiles
+  float2* parts;                         // (m, R) of a tile's part of a row, at tile * tile_step + row * row_step: of many rows beside each other as a tile has them, of few a row's tiles
   uint16_t* x;                           // the rows that count, of 16 bits (null: of 32, whose infinite hidden states give NaN)
   uint32_t rows, rp, tile_step, row_step, vocab, tiles, dp;      // dp: elements of a row of x
   double c;
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_lay_kernel(VocabArgs a, const v
   pack_row<DT>(mine < 0 ? nullptr : (const unsigned char*)src + (size_t)mine * stride * step_elem_bytes(DT), dim, padded, dst + (size_t)blockIdx.x * padded, plane);
 }
 
-// A tile's part of each row: (m, S), and the target's logit where it lies here; for the last piece of a call with gradients the logits as well.
+// A tile's part of each row: (m, R), and the target's logit where it lies here; for the last piece of a call with gradients the logits as well.
 struct VocabStats {
   float2* parts;
   float *zt, *z;                         // z: rows of z_pitch, may be null
@@ -252,18 +253,21 @@ struct VocabStats {
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
+      if (t >= tile.m0 && t < end)       // (few rows of a tile have their target in it)
+#pragma unroll
+        for (int i = 0; i < TILE::MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (tile.m(i) + e == t) {
+              zt[n] = acc[i][j][e];
+              acc[i][j][e] = -INFINITY;
+            }
       const float base = vocab_base(top);
       float s = 0.0f;
 #pragma unroll
       for (int i = 0; i < TILE::MT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s += vocab_exp(acc[i][j][e], base, k);
-      if (t >= tile.m0 && t < end)       // (few rows of a tile have their target in it)
-#pragma unroll
-        for (int i = 0; i < TILE::MT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (tile.m(i) + e == t) zt[n] = acc[i][j][e];
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
       if (lane < 16) part[wave / TILE::WN * TILE::N + (n - tile.n0)] = make_float2(top, s);
@@ -296,7 +300,10 @@ struct VocabStats {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         top = fmaxf(top, v[e]);
-        if (m + e == t && t < end) zt[n] = v[e];
+        if (m + e == t && t < end) {
+          zt[n] = v[e];
+          v[e] = -INFINITY;
+        }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) s += vocab_exp(v[e], vocab_base(top), k);
@@ -312,18 +319,22 @@ struct VocabStats {
   }
 };
 
-// What the n-th of the rows that count comes to, of its largest logit and the sum around it; behind them: nothing.
+// What the n-th of the rows that count comes to, of its largest logit and R; behind them: nothing.
 __device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint32_t count, float top, float s, bool writes) {
   VocabRow r = {0.0f, 0.0f, 0.0f, -1};
   float logp = 0.0f, loss = 0.0f, w = 0.0f;
-  if (n < count && s != 0.0f) {          // (0: no logit above -infinity)
-    int two;
-    const float f = frexpf(s, &two), base = vocab_base(top);
+  const bool none = n < count && top == -INFINITY && s == 0.0f;      // no logit above -infinity
+  if (n < count && !none) {
+    const float base = vocab_base(top), et = vocab_exp(a.zt[n], base, a.k), all = s + et;
     w = a.weight[n];
-    logp = (float)(a.c * ((double)a.zt[n] - (double)base) - ((double)two + (double)__builtin_amdgcn_logf(f)) * kVLog2);
-    loss = -w * logp;
+    if (writes) {
+      int two;
+      const float f = frexpf(all, &two);
+      logp = et == 1.0f ? (float)-log1p((double)s) : (float)(a.c * ((double)a.zt[n] - (double)base) - ((double)two + (double)__builtin_amdgcn_logf(f)) * kVLog2);
+      loss = -w * logp;
+    }
     const float relative = w / *a.top_weight * kDzScale;
-    r = {base, relative / s, relative, a.target[n]};
+    r = {base, relative / all, relative * (s / all), a.target[n]};
   }
   if (!writes) return r;
   a.row[n] = r;
@@ -333,7 +344,7 @@ __device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint
     if (a.logp) a.logp[a.idx[n]] = logp;
     if (a.loss) a.loss[a.idx[n]] = loss;
   }
-  if (n < count && s == 0.0f && a.x)     // its hidden state, which may be infinite, has no part in the products either: 0 times that is NaN
+  if (none && a.x)                       // its hidden state, which may be infinite, has no part in the products either: 0 times that is NaN
     for (uint32_t e = 0; e < a.dp; e += 8u) *(uint4*)(a.x + (size_t)n * a.dp + e) = make_uint4(0, 0, 0, 0);
   return r;
 }
@@ -434,7 +445,7 @@ struct VocabDz {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = r.f * vocab_exp(z[e], r.m, k);
-      if (m + e == t) v[e] -= r.w;
+      if (m + e == t) v[e] = -r.w;
       if (m + e >= left || r.t < 0) v[e] = 0.0f;      // (a row behind those that count may have NaN for logits: 0 times an infinite weight)
     }
     if constexpr (DT == DFX_F32) {

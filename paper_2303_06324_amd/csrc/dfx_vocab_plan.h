@@ -21,7 +21,7 @@ constexpr int gemm_pairs(int dt) { return dt == DFX_F32 ? 6 : 1; }
 constexpr int gemm_few_e(int dt, int nt) { return dt != DFX_F32 && nt == 2 ? 8 : 4; }      // elements of eight rows of W that a lane reads for dX of few rows
 
 struct VocabState { uint32_t count; float g; };       // what is known of a call on the device, first in the workspace: rows that count; scale * largest weight * c / 2^15
-struct VocabRow { float m, f, w; int32_t t; };        // largest logit, w / S, weight (relative, times 2^15), target
+struct VocabRow { float m, f, w; int32_t t; };        // largest logit, w / S, w R / S (w: the row's weight, relative, times 2^15), target
 
 constexpr size_t kTileRows = 256;        // rows of hidden and of weight are padded to tiles of so many
 

@@ -139,3 +139,46 @@ def test_logits_of_few_long_rows(rows, dim, dt):
     inside = 2 * products * steps * 0.5 * (block / steps) * 4 / 3
     between = steps / (2 if dt == "f32" else 8) * 0.5 / 3
     assert rms(errors) <= (2 ** 0.5 * (inside + between) ** 0.5 * rms(sizes) + 8) * U, (rms(errors) / U, rms(sizes))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,dim,vocab,piece", [(1, 64, 300, 0), (20, 1024, 300, 0), (70, 100, 700, 256), (300, 64, 700, 0), (300, 64, 700, 256)])
+def test_expected_tokens(rows, dim, vocab, piece, dt):
+    """A target that is all but certain (1 - p mostly of 1e-9 to 1e-2): logp, and the gradients that are made of 1 - p, keep their digits.  The other tokens' sum R is off by the errors of their logits and of the
+    target's, 8 u for each exponential and its place in the sums, and (48 + V / 256) u as in test_gpu_ends.py, all relative to R; dz by that, and rounded to the inputs' type (f16: to half a step of 2^-39
+    of the weight at least)."""
+    torch, td = _t()
+    dfx, kinds = _dfx()
+    gen = torch.Generator("cuda").manual_seed(150)
+    w = (torch.randn(vocab, dim, generator=gen, device="cuda") * (2.5 / dim ** 0.5)).to(td[dt])
+    t = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+    x = (w[t].float() * (2.0 + 2.0 * torch.rand(rows, 1, generator=gen, device="cuda"))).to(td[dt])
+    lg, hg, vg = Guarded(rows, "f32"), Guarded(rows * dim, dt), Guarded(vocab * dim, "f32")
+    nbytes = dfx.vocab_loss_workspace(rows, dim, vocab, kinds[dt], True, piece)
+    work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    dfx.vocab_loss(rows, dim, vocab, kinds[dt], x.data_ptr(), w.data_ptr(), t.data_ptr(), logp=lg.ptr(), grad_hidden=hg.ptr(), grad_weight=vg.ptr(), grad_dtype=dfx.F32, piece=piece,
+                   workspace=work.data_ptr(), workspace_bytes=nbytes)
+    X, W, at = _np(x), _np(w), np.arange(rows)
+    z = X @ W.T
+    far = z[at, t.cpu().numpy()][:, None] - z
+    others = np.exp(-far)
+    others[at, t.cpu().numpy()] = 0.0
+    R = others.sum(1, keepdims=True)
+    assert float(R.max()) < 1.0 and float(np.median(R)) < 1e-2      # (what the inputs are meant to be)
+    logp = -np.log1p(R[:, 0])
+    left = 2.0 ** -22 if dt == "f32" else 0.0
+    ez = (2 * (dim * (6 if dt == "f32" else 1) + 4) * U + left) * (np.abs(X) @ np.abs(W).T)
+    rel = (ez + ez[at, t.cpu().numpy()][:, None] + (8 + 3 * far) * U)      # of each other token's exponential
+    eR = (others * rel).sum(1, keepdims=True) + (48 + vocab / 256 + 8) * U * R
+    _near(lg.host(), logp, eR[:, 0] + 2 * U * np.abs(logp), "logp")
+    p = others / (1 + R)
+    dz = p.copy()
+    dz[at, t.cpu().numpy()] = -(R / (1 + R))[:, 0]
+    edz = p * (rel + eR + 8 * U)
+    edz[at, t.cpu().numpy()] = (eR * (1 + 2 * R) + 8 * U * R)[:, 0]
+    edz = edz + HALF[dt] * np.abs(dz) + (2.0 ** -40 if dt == "f16" else 0.0)
+    product = 2 * (max(rows, vocab) * (6 if dt == "f32" else 1) + 300) * U + left
+    want = dz @ W
+    _near(hg.host().reshape(rows, dim), want, edz @ np.abs(W) + product * (np.abs(dz) @ np.abs(W)) + (HALF[dt] + 4 * U) * np.abs(want) + TINY[dt], "grad_hidden")
+    want = dz.T @ X
+    _near(vg.host().reshape(vocab, dim), want, edz.T @ np.abs(X) + product * (np.abs(dz).T @ np.abs(X)) + 4 * U * np.abs(want), "grad_weight")
