@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(256) dfx_vocab_sums_kernel(VocabArgs a) { voca
 
 // dz of a tile, to the type of the products: 16-bit inputs have it rounded once, to half a step of their type (two matrices of 16 bits are one product, one of 32 with one of 16 three, which would
 // take three times as long).  8192 x 4096 x 131072 bf16: the gradients are 1.7e-3 of their norm from those of a dz in 32 bits, 48 x 1024 x 32000 f16 2.6e-4; their errors against 64 bits, the rounding
-// of the results among them, grow by 10 to 30 %.  The one scale for all rows keeps f16's steps at 2^-39 of the largest row weight and above: a row of a far smaller weight loses its small probabilities.
+// of the results among them, grow by 10 to 30 %, of a single row up to twice.  The one scale for all rows keeps f16's steps at 2^-39 of the largest row weight and above: a row of a far smaller weight loses its small probabilities.
 template <int DT>
 struct VocabDz {
   const VocabRow* row;
