@@ -33,6 +33,8 @@ def test_more_long_rows_than_a_launch_has():
     dfx.layer_norm(rows, dim, kinds["bf16"], x.data_ptr(), x.data_ptr())
     assert torch.equal(x[at], want) and bool(want.any())
     assert not x[1:2000].any() and not x[-2000:-2].any()      # (the last two are of the five)
+    del x
+    torch.cuda.empty_cache()
 
 
 # Rows that are few and many, dim and vocab, and a piece (0: the library's): hidden states in registers, through LDS and past it; tiles of one piece, whose logits are kept, and of several
