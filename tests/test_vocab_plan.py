@@ -25,7 +25,7 @@ WIDE = [
     ((1290, 704, 9001, 0), dict(logits="all", steps=11, dx_wide=1, dw_wide=1, splits=2, pieces=1), dict(logits="all", steps=11, dx_wide=1, dw_wide=1, splits=2, pieces=1)),
     ((1290, 1000, 6001, 0), dict(logits="all", steps=16, dx_wide=1, dw_wide=1, splits=2, pieces=1), dict(logits="all", steps=16, dx_wide=1, dw_wide=1, splits=2, pieces=1)),
     ((1000, 520, 9001, 0), dict(logits="all", steps=9, dx_wide=1, dw_wide=1, splits=2, pieces=1), dict(logits="all", steps=9, dx_wide=0, dw_wide=1, splits=2, pieces=1)),
-    ((700, 2050, 4001, 3072), dict(dx_wide=1, dw_wide=1, splits=2, pieces=2), dict(dx_wide=1, dw_wide=1, splits=2, pieces=2)),
+    ((700, 2050, 4001, 3584), dict(dx_wide=1, dw_wide=1, splits=2, pieces=2), dict(dx_wide=1, dw_wide=1, splits=2, pieces=2)),
     ((2570, 320, 6001, 0), dict(logits="part", steps=5, dx_wide=1, splits=2, pieces=1), dict(logits="part", steps=5, dx_wide=1, splits=2, pieces=1, keep=0)),
     ((2049, 200, 4101, 512), dict(logits="all", steps=4, dx_wide=1, pieces=9), dict(logits="all", steps=4, dx_wide=1, pieces=9)),
 ]
