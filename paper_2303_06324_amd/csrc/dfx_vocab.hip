@@ -323,7 +323,7 @@ struct VocabStats {
 __device__ __forceinline__ VocabRow row_end(const VocabArgs& a, uint32_t n, uint32_t count, float top, float s, bool writes) {
   VocabRow r = {0.0f, 0.0f, 0.0f, -1};
   float logp = 0.0f, loss = 0.0f, w = 0.0f;
-  const bool none = n < count && top == -INFINITY && s == 0.0f;      // no logit above -infinity
+  const bool none = n < count && top == -INFINITY && s == 0.0f && a.zt[n] == -INFINITY;      // no logit above -infinity, and the target's, which is not in R, no NaN
   if (n < count && !none) {
     const float base = vocab_base(top), et = vocab_exp(a.zt[n], base, a.k), all = s + et;
     w = a.weight[n];

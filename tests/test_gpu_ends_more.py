@@ -184,3 +184,18 @@ def test_expected_tokens(rows, dim, vocab, piece, dt):
     _near(hg.host().reshape(rows, dim), want, edz @ np.abs(W) + product * (np.abs(dz) @ np.abs(W)) + (HALF[dt] + 4 * U) * np.abs(want) + TINY[dt], "grad_hidden")
     want = dz.T @ X
     _near(vg.host().reshape(vocab, dim), want, edz.T @ np.abs(X) + product * (np.abs(dz).T @ np.abs(X)) + 4 * U * np.abs(want), "grad_weight")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,dim,vocab,piece", INFINITE)
+def test_a_target_of_nan_among_minus_infinities(rows, dim, vocab, piece, dt):
+    """The target's logit is not in the sum of the others: its NaN makes the row NaN all the same, and the rest of that token's column."""
+    v = Vocab(rows, dim, vocab, dt, seed=160, weights=None)
+    v.t[5] = 1
+    v.w[:, 7] = -v.w[:, 7].abs() - 0.5
+    v.x[:, 7] = 0.0
+    v.x[5, 7] = float("inf")
+    v.w[1, 7] = float("nan")
+    v.run(piece=piece)
+    on = (v.t >= 0) & (v.t < vocab)
+    assert np.isnan(v.lg.host()[on]).all() and np.isnan(v.og.host()[on]).all() and bool(v.gh[5].isnan().all()) and not v.lg.host()[~on].any()
